@@ -381,6 +381,89 @@ VARRATE_API int varrate_joint_decode_attn(const varrate_shape* shape, const varr
 VARRATE_API int varrate_joint_append_exact(const varrate_shape* shape, varrate_jcache* cache, const void* k_new,
                                            const void* v_new, void* stream);
 
+/* ---- paged cache ------------------------------------------------------------------------
+ * The uncompressed side of a sequence's life: new tokens' queries and keys are normed and
+ * rotated, their rows appended to a cache of pages, the tokens attend over it, and a whole
+ * sequence's rows are gathered into the contiguous [n][G][d] that varrate_compress takes.
+ *
+ * A pool holds n_pages pages of `page` tokens, keys and values alike as [n_pages][G][page][d]
+ * dtype (one head's rows of a page lie together).  A batch of S sequences shares it: table row
+ * s (at table + s table_stride, `width` entries) numbers the pages of sequence s, token t
+ * sitting at slot t % page of page table[s][t / page].  The call's T new tokens are packed,
+ * sequence after sequence: rows q_start[s] .. q_start[s + 1] - 1 belong to sequence s and are
+ * its last tokens, at positions kv_len[s] - (their number) .. kv_len[s] - 1 (kv_len counts
+ * them).  Rows before q_start[0] or from q_start[S] on belong to no sequence: they are not
+ * read and their outputs are left as they were, so a captured call may be padded.
+ *
+ * table, kv_len and q_start are DEVICE int32 arrays and are read when the call runs, so a
+ * captured graph follows their new contents.  They are not checked on the host; the kernels
+ * keep every access inside the buffers: page numbers outside [0, n_pages) name no page (append
+ * drops the row, attention leaves the token out, gather writes zeros), starts are brought into
+ * [0, T], lengths for attention into [0, width page]; append drops the rows of a sequence whose
+ * length lies outside that range and rows at negative positions.  Starts must not fall; of
+ * sequences whose starts fall the outputs are unspecified.  Table rows of several sequences may
+ * share pages (a common prompt) as long as one call's tokens land in different slots.
+ *
+ * d = 128.  Rows of new tokens are [T][heads][d] with a stride between tokens (elements, a
+ * multiple of 16 bytes; heads contiguous), so slices of a fused projection need no copy.
+ * These calls need no zero-filled memory; their workspace holds nothing between calls. */
+typedef struct varrate_pages {
+    void*   k;         /* [n_pages][G][page][d] dtype                                        */
+    void*   v;         /* [n_pages][G][page][d] dtype                                        */
+    int64_t n_pages;   /* 1 .. 2^31 - 1                                                      */
+    int32_t G;         /* KV heads, 1 .. 1024                                                */
+    int32_t d;         /* head dim; must be 128                                              */
+    int32_t page;      /* tokens per page: 16, 32, 64, 128 or 256                            */
+    int32_t dtype;     /* VARRATE_BF16 or VARRATE_F32                                        */
+} varrate_pages;
+
+typedef struct varrate_batch {
+    const int32_t* table;        /* [S] rows of `width` page numbers                           */
+    const int32_t* kv_len;       /* [S] tokens of each sequence, the new ones counted         */
+    const int32_t* q_start;      /* [S + 1] first new row of each sequence; then the end       */
+    int64_t        table_stride; /* entries between table rows                                */
+    int64_t        T;            /* rows of new tokens (padding counted); 0: nothing is done  */
+    int32_t        S;            /* sequences, 1 .. 65536                                     */
+    int32_t        width;        /* table entries per sequence, 1 .. 2^30 / page              */
+} varrate_batch;
+
+/* RMS norm of each head's row and position rotation, in one pass and rounded once:
+ *   y = x / sqrt(mean(x^2) + eps) * w,  z_i = y_i cos a_i - y_{i+64} sin a_i,
+ *   z_{i+64} = y_i sin a_i + y_{i+64} cos a_i,  a_i = pos[t] theta[i] (the exact product),
+ * the layout of shape->rope.  q [T][H][d] with weights wq, k [T][G][d] with wk; either may be NULL
+ * with 0 heads.  Weights are fp32, wq_stride (wk_stride) elements between the heads': 0 (one
+ * weight [d] for all) or 128; NULL: no norm of that side.  theta [64] and pos [T] are device
+ * arrays; theta NULL: no rotation (pos unused).  q_out and k_out may be q and k themselves
+ * (same stride) but must not overlap them otherwise.                                        */
+VARRATE_API int varrate_norm_rotate(int32_t dtype, int64_t T, const void* q, int64_t q_stride, int32_t H,
+                                    const void* k, int64_t k_stride, int32_t G, const int32_t* pos,
+                                    const float* theta, const float* wq, int64_t wq_stride, const float* wk,
+                                    int64_t wk_stride, float eps, void* q_out, int64_t q_out_stride, void* k_out,
+                                    int64_t k_out_stride, void* stream);
+
+/* Writes the batch's new key and value rows ([T][G][d]) into their slots; theta ([64] device,
+ * or NULL) rotates each key by its position first.                                           */
+VARRATE_API int varrate_paged_append(const varrate_pages* pages, const varrate_batch* batch, const void* k_new,
+                                     int64_t k_stride, const void* v_new, int64_t v_stride, const float* theta,
+                                     void* stream);
+
+/* Attention of the batch's new tokens over their sequences: q [T][H][d] -> out [T][H][d], query
+ * head h reading KV head h / (H / G), softmax of scale <q, k> over the keys that the token sees.
+ * causal 1: the token at position p sees keys t <= p, and with window > 0 only p - t < window;
+ * causal 0 (window 0): every new token sees all kv_len[s] keys.  A token that sees no key gets
+ * zeros, and so does one whose visible scores are all -infinity.  Keys and values that a token
+ * does not see (later ones, slots behind the end, unused pages) do not reach its output,
+ * whatever they hold.  scale finite and > 0.  out must not overlap q.                        */
+VARRATE_API size_t varrate_paged_attn_workspace_bytes(const varrate_pages* pages, const varrate_batch* batch, int32_t H);
+VARRATE_API int varrate_paged_attn(const varrate_pages* pages, const varrate_batch* batch, const void* q,
+                                   int64_t q_stride, int32_t H, int32_t causal, int32_t window, float scale, void* out,
+                                   int64_t out_stride, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The first n tokens of one sequence, contiguous: K, V [n][G][d] (n <= width page; table: its
+ * row of page numbers, device).                                                             */
+VARRATE_API int varrate_paged_gather(const varrate_pages* pages, const int32_t* table, int32_t width, int64_t n,
+                                     void* K, void* V, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -21,7 +21,8 @@ from ._lib import CHUNK, COEF_PAD, HEAD_DIM  # noqa: F401
 
 __all__ = ["VarRateError", "Shape", "Cache", "new_cache", "coded_budget", "salience", "allocate",
            "project", "compress", "append_exact", "decode", "decode_noalloc", "QCache", "new_qcache",
-           "quantize", "decode_q", "anchor_search", "anchor_encode", "library"]
+           "quantize", "decode_q", "anchor_search", "anchor_encode", "PagedCache", "PagedBatch", "new_pages",
+           "norm_rotate", "paged_append", "paged_attn", "paged_gather", "library"]
 
 
 class VarRateError(RuntimeError):
@@ -492,3 +493,211 @@ def joint_append_exact(shape: Shape, cache: JCache, k_new: torch.Tensor, v_new: 
                                                 _dev_ptr(v_new, shape.torch_dtype, "v_new"), _stream()))
     cache._update(cc)
     return cache
+
+
+# ---------------------------------------------------------------------------------------
+# Paged cache: sequences before they are compressed.  New tokens' queries and keys are normed
+# and rotated, their rows appended to pages, the tokens attend over them, and a sequence's
+# rows are gathered into the [n][G][d] that compress() takes.
+#
+#     pages = new_pages(n_pages, G=8, page=64)
+#     batch = PagedBatch(table, kv_len, q_start)       # device int32, the new tokens counted
+#     q, k = norm_rotate(q, k, pos=pos, theta=theta, wq=wq, wk=wk)
+#     paged_append(pages, batch, k, v)
+#     out = paged_attn(pages, batch, q)                # causal at each sequence's end
+#     K, V = paged_gather(pages, table[s], n)          # once the prompt is complete
+#
+# These calls run on the current stream of their tensors' device and take what memory they
+# need from torch's allocator in the call, so they may run on several streams at once and be
+# captured into graphs.
+
+_DTYPES = {torch.bfloat16: _lib.VARRATE_BF16, torch.float32: _lib.VARRATE_F32}
+
+
+def _einval(msg: str):
+    raise VarRateError(_lib.VARRATE_EINVAL, msg)
+
+
+class PagedCache:
+    """A pool of pages: k, v [n_pages][G][page][d] (bf16 or fp32), contiguous device tensors."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor):
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.device != v.device:
+            _einval("k and v must be alike, [n_pages][G][page][d]")
+        if k.dtype not in _DTYPES:
+            _einval(f"pages have dtype {k.dtype}, expected torch.bfloat16 or torch.float32")
+        self.k, self.v = k, v
+        self.page, self.G = int(k.shape[2]), int(k.shape[1])
+        self._c = _lib.PagesC(_dev_ptr(k, name="k"), _dev_ptr(v, name="v"), k.shape[0], self.G, k.shape[3], self.page,
+                              _DTYPES[k.dtype])
+
+    def c(self) -> _lib.PagesC:
+        return self._c
+
+
+def new_pages(n_pages: int, G: int, page: int = 64, dtype: str = "bf16", device="cuda") -> PagedCache:
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    k, v = (torch.zeros((n_pages, G, page, HEAD_DIM), dtype=dt, device=device) for _ in range(2))
+    return PagedCache(k, v)
+
+
+def _i32(t: torch.Tensor, dim: int, name: str) -> int:
+    if t.dtype != torch.int32 or not t.is_cuda or t.dim() != dim or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        _einval(f"{name} must be a device int32 tensor of {dim} dimension{'s' if dim > 1 else ''}, entries adjacent")
+    return t.data_ptr()
+
+
+class PagedBatch:
+    """The sequences of one call: table [S][width] page numbers, kv_len [S] tokens of each with the
+    new ones, q_start [S + 1] first packed row of each (device int32).  The arrays are read when a
+    call runs, so their contents may change between calls and graph replays."""
+
+    def __init__(self, table: torch.Tensor, kv_len: torch.Tensor, q_start: torch.Tensor):
+        pt, pl, ps = _i32(table, 2, "table"), _i32(kv_len, 1, "kv_len"), _i32(q_start, 1, "q_start")
+        S, width = int(table.shape[0]), int(table.shape[1])
+        if kv_len.shape[0] != S or q_start.shape[0] != S + 1:
+            _einval(f"kv_len and q_start must have {S} and {S + 1} entries")
+        if kv_len.device != table.device or q_start.device != table.device:
+            _einval("table, kv_len and q_start must be on one device")
+        self.table, self.kv_len, self.q_start = table, kv_len, q_start
+        self._c = (pt, pl, ps, table.stride(0) if S > 1 else width, S, width)
+
+    def c(self, T: int) -> _lib.BatchC:
+        pt, pl, ps, stride, S, width = self._c
+        return _lib.BatchC(pt, pl, ps, stride, T, S, width)
+
+
+def _rows(t: torch.Tensor, dtype, T: Optional[int], heads: Optional[int], device, name: str):
+    """Address and token stride (elements) of rows [T][heads][d]."""
+    if t.dtype != dtype or t.device != device or t.dim() != 3:
+        _einval(f"{name} must be a {dtype} tensor [T][heads][d] on {device}")
+    n, h, d = t.shape
+    if d != HEAD_DIM or (T is not None and n != T) or (heads is not None and h != heads):
+        _einval(f"{name} has shape {tuple(t.shape)}, expected [{'T' if T is None else T}]"
+                f"[{'heads' if heads is None else heads}][{HEAD_DIM}]")
+    s0, s1, s2 = t.stride()
+    if n and (s2 != 1 or (h > 1 and s1 != d)):
+        _einval(f"{name}: the rows of a token's heads must be adjacent")
+    return t.data_ptr(), (s0 if n > 1 else h * d)
+
+
+def _launch(device: torch.device, call, *args):
+    if torch.cuda.current_device() == device.index:
+        rc = call(*args, torch.cuda.current_stream(device).cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            rc = call(*args, torch.cuda.current_stream(device).cuda_stream)
+    if rc:
+        _check(rc)
+
+
+def _f32(t: Optional[torch.Tensor], shapes, device, name: str) -> int:
+    if t is None:
+        return 0
+    if t.dtype != torch.float32 or t.device != device or tuple(t.shape) not in shapes or not t.is_contiguous():
+        _einval(f"{name} must be a contiguous float32 tensor of shape {' or '.join(map(str, shapes))} on {device}")
+    return t.data_ptr()
+
+
+def norm_rotate(q: Optional[torch.Tensor], k: Optional[torch.Tensor] = None, pos: Optional[torch.Tensor] = None,
+                theta: Optional[torch.Tensor] = None, wq: Optional[torch.Tensor] = None,
+                wk: Optional[torch.Tensor] = None, eps: float = 1e-6, q_out: Optional[torch.Tensor] = None,
+                k_out: Optional[torch.Tensor] = None):
+    """RMS norm of each head's row (fp32 weights wq, wk: [d] or [heads][d]; None: no norm) and
+    rotation at positions pos [T] int32 by theta [64] fp32 (None: no rotation), rounded once.
+    q [T][H][d], k [T][G][d] (either may be None; tokens may be strided).  Returns (q_out, k_out)."""
+    some = q if q is not None else k
+    if some is None:
+        _einval("q or k must be given")
+    dev, dt = some.device, some.dtype
+    if not some.is_cuda or dt not in _DTYPES:
+        _einval("q and k must be bf16 or fp32 device tensors")
+    T = int(some.shape[0])
+    side = []
+    for x, w, o, name in ((q, wq, q_out, "q"), (k, wk, k_out, "k")):
+        if x is None:
+            if w is not None or o is not None:
+                _einval(f"w{name} or {name}_out without {name}")
+            side.append((0, 0, 0, 0, 0, 0, 0, None))
+            continue
+        px, sx = _rows(x, dt, T, None, dev, name)
+        heads = int(x.shape[1])
+        pw = _f32(w, ((HEAD_DIM,), (heads, HEAD_DIM)), dev, "w" + name)
+        if o is None:
+            o = torch.empty((T, heads, HEAD_DIM), dtype=dt, device=dev)
+        po, so = _rows(o, dt, T, heads, dev, name + "_out")
+        side.append((px, sx, heads, pw, HEAD_DIM if w is not None and w.dim() == 2 else 0, po, so, o))
+    if theta is not None and pos is None:
+        _einval("rotation needs pos")
+    pp = 0
+    if theta is not None:
+        pp = _i32(pos, 1, "pos")
+        if pos.shape[0] != T or pos.device != dev:
+            _einval(f"pos must have {T} entries on {dev}")
+    a, b = side
+    _launch(dev, library().varrate_norm_rotate, _DTYPES[dt], T, a[0], a[1], a[2], b[0], b[1], b[2], pp,
+            _f32(theta, ((HEAD_DIM // 2,),), dev, "theta"), a[3], a[4], b[3], b[4], eps, a[5], a[6], b[5], b[6])
+    return a[7], b[7]
+
+
+def paged_append(pages: PagedCache, batch: PagedBatch, k: torch.Tensor, v: torch.Tensor,
+                 theta: Optional[torch.Tensor] = None) -> PagedCache:
+    """Write the batch's new rows k, v [T][G][d] into their sequences' pages; theta [64] fp32 rotates
+    each key by its position first."""
+    dev = pages.k.device
+    T = int(k.shape[0])
+    pk, sk = _rows(k, pages.k.dtype, None, pages.G, dev, "k")
+    pv, sv = _rows(v, pages.k.dtype, T, pages.G, dev, "v")
+    if batch.table.device != dev:
+        _einval(f"the batch must be on {dev}")
+    _launch(dev, library().varrate_paged_append, pages.c(), batch.c(T), pk, sk, pv, sv,
+            _f32(theta, ((HEAD_DIM // 2,),), dev, "theta"))
+    return pages
+
+
+def paged_attn_workspace(pages: PagedCache, batch: PagedBatch, T: int, H: int) -> torch.Tensor:
+    need = int(library().varrate_paged_attn_workspace_bytes(pages.c(), batch.c(T), H))
+    return torch.empty(max(need, 16), dtype=torch.uint8, device=pages.k.device)
+
+
+def paged_attn(pages: PagedCache, batch: PagedBatch, q: torch.Tensor, causal: bool = True, window: int = 0,
+               scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+               workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of the batch's new tokens, q [T][H][d], over their sequences' pages (query head h
+    reads KV head h / (H / G)): causal at each sequence's end, with window > 0 over the last `window`
+    keys only; causal=False: every token sees its whole sequence.  scale: 1 / sqrt(d) by default."""
+    dev = pages.k.device
+    T, H = int(q.shape[0]), int(q.shape[1]) if q.dim() == 3 else 0
+    pq, sq = _rows(q, pages.k.dtype, T, None, dev, "q")
+    if batch.table.device != dev:
+        _einval(f"the batch must be on {dev}")
+    if out is None:
+        out = torch.empty((T, H, HEAD_DIM), dtype=q.dtype, device=dev)
+    po, so = _rows(out, q.dtype, T, H, dev, "out")
+    ws = workspace if workspace is not None else paged_attn_workspace(pages, batch, T, H)
+    if not ws.is_cuda or ws.device != dev or not ws.is_contiguous():
+        _einval(f"workspace must be a contiguous tensor on {dev}")
+    _launch(dev, library().varrate_paged_attn, pages.c(), batch.c(T), pq, sq, H, 1 if causal else 0, int(window),
+            HEAD_DIM ** -0.5 if scale is None else scale, po, so, ws.data_ptr(), ws.numel() * ws.element_size())
+    return out
+
+
+def paged_gather(pages: PagedCache, table: torch.Tensor, n: int, K: Optional[torch.Tensor] = None,
+                 V: Optional[torch.Tensor] = None):
+    """The first n tokens of the sequence with page numbers `table` [width]: K, V [n][G][d], as
+    compress() takes them."""
+    dev = pages.k.device
+    pt = _i32(table, 1, "table")
+    if table.device != dev:
+        _einval(f"table must be on {dev}")
+    if n < 0:
+        _einval(f"n={n} is negative")
+    outs = []
+    for x, name in ((K, "K"), (V, "V")):
+        if x is None:
+            x = torch.empty((n, pages.G, HEAD_DIM), dtype=pages.k.dtype, device=dev)
+        elif x.device != dev or tuple(x.shape) != (n, pages.G, HEAD_DIM):
+            _einval(f"{name} must be [{n}][{pages.G}][{HEAD_DIM}] on {dev}")
+        outs.append((x, _dev_ptr(x, pages.k.dtype, name)))
+    _launch(dev, library().varrate_paged_gather, pages.c(), pt, int(table.shape[0]), n, outs[0][1], outs[1][1])
+    return outs[0][0], outs[1][0]

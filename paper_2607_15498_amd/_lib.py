@@ -26,6 +26,8 @@ EXPORTS = (
     "varrate_jcache_bytes", "varrate_joint_compress_workspace_bytes", "varrate_joint_decode_workspace_bytes",
     "varrate_joint_compress", "varrate_joint_decode_attn", "varrate_joint_append_exact",
     "varrate_read_probe",
+    "varrate_norm_rotate", "varrate_paged_append", "varrate_paged_attn_workspace_bytes", "varrate_paged_attn",
+    "varrate_paged_gather",
 )
 DECODE_SCRATCH_BYTES = 8 << 20
 
@@ -76,6 +78,17 @@ class JCacheBytes(ctypes.Structure):
                [(k, ctypes.c_size_t) for k in ("coef", "rank", "offset", "chunk_off", "k_exact", "v_exact")]
 
 
+class PagesC(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("G", ctypes.c_int32),
+                ("d", ctypes.c_int32), ("page", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class BatchC(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("q_start", ctypes.c_void_p),
+                ("table_stride", ctypes.c_int64), ("T", ctypes.c_int64), ("S", ctypes.c_int32),
+                ("width", ctypes.c_int32)]
+
+
 _lib = None
 
 
@@ -117,6 +130,13 @@ def load() -> ctypes.CDLL:
         "varrate_joint_compress": (ctypes.c_int, [P(Shape), vp, vp, vp, vp, P(JCacheC), vp, vp, sz, vp]),
         "varrate_joint_decode_attn": (ctypes.c_int, [P(Shape), P(JCacheC), i32, vp, i32, vp, vp, vp, sz, vp]),
         "varrate_joint_append_exact": (ctypes.c_int, [P(Shape), P(JCacheC), vp, vp, vp]),
+        "varrate_norm_rotate": (ctypes.c_int, [i32, i64, vp, i64, i32, vp, i64, i32, vp, vp, vp, i64, vp, i64,
+                                               ctypes.c_float, vp, i64, vp, i64, vp]),
+        "varrate_paged_append": (ctypes.c_int, [P(PagesC), P(BatchC), vp, i64, vp, i64, vp, vp]),
+        "varrate_paged_attn_workspace_bytes": (sz, [P(PagesC), P(BatchC), i32]),
+        "varrate_paged_attn": (ctypes.c_int, [P(PagesC), P(BatchC), vp, i64, i32, i32, i32, ctypes.c_float, vp, i64,
+                                              vp, sz, vp]),
+        "varrate_paged_gather": (ctypes.c_int, [P(PagesC), vp, i32, i64, vp, vp, vp]),
         "varrate_read_probe": (ctypes.c_int, [vp, ctypes.c_size_t, vp, vp]),
     }
     for name, (res, args) in sig.items():

@@ -14,6 +14,7 @@
 #include <utility>
 
 #include "vr_internal.h"
+#include "vr_pages.h"
 
 using namespace vr;
 
@@ -610,6 +611,152 @@ int varrate_decode_attn_noalloc(const varrate_shape* sh, const varrate_cache* ca
     if ((rc = hip_status(decode_scratch(&scratch), "decode scratch lookup"))) return rc;
     return hip_status(launch_decode(*sh, caches, S, q, Q, PK, PV, out, scratch, (hipStream_t)stream, true),
                       "decode launch");
+}
+
+// ---- paged cache ------------------------------------------------------------------------------
+
+static int check_dtype(int dtype) {
+    if (dtype != VARRATE_BF16 && dtype != VARRATE_F32) return fail(VARRATE_EINVAL, "unknown dtype %d", dtype);
+    return VARRATE_OK;
+}
+
+static int check_pages(const varrate_pages* pg) {
+    if (!pg) return fail(VARRATE_EINVAL, "pages is NULL");
+    if (pg->d != VARRATE_HEAD_DIM) return fail(VARRATE_EUNSUPPORTED, "head dim %d != 128", pg->d);
+    int rc = check_dtype(pg->dtype);
+    if (rc) return rc;
+    if (pg->G < 1 || pg->G > 1024) return fail(VARRATE_EINVAL, "G=%d outside [1, 1024]", pg->G);
+    if (pg->page < PAGE_MIN || pg->page > PAGE_MAX || (pg->page & (pg->page - 1)) != 0)
+        return fail(VARRATE_EUNSUPPORTED, "page=%d: need a power of two in [16, 256]", pg->page);
+    if (pg->n_pages < 1 || pg->n_pages > INT32_MAX)
+        return fail(VARRATE_EINVAL, "n_pages=%lld outside [1, 2^31 - 1]", (long long)pg->n_pages);
+    if (!pg->k || !pg->v) return fail(VARRATE_EINVAL, "pages has a NULL buffer");
+    if (!aligned16(pg->k) || !aligned16(pg->v)) return fail(VARRATE_EINVAL, "page buffers must be 16-byte aligned");
+    return VARRATE_OK;
+}
+
+static int check_width(int32_t width, int32_t page) {
+    if (width < 1 || (int64_t)width * page > ((int64_t)1 << 30))
+        return fail(VARRATE_EINVAL, "table width %d outside [1, 2^30 / page]", width);
+    return VARRATE_OK;
+}
+
+static int check_batch(const varrate_batch* b, int32_t page) {
+    if (!b) return fail(VARRATE_EINVAL, "batch is NULL");
+    if (!b->table || !b->kv_len || !b->q_start) return fail(VARRATE_EINVAL, "batch has a NULL array");
+    if (((uintptr_t)b->table | (uintptr_t)b->kv_len | (uintptr_t)b->q_start) & 3u)
+        return fail(VARRATE_EINVAL, "batch arrays must be 4-byte aligned");
+    if (b->S < 1 || b->S > 65536) return fail(VARRATE_EINVAL, "S=%d outside [1, 65536]", b->S);
+    if (b->T < 0) return fail(VARRATE_EINVAL, "T=%lld is negative", (long long)b->T);
+    int rc = check_width(b->width, page);
+    if (rc) return rc;
+    if (b->table_stride < 0) return fail(VARRATE_EINVAL, "table_stride=%lld is negative", (long long)b->table_stride);
+    return VARRATE_OK;
+}
+
+// rows [T][heads][128] with `stride` elements between tokens; outputs must not overlap themselves
+static int check_rows(const void* p, int64_t stride, int64_t T, int32_t heads, int dtype, bool out, const char* name) {
+    if (!p) return fail(VARRATE_EINVAL, "%s is NULL", name);
+    const int per16 = dtype == VARRATE_BF16 ? 8 : 4;
+    if (!aligned16(p) || stride % per16 != 0)
+        return fail(VARRATE_EINVAL, "%s must be 16-byte aligned, its tokens %d elements or a multiple apart", name, per16);
+    if (stride < 0 || (out && T > 1 && stride < (int64_t)heads * VARRATE_HEAD_DIM))
+        return fail(VARRATE_EINVAL, "%s: %lld elements between tokens", name, (long long)stride);
+    return VARRATE_OK;
+}
+
+// 32-bit row numbers
+static int check_rows_total(int64_t T, int64_t heads) {
+    if (T > ((int64_t)1 << 30) / heads)
+        return fail(VARRATE_EUNSUPPORTED, "T=%lld tokens of %lld heads exceed 2^30 rows", (long long)T, (long long)heads);
+    return VARRATE_OK;
+}
+
+int varrate_norm_rotate(int32_t dtype, int64_t T, const void* q, int64_t q_stride, int32_t H, const void* k,
+                        int64_t k_stride, int32_t G, const int32_t* pos, const float* theta, const float* wq,
+                        int64_t wq_stride, const float* wk, int64_t wk_stride, float eps, void* q_out,
+                        int64_t q_out_stride, void* k_out, int64_t k_out_stride, void* stream) {
+    int rc = check_dtype(dtype);
+    if (rc) return rc;
+    if (T < 0) return fail(VARRATE_EINVAL, "T=%lld is negative", (long long)T);
+    if (H < 0 || G < 0 || H + (int64_t)G < 1 || H > 65536 || G > 65536)
+        return fail(VARRATE_EINVAL, "H=%d G=%d: need one head at least, 65536 at most", H, G);
+    if ((rc = check_rows_total(T, (int64_t)H + G))) return rc;
+    if (!(eps >= 0.f) || !std::isfinite(eps)) return fail(VARRATE_EINVAL, "eps is negative or not finite");
+    if (theta && !pos) return fail(VARRATE_EINVAL, "rotation needs pos");
+    if (((uintptr_t)theta | (uintptr_t)pos) & 3u) return fail(VARRATE_EINVAL, "theta and pos must be 4-byte aligned");
+    for (int side = 0; side < 2; ++side) {
+        const float* w = side ? wk : wq;
+        const int64_t ws = side ? wk_stride : wq_stride;
+        if (w && (!aligned16(w) || (ws != 0 && ws != VARRATE_HEAD_DIM)))
+            return fail(VARRATE_EINVAL, "%s must be 16-byte aligned, its heads 0 or 128 elements apart", side ? "wk" : "wq");
+    }
+    if (T == 0) return VARRATE_OK;
+    if (H && ((rc = check_rows(q, q_stride, T, H, dtype, false, "q")) ||
+              (rc = check_rows(q_out, q_out_stride, T, H, dtype, true, "q_out")))) return rc;
+    if (G && ((rc = check_rows(k, k_stride, T, G, dtype, false, "k")) ||
+              (rc = check_rows(k_out, k_out_stride, T, G, dtype, true, "k_out")))) return rc;
+    if (H && q == q_out && q_stride != q_out_stride && T > 1) return fail(VARRATE_EINVAL, "q_out is q with another stride");
+    if (G && k == k_out && k_stride != k_out_stride && T > 1) return fail(VARRATE_EINVAL, "k_out is k with another stride");
+    const NormRotate n = {q, k, q_out, k_out, q_stride, k_stride, q_out_stride, k_out_stride, wq_stride, wk_stride,
+                          pos, theta, wq, wk, eps, T, H, G};
+    return hip_status(launch_norm_rotate(dtype, n, (hipStream_t)stream), "norm and rotation launch");
+}
+
+int varrate_paged_append(const varrate_pages* pg, const varrate_batch* b, const void* k_new, int64_t k_stride,
+                         const void* v_new, int64_t v_stride, const float* theta, void* stream) {
+    int rc = check_pages(pg);
+    if (rc || (rc = check_batch(b, pg->page)) || (rc = check_rows_total(b->T, 2 * pg->G))) return rc;
+    if ((uintptr_t)theta & 3u) return fail(VARRATE_EINVAL, "theta must be 4-byte aligned");
+    if (b->T == 0) return VARRATE_OK;
+    if ((rc = check_rows(k_new, k_stride, b->T, pg->G, pg->dtype, false, "k_new")) ||
+        (rc = check_rows(v_new, v_stride, b->T, pg->G, pg->dtype, false, "v_new"))) return rc;
+    return hip_status(launch_paged_append(*pg, *b, k_new, k_stride, v_new, v_stride, theta, (hipStream_t)stream),
+                      "paged append launch");
+}
+
+static int check_paged_heads(const varrate_pages* pg, const varrate_batch* b, int32_t H) {
+    int rc = check_pages(pg);
+    if (rc || (rc = check_batch(b, pg->page))) return rc;
+    if (H < 1) return fail(VARRATE_EINVAL, "H=%d must be >= 1", H);
+    if (H % pg->G != 0) return fail(VARRATE_EUNSUPPORTED, "H=%d is not a multiple of G=%d", H, pg->G);
+    return check_rows_total(b->T, H);
+}
+
+size_t varrate_paged_attn_workspace_bytes(const varrate_pages* pg, const varrate_batch* b, int32_t H) {
+    if (check_paged_heads(pg, b, H) || b->T == 0) return 0;
+    return paged_attn_ws_bytes(b->T, b->S, pg->G, H, (int64_t)b->width * pg->page);
+}
+
+int varrate_paged_attn(const varrate_pages* pg, const varrate_batch* b, const void* q, int64_t q_stride, int32_t H,
+                       int32_t causal, int32_t window, float scale, void* out, int64_t out_stride, void* ws,
+                       size_t ws_bytes, void* stream) {
+    int rc = check_paged_heads(pg, b, H);
+    if (rc) return rc;
+    if (causal != 0 && causal != 1) return fail(VARRATE_EINVAL, "causal=%d outside {0, 1}", causal);
+    if (window < 0 || window > (1 << 30)) return fail(VARRATE_EINVAL, "window=%d outside [0, 2^30]", window);
+    if (window && !causal) return fail(VARRATE_EUNSUPPORTED, "a window without causal order");
+    if (!(scale > 0.f) || !std::isfinite(scale)) return fail(VARRATE_EINVAL, "scale must be finite and > 0");
+    if (b->T == 0) return VARRATE_OK;
+    if ((rc = check_rows(q, q_stride, b->T, H, pg->dtype, false, "q")) ||
+        (rc = check_rows(out, out_stride, b->T, H, pg->dtype, true, "out"))) return rc;
+    if (q == out) return fail(VARRATE_EINVAL, "out is q");
+    if ((rc = ws_check(ws, ws_bytes, paged_attn_ws_bytes(b->T, b->S, pg->G, H, (int64_t)b->width * pg->page)))) return rc;
+    return hip_status(launch_paged_attn(*pg, *b, q, q_stride, H, causal, window, scale, out, out_stride, ws,
+                                        (hipStream_t)stream),
+                      "paged attention launch");
+}
+
+int varrate_paged_gather(const varrate_pages* pg, const int32_t* table, int32_t width, int64_t n, void* K, void* V,
+                         void* stream) {
+    int rc = check_pages(pg);
+    if (rc || (rc = check_width(width, pg->page))) return rc;
+    if (!table || ((uintptr_t)table & 3u)) return fail(VARRATE_EINVAL, "table must be non-NULL and 4-byte aligned");
+    if (n < 0 || n > (int64_t)width * pg->page)
+        return fail(VARRATE_EINVAL, "n=%lld outside [0, width page = %lld]", (long long)n, (long long)width * pg->page);
+    if (n == 0) return VARRATE_OK;
+    if (!K || !V || !aligned16(K) || !aligned16(V)) return fail(VARRATE_EINVAL, "K and V must be non-NULL and 16-byte aligned");
+    return hip_status(launch_paged_gather(*pg, table, n, K, V, (hipStream_t)stream), "paged gather launch");
 }
 
 }  // extern "C"

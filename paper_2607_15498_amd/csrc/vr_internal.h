@@ -124,6 +124,25 @@ hipError_t launch_quantize(const varrate_shape& sh, const varrate_cache& c, varr
 size_t decode_group_bytes(const varrate_shape& sh, int S, int Q);
 // this device's address of the fixed decode scratch array (looked up once per device)
 hipError_t decode_scratch(uint8_t** out);
+// paged cache (all arguments checked by the caller)
+struct NormRotate {
+    const void *q, *k;
+    void *q_out, *k_out;
+    int64_t q_stride, k_stride, qo_stride, ko_stride, wq_stride, wk_stride;   // elements
+    const int32_t* pos;
+    const float *theta, *wq, *wk;
+    float eps;
+    int64_t T;
+    int32_t H, G;
+};
+hipError_t launch_norm_rotate(int dtype, const NormRotate& n, hipStream_t st);
+hipError_t launch_paged_append(const varrate_pages& pg, const varrate_batch& b, const void* k, int64_t k_stride,
+                               const void* v, int64_t v_stride, const float* theta, hipStream_t st);
+size_t paged_attn_ws_bytes(int64_t T, int S, int G, int H, int64_t cap);
+hipError_t launch_paged_attn(const varrate_pages& pg, const varrate_batch& b, const void* q, int64_t q_stride, int H,
+                             int causal, int window, float scale, void* out, int64_t out_stride, void* ws,
+                             hipStream_t st);
+hipError_t launch_paged_gather(const varrate_pages& pg, const int32_t* table, int64_t n, void* K, void* V, hipStream_t st);
 // streaming-read probe (measurement aid)
 hipError_t launch_read_probe(const void* src, size_t bytes, uint32_t* sink, hipStream_t st);
 
