@@ -26,9 +26,11 @@ FLAGS = [
 
 # Per-source flags.  decode.hip keeps its value-product accumulators in AGPRs named in inline
 # asm; the compiler's own MFMAs there are kept in VGPR form, so it never allocates an AGPR
-# (tests/test_abi.py checks the generated code for that).
+# (tests/test_abi.py checks the generated code for that).  paged_attn.hip likewise
+# (tests/test_paged_host.py).
 SOURCE_FLAGS = {
     "decode.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=true"],
+    "paged_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=true"],
 }
 
 

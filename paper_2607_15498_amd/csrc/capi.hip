@@ -725,7 +725,7 @@ static int check_paged_heads(const varrate_pages* pg, const varrate_batch* b, in
 
 size_t varrate_paged_attn_workspace_bytes(const varrate_pages* pg, const varrate_batch* b, int32_t H) {
     if (check_paged_heads(pg, b, H) || b->T == 0) return 0;
-    return paged_attn_ws_bytes(b->T, b->S, pg->G, H, (int64_t)b->width * pg->page);
+    return paged_attn_ws_bytes(b->T, b->S, pg->G, H, pg->dtype, (int64_t)b->width * pg->page);
 }
 
 int varrate_paged_attn(const varrate_pages* pg, const varrate_batch* b, const void* q, int64_t q_stride, int32_t H,
@@ -741,7 +741,7 @@ int varrate_paged_attn(const varrate_pages* pg, const varrate_batch* b, const vo
     if ((rc = check_rows(q, q_stride, b->T, H, pg->dtype, false, "q")) ||
         (rc = check_rows(out, out_stride, b->T, H, pg->dtype, true, "out"))) return rc;
     if (q == out) return fail(VARRATE_EINVAL, "out is q");
-    if ((rc = ws_check(ws, ws_bytes, paged_attn_ws_bytes(b->T, b->S, pg->G, H, (int64_t)b->width * pg->page)))) return rc;
+    if ((rc = ws_check(ws, ws_bytes, paged_attn_ws_bytes(b->T, b->S, pg->G, H, pg->dtype, (int64_t)b->width * pg->page)))) return rc;
     return hip_status(launch_paged_attn(*pg, *b, q, q_stride, H, causal, window, scale, out, out_stride, ws,
                                         (hipStream_t)stream),
                       "paged attention launch");

@@ -1,0 +1,850 @@
+// What the paged attention's kernels share: the call's cut, a piece's addresses and masks, the products of
+// 32-key blocks and the few-rows form.  The head of paged_attn.hip describes the whole.
+#pragma once
+#include "vr_internal.h"
+#include "vr_pages.h"
+
+namespace vr {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short pa_s16x4 __attribute__((ext_vector_type(4)));
+
+struct AttnArgs {
+    const void* q;
+    void* out;
+    const void* k;
+    const void* v;
+    const int32_t* table;
+    const int32_t* kv_len;
+    const int32_t* q_start;
+    float* rec;                     // cut calls: partial rows [rec_rows][128], then their [rec_rows][2] (max, sum)
+    int64_t q_stride, out_stride;   // elements between tokens
+    int64_t table_stride;
+    int64_t rec_rows;
+    int32_t T, S, cap, n_pages, G, Hg, shift;
+    int32_t causal, window, lmin;
+    float c;                        // softmax scale x log2 e
+};
+
+// rows of a bad page: 1 KB of zeros
+__device__ const uint4 pa_zeros[64] = {};
+
+// One direct-to-LDS load: 16 bytes per lane from base + off to LDS byte address dst + 16 lane.
+__device__ __forceinline__ void lds_load(const void* base, uint32_t off, uint32_t dst) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(dst)
+                 : "memory", "m0");
+}
+template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+__device__ __forceinline__ f32x16 mfma32(const u32x4& a, const u32x4& b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mfma32(float a, float b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0);
+}
+// a + both halves of a bf16 pair
+__device__ __forceinline__ float add_pair(uint32_t w, float a) {
+    const bf16x2_t one = {(__bf16)1.0f, (__bf16)1.0f};
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w), one, a, false);
+}
+
+// a value that all lanes hold, as a scalar
+__device__ __forceinline__ int32_t first_lane(int32_t v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int64_t first_lane(int64_t v) {
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((int32_t)(uint32_t)v);
+    return (int64_t)((uint64_t)(uint32_t)first_lane((int32_t)(v >> 32)) << 32 | lo);
+}
+
+// ---- the call's cut, computed by every wave from the device lengths ----------------------------
+template <typename V> __device__ __forceinline__ V wave_sum(V v) {
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) v += __shfl_xor(v, m, WAVE);
+    return first_lane(v);
+}
+__device__ __forceinline__ int32_t wave_most(int32_t v) {
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        const int32_t x = __shfl_xor(v, m, WAVE);
+        v = x > v ? x : v;
+    }
+    return first_lane(v);
+}
+__device__ __forceinline__ SeqRange load_range(const AttnArgs& a, int s) {
+    SeqRange r = {0, 0, 0};
+    if (s < a.S) r = seq_range(a.q_start[s], a.q_start[s + 1], a.kv_len[s], a.T, a.cap);
+    return r;
+}
+// `first`: the first 64 sequences, kept for find_unit
+template <int MANY> __device__ __forceinline__ int32_t wave_cut(const AttnArgs& a, SeqRange& first) {
+    const int lane = threadIdx.x & 63;
+    first = load_range(a, lane);
+    int64_t units = 0, work = 0;
+    int32_t longest = 0;
+    for (int s0 = 0; s0 < a.S; s0 += 64) {
+        const SeqRange r = s0 ? load_range(a, s0 + lane) : first;
+        const int64_t t = (int64_t)seq_tiles(r, a.Hg, MANY) * a.G;
+        const int32_t span = seq_span(r, a.window);
+        units += t;
+        work += t * span;
+        if (t && span > longest) longest = span;
+    }
+    longest = wave_most(longest);
+    if (longest <= a.lmin) return WHOLE;
+    units = wave_sum(units);
+    if (units >= PIECES_MAX) return WHOLE;
+    work = wave_sum(work);
+    int32_t best = WHOLE;
+    int64_t cost = cut_cost(units, longest, work, units);
+#pragma unroll 1
+    for (int i = 1; i < CUTS; ++i) {
+        const int32_t L = cut_try(i, work, a.lmin);
+        int64_t n = 0;
+        int32_t most = 0;
+        for (int s0 = 0; s0 < a.S; s0 += 64) {
+            const SeqRange r = s0 ? load_range(a, s0 + lane) : first;
+            const int32_t t = seq_tiles(r, a.Hg, MANY), span = seq_span(r, a.window), np = seq_pieces(span, L);
+            n += (int64_t)t * a.G * np;
+            const int32_t len = t ? piece_len(span, np) : 0;
+            if (len > most) most = len;
+        }
+        const int64_t c = cut_cost(wave_sum(n), wave_most(most), work, units);
+        if (c < cost) {
+            cost = c;
+            best = L;
+        }
+    }
+    return best;
+}
+// The sequence of piece number idx: its pieces are (tile, piece, head) triples, heads innermost and the
+// last tile first (with causal rows it sees the most keys).  base: the sequence's first number; rec: its
+// first row of partial results.
+struct Unit { SeqRange r; int32_t s, np; int64_t base, end, rec; };
+template <int MANY> __device__ __forceinline__ bool find_unit(const AttnArgs& a, int32_t L, const SeqRange& first, int64_t idx, Unit& u) {
+    const int lane = threadIdx.x & 63;
+    int64_t before = 0, rbefore = 0;
+    for (int s0 = 0; s0 < a.S; s0 += 64) {
+        const SeqRange r = s0 ? load_range(a, s0 + lane) : first;
+        const int32_t np = seq_pieces(seq_span(r, a.window), L);
+        const int64_t n = (int64_t)seq_tiles(r, a.Hg, MANY) * np * a.G, nr = np > 1 ? n * tile_rows(r, a.Hg, MANY) : 0;
+        int64_t up = n, rup = nr;              // inclusive scans over the lanes
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) {
+            const int64_t x = __shfl_up(up, m, WAVE), y = __shfl_up(rup, m, WAVE);
+            if (lane >= m) {
+                up += x;
+                rup += y;
+            }
+        }
+        const uint64_t hit = __ballot(before + up > idx);
+        if (hit) {
+            const int l = __builtin_ctzll(hit);
+            u.r.q0 = first_lane(__shfl(r.q0, l, WAVE));
+            u.r.qlen = first_lane(__shfl(r.qlen, l, WAVE));
+            u.r.klen = first_lane(__shfl(r.klen, l, WAVE));
+            u.np = first_lane(__shfl(np, l, WAVE));
+            u.base = first_lane(before + __shfl(up - n, l, WAVE));
+            u.end = first_lane(before + __shfl(up, l, WAVE));
+            u.rec = first_lane(rbefore + __shfl(rup - nr, l, WAVE));
+            u.s = first_lane(s0 + l);
+            return true;
+        }
+        before += first_lane(__shfl(up, 63, WAVE));
+        rbefore += first_lane(__shfl(rup, 63, WAVE));
+    }
+    return false;
+}
+
+template <typename ET>
+struct Form {
+    static constexpr bool BF = sizeof(ET) == 2;
+    static constexpr int ROWB = D * (int)sizeof(ET);       // bytes of a row
+    static constexpr int PPR = ROWB / 16;
+    static constexpr int NF = BF ? 8 : 16;                 // 16-byte fragments of a row per lane: pieces 2 k + h
+    static constexpr int CROWS = 4096 / ROWB;              // rows of a 4 KB chunk (one wave's 4 loads)
+    // few rows: per wave a ring of NST 32-key tiles [K, V]
+    static constexpr int KB = 32 * ROWB;
+    static constexpr int NST = BF ? 2 : 1;
+    static constexpr int RING = NST * 2 * KB;
+    static constexpr int CH = KB / 4096;
+    static constexpr int JOIN = 4 * 32 * (132 + 2) * 4;
+    // many rows: 4 stages of 16 KB of keys and as much of values, one chunk of each per wave
+    static constexpr int SB = 16384;
+    static constexpr int KT = SB / ROWB;                   // keys per stage: 64, fp32 32
+    static constexpr int SPS = KT / 32;                    // 32-key steps per stage
+    static constexpr int STAGES = 4;
+    static constexpr int NC = BF ? 2 : 1;                  // blocks of 32 rows per wave
+    static constexpr int MANY = 4 * NC * 32;
+    static constexpr size_t LDS = 128 * 1024;
+    static_assert(4 * RING <= (int)LDS && JOIN <= (int)LDS && STAGES * 2 * SB <= (int)LDS, "the two forms share it");
+};
+
+// What both forms need of a piece, and the operations on 32-key blocks.
+template <typename ET>
+struct Piece {
+    typedef Form<ET> F;
+    const AttnArgs& a;
+    SeqRange r;
+    int32_t g, lo, hi;                                     // KV head; keys of the piece
+    const uint8_t *kbase, *vbase;                          // the head's rows of page 0
+    const int32_t* trow;
+    int64_t head_bytes;
+    int lane, l32, h;
+    uint32_t off0, kaddr;
+
+    __device__ __forceinline__ Piece(const AttnArgs& a_, const Unit& u, int g_, int32_t lo_, int32_t hi_)
+        : a(a_), r(u.r), g(g_), lo(lo_), hi(hi_) {
+        head_bytes = (int64_t)F::ROWB << a.shift;
+        kbase = (const uint8_t*)a.k + (int64_t)g * head_bytes;
+        vbase = (const uint8_t*)a.v + (int64_t)g * head_bytes;
+        trow = a.table + (int64_t)u.s * a.table_stride;
+        lane = threadIdx.x & 63;
+        l32 = lane & 31;
+        h = lane >> 5;
+        const int lrow = lane / F::PPR;                    // the row that this lane loads of a 1 KB piece
+        off0 = (uint32_t)(lrow * F::ROWB + ((lane % F::PPR) ^ ((lrow & 3) << 2)) * 16);
+        kaddr = (uint32_t)(l32 * F::ROWB + (h ^ (((l32 & 3) << 2) | ((l32 >> 2) & 3))) * 16);
+    }
+    // the page of key t as the table has it (any entry of the sequence's behind its end)
+    __device__ __forceinline__ int32_t raw_page(int32_t t) const { return trow[(t < r.klen ? t : r.klen - 1) >> a.shift]; }
+    // and -1 for one that names none, and behind the end
+    __device__ __forceinline__ int32_t page_of(int32_t raw, int32_t t) const {
+        return t < r.klen ? good_page(raw, a.n_pages) : -1;
+    }
+    // rows t .. t + CROWS - 1 of page p (or zeros): address of the first, and the advance per 1 KB
+    __device__ __forceinline__ const uint8_t* rows_at(const uint8_t* pool, int32_t p, int32_t t) const {
+        const int32_t slot = t & ((1 << a.shift) - 1);
+        return (const uint8_t*)first_lane((int64_t)(
+            p >= 0 ? pool + (int64_t)p * a.G * head_bytes + (int64_t)slot * F::ROWB : (const uint8_t*)pa_zeros));
+    }
+    static __device__ __forceinline__ int advance(int32_t p) { return p >= 0 ? 1024 : 0; }
+    // 1 KB number v of them, chunk `ch` of its tile, into LDS at dst (of the chunk)
+    __device__ __forceinline__ void bring1(const uint8_t* src, int adv, int v, int ch, uint32_t dst) const {
+        // rows 4 v + .. (bf16) or 2 v + .. (fp32): the rest of f(row)
+        const uint32_t fx = F::BF ? (uint32_t)v & 3u : (uint32_t)(((v & 1) << 3) | (((v >> 1) + 2 * (ch & 1)) & 3));
+        lds_load(src + v * adv, off0 ^ (fx << 4), dst + v * 1024);
+    }
+    __device__ __forceinline__ void bring(const uint8_t* pool, int32_t p, int32_t t, int ch, uint32_t dst) const {
+        const uint8_t* src = rows_at(pool, p, t);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) bring1(src, advance(p), v, ch, dst);
+    }
+    // values behind the end in the rows [r0, r1) of a tile of keys from t0 on: not read as data
+    __device__ __forceinline__ void clear_tail(int32_t t0, int32_t r0, int32_t r1, uint8_t* vt) const {
+        const int32_t end = r.klen - t0, stop = (end + 15) & ~15;
+        const int32_t from = end > r0 ? end : r0, to = stop < r1 ? stop : r1;
+        for (int i = lane; i < (to - from) * F::PPR; i += 64)
+            *reinterpret_cast<uint4*>(vt + (from + i / F::PPR) * F::ROWB + (i % F::PPR) * 16) = uint4{0, 0, 0, 0};
+    }
+    // a row's query as B operand
+    __device__ __forceinline__ void query(u32x4 (&qf)[F::NF], int64_t token, int head) const {
+        const uint8_t* src = (const uint8_t*)((const ET*)a.q + token * a.q_stride + (int64_t)head * D);
+#pragma unroll
+        for (int k = 0; k < F::NF; ++k) qf[k] = load16(src + (2 * k + h) * 16);
+    }
+    __device__ __forceinline__ int key_of(int i) const { return 8 * (i >> 2) + 4 * h + (i & 3); }
+    // scores of NC blocks of 32 rows with 32 keys
+    template <int NC>
+    __device__ __forceinline__ void scores(const uint8_t* kt, const u32x4 (&qf)[NC][F::NF], f32x16 (&sc)[NC]) const {
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sc[c][i] = 0.f;
+#pragma unroll
+        for (int k = 0; k < F::NF; ++k) {
+            const u32x4 f = *reinterpret_cast<const u32x4*>(kt + (kaddr ^ (32u * k)));
+            if constexpr (F::BF) {
+#pragma unroll
+                for (int c = 0; c < NC; ++c) sc[c] = mfma32(f, qf[c][k], sc[c]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int c = 0; c < NC; ++c)
+                        sc[c] = mfma32(__uint_as_float(f[e]), __uint_as_float(qf[c][k][e]), sc[c]);
+            }
+        }
+    }
+    // keys of a block from t0 on that the row with keys [mylo, myhi) does not see; gm: 16-key groups with a page
+    __device__ __forceinline__ bool sees(int32_t t, int32_t mylo, int32_t myhi, uint32_t gm_bit) const {
+        return t >= mylo && t < myhi && t >= lo && t < hi && gm_bit;
+    }
+    __device__ __forceinline__ void mask(f32x16& sc, int32_t t0, int32_t mylo, int32_t myhi, uint32_t gm) const {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (!sees(t0 + key_of(i), mylo, myhi, gm >> (i >> 3) & 1u)) sc[i] = -INFINITY;
+    }
+    __device__ __forceinline__ float most(const f32x16& sc) const {
+        float m = sc[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) m = fmaxf(m, sc[i]);
+        return xmax32(m);
+    }
+    // V^T fragment, bf16: keys r0 + 4 h + 0..3 and r0 + 8 + 4 h + 0..3, dim 32 dt + l32
+    __device__ __forceinline__ u32x4 vfrag(const uint8_t* vt, int r0, int dt) const {
+        const int i16 = lane & 15, dh = (lane >> 4) & 1;
+        u32x4 f;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int row = r0 + 8 * e + 4 * h + (i16 >> 2);
+            const int place = (4 * dt + 2 * dh + ((i16 >> 1) & 1)) ^ (((i16 >> 2) << 2) | (2 * e + h));
+            const uint2 v = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (__attribute__((address_space(3))) pa_s16x4*)(vt + row * F::ROWB + place * 16 + (i16 & 1) * 8)));
+            f[2 * e] = v.x;
+            f[2 * e + 1] = v.y;
+        }
+        return f;
+    }
+    // fp32: key r0 + 4 h, dim 32 dt + l32
+    __device__ __forceinline__ float vfrag32(const uint8_t* vt, int r0, int dt) const {
+        const int row = r0 + 4 * h, f = ((row & 3) << 2) | ((row >> 2) & 3);
+        return *reinterpret_cast<const float*>(vt + row * F::ROWB + ((8 * dt + (l32 >> 2)) ^ f) * 16 + (l32 & 3) * 4);
+    }
+    // acc += V^T P^T of 32 keys; p: the weights, packed in pairs for bf16
+    template <int NC>
+    __device__ __forceinline__ void values(const uint8_t* vt, const u32x4 (&p)[NC][2], f32x16 (&acc)[NC][4]) const {
+#pragma unroll
+        for (int mm = 0; mm < 2; ++mm)
+#pragma unroll
+            for (int dt = 0; dt < 4; ++dt) {
+                const u32x4 f = vfrag(vt, 16 * mm, dt);
+#pragma unroll
+                for (int c = 0; c < NC; ++c) acc[c][dt] = mfma32(f, p[c][mm], acc[c][dt]);
+            }
+    }
+    template <int NC>
+    __device__ __forceinline__ void values(const uint8_t* vt, const f32x16 (&p)[NC], f32x16 (&acc)[NC][4]) const {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+#pragma unroll
+            for (int dt = 0; dt < 4; ++dt) {
+                const float f = vfrag32(vt, 8 * (i >> 2) + (i & 3), dt);
+#pragma unroll
+                for (int c = 0; c < NC; ++c) acc[c][dt] = mfma32(f, p[c][i], acc[c][dt]);
+            }
+    }
+    // A masked block whose values hold infinities or NaN: 0 x inf is not 0, so a row must not meet
+    // the values of keys that it does not see.  One key at a time, kept by the rows that see it.
+    __device__ __forceinline__ bool odd_values(const uint8_t* vt) const {
+        uint32_t odd = 0;
+        for (int i = lane; i < F::KB / 16; i += 64) {
+            const u32x4 w = *reinterpret_cast<const u32x4*>(vt + 16 * i);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                odd |= F::BF ? ((w[k] & 0x7F807F80u) + 0x00800080u) & 0x80008000u
+                             : ((w[k] & 0x7F800000u) + 0x00800000u) & 0x80000000u;
+        }
+        return __ballot(odd != 0) != 0;
+    }
+    template <typename P>
+    __device__ __forceinline__ void values_by_key(const uint8_t* vt, const P& p, f32x16& acc, int dt, int32_t t0, int32_t mylo,
+                                                  int32_t myhi, uint32_t gm) const {
+#pragma unroll 1
+        for (int kk = 0; kk < 32; ++kk) {                  // lanes of half (kk / 4) % 2 hold it
+            const bool see = sees(t0 + kk, mylo, myhi, gm >> (kk >> 4) & 1u);
+            const bool mine = ((kk >> 2) & 1) == h;
+            const int slot = 4 * ((kk >> 3) & 1) + (kk & 3);
+            f32x16 with;
+            if constexpr (F::BF) {
+                u32x4 keep, pk;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    keep[k] = mine && (slot >> 1) == k ? (slot & 1 ? 0xFFFF0000u : 0xFFFFu) : 0u;
+                    pk[k] = (kk < 16 ? p[0][k] : p[1][k]) & keep[k];
+                }
+                with = mfma32(vfrag(vt, kk & 16, dt) & keep, pk, acc);
+            } else {
+                float pf = 0.f;
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (i == 8 * (kk >> 4) + slot) pf = mine ? p[i] : 0.f;
+                const float v = vfrag32(vt, (kk & 16) + 8 * ((kk >> 3) & 1) + (kk & 3), dt);
+                with = mfma32(mine ? v : 0.f, pf, acc);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[i] = see ? with[i] : acc[i];
+        }
+    }
+};
+
+// weights exp2(c x + off) of 32 keys: packed in pairs and summed as rounded (bf16), or in place (fp32)
+__device__ __forceinline__ void weights(f32x16& sc, float c, float off, u32x4 (&p)[2], float& l) {
+    float l0 = 0.f, l1 = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const uint32_t w = cvt_bf16x2(__builtin_amdgcn_exp2f(fmaf(sc[2 * k], c, off)),
+                                      __builtin_amdgcn_exp2f(fmaf(sc[2 * k + 1], c, off)));
+        p[k >> 2][k & 3] = w;
+        if (k & 1) l1 = add_pair(w, l1);
+        else l0 = add_pair(w, l0);
+    }
+    l += l0 + l1;
+}
+__device__ __forceinline__ void weights(f32x16& sc, float c, float off, float& l) {
+    float l0 = 0.f, l1 = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+        sc[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], c, off));
+        sc[i + 1] = __builtin_amdgcn_exp2f(fmaf(sc[i + 1], c, off));
+        l0 += sc[i];
+        l1 += sc[i + 1];
+    }
+    l += l0 + l1;
+}
+
+// A row's running maximum m (of raw scores), off = -c m and its sum.  The maximum that the weights
+// are taken against follows the true one only when that is SLACK powers of two above it: the weights
+// then reach 2^SLACK, which neither bf16's exponent nor the fp32 sums mind, and the sums are rescaled
+// a few times per piece instead of at every block.
+constexpr float SLACK = 8.f;
+struct Running {
+    float m = -INFINITY, off = 0.f, l = 0.f;
+    // the factor for what has been summed so far
+    __device__ __forceinline__ float raise(float mt, float c) {
+        const float mn = fmaxf(m, mt), mu = mn == -INFINITY ? 0.f : mn;   // nothing seen yet: every weight is 0
+        const float f = __builtin_amdgcn_exp2f((m - mu) * c);
+        m = mn;
+        off = -mu * c;
+        l *= f;
+        return f;
+    }
+};
+
+template <typename ET>
+__device__ __forceinline__ void store4(ET* dst, float o0, float o1, float o2, float o3) {
+    if constexpr (sizeof(ET) == 2) *reinterpret_cast<uint2*>(dst) = uint2{cvt_bf16x2(o0, o1), cvt_bf16x2(o2, o3)};
+    else *reinterpret_cast<f32x4*>(dst) = f32x4{o0, o1, o2, o3};
+}
+
+// Few rows: rows 0 .. rows - 1 of the sequence's one tile.
+template <typename ET>
+__device__ __forceinline__ void few_rows(const Piece<ET>& P, uint8_t* smem, int rows, bool cut, int64_t rec_row) {
+    typedef Form<ET> F;
+    const AttnArgs& a = P.a;
+    const SeqRange& r = P.r;
+    const int wave = first_lane((int)(threadIdx.x >> 6)), lane = P.lane, l32 = P.l32, h = P.h;
+    const int Hg = a.Hg, g = P.g, lo = P.lo, hi = P.hi;
+    uint8_t* ring = smem + wave * F::RING;
+    const uint32_t ring0 = first_lane((int)(uint32_t)(size_t)(__attribute__((address_space(3))) uint8_t*)ring);
+    const int myrow = l32 < rows ? l32 : 0, tok = myrow / Hg;
+    int32_t mylo, myhi, firsthi, lastlo, x;
+    row_keys(r, tok, a.causal, a.window, mylo, myhi);
+    row_keys(r, 0, a.causal, a.window, x, firsthi);
+    row_keys(r, (rows - 1) / Hg, a.causal, a.window, lastlo, x);
+    u32x4 qf[1][F::NF];
+    P.query(qf[0], r.q0 + tok, g * Hg + myrow % Hg);
+    Running run;
+    f32x16 acc[1][4], sc[1];
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[0][dt][i] = 0.f;
+
+    // pages of the two 16-key groups of the wave's next 32 tiles, one a lane
+    constexpr int L = 4 * F::CH, step = 4 * 32;            // loads of a tile's keys (or values); keys to the next tile
+    int32_t window = 0, page[2];
+    int at = 32;
+    auto fetch = [&](int32_t t) {
+        if (at == 32) {
+            const int32_t tl = t + (lane >> 1) * step + (lane & 1) * 16;
+            window = P.page_of(P.raw_page(tl), tl);
+            at = 0;
+        }
+        page[0] = __builtin_amdgcn_readlane(window, 2 * at);
+        page[1] = __builtin_amdgcn_readlane(window, 2 * at + 1);
+        ++at;
+    };
+    auto bring = [&](const uint8_t* pool, int32_t t, uint32_t dst) {
+#pragma unroll
+        for (int c = 0; c < F::CH; ++c) P.bring(pool, page[c * F::CROWS / 16], t + c * F::CROWS, c, dst + c * 4096);
+    };
+    auto groups = [&]() { return (page[0] >= 0 ? 1u : 0u) | (page[1] >= 0 ? 2u : 0u); };
+    int32_t t0 = (lo & ~31) + 32 * wave;
+    uint32_t gm_in = 0;
+    if (t0 < hi) {
+        fetch(t0);
+        bring(P.kbase, t0, ring0);
+        bring(P.vbase, t0, ring0 + F::KB);
+        gm_in = groups();
+    }
+    for (int st = 0; t0 < hi; t0 += step) {
+        const uint32_t gm = gm_in;
+        uint8_t* kt = ring + st * 2 * F::KB;
+        const int32_t tn = t0 + step;
+        const bool more = tn < hi;
+        const bool masked = t0 < lastlo || t0 < lo || t0 + 32 > firsthi || t0 + 32 > hi || gm != 3u;
+        u32x4 p[1][2];
+        auto softmax = [&]() {
+            P.template scores<1>(kt, qf, sc);
+            if (masked) P.mask(sc[0], t0, mylo, myhi, gm);
+            const float mt = P.most(sc[0]);
+            if (__any(mt > run.m + SLACK / a.c)) {
+                const float f = run.raise(mt, a.c);
+#pragma unroll
+                for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[0][dt][i] *= f;
+            }
+            if constexpr (F::BF) weights(sc[0], a.c, run.off, p[0], run.l);
+            else weights(sc[0], a.c, run.off, run.l);
+        };
+        if constexpr (F::NST == 2) {
+            st ^= 1;
+            const uint32_t next = ring0 + st * 2 * F::KB;
+            wait_lds();                                    // the other tile has been read
+            if (more) {
+                fetch(tn);
+                bring(P.kbase, tn, next);
+                bring(P.vbase, tn, next + F::KB);
+                gm_in = groups();
+                wait_loads<3 * L>();
+            } else wait_loads<L>();
+            softmax();
+            if (more) wait_loads<2 * L>();
+            else wait_loads<0>();
+        } else {
+            wait_loads<L>();
+            softmax();
+            wait_lds();                                    // the keys have been read
+            if (more) {
+                fetch(tn);
+                bring(P.kbase, tn, ring0);
+                wait_loads<L>();
+            } else wait_loads<0>();
+        }
+        uint8_t* vt = kt + F::KB;
+        P.clear_tail(t0, 0, 32, vt);
+        if constexpr (F::BF) {
+            if (masked && P.odd_values(vt))
+#pragma unroll
+                for (int dt = 0; dt < 4; ++dt) P.values_by_key(vt, p[0], acc[0][dt], dt, t0, mylo, myhi, gm);
+            else P.template values<1>(vt, p, acc);
+        } else {
+            if (masked && P.odd_values(vt))
+#pragma unroll
+                for (int dt = 0; dt < 4; ++dt) P.values_by_key(vt, sc[0], acc[0][dt], dt, t0, mylo, myhi, gm);
+            else P.template values<1>(vt, sc, acc);
+            wait_lds();                                    // the values have been read
+            if (more) {
+                bring(P.vbase, tn, ring0 + F::KB);
+                gm_in = groups();
+            }
+        }
+    }
+    run.l = xsum32(run.l);
+    __syncthreads();                                       // every wave is done with its ring
+    float* js = (float*)smem;                              // [4][32][132] sums
+    float* jm = js + 4 * 32 * 132;                         // [4][32][2]
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+            *reinterpret_cast<f32x4*>(js + (wave * 32 + l32) * 132 + 32 * dt + 2 * i + 4 * h) =
+                f32x4{acc[0][dt][i], acc[0][dt][i + 1], acc[0][dt][i + 2], acc[0][dt][i + 3]};
+    if (h == 0) *reinterpret_cast<float2*>(jm + (wave * 32 + l32) * 2) = float2{run.m, run.l};
+    __syncthreads();
+    const int row = threadIdx.x >> 3, d0 = 16 * (threadIdx.x & 7);
+    if (row < rows) {
+        float mw[4], lw[4], M = -INFINITY, Ls = 0.f, o[16];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float2 v = *reinterpret_cast<const float2*>(jm + (w * 32 + row) * 2);
+            mw[w] = v.x;
+            lw[w] = v.y;
+            M = fmaxf(M, v.x);
+        }
+        const float mu = M == -INFINITY ? 0.f : M;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[i] = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float f = __builtin_amdgcn_exp2f((mw[w] - mu) * a.c);
+            Ls = fmaf(f, lw[w], Ls);
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const f32x4 v = *reinterpret_cast<const f32x4*>(js + (w * 32 + row) * 132 + d0 + i);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) o[i + k] = fmaf(f, v[k], o[i + k]);
+            }
+        }
+        if (cut) {
+            float* dst = a.rec + (rec_row + row) * D + d0;
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) *reinterpret_cast<f32x4*>(dst + i) = f32x4{o[i], o[i + 1], o[i + 2], o[i + 3]};
+            if (d0 == 0) *reinterpret_cast<float2*>(a.rec + a.rec_rows * D + (rec_row + row) * 2) = float2{M, Ls};
+        } else {
+            const float inv = Ls == 0.f ? 0.f : 1.f / Ls;
+            ET* dst = (ET*)a.out + (int64_t)(r.q0 + row / Hg) * a.out_stride + (int64_t)(g * Hg + row % Hg) * D + d0;
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) store4<ET>(dst + i, o[i] * inv, o[i + 1] * inv, o[i + 2] * inv, o[i + 3] * inv);
+        }
+    }
+    __syncthreads();                                       // the rings are free again
+}
+
+
+// Many rows, what bf16 and fp32 share: rows row0 .. row0 + rows - 1 of the sequence, 32 NC of them a wave,
+// the key stages and which steps of 32 keys the wave's rows see.
+template <typename ET>
+struct Many {
+    typedef Form<ET> F;
+    static constexpr int NC = F::NC;
+    const Piece<ET>& P;
+    uint8_t* smem;
+    uint32_t lds0;
+    int wave, crow;                                        // crow: first row of the wave's chunk of a stage
+    int32_t row0, rows, wrow, t_first, stages;
+    int32_t jf, jl, mf, ml;                                // steps that some row sees: [jf, jl), every row whole: [mf, ml)
+    // pages of the 16-key groups of a window of 64 groups, one a lane: the one that is being brought, the raw
+    // entries of the next, and which groups of the last two windows have a page
+    static constexpr int SPW = 1024 / F::KT;               // stages per window
+    int32_t window, raw;
+    uint64_t has[2];
+    bool bad;                                              // some key before the end has had none
+    const uint8_t *ksrc, *vsrc;                            // of the stage that is being brought
+    int adv;
+    uint32_t dst;
+
+    __device__ __forceinline__ Many(const Piece<ET>& P_, uint8_t* smem_, int32_t row0_, int32_t rows_)
+        : P(P_), smem(smem_), row0(row0_), rows(rows_) {
+        const AttnArgs& a = P.a;
+        lds0 = first_lane((int)(uint32_t)(size_t)(__attribute__((address_space(3))) uint8_t*)smem);
+        wave = first_lane((int)(threadIdx.x >> 6));
+        crow = wave * F::CROWS;
+        wrow = 32 * NC * wave;
+        t_first = P.lo & ~(F::KT - 1);
+        stages = P.hi > P.lo ? (P.hi - t_first + F::KT - 1) / F::KT : 0;
+        jf = jl = mf = ml = 0;
+        window = raw = 0;
+        has[0] = has[1] = 0;
+        bad = false;
+        ksrc = vsrc = nullptr;
+        adv = 0;
+        dst = 0;
+        const int32_t n = rows - wrow < 32 * NC ? rows - wrow : 32 * NC;
+        if (n > 0) {
+            int32_t lo0, hi0, lo1, hi1;
+            row_keys(P.r, (row0 + wrow) / a.Hg, a.causal, a.window, lo0, hi0);
+            row_keys(P.r, (row0 + wrow + n - 1) / a.Hg, a.causal, a.window, lo1, hi1);
+            jf = first_lane(within(lo0) >> 5);
+            jl = first_lane((within(hi1) + 31) >> 5);
+            mf = first_lane((within(lo1) + 31) >> 5);
+            ml = first_lane(within(hi0) >> 5);
+        }
+    }
+    // token (of the sequence) and query head of lane l32's row of block c, and the keys that it sees
+    __device__ __forceinline__ void row_of(int c, int l32, int32_t& tok, int32_t& head) const {
+        const int32_t i = wrow + 32 * c + l32, row = row0 + (i < rows ? i : 0);
+        tok = row / P.a.Hg;
+        head = P.g * P.a.Hg + row % P.a.Hg;
+    }
+    __device__ __forceinline__ void keys_seen(int c, int l32, int32_t& lo, int32_t& hi) const {
+        int32_t tok, head;
+        row_of(c, l32, tok, head);
+        row_keys(P.r, tok, P.a.causal, P.a.window, lo, hi);
+    }
+    __device__ __forceinline__ int32_t within(int32_t t) const { return (t < P.lo ? P.lo : t > P.hi ? P.hi : t) - t_first; }
+    __device__ __forceinline__ int32_t window_key(int w) const { return t_first + 1024 * w + 16 * P.lane; }
+    // stage s is to be brought: its addresses ...
+    __device__ __forceinline__ void aim(int s) {
+        const int w = s / SPW, in = s % SPW;
+        if (in == 0) {                                     // a new window: its entries were asked for half a window ago
+            if (w == 0) raw = P.raw_page(window_key(0));
+            window = P.page_of(raw, window_key(w));
+            const uint64_t m = __ballot(window >= 0);
+            bad = bad || __ballot(window < 0 && window_key(w) < P.r.klen) != 0;
+            if (w & 1) has[1] = m;
+            else has[0] = m;
+        }
+        if (in == SPW / 2) raw = P.raw_page(window_key(w + 1));
+        const int32_t page = __builtin_amdgcn_readlane(window, (in * F::KT + crow) / 16);
+        const int32_t t = t_first + s * F::KT + crow;
+        ksrc = P.rows_at(P.kbase, page, t);
+        vsrc = P.rows_at(P.vbase, page, t);
+        adv = P.advance(page);
+        dst = lds0 + (s & 3) * 2 * F::SB + wave * 4096;
+    }
+    // ... and its 8 loads, the keys' first
+    __device__ __forceinline__ void bring(int i) const {
+        if (i < 4) P.bring1(ksrc, adv, i, wave, dst);
+        else P.bring1(vsrc, adv, i - 4, wave, dst + F::SB);
+    }
+    __device__ __forceinline__ void issue(int s) {
+        aim(s);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) bring(i);
+    }
+    __device__ __forceinline__ void begin() {
+        if (stages > 0) issue(0);
+        if (stages > 1) issue(1);
+    }
+    // stage s has arrived, and stage s - 2 is free (every wave is past it): stage s + 2 may follow
+    __device__ __forceinline__ void arrive(int s) const {
+        if (s + 1 < stages) wait_loads<8>();
+        else wait_loads<0>();
+        P.clear_tail(t_first + s * F::KT, crow, crow + F::CROWS, smem + (s & 3) * 2 * F::SB + F::SB);
+        __syncthreads();
+    }
+    // which 16-key groups of step j have a page (j within two windows of what is being brought)
+    __device__ __forceinline__ uint32_t gm_of(int j) const {
+        return (uint32_t)((j >> 5 & 1 ? has[1] : has[0]) >> (2 * (j & 31))) & 3u;
+    }
+    __device__ __forceinline__ uint8_t* keys_of(int j) const { return smem + (j / F::SPS & 3) * 2 * F::SB + (j % F::SPS) * F::KB; }
+    __device__ __forceinline__ uint8_t* values_of(int j) const { return keys_of(j) + F::SB; }
+    __device__ __forceinline__ bool masked(int j) const { return j < mf || j >= ml || gm_of(j) != 3u; }
+    // block c's rows: sums (of 32 dims dt) and, with `last`, maximum and sum
+    __device__ __forceinline__ void put(int c, int dt, const f32x16& o, const Running& run, float l, bool cut, int64_t rec_row,
+                                        bool last) const {
+        const AttnArgs& a = P.a;
+        const int i0 = wrow + 32 * c + P.l32;
+        if (i0 >= rows) return;
+        if (cut) {
+            float* dst = a.rec + (rec_row + i0) * D + 32 * dt + 4 * P.h;
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) *reinterpret_cast<f32x4*>(dst + 2 * i) = f32x4{o[i], o[i + 1], o[i + 2], o[i + 3]};
+            if (last && P.h == 0) *reinterpret_cast<float2*>(a.rec + a.rec_rows * D + (rec_row + i0) * 2) = float2{run.m, l};
+        } else {
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            int32_t tok, head;
+            row_of(c, P.l32, tok, head);
+            ET* dst = (ET*)a.out + (int64_t)(P.r.q0 + tok) * a.out_stride + (int64_t)head * D + 32 * dt + 4 * P.h;
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) store4<ET>(dst + 2 * i, o[i] * inv, o[i + 1] * inv, o[i + 2] * inv, o[i + 3] * inv);
+        }
+    }
+};
+
+template <typename ET>
+__device__ void many_rows(const Piece<ET>& P, uint8_t* smem, int32_t row0, int32_t rows, bool cut, int64_t rec_row);
+
+// grid: at most one workgroup per slot, a multiple of 8.  Workgroup b takes piece numbers b, then the
+// numbers of each further round in turned order (the pieces of a sequence shrink along its numbers;
+// turning gives every workgroup long and short ones), b % 8 kept: heads stay on their XCD's L2.
+template <typename ET>
+__global__ __launch_bounds__(256, 1) void paged_attn_kernel(AttnArgs a) {
+    constexpr int MANY = Form<ET>::MANY;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    SeqRange first;
+    const int32_t L = wave_cut<MANY>(a, first);
+    Unit u;
+    u.base = 0;
+    u.end = 0;
+    for (int round = 0;; ++round) {
+        const uint32_t b = blockIdx.x, n = gridDim.x;
+        const int64_t idx = (int64_t)round * n + (round & 1 ? ((n - 1 - b) & ~7u) | (b & 7u) : b);
+        if (idx >= u.end && !find_unit<MANY>(a, L, first, idx, u)) break;
+        const SeqRange r = u.r;
+        const uint32_t in = (uint32_t)(idx - u.base), G = (uint32_t)a.G;
+        const int g = (int)(in % G), piece = (int)(in / G % (uint32_t)u.np);
+        const int tile = seq_tiles(r, a.Hg, MANY) - 1 - (int)(in / G / (uint32_t)u.np);
+        const int bm = tile_rows(r, a.Hg, MANY);
+        const int32_t row0 = tile * bm;
+        const int32_t rows = (int32_t)(seq_rows(r, a.Hg) - row0 < bm ? seq_rows(r, a.Hg) - row0 : bm);
+        // keys that the tile's rows see, and of them this piece
+        int32_t lo, hi, x;
+        row_keys(r, row0 / a.Hg, a.causal, a.window, lo, x);
+        row_keys(r, (row0 + rows - 1) / a.Hg, a.causal, a.window, x, hi);
+        const bool cut = u.np > 1;
+        if (cut) {
+            const int32_t len = piece_len(seq_span(r, a.window), u.np);
+            const int64_t p0 = seq_first(r, a.window) + (int64_t)piece * len;
+            if (lo < p0) lo = (int32_t)(p0 < r.klen ? p0 : r.klen);
+            if (hi > p0 + len) hi = (int32_t)(p0 + len);
+        }
+        lo = first_lane(lo);
+        hi = first_lane(hi > lo ? hi : lo);                // an empty piece: no keys, weight 0
+        const int64_t rec_row = u.rec + (int64_t)in * bm;
+        if (cut && rec_row + bm > a.rec_rows) continue;    // starts that fall: no room for their pieces (uniform)
+        const Piece<ET> P(a, u, g, lo, hi);
+        if (bm == ROWS_FEW) few_rows<ET>(P, smem, rows, cut, rec_row);
+        else many_rows<ET>(P, smem, row0, rows, cut, rec_row);
+    }
+}
+
+// Joins the pieces of cut sequences, up to JOIN_ROWS rows of a tile a workgroup: its waves take every
+// fourth row of many, or of few rows every fourth piece of one.
+constexpr int JOIN_ROWS = 32;
+template <typename ET>
+__global__ __launch_bounds__(256) void paged_join_kernel(AttnArgs a) {
+    constexpr int MANY = Form<ET>::MANY;
+    __shared__ float so[4][D];
+    __shared__ float sl[4];
+    SeqRange first;
+    const int32_t L = wave_cut<MANY>(a, first);
+    if (L == WHOLE) return;
+    const int wave = first_lane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
+    const float* rec_ml = a.rec + a.rec_rows * D;
+    Unit u;
+    u.base = u.end = 0;
+    // work numbers: piece numbers x JOIN parts; the parts of piece 0 of every tile do the joining
+    constexpr int parts = MANY / JOIN_ROWS;
+    for (int64_t w = blockIdx.x;; w += gridDim.x) {
+        const int64_t idx = w / parts;
+        const int part = (int)(w % parts);
+        if ((idx >= u.end || idx < u.base) && !find_unit<MANY>(a, L, first, idx, u)) break;
+        const uint32_t in = (uint32_t)(idx - u.base), G = (uint32_t)a.G;
+        if (u.np <= 1 || in / G % (uint32_t)u.np != 0) continue;
+        const SeqRange r = u.r;
+        const int g = (int)(in % G), tile = seq_tiles(r, a.Hg, MANY) - 1 - (int)(in / G / (uint32_t)u.np);
+        const int bm = tile_rows(r, a.Hg, MANY);
+        const int32_t row0 = tile * bm;
+        const int32_t rows = (int32_t)(seq_rows(r, a.Hg) - row0 < bm ? seq_rows(r, a.Hg) - row0 : bm);
+        const int64_t rec0 = u.rec + (int64_t)in * bm, stride = (int64_t)G * bm;   // piece p's rows: rec0 + p stride
+        if (rec0 + (u.np - 1) * stride + bm > a.rec_rows) continue;
+        const bool few = bm == ROWS_FEW;
+        // few rows: parts share the rows out, one row at a time for the whole workgroup
+        for (int i = few ? part : part * JOIN_ROWS + wave; i < rows && (few || i < (part + 1) * JOIN_ROWS); i += few ? parts : 4) {
+            float M = -INFINITY;
+            for (int p = lane; p < u.np; p += 64) M = fmaxf(M, rec_ml[(rec0 + p * stride + i) * 2]);
+#pragma unroll
+            for (int x = 1; x < 64; x <<= 1) M = fmaxf(M, __shfl_xor(M, x, WAVE));
+            const float mu = M == -INFINITY ? 0.f : M;
+            float o0 = 0.f, o1 = 0.f, l = 0.f;
+#pragma unroll 4
+            for (int p = few ? wave : 0; p < u.np; p += few ? 4 : 1) {
+                const int64_t rr = rec0 + p * stride + i;
+                const float2 ml = *reinterpret_cast<const float2*>(rec_ml + rr * 2);
+                const float2 v = *reinterpret_cast<const float2*>(a.rec + rr * D + 2 * lane);
+                const float f = __builtin_amdgcn_exp2f((ml.x - mu) * a.c);
+                l = fmaf(f, ml.y, l);
+                o0 = fmaf(f, v.x, o0);
+                o1 = fmaf(f, v.y, o1);
+            }
+            if (few) {
+                __syncthreads();
+                so[wave][2 * lane] = o0;
+                so[wave][2 * lane + 1] = o1;
+                if (lane == 0) sl[wave] = l;
+                __syncthreads();
+                if (wave) continue;
+                l = (sl[0] + sl[1]) + (sl[2] + sl[3]);
+                o0 = (so[0][2 * lane] + so[1][2 * lane]) + (so[2][2 * lane] + so[3][2 * lane]);
+                o1 = (so[0][2 * lane + 1] + so[1][2 * lane + 1]) + (so[2][2 * lane + 1] + so[3][2 * lane + 1]);
+            }
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            const int32_t row = row0 + i;
+            ET* dst = (ET*)a.out + (int64_t)(r.q0 + row / a.Hg) * a.out_stride + (int64_t)(g * a.Hg + row % a.Hg) * D + 2 * lane;
+            if constexpr (sizeof(ET) == 2) *reinterpret_cast<uint32_t*>(dst) = cvt_bf16x2(o0 * inv, o1 * inv);
+            else *reinterpret_cast<float2*>(dst) = float2{o0 * inv, o1 * inv};
+        }
+    }
+}
+
+// SLOTS workgroups, and the second launch unless the tables are too short for a cut
+template <typename ET>
+hipError_t launch_paged(const AttnArgs& a, int64_t pieces, hipStream_t st) {
+    const void* fn = (const void*)paged_attn_kernel<ET>;
+    hipError_t e = ensure_lds_limit(fn, Form<ET>::LDS);
+    if (e != hipSuccess) return e;
+    const unsigned grid = pieces < SLOTS ? ((unsigned)pieces + 7) & ~7u : SLOTS;
+    paged_attn_kernel<ET><<<grid, 256, Form<ET>::LDS, st>>>(a);
+    if ((e = hipGetLastError()) != hipSuccess || a.cap <= a.lmin) return e;
+    const int64_t parts = pieces * (Form<ET>::MANY / JOIN_ROWS);
+    paged_join_kernel<ET><<<(unsigned)(parts < 2048 ? parts : 2048), 256, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t launch_paged_bf16(const AttnArgs& a, int64_t pieces, hipStream_t st);
+hipError_t launch_paged_f32(const AttnArgs& a, int64_t pieces, hipStream_t st);
+
+}  // namespace vr

@@ -138,7 +138,7 @@ struct NormRotate {
 hipError_t launch_norm_rotate(int dtype, const NormRotate& n, hipStream_t st);
 hipError_t launch_paged_append(const varrate_pages& pg, const varrate_batch& b, const void* k, int64_t k_stride,
                                const void* v, int64_t v_stride, const float* theta, hipStream_t st);
-size_t paged_attn_ws_bytes(int64_t T, int S, int G, int H, int64_t cap);
+size_t paged_attn_ws_bytes(int64_t T, int S, int G, int H, int dtype, int64_t cap);
 hipError_t launch_paged_attn(const varrate_pages& pg, const varrate_batch& b, const void* q, int64_t q_stride, int H,
                              int causal, int window, float scale, void* out, int64_t out_stride, void* ws,
                              hipStream_t st);

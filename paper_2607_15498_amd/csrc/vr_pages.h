@@ -47,12 +47,21 @@ VR_HD int find_seq(const int32_t* q_start, int S, int32_t i) {
 VR_HD int32_t good_page(int32_t page, int32_t n_pages) { return page >= 0 && page < n_pages ? page : -1; }
 
 // ---- how the attention is cut ----------------------------------------------------------------
-// The rows of one (sequence, KV head) are its qlen x Hg (new token, query head) pairs, token-major,
-// in tiles of BM rows; the keys that any of the sequence's rows sees, [first, klen), are cut into
-// pieces of L tokens.  L is one number for the whole call, so that long sequences get more pieces.
-struct Cut { int64_t units; int64_t L; };      // units: (sequence, tile) pairs; L: tokens per piece
+// The rows of one (sequence, KV head) are its qlen x Hg (new token, query head) pairs, token-major.
+// Up to ROWS_FEW of them make one tile, whose keys a workgroup's waves divide among themselves; more
+// are cut into tiles of `many` rows (256, fp32 128), which the waves divide.  The keys that any of the sequence's
+// rows sees are cut into equal pieces, of about L tokens at most: one number for the whole call, so
+// that long sequences get more pieces.
+constexpr int ROWS_FEW = 32;
+constexpr int SLOTS = 256;                     // workgroups that the card holds at once (one per CU)
+constexpr int32_t WHOLE = INT32_MAX;           // L of a call that is not cut
 
-VR_HD int32_t seq_tiles(SeqRange r, int Hg, int BM) { return (int32_t)(((int64_t)r.qlen * Hg + BM - 1) / BM); }
+VR_HD int64_t seq_rows(SeqRange r, int Hg) { return (int64_t)r.qlen * Hg; }
+VR_HD int tile_rows(SeqRange r, int Hg, int many) { return seq_rows(r, Hg) <= ROWS_FEW ? ROWS_FEW : many; }
+VR_HD int32_t seq_tiles(SeqRange r, int Hg, int many) {
+    const int bm = tile_rows(r, Hg, many);
+    return (int32_t)((seq_rows(r, Hg) + bm - 1) / bm);
+}
 // first key that the sequence's first row sees, at a multiple of 64
 VR_HD int32_t seq_first(SeqRange r, int window) {
     if (!window) return 0;
@@ -60,22 +69,50 @@ VR_HD int32_t seq_first(SeqRange r, int window) {
     return f > 0 ? (int32_t)(f < r.klen ? f : r.klen) & ~63 : 0;
 }
 VR_HD int32_t seq_span(SeqRange r, int window) { return r.klen - seq_first(r, window); }
-// piece length from the sums over the sequences of tiles and tiles x span: about `target` pieces
-// over all G heads, none shorter than lmin; without splitting when there are units enough
-VR_HD int64_t cut_len(int64_t units, int64_t work, int G, int target, int lmin) {
-    if (units * G >= target) return INT64_MAX / 2;
-    const int64_t per = (work * G + target - 1) / target;
-    const int64_t L = (per + 127) / 128 * 128;
-    return L < lmin ? lmin : L;
+VR_HD int32_t seq_pieces(int32_t span, int32_t L) {
+    return span <= L ? 1 : (int32_t)(((uint32_t)span + (uint32_t)L - 1) / (uint32_t)L);
 }
-VR_HD int32_t seq_pieces(int32_t span, int64_t L) {
-    return span <= L ? 1 : (int32_t)((span + L - 1) / L);
+// tokens of each of a span's np pieces
+VR_HD int32_t piece_len(int32_t span, int np) {
+    return np == 1 ? span : (int32_t)((((uint32_t)span + (uint32_t)np - 1) / (uint32_t)np + 63) & ~63u);
 }
-// most (unit, head, piece) triples of any call with T rows and S sequences
-VR_HD int64_t max_pieces(int64_t T, int S, int G, int Hg, int BM, int target, int64_t cap, int lmin) {
-    const int64_t units = G * (T * Hg / BM + (S < T ? S : T));
-    const int64_t most = units * ((cap + lmin - 1) / lmin);   // no piece is shorter than lmin
-    return units + target < most ? units + target : most;
+
+// How many pieces: the cut with the shortest estimated time, in tokens that one workgroup passes.
+// Candidate 0 is uncut; candidate i aims at i pieces for every slot.  A cut into P pieces
+// takes ceil(P / SLOTS) rounds of the longest piece and COST_PIECE (its start and its end) each, and
+// COST_JOIN for the second launch.
+constexpr int CUTS = 5;
+constexpr int PIECES_MAX = 4 * SLOTS;          // of a cut call (an uncut one may have any number)
+constexpr int COST_PIECE = 128, COST_JOIN = 256;
+// work: sum of tiles x span over sequences and heads
+VR_HD int32_t cut_try(int i, int64_t work, int lmin) {
+    if (i == 0) return WHOLE;
+    const int64_t slot = (work + SLOTS - 1) / SLOTS;
+    const uint32_t L = ((uint32_t)(slot < (1 << 30) ? slot : (1 << 30)) + (uint32_t)i - 1) / (uint32_t)i;
+    return L < (uint32_t)lmin ? lmin : (int32_t)((L + 63) & ~63u);
+}
+// pieces: all of them; longest: tokens of the longest; units: pieces of the uncut call
+VR_HD int64_t cut_cost(int64_t pieces, int64_t longest, int64_t work, int64_t units) {
+    if (pieces > units && pieces > PIECES_MAX) return INT64_MAX;
+    const int64_t rounds = (pieces + SLOTS - 1) / SLOTS;
+    int64_t t = rounds * longest;
+    // unlike pieces even out over several rounds (a sequence's longest come first)
+    if (rounds > 1 && t > work / SLOTS + longest) t = work / SLOTS + longest;
+    return t + rounds * COST_PIECE + (pieces > units ? COST_JOIN : 0);
+}
+
+// most pieces of any call with T rows and S sequences whose tables hold `cap` tokens
+VR_HD int64_t max_pieces(int64_t T, int S, int G, int Hg, int many, int64_t cap, int lmin) {
+    const int64_t units = G * (T * Hg / many + (S < T ? S : T));
+    const int64_t most = units * ((cap + lmin - 1) / lmin);
+    const int64_t cut = most < PIECES_MAX ? most : PIECES_MAX;
+    return units > cut ? units : cut;
+}
+// most rows of partial results
+VR_HD int64_t max_records(int64_t T, int S, int G, int Hg, int many, int64_t cap, int lmin) {
+    if (cap <= lmin) return 0;
+    const int64_t p = max_pieces(T, S, G, Hg, many, cap, lmin);
+    return (p < PIECES_MAX ? p : PIECES_MAX) * (T * Hg <= ROWS_FEW ? ROWS_FEW : many);
 }
 
 // Keys [lo, hi) that row `row` of the sequence sees (none when hi <= lo).

@@ -8,9 +8,11 @@ Bounds, element by element, with u the rounding of a type (half a step: bf16 2^-
   attention          scores: 128 products summed in fp32, 128 u32 c sum|q k|; the exponent's own
                      product and sum 3 u32 (|c x| + |c m|) and the exponential 2 u32.  A weight's
                      error is at most twice that exponent error D (in maximum and in sum).  Weights
-                     of bf16 layers are rounded: u.  Sums of n weighted values: n u32.  With A =
-                     sum p |v| / sum p: |error| <= (u_p + 4 D + (n + 256) u32) A + u |o|, and the
-                     rounding of the output is of a value that far off: another (1 + u).
+                     of bf16 layers are rounded, u, in their products with the values and in their
+                     sum alike: sum p e (v - o) / sum p, at most u (A + |o|) with A = sum p |v| /
+                     sum p.  Sums of n weighted values: n u32.  Together |error| <= u_p (A + |o|) +
+                     (4 D + (n + 256) u32) A, and the rounding of the output, u |o|, is of a value
+                     that far off: another (1 + u).
   append, gather     copies are exact; a rotated key as above.
 """
 import math
@@ -231,7 +233,7 @@ def attn_ref(pool, q, q_len, H, causal=True, window=0, scale=None):
                 mag = c * (k.abs() @ x.abs())
                 dx = float((128 * U32 * mag + 3 * U32 * (sc.abs() + sc.abs().max())).max()) + 2 * U32
                 u = U[pool.dtype]
-                e = ((u if pool.dtype == "bf16" else 0) + 4 * dx + (len(t) + 256) * U32) * A
+                e = (u if pool.dtype == "bf16" else 0) * (A + o.abs()) + (4 * dx + (len(t) + 256) * U32) * A
                 ref[at + i, h] = o
                 tol[at + i, h] = (e + u * o.abs()) * (1 + u) + 1e-38
         at += m
