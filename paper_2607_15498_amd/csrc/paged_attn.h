@@ -168,7 +168,7 @@ struct Form {
     static constexpr int RING = NST * 2 * KB;
     static constexpr int CH = KB / 4096;
     static constexpr int JOIN = 4 * 32 * (132 + 2) * 4;
-    // many rows: 4 stages of 16 KB of keys and as much of values, one chunk of each per wave
+    // many rows: 4 stages of 16 KB of keys, then as many of values; one chunk of each per wave
     static constexpr int SB = 16384;
     static constexpr int KT = SB / ROWB;                   // keys per stage: 64, fp32 32
     static constexpr int SPS = KT / 32;                    // 32-key steps per stage
@@ -176,6 +176,7 @@ struct Form {
     static constexpr int NC = BF ? 2 : 1;                  // blocks of 32 rows per wave
     static constexpr int MANY = 4 * NC * 32;
     static constexpr size_t LDS = 128 * 1024;
+    static_assert(SB == SPS * KB, "steps follow each other");
     static_assert(4 * RING <= (int)LDS && JOIN <= (int)LDS && STAGES * 2 * SB <= (int)LDS, "the two forms share it");
 };
 
@@ -662,12 +663,12 @@ struct Many {
         ksrc = P.rows_at(P.kbase, page, t);
         vsrc = P.rows_at(P.vbase, page, t);
         adv = P.advance(page);
-        dst = lds0 + (s & 3) * 2 * F::SB + wave * 4096;
+        dst = lds0 + (s & 3) * F::SB + wave * 4096;
     }
     // ... and its 8 loads, the keys' first
     __device__ __forceinline__ void bring(int i) const {
         if (i < 4) P.bring1(ksrc, adv, i, wave, dst);
-        else P.bring1(vsrc, adv, i - 4, wave, dst + F::SB);
+        else P.bring1(vsrc, adv, i - 4, wave, dst + F::STAGES * F::SB);
     }
     __device__ __forceinline__ void issue(int s) {
         aim(s);
@@ -675,22 +676,26 @@ struct Many {
         for (int i = 0; i < 8; ++i) bring(i);
     }
     __device__ __forceinline__ void begin() {
-        if (stages > 0) issue(0);
-        if (stages > 1) issue(1);
+        issue(0);
+        issue(1);
     }
-    // stage s has arrived, and stage s - 2 is free (every wave is past it): stage s + 2 may follow
+    // Stage s has arrived, and stage s - 2 is free (every wave is past it): stage s + 2 follows.  Every stage is
+    // followed by others, so that the counts stay the same; those behind the last bring rows that nothing reads.
     __device__ __forceinline__ void arrive(int s) const {
-        if (s + 1 < stages) wait_loads<8>();
-        else wait_loads<0>();
-        P.clear_tail(t_first + s * F::KT, crow, crow + F::CROWS, smem + (s & 3) * 2 * F::SB + F::SB);
+        wait_loads<8>();
+        P.clear_tail(t_first + s * F::KT, crow, crow + F::CROWS, smem + (F::STAGES + (s & 3)) * F::SB);
         __syncthreads();
+    }
+    __device__ __forceinline__ void finish() const {
+        wait_loads<0>();
+        __syncthreads();                                   // the stages are free again
     }
     // which 16-key groups of step j have a page (j within two windows of what is being brought)
     __device__ __forceinline__ uint32_t gm_of(int j) const {
         return (uint32_t)((j >> 5 & 1 ? has[1] : has[0]) >> (2 * (j & 31))) & 3u;
     }
-    __device__ __forceinline__ uint8_t* keys_of(int j) const { return smem + (j / F::SPS & 3) * 2 * F::SB + (j % F::SPS) * F::KB; }
-    __device__ __forceinline__ uint8_t* values_of(int j) const { return keys_of(j) + F::SB; }
+    __device__ __forceinline__ uint8_t* keys_of(int j) const { return smem + ((uint32_t)j * F::KB & (F::STAGES * F::SB - 1)); }
+    __device__ __forceinline__ uint8_t* values_of(int j) const { return keys_of(j) + F::STAGES * F::SB; }
     __device__ __forceinline__ bool masked(int j) const { return j < mf || j >= ml || gm_of(j) != 3u; }
     // block c's rows: sums (of 32 dims dt) and, with `last`, maximum and sum
     __device__ __forceinline__ void put(int c, int dt, const f32x16& o, const Running& run, float l, bool cut, int64_t rec_row,

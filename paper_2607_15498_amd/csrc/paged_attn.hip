@@ -69,7 +69,7 @@ __device__ __forceinline__ void settle() { asm volatile("s_nop 15\n\ts_nop 3" ::
 template <int K, bool WAIT = false> __device__ __forceinline__ void score(f32x16& s0, f32x16& s1, const u32x4& f) {
     constexpr int q0 = QBASE + 4 * K, q1 = QBASE + 4 * (8 + K);
 #define PA_SCORE(pre, c0, c1, o) asm volatile(pre "v_mfma_f32_32x32x16_bf16 %0, %2, a[%3:%4], " c0 "\n\t" \
-    "v_mfma_f32_32x32x16_bf16 %1, %2, a[%5:%6], " c1 : o(s0), o(s1) : "v"(f), "n"(q0), "n"(q0 + 3), "n"(q1), "n"(q1 + 3))
+    "v_mfma_f32_32x32x16_bf16 %1, %2, a[%5:%6], " c1 : o(s0), o(s1) : "v"(f), "n"(q0), "n"(q0 + 3), "n"(q1), "n"(q1 + 3) : PA_AGPRS)
     if constexpr (K == 0 && WAIT) PA_SCORE("s_nop 3\n\t", "0", "0", "=&v");
     else if constexpr (K == 0) PA_SCORE("", "0", "0", "=&v");
     else if constexpr (WAIT) PA_SCORE("s_nop 3\n\t", "%0", "%1", "+v");
@@ -81,7 +81,7 @@ template <int DT, bool WAIT = false> __device__ __forceinline__ void value(const
     constexpr int a0 = 16 * DT, a1 = 16 * (4 + DT);
 #define PA_VALUE(pre) asm volatile(pre "v_mfma_f32_32x32x16_bf16 a[%3:%4], %0, %1, a[%3:%4]\n\t" \
     "v_mfma_f32_32x32x16_bf16 a[%5:%6], %0, %2, a[%5:%6]" \
-    ::"v"(f), "v"(p0), "v"(p1), "n"(a0), "n"(a0 + 15), "n"(a1), "n"(a1 + 15))
+    ::"v"(f), "v"(p0), "v"(p1), "n"(a0), "n"(a0 + 15), "n"(a1), "n"(a1 + 15) : PA_AGPRS)
     if constexpr (WAIT) PA_VALUE("s_nop 3\n\t");
     else PA_VALUE("");
 #undef PA_VALUE
@@ -99,7 +99,7 @@ __device__ __forceinline__ void many_rows<uint16_t>(const Piece<uint16_t>& P, ui
     typedef Form<uint16_t> F;
     const AttnArgs& a = P.a;
     Many<uint16_t> M(P, smem, row0, rows);
-    M.begin();
+    if (M.stages) M.begin();
     Running run[2];
     settle();
     static_for<128>([&](auto i) { agpr_set<i>(0u); });
@@ -118,47 +118,47 @@ __device__ __forceinline__ void many_rows<uint16_t>(const Piece<uint16_t>& P, ui
     f32x16 sc[2][2];
     u32x4 p[2][2][2];
     float pend[2] = {1.f, 1.f}, limit[2] = {-INFINITY, -INFINITY};       // limit: scores above it raise the maximum
+    float mx[2] = {-INFINITY, -INFINITY};                  // this lane's maxima of the last step's scores
     bool pending = false;
-    // m0, m1: the maxima of step j's scores in this lane; after the value products of j - 2
-    auto close = [&](float m0, float m1) {
-        if (pending) {                                     // the products of j - 2 were of the old maximum
+    // Before the weights of step j - 1, after its scores and the value products of j - 3.
+    auto follow = [&]() {
+        if (!(__any(mx[0] > limit[0] || mx[1] > limit[1]) || pending)) return;
+        if (pending) {                                     // the products of j - 3 were of the old maximum
             settle();
             static_for<128>([&](auto i) { agpr_set<i>(__float_as_uint(agpr_get<i>() * pend[i / 64])); });
             settle();
             pending = false;
         }
-        if (__any(m0 > limit[0] || m1 > limit[1])) {
-            pend[0] = run[0].raise(xmax32(m0), a.c);       // and those of j - 1 will be: scaled after them
-            pend[1] = run[1].raise(xmax32(m1), a.c);
+        if (__any(mx[0] > limit[0] || mx[1] > limit[1])) {
+            pend[0] = run[0].raise(xmax32(mx[0]), a.c);    // and those of j - 2 will be: scaled after them
+            pend[1] = run[1].raise(xmax32(mx[1]), a.c);
             limit[0] = run[0].m + slack;
             limit[1] = run[1].m + slack;
             pending = true;
         }
     };
     auto kfrag = [&](int j, int k) { return *reinterpret_cast<const u32x4*>(M.keys_of(j) + (P.kaddr ^ (32u * k))); };
-    // two weights of block c of step j - 1 (e: the parity of j)
-    auto pair = [&](auto par, int c, int k) {
+    // two weights of block c of step j - 1 (e: the parity of j): the exponentials, and packing and summing them
+    float ea, eb;
+    auto weigh = [&](auto par, int c, int k) {
         constexpr int e = decltype(par)::value;
-        uint32_t w = cvt_bf16x2(__builtin_amdgcn_exp2f(fmaf(sc[1 - e][c][2 * k], a.c, run[c].off)),
-                                __builtin_amdgcn_exp2f(fmaf(sc[1 - e][c][2 * k + 1], a.c, run[c].off)));
-        asm volatile("" : "+v"(w));                        // here, not where it is used
+        ea = __builtin_amdgcn_exp2f(fmaf(sc[1 - e][c][2 * k], a.c, run[c].off));
+        eb = __builtin_amdgcn_exp2f(fmaf(sc[1 - e][c][2 * k + 1], a.c, run[c].off));
+    };
+    auto pack = [&](auto par, int c, int k) {
+        constexpr int e = decltype(par)::value;
+        uint32_t w = cvt_bf16x2(ea, eb);
+        run[c].l += ea;
+        run[c].l += eb;
+        asm volatile("" : "+v"(w), "+v"(run[c].l));        // here, not where it is used
         p[1 - e][c][k >> 2][k & 3] = w;
-        run[c].l = add_pair(w, run[c].l);
-        asm volatile("" : "+v"(run[c].l));
     };
-    // The next stage and the one to follow it: an odd step waits for the stage of the step after it and brings
-    // the first half of two stages on, the next even one the second half.
+    // An odd step waits for the stage of the step after it and brings the first half of two stages on, the next
+    // even one the second half.
     auto stage_ready = [&](int j) {
-        const int s = (j + 1) / 2;
-        if (s < M.stages) M.arrive(s);
-        if (s + 2 < M.stages) M.aim(s + 2);
-    };
-    auto bring_half = [&](auto par, int j) {
-        constexpr int e = decltype(par)::value;
-        const int s = (j + 1) / 2;
-        if (s >= 1 && s + 2 < M.stages)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) M.bring(4 * (1 - e) + i);
+        const int s = (j + 1) >> 1;
+        M.arrive(s);
+        M.aim(s + 2);
     };
     // step j with nothing to mask in j and j - 2; kf: its key fragments, replaced by those of j + 1
     auto fast = [&](auto par, int j, u32x4 (&kf)[8]) {
@@ -169,15 +169,22 @@ __device__ __forceinline__ void many_rows<uint16_t>(const Piece<uint16_t>& P, ui
         static_for<8>([&](auto k) {
             score<k>(s0, s1, kf[k]);
             vf[k] = P.vfrag(vt, 16 * (k >> 2), k & 3);
-            pair(par, 0, k);
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (k == 0) follow();
+            if constexpr (k >= 1) pack(par, 0, k - 1);
+            weigh(par, 0, k);
             __builtin_amdgcn_sched_barrier(0);
         });
         if constexpr (e == 1) stage_ready(j);
-        float m0 = -INFINITY, m1 = -INFINITY;
+        mx[0] = mx[1] = -INFINITY;
         static_for<8>([&](auto n) {
             value<n & 3>(vf[n], p[e][0][n >> 2], p[e][1][n >> 2]);
             kf[n] = kfrag(j + 1, n);
-            pair(par, 1, n);
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (n == 0) pack(par, 0, 7);
+            else pack(par, 1, n - 1);
+            weigh(par, 1, n);
+            if constexpr (n >= 2 && n < 6) M.bring(4 * (1 - e) + n - 2);
             // the scores' last products were issued before the two pairs of value products that have gone
             // by, each product 8 passes long: they are there
             if constexpr (n == 1) asm volatile("" : "+v"(s0), "+v"(s1));
@@ -185,13 +192,12 @@ __device__ __forceinline__ void many_rows<uint16_t>(const Piece<uint16_t>& P, ui
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
                     if (i * 6 / 8 == n - 2) {
-                        asm volatile("v_max3_f32 %0, %0, %1, %2" : "+v"(m0) : "v"(s0[2 * i]), "v"(s0[2 * i + 1]));
-                        asm volatile("v_max3_f32 %0, %0, %1, %2" : "+v"(m1) : "v"(s1[2 * i]), "v"(s1[2 * i + 1]));
+                        asm volatile("v_max3_f32 %0, %0, %1, %2" : "+v"(mx[0]) : "v"(s0[2 * i]), "v"(s0[2 * i + 1]));
+                        asm volatile("v_max3_f32 %0, %0, %1, %2" : "+v"(mx[1]) : "v"(s1[2 * i]), "v"(s1[2 * i + 1]));
                     }
             __builtin_amdgcn_sched_barrier(0);
         });
-        bring_half(par, j);
-        close(m0, m1);
+        pack(par, 1, 7);
     };
     // any step
     auto slow = [&](auto par, int j) {
@@ -202,11 +208,15 @@ __device__ __forceinline__ void many_rows<uint16_t>(const Piece<uint16_t>& P, ui
         // the lane's numbers anew, or what the masks need of them is kept in registers for the whole loop
         Piece<uint16_t> L = P;
         asm volatile("" : "+v"(L.lane), "+v"(L.l32), "+v"(L.h));
+        follow();
         if (ex)
 #pragma unroll
             for (int c = 0; c < 2; ++c)
 #pragma unroll
-                for (int k = 0; k < 8; ++k) pair(par, c, k);
+                for (int k = 0; k < 8; ++k) {
+                    weigh(par, c, k);
+                    pack(par, c, k);
+                }
         if (pv) {
             settle();
             if (M.masked(j - 2) && L.odd_values(vt)) {
@@ -227,7 +237,7 @@ __device__ __forceinline__ void many_rows<uint16_t>(const Piece<uint16_t>& P, ui
                     value<n & 3, true>(f, p[e][0][n >> 2], p[e][1][n >> 2]);
                 });
         }
-        float m0 = -INFINITY, m1 = -INFINITY;
+        mx[0] = mx[1] = -INFINITY;
         if (qk) {
             static_for<8>([&](auto k) { score<k, true>(s0, s1, kfrag(j, k)); });
             settle();
@@ -241,21 +251,22 @@ __device__ __forceinline__ void many_rows<uint16_t>(const Piece<uint16_t>& P, ui
                 }
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                m0 = fmaxf(m0, s0[i]);
-                m1 = fmaxf(m1, s1[i]);
+                mx[0] = fmaxf(mx[0], s0[i]);
+                mx[1] = fmaxf(mx[1], s1[i]);
             }
         }
         if constexpr (e == 1) stage_ready(j);
-        bring_half(par, j);
-        close(m0, m1);
+        if (e == 1 || j > 0)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) M.bring(4 * (1 - e) + i);
     };
     const std::integral_constant<int, 0> even{};
     const std::integral_constant<int, 1> odd{};
-    if (M.stages > 0) {
+    if (M.stages) {
         M.arrive(0);
-        if (M.stages > 2) M.issue(2);
+        M.issue(2);
     }
-    const int32_t end = 2 * M.stages + 2;                  // one stage's steps more: the last weights and values
+    const int32_t end = M.stages ? 2 * M.stages + 2 : 0;   // one stage's steps more: the last weights and values
     for (int j = 0; j < end;) {
         if (j >= M.mf + 2 && j + 1 < M.ml && !M.bad) {
             u32x4 kf[8];
@@ -281,7 +292,7 @@ __device__ __forceinline__ void many_rows<uint16_t>(const Piece<uint16_t>& P, ui
             M.put(c, dt, o, run[c], l, cut, rec_row, dt == 3);
         });
     });
-    __syncthreads();                                       // the stages are free again
+    M.finish();
 }
 
 hipError_t launch_paged_bf16(const AttnArgs& a, int64_t pieces, hipStream_t st) { return launch_paged<uint16_t>(a, pieces, st); }

@@ -9,7 +9,7 @@ __device__ __forceinline__ void many_rows<float>(const Piece<float>& P, uint8_t*
                                                  int64_t rec_row) {
     const AttnArgs& a = P.a;
     Many<float> M(P, smem, row0, rows);
-    M.begin();
+    if (M.stages) M.begin();
     Running run;
     u32x4 qf[1][16];
     int32_t tok, head, mylo, myhi;
@@ -24,7 +24,7 @@ __device__ __forceinline__ void many_rows<float>(const Piece<float>& P, uint8_t*
     const float slack = SLACK / a.c;
     for (int j = 0; j < M.stages; ++j) {
         M.arrive(j);
-        if (j + 2 < M.stages) M.issue(j + 2);
+        M.issue(j + 2);
         if (j < M.jf || j >= M.jl) continue;
         f32x16 sc[1];
         P.template scores<1>(M.keys_of(j), qf, sc);
@@ -48,7 +48,7 @@ __device__ __forceinline__ void many_rows<float>(const Piece<float>& P, uint8_t*
     const float l = xsum32(run.l);
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt) M.put(0, dt, acc[0][dt], run, l, cut, rec_row, dt == 3);
-    __syncthreads();                                       // the stages are free again
+    M.finish();
 }
 
 hipError_t launch_paged_f32(const AttnArgs& a, int64_t pieces, hipStream_t st) { return launch_paged<float>(a, pieces, st); }
