@@ -212,11 +212,13 @@ struct Piece {
     __device__ __forceinline__ int32_t page_of(int32_t raw, int32_t t) const {
         return t < r.klen ? good_page(raw, a.n_pages) : -1;
     }
+    // where the rows from t on of page p lie in a head's rows of the pool
+    __device__ __forceinline__ int64_t offset_of(int32_t p, int32_t t) const {
+        return (int64_t)p * a.G * head_bytes + (int64_t)(t & ((1 << a.shift) - 1)) * F::ROWB;
+    }
     // rows t .. t + CROWS - 1 of page p (or zeros): address of the first, and the advance per 1 KB
     __device__ __forceinline__ const uint8_t* rows_at(const uint8_t* pool, int32_t p, int32_t t) const {
-        const int32_t slot = t & ((1 << a.shift) - 1);
-        return (const uint8_t*)first_lane((int64_t)(
-            p >= 0 ? pool + (int64_t)p * a.G * head_bytes + (int64_t)slot * F::ROWB : (const uint8_t*)pa_zeros));
+        return (const uint8_t*)first_lane((int64_t)(p >= 0 ? pool + offset_of(p, t) : (const uint8_t*)pa_zeros));
     }
     static __device__ __forceinline__ int advance(int32_t p) { return p >= 0 ? 1024 : 0; }
     // 1 KB number v of them, chunk `ch` of its tile, into LDS at dst (of the chunk)
@@ -599,7 +601,8 @@ struct Many {
     // pages of the 16-key groups of a window of 64 groups, one a lane: the one that is being brought, the raw
     // entries of the next, and which groups of the last two windows have a page
     static constexpr int SPW = 1024 / F::KT;               // stages per window
-    int32_t window, raw;
+    int32_t raw;
+    const uint8_t *kwin, *vwin;                            // of the window: its groups' first rows
     uint64_t has[2];
     bool bad;                                              // some key before the end has had none
     const uint8_t *ksrc, *vsrc;                            // of the stage that is being brought
@@ -616,7 +619,8 @@ struct Many {
         t_first = P.lo & ~(F::KT - 1);
         stages = P.hi > P.lo ? (P.hi - t_first + F::KT - 1) / F::KT : 0;
         jf = jl = mf = ml = 0;
-        window = raw = 0;
+        raw = 0;
+        kwin = vwin = nullptr;
         has[0] = has[1] = 0;
         bad = false;
         ksrc = vsrc = nullptr;
@@ -646,23 +650,30 @@ struct Many {
     }
     __device__ __forceinline__ int32_t within(int32_t t) const { return (t < P.lo ? P.lo : t > P.hi ? P.hi : t) - t_first; }
     __device__ __forceinline__ int32_t window_key(int w) const { return t_first + 1024 * w + 16 * P.lane; }
+    static __device__ __forceinline__ const uint8_t* lane_of(const uint8_t* p, int lane) {
+        const uint64_t v = (uint64_t)p;
+        return (const uint8_t*)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 |
+                                (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane));
+    }
     // stage s is to be brought: its addresses ...
     __device__ __forceinline__ void aim(int s) {
         const int w = s / SPW, in = s % SPW;
         if (in == 0) {                                     // a new window: its entries were asked for half a window ago
             if (w == 0) raw = P.raw_page(window_key(0));
-            window = P.page_of(raw, window_key(w));
-            const uint64_t m = __ballot(window >= 0);
-            bad = bad || __ballot(window < 0 && window_key(w) < P.r.klen) != 0;
+            const int32_t t = window_key(w), page = P.page_of(raw, t);
+            const uint64_t m = __ballot(page >= 0);
+            bad = bad || __ballot(page < 0 && t < P.r.klen) != 0;
+            kwin = page >= 0 ? P.kbase + P.offset_of(page, t) : (const uint8_t*)pa_zeros;
+            vwin = page >= 0 ? P.vbase + P.offset_of(page, t) : (const uint8_t*)pa_zeros;
             if (w & 1) has[1] = m;
             else has[0] = m;
         }
         if (in == SPW / 2) raw = P.raw_page(window_key(w + 1));
-        const int32_t page = __builtin_amdgcn_readlane(window, (in * F::KT + crow) / 16);
-        const int32_t t = t_first + s * F::KT + crow;
-        ksrc = P.rows_at(P.kbase, page, t);
-        vsrc = P.rows_at(P.vbase, page, t);
-        adv = P.advance(page);
+        const int group = (in * F::KT + crow) / 16;
+        adv = (w & 1 ? has[1] : has[0]) >> group & 1 ? 1024 : 0;
+        const int rest = adv ? crow % 16 * F::ROWB : 0;
+        ksrc = lane_of(kwin, group) + rest;
+        vsrc = lane_of(vwin, group) + rest;
         dst = lds0 + (s & 3) * F::SB + wave * 4096;
     }
     // ... and its 8 loads, the keys' first

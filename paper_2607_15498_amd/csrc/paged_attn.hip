@@ -65,23 +65,22 @@ __device__ __forceinline__ void settle() { asm volatile("s_nop 15\n\ts_nop 3" ::
 // A product may not follow within 2 wait states the vector instruction that wrote one of its operands.  The
 // interleaved steps read theirs from LDS or an iteration before (the test of the generated code looks for
 // that); elsewhere WAIT.
-// s += K Q^T of fragment k, both blocks; k = 0 starts them
-template <int K, bool WAIT = false> __device__ __forceinline__ void score(f32x16& s0, f32x16& s1, const u32x4& f) {
-    constexpr int q0 = QBASE + 4 * K, q1 = QBASE + 4 * (8 + K);
-#define PA_SCORE(pre, c0, c1, o) asm volatile(pre "v_mfma_f32_32x32x16_bf16 %0, %2, a[%3:%4], " c0 "\n\t" \
-    "v_mfma_f32_32x32x16_bf16 %1, %2, a[%5:%6], " c1 : o(s0), o(s1) : "v"(f), "n"(q0), "n"(q0 + 3), "n"(q1), "n"(q1 + 3) : PA_AGPRS)
-    if constexpr (K == 0 && WAIT) PA_SCORE("s_nop 3\n\t", "0", "0", "=&v");
-    else if constexpr (K == 0) PA_SCORE("", "0", "0", "=&v");
-    else if constexpr (WAIT) PA_SCORE("s_nop 3\n\t", "%0", "%1", "+v");
-    else PA_SCORE("", "%0", "%1", "+v");
+// s += K Q^T of fragment K, block C; K = 0 starts it
+template <int K, int C, bool WAIT = false> __device__ __forceinline__ void score(f32x16& s, const u32x4& f) {
+    constexpr int q = QBASE + 4 * (8 * C + K);
+#define PA_SCORE(pre, c, o) \
+    asm volatile(pre "v_mfma_f32_32x32x16_bf16 %0, %1, a[%2:%3], " c : o(s) : "v"(f), "n"(q), "n"(q + 3) : PA_AGPRS)
+    if constexpr (K == 0 && WAIT) PA_SCORE("s_nop 3\n\t", "0", "=&v");
+    else if constexpr (K == 0) PA_SCORE("", "0", "=&v");
+    else if constexpr (WAIT) PA_SCORE("s_nop 3\n\t", "%0", "+v");
+    else PA_SCORE("", "%0", "+v");
 #undef PA_SCORE
 }
-// sums of dims 32 DT .. += V^T P^T, both blocks
-template <int DT, bool WAIT = false> __device__ __forceinline__ void value(const u32x4& f, const u32x4& p0, const u32x4& p1) {
-    constexpr int a0 = 16 * DT, a1 = 16 * (4 + DT);
-#define PA_VALUE(pre) asm volatile(pre "v_mfma_f32_32x32x16_bf16 a[%3:%4], %0, %1, a[%3:%4]\n\t" \
-    "v_mfma_f32_32x32x16_bf16 a[%5:%6], %0, %2, a[%5:%6]" \
-    ::"v"(f), "v"(p0), "v"(p1), "n"(a0), "n"(a0 + 15), "n"(a1), "n"(a1 + 15) : PA_AGPRS)
+// sums of block C, dims 32 DT .. += V^T P^T
+template <int DT, int C, bool WAIT = false> __device__ __forceinline__ void value(const u32x4& f, const u32x4& p) {
+    constexpr int o = 16 * (4 * C + DT);
+#define PA_VALUE(pre) \
+    asm volatile(pre "v_mfma_f32_32x32x16_bf16 a[%2:%3], %0, %1, a[%2:%3]" ::"v"(f), "v"(p), "n"(o), "n"(o + 15) : PA_AGPRS)
     if constexpr (WAIT) PA_VALUE("s_nop 3\n\t");
     else PA_VALUE("");
 #undef PA_VALUE
@@ -91,8 +90,10 @@ template <int DT, bool WAIT = false> __device__ __forceinline__ void value(const
 // (32 keys) has two halves: in the first the scores of j are formed while the exponentials of the first block of
 // j - 1 are taken and the value fragments of j - 2 are read, in the second the value products of j - 2 while the
 // exponentials of the second block and the maximum of j are taken and the key fragments of j + 1 are read; each
-// half is 16 products of 32 cycles, about as much vector work, and every second step one stage's 8 loads.  A step
-// that needs a mask, the first two and the last two go through the same one after another.
+// half is 16 products of 32 cycles, about as much vector work, and half of a stage's 8 loads in the second.  A wave
+// issues in order, and a product waits for the one before it: between any two stand about 32 cycles of other work
+// (two products back to back, then twice as much: 117 cycles a pair instead of 90).  A step that needs a mask, the
+// first two and the last two go through the same one after another.
 template <>
 __device__ __forceinline__ void many_rows<uint16_t>(const Piece<uint16_t>& P, uint8_t* smem, int32_t row0, int32_t rows,
                                                     bool cut, int64_t rec_row) {
@@ -119,6 +120,7 @@ __device__ __forceinline__ void many_rows<uint16_t>(const Piece<uint16_t>& P, ui
     u32x4 p[2][2][2];
     float pend[2] = {1.f, 1.f}, limit[2] = {-INFINITY, -INFINITY};       // limit: scores above it raise the maximum
     float mx[2] = {-INFINITY, -INFINITY};                  // this lane's maxima of the last step's scores
+    float lb[2] = {0.f, 0.f};                              // every second weight's part of the sums
     bool pending = false;
     // Before the weights of step j - 1, after its scores and the value products of j - 3.
     auto follow = [&]() {
@@ -132,6 +134,8 @@ __device__ __forceinline__ void many_rows<uint16_t>(const Piece<uint16_t>& P, ui
         if (__any(mx[0] > limit[0] || mx[1] > limit[1])) {
             pend[0] = run[0].raise(xmax32(mx[0]), a.c);    // and those of j - 2 will be: scaled after them
             pend[1] = run[1].raise(xmax32(mx[1]), a.c);
+            lb[0] *= pend[0];
+            lb[1] *= pend[1];
             limit[0] = run[0].m + slack;
             limit[1] = run[1].m + slack;
             pending = true;
@@ -149,8 +153,8 @@ __device__ __forceinline__ void many_rows<uint16_t>(const Piece<uint16_t>& P, ui
         constexpr int e = decltype(par)::value;
         uint32_t w = cvt_bf16x2(ea, eb);
         run[c].l += ea;
-        run[c].l += eb;
-        asm volatile("" : "+v"(w), "+v"(run[c].l));        // here, not where it is used
+        lb[c] += eb;
+        asm volatile("" : "+v"(w), "+v"(run[c].l), "+v"(lb[c]));     // here, not where they are used
         p[1 - e][c][k >> 2][k & 3] = w;
     };
     // An odd step waits for the stage of the step after it and brings the first half of two stages on, the next
@@ -167,24 +171,25 @@ __device__ __forceinline__ void many_rows<uint16_t>(const Piece<uint16_t>& P, ui
         const uint8_t* vt = M.values_of(j - 2);
         u32x4 vf[8];
         static_for<8>([&](auto k) {
-            score<k>(s0, s1, kf[k]);
-            vf[k] = P.vfrag(vt, 16 * (k >> 2), k & 3);
-            __builtin_amdgcn_sched_barrier(0);
+            score<k, 0>(s0, kf[k]);
             if constexpr (k == 0) follow();
-            if constexpr (k >= 1) pack(par, 0, k - 1);
             weigh(par, 0, k);
+            __builtin_amdgcn_sched_barrier(0);
+            score<k, 1>(s1, kf[k]);
+            vf[k] = P.vfrag(vt, 16 * (k >> 2), k & 3);
+            pack(par, 0, k);
             __builtin_amdgcn_sched_barrier(0);
         });
         if constexpr (e == 1) stage_ready(j);
         mx[0] = mx[1] = -INFINITY;
         static_for<8>([&](auto n) {
-            value<n & 3>(vf[n], p[e][0][n >> 2], p[e][1][n >> 2]);
-            kf[n] = kfrag(j + 1, n);
-            __builtin_amdgcn_sched_barrier(0);
-            if constexpr (n == 0) pack(par, 0, 7);
-            else pack(par, 1, n - 1);
+            value<n & 3, 0>(vf[n], p[e][0][n >> 2]);
             weigh(par, 1, n);
             if constexpr (n >= 2 && n < 6) M.bring(4 * (1 - e) + n - 2);
+            __builtin_amdgcn_sched_barrier(0);
+            value<n & 3, 1>(vf[n], p[e][1][n >> 2]);
+            kf[n] = kfrag(j + 1, n);
+            pack(par, 1, n);
             // the scores' last products were issued before the two pairs of value products that have gone
             // by, each product 8 passes long: they are there
             if constexpr (n == 1) asm volatile("" : "+v"(s0), "+v"(s1));
@@ -197,7 +202,6 @@ __device__ __forceinline__ void many_rows<uint16_t>(const Piece<uint16_t>& P, ui
                     }
             __builtin_amdgcn_sched_barrier(0);
         });
-        pack(par, 1, 7);
     };
     // any step
     auto slow = [&](auto par, int j) {
@@ -234,12 +238,17 @@ __device__ __forceinline__ void many_rows<uint16_t>(const Piece<uint16_t>& P, ui
             } else
                 static_for<8>([&](auto n) {
                     const u32x4 f = L.vfrag(vt, 16 * (n >> 2), n & 3);
-                    value<n & 3, true>(f, p[e][0][n >> 2], p[e][1][n >> 2]);
+                    value<n & 3, 0, true>(f, p[e][0][n >> 2]);
+                    value<n & 3, 1, true>(f, p[e][1][n >> 2]);
                 });
         }
         mx[0] = mx[1] = -INFINITY;
         if (qk) {
-            static_for<8>([&](auto k) { score<k, true>(s0, s1, kfrag(j, k)); });
+            static_for<8>([&](auto k) {
+                const u32x4 f = kfrag(j, k);
+                score<k, 0, true>(s0, f);
+                score<k, 1, true>(s1, f);
+            });
             settle();
             asm volatile("" : "+v"(s0), "+v"(s1));
             if (M.masked(j))
@@ -285,7 +294,7 @@ __device__ __forceinline__ void many_rows<uint16_t>(const Piece<uint16_t>& P, ui
     }
     settle();
     static_for<2>([&](auto c) {
-        const float l = xsum32(run[c].l);
+        const float l = xsum32(run[c].l + lb[c]);
         static_for<4>([&](auto dt) {
             f32x16 o;
             static_for<16>([&](auto i) { o[i.value] = agpr_get<16 * (4 * c + dt) + i>(); });
