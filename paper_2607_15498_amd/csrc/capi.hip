@@ -741,7 +741,8 @@ int varrate_paged_attn(const varrate_pages* pg, const varrate_batch* b, const vo
     if ((rc = check_rows(q, q_stride, b->T, H, pg->dtype, false, "q")) ||
         (rc = check_rows(out, out_stride, b->T, H, pg->dtype, true, "out"))) return rc;
     if (q == out) return fail(VARRATE_EINVAL, "out is q");
-    if ((rc = ws_check(ws, ws_bytes, paged_attn_ws_bytes(b->T, b->S, pg->G, H, pg->dtype, (int64_t)b->width * pg->page)))) return rc;
+    const size_t need = paged_attn_ws_bytes(b->T, b->S, pg->G, H, pg->dtype, (int64_t)b->width * pg->page);
+    if (need && (rc = ws_check(ws, ws_bytes, need))) return rc;
     return hip_status(launch_paged_attn(*pg, *b, q, q_stride, H, causal, window, scale, out, out_stride, ws,
                                         (hipStream_t)stream),
                       "paged attention launch");

@@ -56,15 +56,19 @@ __device__ __forceinline__ int64_t first_lane(int64_t v) {
     return (int64_t)((uint64_t)(uint32_t)first_lane((int32_t)(v >> 32)) << 32 | lo);
 }
 
+__device__ __forceinline__ int64_t lane64(int64_t v, int lane) {
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 |
+                     (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane));
+}
+
 // ---- the call's cut, computed by every wave from the device lengths ----------------------------
-template <typename V> __device__ __forceinline__ V wave_sum(V v) {
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) v += __shfl_xor(v, m, WAVE);
+// Reductions over the first `n` lanes (the others hold nothing), to a scalar.
+template <typename V> __device__ __forceinline__ V wave_sum(V v, int n) {
+    for (int m = 1; m < n; m <<= 1) v += __shfl_xor(v, m, WAVE);
     return first_lane(v);
 }
-__device__ __forceinline__ int32_t wave_most(int32_t v) {
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
+__device__ __forceinline__ int32_t wave_most(int32_t v, int n) {
+    for (int m = 1; m < n; m <<= 1) {
         const int32_t x = __shfl_xor(v, m, WAVE);
         v = x > v ? x : v;
     }
@@ -75,10 +79,11 @@ __device__ __forceinline__ SeqRange load_range(const AttnArgs& a, int s) {
     if (s < a.S) r = seq_range(a.q_start[s], a.q_start[s + 1], a.kv_len[s], a.T, a.cap);
     return r;
 }
-// `first`: the first 64 sequences, kept for find_unit
-template <int MANY> __device__ __forceinline__ int32_t wave_cut(const AttnArgs& a, SeqRange& first) {
-    const int lane = threadIdx.x & 63;
-    first = load_range(a, lane);
+// `first`: the first 64 sequences, kept for find_unit.  Counts are held to 2^24 a lane: more than PIECES_MAX
+// is enough to know.
+struct Plan { int32_t L, pieces; };
+template <int MANY> __device__ __forceinline__ Plan wave_plan(const AttnArgs& a, const SeqRange& first) {
+    const int lane = threadIdx.x & 63, n = a.S < 64 ? a.S : 64;
     int64_t units = 0, work = 0;
     int32_t longest = 0;
     for (int s0 = 0; s0 < a.S; s0 += 64) {
@@ -89,68 +94,83 @@ template <int MANY> __device__ __forceinline__ int32_t wave_cut(const AttnArgs& 
         work += t * span;
         if (t && span > longest) longest = span;
     }
-    longest = wave_most(longest);
-    if (longest <= a.lmin) return WHOLE;
-    units = wave_sum(units);
-    if (units >= PIECES_MAX) return WHOLE;
-    work = wave_sum(work);
-    int32_t best = WHOLE;
+    longest = wave_most(longest, n);
+    units = wave_sum(units, n);
+    Plan best = {WHOLE, units < INT32_MAX ? (int32_t)units : INT32_MAX};
+    if (longest <= a.lmin || units >= PIECES_MAX) return best;
+    work = wave_sum(work, n);
     int64_t cost = cut_cost(units, longest, work, units);
-#pragma unroll 1
+    int32_t L[CUTS], np[CUTS], most[CUTS];
+#pragma unroll
     for (int i = 1; i < CUTS; ++i) {
-        const int32_t L = cut_try(i, work, a.lmin);
-        int64_t n = 0;
-        int32_t most = 0;
-        for (int s0 = 0; s0 < a.S; s0 += 64) {
-            const SeqRange r = s0 ? load_range(a, s0 + lane) : first;
-            const int32_t t = seq_tiles(r, a.Hg, MANY), span = seq_span(r, a.window), np = seq_pieces(span, L);
-            n += (int64_t)t * a.G * np;
-            const int32_t len = t ? piece_len(span, np) : 0;
-            if (len > most) most = len;
+        L[i] = cut_try(i, work, a.lmin);
+        np[i] = most[i] = 0;
+    }
+    for (int s0 = 0; s0 < a.S; s0 += 64) {
+        const SeqRange r = s0 ? load_range(a, s0 + lane) : first;
+        const int32_t t = seq_tiles(r, a.Hg, MANY) * a.G, span = seq_span(r, a.window);     // t < PIECES_MAX
+#pragma unroll
+        for (int i = 1; i < CUTS; ++i) {
+            const int32_t m = seq_pieces(span, L[i]), len = t ? piece_len(span, m) : 0;
+            const int64_t sum = np[i] + (int64_t)t * m;
+            np[i] = sum < (1 << 24) ? (int32_t)sum : 1 << 24;
+            if (len > most[i]) most[i] = len;
         }
-        const int64_t c = cut_cost(wave_sum(n), wave_most(most), work, units);
+    }
+    for (int m = 1; m < n; m <<= 1)
+#pragma unroll
+        for (int i = 1; i < CUTS; ++i) {
+            np[i] += __shfl_xor(np[i], m, WAVE);
+            const int32_t x = __shfl_xor(most[i], m, WAVE);
+            most[i] = x > most[i] ? x : most[i];
+        }
+#pragma unroll
+    for (int i = 1; i < CUTS; ++i) {
+        const int32_t count = first_lane(np[i]);
+        const int64_t c = cut_cost(count, first_lane(most[i]), work, units);
         if (c < cost) {
             cost = c;
-            best = L;
+            best = {L[i], count};
         }
     }
     return best;
 }
-// The sequence of piece number idx: its pieces are (tile, piece, head) triples, heads innermost and the
-// last tile first (with causal rows it sees the most keys).  base: the sequence's first number; rec: its
-// first row of partial results.
+// The sequence of number idx.  A sequence's pieces are (tile, piece, head) triples, heads innermost and the last
+// tile first (with causal rows it sees the most keys); TILES: numbers count the (tile, head) pairs of cut sequences
+// alone.  base, end: the sequence's numbers; rec: its first row of partial results.
 struct Unit { SeqRange r; int32_t s, np; int64_t base, end, rec; };
-template <int MANY> __device__ __forceinline__ bool find_unit(const AttnArgs& a, int32_t L, const SeqRange& first, int64_t idx, Unit& u) {
-    const int lane = threadIdx.x & 63;
+template <int MANY, bool TILES>
+__device__ __forceinline__ bool find_unit(const AttnArgs& a, int32_t L, const SeqRange& first, int64_t idx, Unit& u) {
+    const int lane = threadIdx.x & 63, lanes = a.S < 64 ? a.S : 64;
     int64_t before = 0, rbefore = 0;
     for (int s0 = 0; s0 < a.S; s0 += 64) {
         const SeqRange r = s0 ? load_range(a, s0 + lane) : first;
         const int32_t np = seq_pieces(seq_span(r, a.window), L);
-        const int64_t n = (int64_t)seq_tiles(r, a.Hg, MANY) * np * a.G, nr = np > 1 ? n * tile_rows(r, a.Hg, MANY) : 0;
+        const int64_t t = (int64_t)seq_tiles(r, a.Hg, MANY) * a.G, nr = np > 1 ? t * np * tile_rows(r, a.Hg, MANY) : 0;
+        const int64_t n = TILES ? (np > 1 ? t : 0) : t * np;
         int64_t up = n, rup = nr;              // inclusive scans over the lanes
-#pragma unroll
-        for (int m = 1; m < 64; m <<= 1) {
+        for (int m = 1; m < lanes; m <<= 1) {
             const int64_t x = __shfl_up(up, m, WAVE), y = __shfl_up(rup, m, WAVE);
             if (lane >= m) {
                 up += x;
                 rup += y;
             }
         }
-        const uint64_t hit = __ballot(before + up > idx);
+        const uint64_t hit = __ballot(lane < lanes && before + up > idx);
         if (hit) {
             const int l = __builtin_ctzll(hit);
-            u.r.q0 = first_lane(__shfl(r.q0, l, WAVE));
-            u.r.qlen = first_lane(__shfl(r.qlen, l, WAVE));
-            u.r.klen = first_lane(__shfl(r.klen, l, WAVE));
-            u.np = first_lane(__shfl(np, l, WAVE));
-            u.base = first_lane(before + __shfl(up - n, l, WAVE));
-            u.end = first_lane(before + __shfl(up, l, WAVE));
-            u.rec = first_lane(rbefore + __shfl(rup - nr, l, WAVE));
-            u.s = first_lane(s0 + l);
+            u.r.q0 = __builtin_amdgcn_readlane(r.q0, l);
+            u.r.qlen = __builtin_amdgcn_readlane(r.qlen, l);
+            u.r.klen = __builtin_amdgcn_readlane(r.klen, l);
+            u.np = __builtin_amdgcn_readlane(np, l);
+            u.base = before + lane64(up - n, l);
+            u.end = before + lane64(up, l);
+            u.rec = rbefore + lane64(rup - nr, l);
+            u.s = s0 + l;
             return true;
         }
-        before += first_lane(__shfl(up, 63, WAVE));
-        rbefore += first_lane(__shfl(rup, 63, WAVE));
+        before += lane64(up, lanes - 1);
+        rbefore += lane64(rup, lanes - 1);
     }
     return false;
 }
@@ -179,6 +199,9 @@ struct Form {
     static_assert(SB == SPS * KB, "steps follow each other");
     static_assert(4 * RING <= (int)LDS && JOIN <= (int)LDS && STAGES * 2 * SB <= (int)LDS, "the two forms share it");
 };
+
+// the call's L for the second launch, behind the partial rows
+__device__ __forceinline__ int32_t* plan_of(const AttnArgs& a) { return (int32_t*)(a.rec + a.rec_rows * (D + 2)); }
 
 // What both forms need of a piece, and the operations on 32-key blocks.
 template <typename ET>
@@ -650,11 +673,6 @@ struct Many {
     }
     __device__ __forceinline__ int32_t within(int32_t t) const { return (t < P.lo ? P.lo : t > P.hi ? P.hi : t) - t_first; }
     __device__ __forceinline__ int32_t window_key(int w) const { return t_first + 1024 * w + 16 * P.lane; }
-    static __device__ __forceinline__ const uint8_t* lane_of(const uint8_t* p, int lane) {
-        const uint64_t v = (uint64_t)p;
-        return (const uint8_t*)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 |
-                                (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane));
-    }
     // stage s is to be brought: its addresses ...
     __device__ __forceinline__ void aim(int s) {
         const int w = s / SPW, in = s % SPW;
@@ -672,8 +690,8 @@ struct Many {
         const int group = (in * F::KT + crow) / 16;
         adv = (w & 1 ? has[1] : has[0]) >> group & 1 ? 1024 : 0;
         const int rest = adv ? crow % 16 * F::ROWB : 0;
-        ksrc = lane_of(kwin, group) + rest;
-        vsrc = lane_of(vwin, group) + rest;
+        ksrc = (const uint8_t*)lane64((int64_t)kwin, group) + rest;
+        vsrc = (const uint8_t*)lane64((int64_t)vwin, group) + rest;
         dst = lds0 + (s & 3) * F::SB + wave * 4096;
     }
     // ... and its 8 loads, the keys' first
@@ -733,22 +751,29 @@ struct Many {
 template <typename ET>
 __device__ void many_rows(const Piece<ET>& P, uint8_t* smem, int32_t row0, int32_t rows, bool cut, int64_t rec_row);
 
-// grid: at most one workgroup per slot, a multiple of 8.  Workgroup b takes piece numbers b, then the
-// numbers of each further round in turned order (the pieces of a sequence shrink along its numbers;
-// turning gives every workgroup long and short ones), b % 8 kept: heads stay on their XCD's L2.
+// grid: at most one workgroup per slot, a multiple of 8.  Workgroup b takes one piece number of every round of
+// gridDim: b, then in turned order (the pieces of a sequence shrink along its numbers; turning gives every
+// workgroup long and short ones), b % 8 kept: heads stay on their XCD's L2.  Half of the workgroups go through
+// the rounds backwards, so that the single tokens' reads and the chunks' products overlap.
 template <typename ET>
 __global__ __launch_bounds__(256, 1) void paged_attn_kernel(AttnArgs a) {
     constexpr int MANY = Form<ET>::MANY;
     extern __shared__ __align__(1024) uint8_t smem[];
-    SeqRange first;
-    const int32_t L = wave_cut<MANY>(a, first);
+    const SeqRange first = load_range(a, threadIdx.x & 63);
+    const Plan plan = wave_plan<MANY>(a, first);
+    if (a.rec_rows && blockIdx.x == 0 && threadIdx.x == 0) *plan_of(a) = plan.L;
+    const int32_t L = plan.L;
+    const uint32_t b = blockIdx.x, n = gridDim.x;
+    const int rounds = (int)(((uint32_t)plan.pieces + n - 1) / n);
     Unit u;
-    u.base = 0;
-    u.end = 0;
-    for (int round = 0;; ++round) {
-        const uint32_t b = blockIdx.x, n = gridDim.x;
+    u.base = u.end = 0;
+    for (int k = 0; k < rounds; ++k) {
+        const int round = b & 8 ? rounds - 1 - k : k;
         const int64_t idx = (int64_t)round * n + (round & 1 ? ((n - 1 - b) & ~7u) | (b & 7u) : b);
-        if (idx >= u.end && !find_unit<MANY>(a, L, first, idx, u)) break;
+        if ((idx >= u.end || idx < u.base) && !find_unit<MANY, false>(a, L, first, idx, u)) {
+            u.base = u.end = 0;
+            continue;                                      // behind the last piece
+        }
         const SeqRange r = u.r;
         const uint32_t in = (uint32_t)(idx - u.base), G = (uint32_t)a.G;
         const int g = (int)(in % G), piece = (int)(in / G % (uint32_t)u.np);
@@ -777,7 +802,7 @@ __global__ __launch_bounds__(256, 1) void paged_attn_kernel(AttnArgs a) {
     }
 }
 
-// Joins the pieces of cut sequences, up to JOIN_ROWS rows of a tile a workgroup: its waves take every
+// Joins the pieces of cut sequences, up to JOIN_ROWS rows of a (tile, head) pair a workgroup: its waves take every
 // fourth row of many, or of few rows every fourth piece of one.
 constexpr int JOIN_ROWS = 32;
 template <typename ET>
@@ -785,21 +810,20 @@ __global__ __launch_bounds__(256) void paged_join_kernel(AttnArgs a) {
     constexpr int MANY = Form<ET>::MANY;
     __shared__ float so[4][D];
     __shared__ float sl[4];
-    SeqRange first;
-    const int32_t L = wave_cut<MANY>(a, first);
+    const SeqRange first = load_range(a, threadIdx.x & 63);
+    const int32_t L = first_lane(*plan_of(a));
     if (L == WHOLE) return;
     const int wave = first_lane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
     const float* rec_ml = a.rec + a.rec_rows * D;
     Unit u;
     u.base = u.end = 0;
-    // work numbers: piece numbers x JOIN parts; the parts of piece 0 of every tile do the joining
     constexpr int parts = MANY / JOIN_ROWS;
     for (int64_t w = blockIdx.x;; w += gridDim.x) {
         const int64_t idx = w / parts;
         const int part = (int)(w % parts);
-        if ((idx >= u.end || idx < u.base) && !find_unit<MANY>(a, L, first, idx, u)) break;
-        const uint32_t in = (uint32_t)(idx - u.base), G = (uint32_t)a.G;
-        if (u.np <= 1 || in / G % (uint32_t)u.np != 0) continue;
+        if (idx >= u.end && !find_unit<MANY, true>(a, L, first, idx, u)) break;
+        const uint32_t pair = (uint32_t)(idx - u.base), G = (uint32_t)a.G;
+        const uint32_t in = pair / G * (uint32_t)u.np * G + pair % G;       // the number of its piece 0
         const SeqRange r = u.r;
         const int g = (int)(in % G), tile = seq_tiles(r, a.Hg, MANY) - 1 - (int)(in / G / (uint32_t)u.np);
         const int bm = tile_rows(r, a.Hg, MANY);
@@ -848,19 +872,19 @@ __global__ __launch_bounds__(256) void paged_join_kernel(AttnArgs a) {
 
 // SLOTS workgroups, and the second launch unless the tables are too short for a cut
 template <typename ET>
-hipError_t launch_paged(const AttnArgs& a, int64_t pieces, hipStream_t st) {
+hipError_t launch_paged(const AttnArgs& a, int64_t units, int64_t pieces, hipStream_t st) {
     const void* fn = (const void*)paged_attn_kernel<ET>;
     hipError_t e = ensure_lds_limit(fn, Form<ET>::LDS);
     if (e != hipSuccess) return e;
     const unsigned grid = pieces < SLOTS ? ((unsigned)pieces + 7) & ~7u : SLOTS;
     paged_attn_kernel<ET><<<grid, 256, Form<ET>::LDS, st>>>(a);
-    if ((e = hipGetLastError()) != hipSuccess || a.cap <= a.lmin) return e;
-    const int64_t parts = pieces * (Form<ET>::MANY / JOIN_ROWS);
-    paged_join_kernel<ET><<<(unsigned)(parts < 2048 ? parts : 2048), 256, 0, st>>>(a);
+    if ((e = hipGetLastError()) != hipSuccess || !a.rec_rows) return e;
+    const int64_t parts = units * (Form<ET>::MANY / JOIN_ROWS);
+    paged_join_kernel<ET><<<(unsigned)(parts < 1024 ? parts : 1024), 256, 0, st>>>(a);
     return hipGetLastError();
 }
 
-hipError_t launch_paged_bf16(const AttnArgs& a, int64_t pieces, hipStream_t st);
-hipError_t launch_paged_f32(const AttnArgs& a, int64_t pieces, hipStream_t st);
+hipError_t launch_paged_bf16(const AttnArgs& a, int64_t units, int64_t pieces, hipStream_t st);
+hipError_t launch_paged_f32(const AttnArgs& a, int64_t units, int64_t pieces, hipStream_t st);
 
 }  // namespace vr

@@ -304,14 +304,15 @@ __device__ __forceinline__ void many_rows<uint16_t>(const Piece<uint16_t>& P, ui
     M.finish();
 }
 
-hipError_t launch_paged_bf16(const AttnArgs& a, int64_t pieces, hipStream_t st) { return launch_paged<uint16_t>(a, pieces, st); }
+hipError_t launch_paged_bf16(const AttnArgs& a, int64_t units, int64_t pieces, hipStream_t st) { return launch_paged<uint16_t>(a, units, pieces, st); }
 
 // ---- host ------------------------------------------------------------------------------------
 constexpr int LMIN = 512;          // shortest piece, in tokens
 static int many_of(int dtype) { return dtype == VARRATE_BF16 ? Form<uint16_t>::MANY : Form<float>::MANY; }
 
 size_t paged_attn_ws_bytes(int64_t T, int S, int G, int H, int dtype, int64_t cap) {
-    return (size_t)max_records(T, S, G, H / G, many_of(dtype), cap, LMIN) * (D + 2) * 4;
+    const int64_t rows = max_records(T, S, G, H / G, many_of(dtype), cap, LMIN);
+    return rows ? (size_t)rows * (D + 2) * 4 + 16 : 0;
 }
 
 hipError_t launch_paged_attn(const varrate_pages& pg, const varrate_batch& b, const void* q, int64_t q_stride, int H,
@@ -341,8 +342,9 @@ hipError_t launch_paged_attn(const varrate_pages& pg, const varrate_batch& b, co
     a.c = scale * 1.4426950408889634f;
     const int many = many_of(pg.dtype);
     a.rec_rows = max_records(b.T, b.S, pg.G, a.Hg, many, a.cap, LMIN);
+    const int64_t units = max_units(b.T, b.S, pg.G, a.Hg, many);
     const int64_t pieces = max_pieces(b.T, b.S, pg.G, a.Hg, many, a.cap, LMIN);
-    return pg.dtype == VARRATE_BF16 ? launch_paged_bf16(a, pieces, st) : launch_paged_f32(a, pieces, st);
+    return pg.dtype == VARRATE_BF16 ? launch_paged_bf16(a, units, pieces, st) : launch_paged_f32(a, units, pieces, st);
 }
 
 }  // namespace vr

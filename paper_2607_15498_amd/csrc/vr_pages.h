@@ -101,9 +101,10 @@ VR_HD int64_t cut_cost(int64_t pieces, int64_t longest, int64_t work, int64_t un
     return t + rounds * COST_PIECE + (pieces > units ? COST_JOIN : 0);
 }
 
-// most pieces of any call with T rows and S sequences whose tables hold `cap` tokens
+// most (tile, head) pairs and pieces of any call with T rows and S sequences whose tables hold `cap` tokens
+VR_HD int64_t max_units(int64_t T, int S, int G, int Hg, int many) { return G * (T * Hg / many + (S < T ? S : T)); }
 VR_HD int64_t max_pieces(int64_t T, int S, int G, int Hg, int many, int64_t cap, int lmin) {
-    const int64_t units = G * (T * Hg / many + (S < T ? S : T));
+    const int64_t units = max_units(T, S, G, Hg, many);
     const int64_t most = units * ((cap + lmin - 1) / lmin);
     const int64_t cut = most < PIECES_MAX ? most : PIECES_MAX;
     return units > cut ? units : cut;
