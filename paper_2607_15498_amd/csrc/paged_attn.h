@@ -1,6 +1,8 @@
 // What the paged attention's kernels share: the call's cut, a piece's addresses and masks, the products of
 // 32-key blocks and the few-rows form.  The head of paged_attn.hip describes the whole.
 #pragma once
+#include <type_traits>
+
 #include "vr_internal.h"
 #include "vr_pages.h"
 
@@ -22,7 +24,8 @@ struct AttnArgs {
     int64_t table_stride;
     int64_t rec_rows;
     int32_t T, S, cap, n_pages, G, Hg, shift;
-    int32_t causal, window, lmin;
+    int32_t causal, window;
+    Costs costs;
     float c;                        // softmax scale x log2 e
 };
 
@@ -82,52 +85,60 @@ __device__ __forceinline__ SeqRange load_range(const AttnArgs& a, int s) {
 // `first`: the first 64 sequences, kept for find_unit.  Counts are held to 2^24 a lane: more than PIECES_MAX
 // is enough to know.
 struct Plan { int32_t L, pieces; };
-template <int MANY> __device__ __forceinline__ Plan wave_plan(const AttnArgs& a, const SeqRange& first) {
+__device__ __forceinline__ Plan wave_plan(const AttnArgs& a, const SeqRange& first) {
     const int lane = threadIdx.x & 63, n = a.S < 64 ? a.S : 64;
-    int64_t units = 0, work = 0;
+    int64_t units = 0, work = 0, spans = 0;
     int32_t longest = 0;
+    uint64_t many = 0;
     for (int s0 = 0; s0 < a.S; s0 += 64) {
         const SeqRange r = s0 ? load_range(a, s0 + lane) : first;
-        const int64_t t = (int64_t)seq_tiles(r, a.Hg, MANY) * a.G;
-        const int32_t span = seq_span(r, a.window);
+        const int64_t t = (int64_t)seq_tiles(r, a.Hg) * a.G;
+        const int32_t span = seq_span(r, a.Hg, a.window);
         units += t;
-        work += t * span;
+        const int32_t c = key_cost(r, a.Hg, a.costs);
+        work += t * seq_mean(r, span, a.causal) * c;
+        spans += t * span * c;
         if (t && span > longest) longest = span;
+        many |= __ballot(tile_rows(r, a.Hg) != ROWS_FEW);
     }
     longest = wave_most(longest, n);
     units = wave_sum(units, n);
     Plan best = {WHOLE, units < INT32_MAX ? (int32_t)units : INT32_MAX};
-    if (longest <= a.lmin || units >= PIECES_MAX) return best;
+    if (longest <= a.costs.lmin || units >= PIECES_MAX) return best;
     work = wave_sum(work, n);
-    int64_t cost = cut_cost(units, longest, work, units);
-    int32_t L[CUTS], np[CUTS], most[CUTS];
+    spans = wave_sum(spans, n);
+    int32_t L[CUTS], np[CUTS];
+    int64_t most[CUTS];
 #pragma unroll
-    for (int i = 1; i < CUTS; ++i) {
-        L[i] = cut_try(i, work, a.lmin);
-        np[i] = most[i] = 0;
+    for (int i = 0; i < CUTS; ++i) {
+        L[i] = cut_try(i, spans);
+        np[i] = 0;
+        most[i] = 0;
     }
     for (int s0 = 0; s0 < a.S; s0 += 64) {
         const SeqRange r = s0 ? load_range(a, s0 + lane) : first;
-        const int32_t t = seq_tiles(r, a.Hg, MANY) * a.G, span = seq_span(r, a.window);     // t < PIECES_MAX
+        const int32_t t = seq_tiles(r, a.Hg) * a.G, span = seq_span(r, a.Hg, a.window);       // t < PIECES_MAX
+        const int32_t c = key_cost(r, a.Hg, a.costs);
 #pragma unroll
-        for (int i = 1; i < CUTS; ++i) {
-            const int32_t m = seq_pieces(span, L[i]), len = t ? piece_len(span, m) : 0;
-            const int64_t sum = np[i] + (int64_t)t * m;
+        for (int i = 0; i < CUTS; ++i) {
+            const int32_t m = seq_pieces(span, c, L[i], a.costs.lmin);
+            const int64_t len = t ? (int64_t)piece_len(span, m) * c : 0, sum = np[i] + (int64_t)t * m;
             np[i] = sum < (1 << 24) ? (int32_t)sum : 1 << 24;
             if (len > most[i]) most[i] = len;
         }
     }
     for (int m = 1; m < n; m <<= 1)
 #pragma unroll
-        for (int i = 1; i < CUTS; ++i) {
+        for (int i = 0; i < CUTS; ++i) {
             np[i] += __shfl_xor(np[i], m, WAVE);
-            const int32_t x = __shfl_xor(most[i], m, WAVE);
+            const int64_t x = __shfl_xor(most[i], m, WAVE);
             most[i] = x > most[i] ? x : most[i];
         }
+    int64_t cost = INT64_MAX;
 #pragma unroll
-    for (int i = 1; i < CUTS; ++i) {
+    for (int i = 0; i < CUTS; ++i) {
         const int32_t count = first_lane(np[i]);
-        const int64_t c = cut_cost(count, first_lane(most[i]), work, units);
+        const int64_t c = cut_cost(count, first_lane(most[i]), work, units, many == 0, a.costs);
         if (c < cost) {
             cost = c;
             best = {L[i], count};
@@ -136,18 +147,21 @@ template <int MANY> __device__ __forceinline__ Plan wave_plan(const AttnArgs& a,
     return best;
 }
 // The sequence of number idx.  A sequence's pieces are (tile, piece, head) triples, heads innermost and the last
-// tile first (with causal rows it sees the most keys); TILES: numbers count the (tile, head) pairs of cut sequences
-// alone.  base, end: the sequence's numbers; rec: its first row of partial results.
+// tile first (with causal rows it sees the most keys); JOIN: numbers count the second launch's work, (JOIN_ROWS rows,
+// head) pairs of cut sequences, of few rows (row, head) pairs.  base, end: the sequence's numbers; rec: its first row of
+// partial results.
+constexpr int JOIN_ROWS = 4;
 struct Unit { SeqRange r; int32_t s, np; int64_t base, end, rec; };
-template <int MANY, bool TILES>
+template <bool JOIN>
 __device__ __forceinline__ bool find_unit(const AttnArgs& a, int32_t L, const SeqRange& first, int64_t idx, Unit& u) {
     const int lane = threadIdx.x & 63, lanes = a.S < 64 ? a.S : 64;
     int64_t before = 0, rbefore = 0;
     for (int s0 = 0; s0 < a.S; s0 += 64) {
         const SeqRange r = s0 ? load_range(a, s0 + lane) : first;
-        const int32_t np = seq_pieces(seq_span(r, a.window), L);
-        const int64_t t = (int64_t)seq_tiles(r, a.Hg, MANY) * a.G, nr = np > 1 ? t * np * tile_rows(r, a.Hg, MANY) : 0;
-        const int64_t n = TILES ? (np > 1 ? t : 0) : t * np;
+        const int32_t np = seq_pieces(seq_span(r, a.Hg, a.window), key_cost(r, a.Hg, a.costs), L, a.costs.lmin);
+        const int64_t t = (int64_t)seq_tiles(r, a.Hg) * a.G, nr = np > 1 ? t * np * tile_rows(r, a.Hg) : 0;
+        const int64_t rows = seq_rows(r, a.Hg), parts = rows <= ROWS_FEW ? rows : (rows + JOIN_ROWS - 1) / JOIN_ROWS;
+        const int64_t n = JOIN ? (np > 1 ? parts * a.G : 0) : t * np;
         int64_t up = n, rup = nr;              // inclusive scans over the lanes
         for (int m = 1; m < lanes; m <<= 1) {
             const int64_t x = __shfl_up(up, m, WAVE), y = __shfl_up(rup, m, WAVE);
@@ -181,20 +195,20 @@ struct Form {
     static constexpr int ROWB = D * (int)sizeof(ET);       // bytes of a row
     static constexpr int PPR = ROWB / 16;
     static constexpr int NF = BF ? 8 : 16;                 // 16-byte fragments of a row per lane: pieces 2 k + h
-    static constexpr int CROWS = 4096 / ROWB;              // rows of a 4 KB chunk (one wave's 4 loads)
-    // few rows: per wave a ring of NST 32-key tiles [K, V]
+    static constexpr int NC = BF ? 2 : 1;                  // many rows: blocks of 32 rows per wave
+    static constexpr int WAVES = ROWS_MANY / (32 * NC);    // 4; fp32 8, two a SIMD
+    // few rows: for each of 4 waves a ring of NST 32-key tiles [K, V], brought in chunks of 4 KB
     static constexpr int KB = 32 * ROWB;
     static constexpr int NST = BF ? 2 : 1;
     static constexpr int RING = NST * 2 * KB;
-    static constexpr int CH = KB / 4096;
+    static constexpr int CH = KB / 4096, CROWS = 4096 / ROWB;
     static constexpr int JOIN = 4 * 32 * (132 + 2) * 4;
-    // many rows: 4 stages of 16 KB of keys, then as many of values; one chunk of each per wave
+    // many rows: 4 stages of 16 KB of keys, then as many of values; every wave brings LPW KB of either
     static constexpr int SB = 16384;
     static constexpr int KT = SB / ROWB;                   // keys per stage: 64, fp32 32
     static constexpr int SPS = KT / 32;                    // 32-key steps per stage
     static constexpr int STAGES = 4;
-    static constexpr int NC = BF ? 2 : 1;                  // blocks of 32 rows per wave
-    static constexpr int MANY = 4 * NC * 32;
+    static constexpr int LPW = SB / 1024 / WAVES, WROWS = LPW * 1024 / ROWB;
     static constexpr size_t LDS = 128 * 1024;
     static_assert(SB == SPS * KB, "steps follow each other");
     static_assert(4 * RING <= (int)LDS && JOIN <= (int)LDS && STAGES * 2 * SB <= (int)LDS, "the two forms share it");
@@ -229,6 +243,13 @@ struct Piece {
         off0 = (uint32_t)(lrow * F::ROWB + ((lane % F::PPR) ^ ((lrow & 3) << 2)) * 16);
         kaddr = (uint32_t)(l32 * F::ROWB + (h ^ (((l32 & 3) << 2) | ((l32 >> 2) & 3))) * 16);
     }
+    // the same piece with the lane's numbers anew: what the rare masked steps derive from them is not kept in
+    // registers for the whole loop
+    __device__ __forceinline__ Piece anew() const {
+        Piece p = *this;
+        asm volatile("" : "+v"(p.lane), "+v"(p.l32), "+v"(p.h));
+        return p;
+    }
     // the page of key t as the table has it (any entry of the sequence's behind its end)
     __device__ __forceinline__ int32_t raw_page(int32_t t) const { return trow[(t < r.klen ? t : r.klen - 1) >> a.shift]; }
     // and -1 for one that names none, and behind the end
@@ -239,21 +260,19 @@ struct Piece {
     __device__ __forceinline__ int64_t offset_of(int32_t p, int32_t t) const {
         return (int64_t)p * a.G * head_bytes + (int64_t)(t & ((1 << a.shift) - 1)) * F::ROWB;
     }
-    // rows t .. t + CROWS - 1 of page p (or zeros): address of the first, and the advance per 1 KB
+    // rows from t on of page p (or zeros): address of the first, and the advance per 1 KB
     __device__ __forceinline__ const uint8_t* rows_at(const uint8_t* pool, int32_t p, int32_t t) const {
         return (const uint8_t*)first_lane((int64_t)(p >= 0 ? pool + offset_of(p, t) : (const uint8_t*)pa_zeros));
     }
     static __device__ __forceinline__ int advance(int32_t p) { return p >= 0 ? 1024 : 0; }
-    // 1 KB number v of them, chunk `ch` of its tile, into LDS at dst (of the chunk)
-    __device__ __forceinline__ void bring1(const uint8_t* src, int adv, int v, int ch, uint32_t dst) const {
+    // 1 KB number v of them into LDS at dst (of number 0); row 0 of number 0 is row 4 `quad` of its block
+    template <bool VALUES>
+    __device__ __forceinline__ void bring1(const uint8_t* src, int adv, int v, int quad, uint32_t dst) const {
         // rows 4 v + .. (bf16) or 2 v + .. (fp32): the rest of f(row)
-        const uint32_t fx = F::BF ? (uint32_t)v & 3u : (uint32_t)(((v & 1) << 3) | (((v >> 1) + 2 * (ch & 1)) & 3));
-        lds_load(src + v * adv, off0 ^ (fx << 4), dst + v * 1024);
-    }
-    __device__ __forceinline__ void bring(const uint8_t* pool, int32_t p, int32_t t, int ch, uint32_t dst) const {
-        const uint8_t* src = rows_at(pool, p, t);
-#pragma unroll
-        for (int v = 0; v < 4; ++v) bring1(src, advance(p), v, ch, dst);
+        if constexpr (F::BF) lds_load(src + v * adv, off0 ^ (((uint32_t)(quad + v) & 3u) << 4), dst + v * 1024);
+        else if constexpr (!VALUES)
+            lds_load(src + v * adv, off0 ^ ((uint32_t)((v & 1) << 3 | ((quad + (v >> 1)) & 3)) << 4), dst + v * 1024);
+        else lds_load(src + v * adv, (16u * (uint32_t)lane) ^ (((uint32_t)(quad + (v >> 1)) & 1u) << 7), dst + v * 1024);
     }
     // values behind the end in the rows [r0, r1) of a tile of keys from t0 on: not read as data
     __device__ __forceinline__ void clear_tail(int32_t t0, int32_t r0, int32_t r1, uint8_t* vt) const {
@@ -278,7 +297,7 @@ struct Piece {
             for (int i = 0; i < 16; ++i) sc[c][i] = 0.f;
 #pragma unroll
         for (int k = 0; k < F::NF; ++k) {
-            const u32x4 f = *reinterpret_cast<const u32x4*>(kt + (kaddr ^ (32u * k)));
+            const u32x4 f = *reinterpret_cast<const u32x4*>(kt + (kaddr ^ (32u * (k & 7))) + 256 * (k >> 3));
             if constexpr (F::BF) {
 #pragma unroll
                 for (int c = 0; c < NC; ++c) sc[c] = mfma32(f, qf[c][k], sc[c]);
@@ -321,74 +340,82 @@ struct Piece {
         }
         return f;
     }
-    // fp32: key r0 + 4 h, dim 32 dt + l32
+    // fp32: key r0 + 4 h (bit 2 of r0 is 0), dim 32 dt + l32: 128 bytes of each of two rows, h of them in the other
+    // half of the banks
     __device__ __forceinline__ float vfrag32(const uint8_t* vt, int r0, int dt) const {
-        const int row = r0 + 4 * h, f = ((row & 3) << 2) | ((row >> 2) & 3);
-        return *reinterpret_cast<const float*>(vt + row * F::ROWB + ((8 * dt + (l32 >> 2)) ^ f) * 16 + (l32 & 3) * 4);
+        const int at = 4 * h * F::ROWB + (dt & 1 ? -128 * h : 128 * h) + 4 * l32;
+        return *reinterpret_cast<const float*>(vt + r0 * F::ROWB + 128 * dt + at);
     }
-    // acc += V^T P^T of 32 keys; p: the weights, packed in pairs for bf16
-    template <int NC>
+    // x with infinities and NaN made 0: one fp32, or a bf16 pair
+    static __device__ __forceinline__ uint32_t finite(uint32_t x) {
+        if constexpr (F::BF) return x & ~((((x & 0x7F807F80u) + 0x00800080u) >> 15 & 0x00010001u) * 0xFFFFu);
+        else return (x & 0x7F800000u) == 0x7F800000u ? 0u : x;
+    }
+    // acc += V^T P^T of 32 keys; p: the weights, packed in pairs for bf16.  FINITE: of their finite values alone.
+    template <int NC, bool FINITE = false>
     __device__ __forceinline__ void values(const uint8_t* vt, const u32x4 (&p)[NC][2], f32x16 (&acc)[NC][4]) const {
 #pragma unroll
         for (int mm = 0; mm < 2; ++mm)
 #pragma unroll
             for (int dt = 0; dt < 4; ++dt) {
-                const u32x4 f = vfrag(vt, 16 * mm, dt);
+                u32x4 f = vfrag(vt, 16 * mm, dt);
+                if constexpr (FINITE)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) f[k] = finite(f[k]);
 #pragma unroll
                 for (int c = 0; c < NC; ++c) acc[c][dt] = mfma32(f, p[c][mm], acc[c][dt]);
             }
     }
-    template <int NC>
+    template <int NC, bool FINITE = false>
     __device__ __forceinline__ void values(const uint8_t* vt, const f32x16 (&p)[NC], f32x16 (&acc)[NC][4]) const {
 #pragma unroll
         for (int i = 0; i < 16; ++i)
 #pragma unroll
             for (int dt = 0; dt < 4; ++dt) {
-                const float f = vfrag32(vt, 8 * (i >> 2) + (i & 3), dt);
+                float f = vfrag32(vt, 8 * (i >> 2) + (i & 3), dt);
+                if constexpr (FINITE) f = __uint_as_float(finite(__float_as_uint(f)));
 #pragma unroll
                 for (int c = 0; c < NC; ++c) acc[c][dt] = mfma32(f, p[c][i], acc[c][dt]);
             }
     }
-    // A masked block whose values hold infinities or NaN: 0 x inf is not 0, so a row must not meet
-    // the values of keys that it does not see.  One key at a time, kept by the rows that see it.
+    // A masked block whose values hold infinities or NaN: 0 x inf is not 0, so a row must not meet the values of keys
+    // that it does not see.  The products take the finite values, and every row adds the others of the keys that it sees.
     __device__ __forceinline__ bool odd_values(const uint8_t* vt) const {
         uint32_t odd = 0;
         for (int i = lane; i < F::KB / 16; i += 64) {
             const u32x4 w = *reinterpret_cast<const u32x4*>(vt + 16 * i);
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                odd |= F::BF ? ((w[k] & 0x7F807F80u) + 0x00800080u) & 0x80008000u
-                             : ((w[k] & 0x7F800000u) + 0x00800000u) & 0x80000000u;
+            for (int k = 0; k < 4; ++k) odd |= w[k] ^ finite(w[k]);
         }
         return __ballot(odd != 0) != 0;
     }
-    template <typename P>
-    __device__ __forceinline__ void values_by_key(const uint8_t* vt, const P& p, f32x16& acc, int dt, int32_t t0, int32_t mylo,
-                                                  int32_t myhi, uint32_t gm) const {
+    // add(dt, i, x): x to the lane's sum of dim 32 dt + 8 (i / 4) + 4 h + i % 4
+    template <typename A>
+    __device__ __forceinline__ void add_odd(const uint8_t* vt, int32_t t0, int32_t mylo, int32_t myhi, uint32_t gm, A&& add) const {
 #pragma unroll 1
-        for (int kk = 0; kk < 32; ++kk) {                  // lanes of half (kk / 4) % 2 hold it
+        for (int kk = 0; kk < 32; ++kk) {
             const bool see = sees(t0 + kk, mylo, myhi, gm >> (kk >> 4) & 1u);
-            const bool mine = ((kk >> 2) & 1) == h;
-            const int slot = 4 * ((kk >> 3) & 1) + (kk & 3);
-            f32x16 with;
-            if constexpr (F::BF) {
-                u32x4 keep, pk;
+            const int f = F::BF ? ((kk & 3) << 2) | ((kk >> 2) & 3) : ((kk >> 2) & 1) << 3;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    keep[k] = mine && (slot >> 1) == k ? (slot & 1 ? 0xFFFF0000u : 0xFFFFu) : 0u;
-                    pk[k] = (kk < 16 ? p[0][k] : p[1][k]) & keep[k];
+            for (int n = 0; n < 16; ++n) {                 // dims 8 n + 4 h ..
+                const int byte = (8 * n + 4 * h) * (int)sizeof(ET);
+                const uint8_t* at = vt + kk * F::ROWB + (((byte >> 4) ^ f) << 4) + (byte & 15);
+                float x[4];
+                if constexpr (F::BF) {
+                    const uint2 w = *reinterpret_cast<const uint2*>(at);
+                    const uint2 o = {w.x ^ finite(w.x), w.y ^ finite(w.y)};   // the others alone
+                    x[0] = bf_lo(o.x);
+                    x[1] = bf_hi(o.x);
+                    x[2] = bf_lo(o.y);
+                    x[3] = bf_hi(o.y);
+                } else {
+                    const u32x4 w = *reinterpret_cast<const u32x4*>(at);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) x[k] = __uint_as_float(w[k] ^ finite(w[k]));
                 }
-                with = mfma32(vfrag(vt, kk & 16, dt) & keep, pk, acc);
-            } else {
-                float pf = 0.f;
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (i == 8 * (kk >> 4) + slot) pf = mine ? p[i] : 0.f;
-                const float v = vfrag32(vt, (kk & 16) + 8 * ((kk >> 3) & 1) + (kk & 3), dt);
-                with = mfma32(mine ? v : 0.f, pf, acc);
+                for (int k = 0; k < 4; ++k) add(n >> 2, 4 * (n & 3) + k, see ? x[k] : 0.f);
             }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[i] = see ? with[i] : acc[i];
         }
     }
 };
@@ -450,7 +477,7 @@ __device__ __forceinline__ void few_rows(const Piece<ET>& P, uint8_t* smem, int 
     const SeqRange& r = P.r;
     const int wave = first_lane((int)(threadIdx.x >> 6)), lane = P.lane, l32 = P.l32, h = P.h;
     const int Hg = a.Hg, g = P.g, lo = P.lo, hi = P.hi;
-    uint8_t* ring = smem + wave * F::RING;
+    uint8_t* ring = smem + (wave & 3) * F::RING;
     const uint32_t ring0 = first_lane((int)(uint32_t)(size_t)(__attribute__((address_space(3))) uint8_t*)ring);
     const int myrow = l32 < rows ? l32 : 0, tok = myrow / Hg;
     int32_t mylo, myhi, firsthi, lastlo, x;
@@ -480,17 +507,23 @@ __device__ __forceinline__ void few_rows(const Piece<ET>& P, uint8_t* smem, int 
         page[1] = __builtin_amdgcn_readlane(window, 2 * at + 1);
         ++at;
     };
-    auto bring = [&](const uint8_t* pool, int32_t t, uint32_t dst) {
+    auto bring = [&](auto values, const uint8_t* pool, int32_t t, uint32_t dst) {
 #pragma unroll
-        for (int c = 0; c < F::CH; ++c) P.bring(pool, page[c * F::CROWS / 16], t + c * F::CROWS, c, dst + c * 4096);
+        for (int c = 0; c < F::CH; ++c) {
+            const int32_t pg = page[c * F::CROWS / 16];
+            const uint8_t* src = P.rows_at(pool, pg, t + c * F::CROWS);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) P.template bring1<values>(src, P.advance(pg), v, c * F::CROWS / 4, dst + c * 4096);
+        }
     };
     auto groups = [&]() { return (page[0] >= 0 ? 1u : 0u) | (page[1] >= 0 ? 2u : 0u); };
     int32_t t0 = (lo & ~31) + 32 * wave;
     uint32_t gm_in = 0;
+    if (wave >= 4) t0 = hi;                                // fp32: the other four have nothing to do here
     if (t0 < hi) {
         fetch(t0);
-        bring(P.kbase, t0, ring0);
-        bring(P.vbase, t0, ring0 + F::KB);
+        bring(std::false_type(), P.kbase, t0, ring0);
+        bring(std::true_type(), P.vbase, t0, ring0 + F::KB);
         gm_in = groups();
     }
     for (int st = 0; t0 < hi; t0 += step) {
@@ -502,7 +535,7 @@ __device__ __forceinline__ void few_rows(const Piece<ET>& P, uint8_t* smem, int 
         u32x4 p[1][2];
         auto softmax = [&]() {
             P.template scores<1>(kt, qf, sc);
-            if (masked) P.mask(sc[0], t0, mylo, myhi, gm);
+            if (masked) P.anew().mask(sc[0], t0, mylo, myhi, gm);
             const float mt = P.most(sc[0]);
             if (__any(mt > run.m + SLACK / a.c)) {
                 const float f = run.raise(mt, a.c);
@@ -520,8 +553,8 @@ __device__ __forceinline__ void few_rows(const Piece<ET>& P, uint8_t* smem, int 
             wait_lds();                                    // the other tile has been read
             if (more) {
                 fetch(tn);
-                bring(P.kbase, tn, next);
-                bring(P.vbase, tn, next + F::KB);
+                bring(std::false_type(), P.kbase, tn, next);
+                bring(std::true_type(), P.vbase, tn, next + F::KB);
                 gm_in = groups();
                 wait_loads<3 * L>();
             } else wait_loads<L>();
@@ -534,25 +567,25 @@ __device__ __forceinline__ void few_rows(const Piece<ET>& P, uint8_t* smem, int 
             wait_lds();                                    // the keys have been read
             if (more) {
                 fetch(tn);
-                bring(P.kbase, tn, ring0);
+                bring(std::false_type(), P.kbase, tn, ring0);
                 wait_loads<L>();
             } else wait_loads<0>();
         }
         uint8_t* vt = kt + F::KB;
         P.clear_tail(t0, 0, 32, vt);
+        const bool odd = masked && P.anew().odd_values(vt);
         if constexpr (F::BF) {
-            if (masked && P.odd_values(vt))
-#pragma unroll
-                for (int dt = 0; dt < 4; ++dt) P.values_by_key(vt, p[0], acc[0][dt], dt, t0, mylo, myhi, gm);
+            if (odd) P.anew().template values<1, true>(vt, p, acc);
             else P.template values<1>(vt, p, acc);
         } else {
-            if (masked && P.odd_values(vt))
-#pragma unroll
-                for (int dt = 0; dt < 4; ++dt) P.values_by_key(vt, sc[0], acc[0][dt], dt, t0, mylo, myhi, gm);
+            if (odd) P.anew().template values<1, true>(vt, sc, acc);
             else P.template values<1>(vt, sc, acc);
+        }
+        if (odd) P.anew().add_odd(vt, t0, mylo, myhi, gm, [&](int dt, int i, float x) { acc[0][dt][i] += x; });
+        if constexpr (!F::BF) {
             wait_lds();                                    // the values have been read
             if (more) {
-                bring(P.vbase, tn, ring0 + F::KB);
+                bring(std::true_type(), P.vbase, tn, ring0 + F::KB);
                 gm_in = groups();
             }
         }
@@ -561,16 +594,17 @@ __device__ __forceinline__ void few_rows(const Piece<ET>& P, uint8_t* smem, int 
     __syncthreads();                                       // every wave is done with its ring
     float* js = (float*)smem;                              // [4][32][132] sums
     float* jm = js + 4 * 32 * 132;                         // [4][32][2]
+    if (wave < 4)
 #pragma unroll
-    for (int dt = 0; dt < 4; ++dt)
+        for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
-        for (int i = 0; i < 16; i += 4)
-            *reinterpret_cast<f32x4*>(js + (wave * 32 + l32) * 132 + 32 * dt + 2 * i + 4 * h) =
-                f32x4{acc[0][dt][i], acc[0][dt][i + 1], acc[0][dt][i + 2], acc[0][dt][i + 3]};
-    if (h == 0) *reinterpret_cast<float2*>(jm + (wave * 32 + l32) * 2) = float2{run.m, run.l};
+            for (int i = 0; i < 16; i += 4)
+                *reinterpret_cast<f32x4*>(js + (wave * 32 + l32) * 132 + 32 * dt + 2 * i + 4 * h) =
+                    f32x4{acc[0][dt][i], acc[0][dt][i + 1], acc[0][dt][i + 2], acc[0][dt][i + 3]};
+    if (wave < 4 && h == 0) *reinterpret_cast<float2*>(jm + (wave * 32 + l32) * 2) = float2{run.m, run.l};
     __syncthreads();
     const int row = threadIdx.x >> 3, d0 = 16 * (threadIdx.x & 7);
-    if (row < rows) {
+    if (row < rows) {                                      // at most 32, a thread each 16 dims
         float mw[4], lw[4], M = -INFINITY, Ls = 0.f, o[16];
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
@@ -618,7 +652,7 @@ struct Many {
     const Piece<ET>& P;
     uint8_t* smem;
     uint32_t lds0;
-    int wave, crow;                                        // crow: first row of the wave's chunk of a stage
+    int wave, crow;                                        // crow: the first of the wave's rows of a stage
     int32_t row0, rows, wrow, t_first, stages;
     int32_t jf, jl, mf, ml;                                // steps that some row sees: [jf, jl), every row whole: [mf, ml)
     // pages of the 16-key groups of a window of 64 groups, one a lane: the one that is being brought, the raw
@@ -637,7 +671,7 @@ struct Many {
         const AttnArgs& a = P.a;
         lds0 = first_lane((int)(uint32_t)(size_t)(__attribute__((address_space(3))) uint8_t*)smem);
         wave = first_lane((int)(threadIdx.x >> 6));
-        crow = wave * F::CROWS;
+        crow = wave * F::WROWS;
         wrow = 32 * NC * wave;
         t_first = P.lo & ~(F::KT - 1);
         stages = P.hi > P.lo ? (P.hi - t_first + F::KT - 1) / F::KT : 0;
@@ -692,17 +726,17 @@ struct Many {
         const int rest = adv ? crow % 16 * F::ROWB : 0;
         ksrc = (const uint8_t*)lane64((int64_t)kwin, group) + rest;
         vsrc = (const uint8_t*)lane64((int64_t)vwin, group) + rest;
-        dst = lds0 + (s & 3) * F::SB + wave * 4096;
+        dst = lds0 + (s & 3) * F::SB + wave * F::LPW * 1024;
     }
-    // ... and its 8 loads, the keys' first
+    // ... and its loads, the keys' first
     __device__ __forceinline__ void bring(int i) const {
-        if (i < 4) P.bring1(ksrc, adv, i, wave, dst);
-        else P.bring1(vsrc, adv, i - 4, wave, dst + F::STAGES * F::SB);
+        if (i < F::LPW) P.template bring1<false>(ksrc, adv, i, crow / 4, dst);
+        else P.template bring1<true>(vsrc, adv, i - F::LPW, crow / 4, dst + F::STAGES * F::SB);
     }
     __device__ __forceinline__ void issue(int s) {
         aim(s);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) bring(i);
+        for (int i = 0; i < 2 * F::LPW; ++i) bring(i);
     }
     __device__ __forceinline__ void begin() {
         issue(0);
@@ -711,8 +745,8 @@ struct Many {
     // Stage s has arrived, and stage s - 2 is free (every wave is past it): stage s + 2 follows.  Every stage is
     // followed by others, so that the counts stay the same; those behind the last bring rows that nothing reads.
     __device__ __forceinline__ void arrive(int s) const {
-        wait_loads<8>();
-        P.clear_tail(t_first + s * F::KT, crow, crow + F::CROWS, smem + (F::STAGES + (s & 3)) * F::SB);
+        wait_loads<2 * F::LPW>();
+        P.clear_tail(t_first + s * F::KT, crow, crow + F::WROWS, smem + (F::STAGES + (s & 3)) * F::SB);
         __syncthreads();
     }
     __device__ __forceinline__ void finish() const {
@@ -756,11 +790,10 @@ __device__ void many_rows(const Piece<ET>& P, uint8_t* smem, int32_t row0, int32
 // workgroup long and short ones), b % 8 kept: heads stay on their XCD's L2.  Half of the workgroups go through
 // the rounds backwards, so that the single tokens' reads and the chunks' products overlap.
 template <typename ET>
-__global__ __launch_bounds__(256, 1) void paged_attn_kernel(AttnArgs a) {
-    constexpr int MANY = Form<ET>::MANY;
+__global__ __launch_bounds__(64 * Form<ET>::WAVES, 1) void paged_attn_kernel(AttnArgs a) {
     extern __shared__ __align__(1024) uint8_t smem[];
     const SeqRange first = load_range(a, threadIdx.x & 63);
-    const Plan plan = wave_plan<MANY>(a, first);
+    const Plan plan = wave_plan(a, first);
     if (a.rec_rows && blockIdx.x == 0 && threadIdx.x == 0) *plan_of(a) = plan.L;
     const int32_t L = plan.L;
     const uint32_t b = blockIdx.x, n = gridDim.x;
@@ -770,15 +803,15 @@ __global__ __launch_bounds__(256, 1) void paged_attn_kernel(AttnArgs a) {
     for (int k = 0; k < rounds; ++k) {
         const int round = b & 8 ? rounds - 1 - k : k;
         const int64_t idx = (int64_t)round * n + (round & 1 ? ((n - 1 - b) & ~7u) | (b & 7u) : b);
-        if ((idx >= u.end || idx < u.base) && !find_unit<MANY, false>(a, L, first, idx, u)) {
+        if ((idx >= u.end || idx < u.base) && !find_unit<false>(a, L, first, idx, u)) {
             u.base = u.end = 0;
             continue;                                      // behind the last piece
         }
         const SeqRange r = u.r;
         const uint32_t in = (uint32_t)(idx - u.base), G = (uint32_t)a.G;
         const int g = (int)(in % G), piece = (int)(in / G % (uint32_t)u.np);
-        const int tile = seq_tiles(r, a.Hg, MANY) - 1 - (int)(in / G / (uint32_t)u.np);
-        const int bm = tile_rows(r, a.Hg, MANY);
+        const int tile = seq_tiles(r, a.Hg) - 1 - (int)(in / G / (uint32_t)u.np);
+        const int bm = tile_rows(r, a.Hg);
         const int32_t row0 = tile * bm;
         const int32_t rows = (int32_t)(seq_rows(r, a.Hg) - row0 < bm ? seq_rows(r, a.Hg) - row0 : bm);
         // keys that the tile's rows see, and of them this piece
@@ -787,8 +820,8 @@ __global__ __launch_bounds__(256, 1) void paged_attn_kernel(AttnArgs a) {
         row_keys(r, (row0 + rows - 1) / a.Hg, a.causal, a.window, x, hi);
         const bool cut = u.np > 1;
         if (cut) {
-            const int32_t len = piece_len(seq_span(r, a.window), u.np);
-            const int64_t p0 = seq_first(r, a.window) + (int64_t)piece * len;
+            const int32_t len = piece_len(seq_span(r, a.Hg, a.window), u.np);
+            const int64_t p0 = (lo & ~63) + (int64_t)piece * len;
             if (lo < p0) lo = (int32_t)(p0 < r.klen ? p0 : r.klen);
             if (hi > p0 + len) hi = (int32_t)(p0 + len);
         }
@@ -802,14 +835,14 @@ __global__ __launch_bounds__(256, 1) void paged_attn_kernel(AttnArgs a) {
     }
 }
 
-// Joins the pieces of cut sequences, up to JOIN_ROWS rows of a (tile, head) pair a workgroup: its waves take every
-// fourth row of many, or of few rows every fourth piece of one.
-constexpr int JOIN_ROWS = 32;
+// Joins the pieces of cut sequences: a workgroup takes JOIN_ROWS rows of a head, a wave each, or of few rows one,
+// every fourth piece a wave.  A wave takes 8 pieces at a time with a running maximum, so that nothing waits for all
+// maxima first.  It is a chain of reads that the other dies have just written, about 2 us each: rows in parallel
+// are what helps (32 rows a workgroup: 126 us for 256 rows of 8 heads in 32 pieces; 4: 11 us).
 template <typename ET>
 __global__ __launch_bounds__(256) void paged_join_kernel(AttnArgs a) {
-    constexpr int MANY = Form<ET>::MANY;
     __shared__ float so[4][D];
-    __shared__ float sl[4];
+    __shared__ float sl[4][2];
     const SeqRange first = load_range(a, threadIdx.x & 63);
     const int32_t L = first_lane(*plan_of(a));
     if (L == WHOLE) return;
@@ -817,53 +850,69 @@ __global__ __launch_bounds__(256) void paged_join_kernel(AttnArgs a) {
     const float* rec_ml = a.rec + a.rec_rows * D;
     Unit u;
     u.base = u.end = 0;
-    constexpr int parts = MANY / JOIN_ROWS;
-    for (int64_t w = blockIdx.x;; w += gridDim.x) {
-        const int64_t idx = w / parts;
-        const int part = (int)(w % parts);
-        if (idx >= u.end && !find_unit<MANY, true>(a, L, first, idx, u)) break;
-        const uint32_t pair = (uint32_t)(idx - u.base), G = (uint32_t)a.G;
-        const uint32_t in = pair / G * (uint32_t)u.np * G + pair % G;       // the number of its piece 0
+    for (int64_t idx = blockIdx.x;; idx += gridDim.x) {
+        if (idx >= u.end && !find_unit<true>(a, L, first, idx, u)) break;
         const SeqRange r = u.r;
-        const int g = (int)(in % G), tile = seq_tiles(r, a.Hg, MANY) - 1 - (int)(in / G / (uint32_t)u.np);
-        const int bm = tile_rows(r, a.Hg, MANY);
-        const int32_t row0 = tile * bm;
-        const int32_t rows = (int32_t)(seq_rows(r, a.Hg) - row0 < bm ? seq_rows(r, a.Hg) - row0 : bm);
-        const int64_t rec0 = u.rec + (int64_t)in * bm, stride = (int64_t)G * bm;   // piece p's rows: rec0 + p stride
-        if (rec0 + (u.np - 1) * stride + bm > a.rec_rows) continue;
+        const uint32_t in = (uint32_t)(idx - u.base), G = (uint32_t)a.G;
+        const int g = (int)(in % G), bm = tile_rows(r, a.Hg);
         const bool few = bm == ROWS_FEW;
-        // few rows: parts share the rows out, one row at a time for the whole workgroup
-        for (int i = few ? part : part * JOIN_ROWS + wave; i < rows && (few || i < (part + 1) * JOIN_ROWS); i += few ? parts : 4) {
-            float M = -INFINITY;
-            for (int p = lane; p < u.np; p += 64) M = fmaxf(M, rec_ml[(rec0 + p * stride + i) * 2]);
+        const int64_t row = few ? in / G : (int64_t)(in / G) * JOIN_ROWS + wave;
+        const int tile = (int)(row / bm), i = (int)(row % bm);
+        const int64_t number = (int64_t)(seq_tiles(r, a.Hg) - 1 - tile) * u.np * G + g;      // of the tile's piece 0
+        const int64_t rec0 = u.rec + number * bm, stride = (int64_t)G * bm;   // piece p's rows: rec0 + p stride
+        if (rec0 + (u.np - 1) * stride + bm > a.rec_rows) continue;           // as the first launch (few: uniform)
+        if (row < seq_rows(r, a.Hg)) {
+            float M = -INFINITY, o0 = 0.f, o1 = 0.f, l = 0.f;
+            const int p0 = few ? wave : 0, ps = few ? 4 : 1;
+            for (int p = p0; p < u.np; p += 8 * ps) {
+                float2 ml[8], v[8];
 #pragma unroll
-            for (int x = 1; x < 64; x <<= 1) M = fmaxf(M, __shfl_xor(M, x, WAVE));
-            const float mu = M == -INFINITY ? 0.f : M;
-            float o0 = 0.f, o1 = 0.f, l = 0.f;
-#pragma unroll 4
-            for (int p = few ? wave : 0; p < u.np; p += few ? 4 : 1) {
-                const int64_t rr = rec0 + p * stride + i;
-                const float2 ml = *reinterpret_cast<const float2*>(rec_ml + rr * 2);
-                const float2 v = *reinterpret_cast<const float2*>(a.rec + rr * D + 2 * lane);
-                const float f = __builtin_amdgcn_exp2f((ml.x - mu) * a.c);
-                l = fmaf(f, ml.y, l);
-                o0 = fmaf(f, v.x, o0);
-                o1 = fmaf(f, v.y, o1);
+                for (int k = 0; k < 8; ++k) {              // past the last piece: the last again, weight 0
+                    const int q = p + k * ps < u.np ? p + k * ps : u.np - 1;
+                    const int64_t rr = rec0 + q * stride + i;
+                    ml[k] = *reinterpret_cast<const float2*>(rec_ml + rr * 2);
+                    v[k] = *reinterpret_cast<const float2*>(a.rec + rr * D + 2 * lane);
+                }
+                float mn = M;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) mn = fmaxf(mn, ml[k].x);
+                const float mu = mn == -INFINITY ? 0.f : mn, f0 = __builtin_amdgcn_exp2f((M - mu) * a.c);
+                M = mn;
+                l *= f0;
+                o0 *= f0;
+                o1 *= f0;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    if (p + k * ps >= u.np) continue;
+                    const float f = __builtin_amdgcn_exp2f((ml[k].x - mu) * a.c);
+                    l = fmaf(f, ml[k].y, l);
+                    o0 = fmaf(f, v[k].x, o0);
+                    o1 = fmaf(f, v[k].y, o1);
+                }
             }
             if (few) {
                 __syncthreads();
                 so[wave][2 * lane] = o0;
                 so[wave][2 * lane + 1] = o1;
-                if (lane == 0) sl[wave] = l;
+                if (lane == 0) {
+                    sl[wave][0] = M;
+                    sl[wave][1] = l;
+                }
                 __syncthreads();
                 if (wave) continue;
-                l = (sl[0] + sl[1]) + (sl[2] + sl[3]);
-                o0 = (so[0][2 * lane] + so[1][2 * lane]) + (so[2][2 * lane] + so[3][2 * lane]);
-                o1 = (so[0][2 * lane + 1] + so[1][2 * lane + 1]) + (so[2][2 * lane + 1] + so[3][2 * lane + 1]);
+                M = fmaxf(fmaxf(sl[0][0], sl[1][0]), fmaxf(sl[2][0], sl[3][0]));
+                const float mu = M == -INFINITY ? 0.f : M;
+                o0 = o1 = l = 0.f;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float f = __builtin_amdgcn_exp2f((sl[k][0] - mu) * a.c);
+                    l = fmaf(f, sl[k][1], l);
+                    o0 = fmaf(f, so[k][2 * lane], o0);
+                    o1 = fmaf(f, so[k][2 * lane + 1], o1);
+                }
             }
             const float inv = l == 0.f ? 0.f : 1.f / l;
-            const int32_t row = row0 + i;
-            ET* dst = (ET*)a.out + (int64_t)(r.q0 + row / a.Hg) * a.out_stride + (int64_t)(g * a.Hg + row % a.Hg) * D + 2 * lane;
+            ET* dst = (ET*)a.out + (r.q0 + row / a.Hg) * a.out_stride + (g * a.Hg + row % a.Hg) * D + 2 * lane;
             if constexpr (sizeof(ET) == 2) *reinterpret_cast<uint32_t*>(dst) = cvt_bf16x2(o0 * inv, o1 * inv);
             else *reinterpret_cast<float2*>(dst) = float2{o0 * inv, o1 * inv};
         }
@@ -872,19 +921,19 @@ __global__ __launch_bounds__(256) void paged_join_kernel(AttnArgs a) {
 
 // SLOTS workgroups, and the second launch unless the tables are too short for a cut
 template <typename ET>
-hipError_t launch_paged(const AttnArgs& a, int64_t units, int64_t pieces, hipStream_t st) {
+hipError_t launch_paged(const AttnArgs& a, int64_t pieces, hipStream_t st) {
     const void* fn = (const void*)paged_attn_kernel<ET>;
     hipError_t e = ensure_lds_limit(fn, Form<ET>::LDS);
     if (e != hipSuccess) return e;
     const unsigned grid = pieces < SLOTS ? ((unsigned)pieces + 7) & ~7u : SLOTS;
-    paged_attn_kernel<ET><<<grid, 256, Form<ET>::LDS, st>>>(a);
+    paged_attn_kernel<ET><<<grid, 64 * Form<ET>::WAVES, Form<ET>::LDS, st>>>(a);
     if ((e = hipGetLastError()) != hipSuccess || !a.rec_rows) return e;
-    const int64_t parts = units * (Form<ET>::MANY / JOIN_ROWS);
-    paged_join_kernel<ET><<<(unsigned)(parts < 1024 ? parts : 1024), 256, 0, st>>>(a);
+    const int64_t rows = (int64_t)a.T * a.G * a.Hg;
+    paged_join_kernel<ET><<<(unsigned)(rows < 2048 ? rows : 2048), 256, 0, st>>>(a);
     return hipGetLastError();
 }
 
-hipError_t launch_paged_bf16(const AttnArgs& a, int64_t units, int64_t pieces, hipStream_t st);
-hipError_t launch_paged_f32(const AttnArgs& a, int64_t units, int64_t pieces, hipStream_t st);
+hipError_t launch_paged_bf16(const AttnArgs& a, int64_t pieces, hipStream_t st);
+hipError_t launch_paged_f32(const AttnArgs& a, int64_t pieces, hipStream_t st);
 
 }  // namespace vr

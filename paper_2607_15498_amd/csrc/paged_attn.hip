@@ -18,7 +18,8 @@
 //
 // Keys and values come by direct-to-LDS loads of 1 KB (whole rows).  Row r's 16-byte piece c lies at
 // place c ^ f(r), f(r) = 4 (r % 4) + (r / 4) % 4, which spreads the K fragment reads (32 rows, one
-// piece) and the transposing V reads (8 rows, 4 pieces) over all banks.
+// piece) and the transposing V reads (8 rows, 4 pieces) over all banks; fp32 values, read 128 bytes of
+// two rows at a time, at place c ^ 8 ((r / 4) % 2).
 #include <type_traits>
 #include <utility>
 
@@ -209,9 +210,7 @@ __device__ __forceinline__ void many_rows<uint16_t>(const Piece<uint16_t>& P, ui
         f32x16 &s0 = sc[e][0], &s1 = sc[e][1];
         const uint8_t* vt = M.values_of(j - 2);
         const bool qk = j >= M.jf && j < M.jl, ex = j - 1 >= M.jf && j - 1 < M.jl, pv = j - 2 >= M.jf && j - 2 < M.jl;
-        // the lane's numbers anew, or what the masks need of them is kept in registers for the whole loop
-        Piece<uint16_t> L = P;
-        asm volatile("" : "+v"(L.lane), "+v"(L.l32), "+v"(L.h));
+        const Piece<uint16_t> L = P.anew();
         follow();
         if (ex)
 #pragma unroll
@@ -223,24 +222,28 @@ __device__ __forceinline__ void many_rows<uint16_t>(const Piece<uint16_t>& P, ui
                 }
         if (pv) {
             settle();
-            if (M.masked(j - 2) && L.odd_values(vt)) {
+            const bool odd = M.masked(j - 2) && L.odd_values(vt);
+            static_for<8>([&](auto n) {
+                u32x4 f = L.vfrag(vt, 16 * (n >> 2), n & 3);
+                if (odd)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) f[k] = L.finite(f[k]);
+                value<n & 3, 0, true>(f, p[e][0][n >> 2]);
+                value<n & 3, 1, true>(f, p[e][1][n >> 2]);
+            });
+            if (odd) {
+                settle();
                 static_for<2>([&](auto c) {
                     int32_t lo, hi;
                     M.keys_seen(c, L.l32, lo, hi);
-                    static_for<4>([&](auto dt) {
-                        f32x16 o;
-                        static_for<16>([&](auto i) { o[i.value] = agpr_get<16 * (4 * c + dt) + i>(); });
-                        L.values_by_key(vt, p[e][c], o, dt, M.t_first + 32 * (j - 2), lo, hi, M.gm_of(j - 2));
-                        static_for<16>([&](auto i) { agpr_set<16 * (4 * c + dt) + i>(__float_as_uint(o[i.value])); });
-                    });
+                    f32x16 o[4];
+                    static_for<64>([&](auto i) { o[i / 16][i % 16] = 0.f; });
+                    L.add_odd(vt, M.t_first + 32 * (j - 2), lo, hi, M.gm_of(j - 2),
+                              [&](int dt, int i, float x) { o[dt][i] += x; });
+                    static_for<64>([&](auto i) { agpr_set<64 * c + i>(__float_as_uint(agpr_get<64 * c + i>() + o[i / 16][i % 16])); });
                 });
                 settle();
-            } else
-                static_for<8>([&](auto n) {
-                    const u32x4 f = L.vfrag(vt, 16 * (n >> 2), n & 3);
-                    value<n & 3, 0, true>(f, p[e][0][n >> 2]);
-                    value<n & 3, 1, true>(f, p[e][1][n >> 2]);
-                });
+            }
         }
         mx[0] = mx[1] = -INFINITY;
         if (qk) {
@@ -304,14 +307,11 @@ __device__ __forceinline__ void many_rows<uint16_t>(const Piece<uint16_t>& P, ui
     M.finish();
 }
 
-hipError_t launch_paged_bf16(const AttnArgs& a, int64_t units, int64_t pieces, hipStream_t st) { return launch_paged<uint16_t>(a, units, pieces, st); }
+hipError_t launch_paged_bf16(const AttnArgs& a, int64_t pieces, hipStream_t st) { return launch_paged<uint16_t>(a, pieces, st); }
 
 // ---- host ------------------------------------------------------------------------------------
-constexpr int LMIN = 512;          // shortest piece, in tokens
-static int many_of(int dtype) { return dtype == VARRATE_BF16 ? Form<uint16_t>::MANY : Form<float>::MANY; }
-
 size_t paged_attn_ws_bytes(int64_t T, int S, int G, int H, int dtype, int64_t cap) {
-    const int64_t rows = max_records(T, S, G, H / G, many_of(dtype), cap, LMIN);
+    const int64_t rows = max_records(T, S, G, H / G, cap, costs_of(dtype == VARRATE_BF16).lmin);
     return rows ? (size_t)rows * (D + 2) * 4 + 16 : 0;
 }
 
@@ -338,13 +338,11 @@ hipError_t launch_paged_attn(const varrate_pages& pg, const varrate_batch& b, co
     a.shift = __builtin_ctz((unsigned)pg.page);
     a.causal = causal;
     a.window = window;
-    a.lmin = LMIN;
+    a.costs = costs_of(pg.dtype == VARRATE_BF16);
     a.c = scale * 1.4426950408889634f;
-    const int many = many_of(pg.dtype);
-    a.rec_rows = max_records(b.T, b.S, pg.G, a.Hg, many, a.cap, LMIN);
-    const int64_t units = max_units(b.T, b.S, pg.G, a.Hg, many);
-    const int64_t pieces = max_pieces(b.T, b.S, pg.G, a.Hg, many, a.cap, LMIN);
-    return pg.dtype == VARRATE_BF16 ? launch_paged_bf16(a, units, pieces, st) : launch_paged_f32(a, units, pieces, st);
+    a.rec_rows = max_records(b.T, b.S, pg.G, a.Hg, a.cap, a.costs.lmin);
+    const int64_t pieces = max_pieces(b.T, b.S, pg.G, a.Hg, a.cap, a.costs.lmin);
+    return pg.dtype == VARRATE_BF16 ? launch_paged_bf16(a, pieces, st) : launch_paged_f32(a, pieces, st);
 }
 
 }  // namespace vr

@@ -1,5 +1,6 @@
-// The fp32 kernel of the paged attention (paged_attn.hip), whose products take 16 times as long as bf16's: one
-// step after another keeps the matrix cores busy.
+// The fp32 kernel of the paged attention (paged_attn.hip).  Its products take 16 times as long as bf16's, so its
+// many-rows form goes one step after another, 32 rows a wave and two waves a SIMD: while one takes exponentials
+// or waits for a fragment, the other's products run.
 #include "paged_attn.h"
 
 namespace vr {
@@ -12,11 +13,10 @@ __device__ __forceinline__ void many_rows<float>(const Piece<float>& P, uint8_t*
     if (M.stages) M.begin();
     Running run;
     u32x4 qf[1][16];
-    int32_t tok, head, mylo, myhi;
-    M.row_of(0, P.l32, tok, head);
-    M.keys_seen(0, P.l32, mylo, myhi);
-    P.query(qf[0], P.r.q0 + tok, head);
     f32x16 acc[1][4];
+    int32_t tok, head;
+    M.row_of(0, P.l32, tok, head);
+    P.query(qf[0], P.r.q0 + tok, head);
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
@@ -29,7 +29,13 @@ __device__ __forceinline__ void many_rows<float>(const Piece<float>& P, uint8_t*
         f32x16 sc[1];
         P.template scores<1>(M.keys_of(j), qf, sc);
         const bool masked = M.masked(j);
-        if (masked) P.mask(sc[0], M.t_first + 32 * j, mylo, myhi, M.gm_of(j));
+        const int32_t t0 = M.t_first + 32 * j;
+        if (masked) {
+            const Piece<float> A = P.anew();
+            int32_t lo, hi;
+            M.keys_seen(0, A.l32, lo, hi);
+            A.mask(sc[0], t0, lo, hi, M.gm_of(j));
+        }
         const float mt = P.most(sc[0]);
         if (__any(mt > run.m + slack)) {
             const float f = run.raise(mt, a.c);
@@ -39,11 +45,14 @@ __device__ __forceinline__ void many_rows<float>(const Piece<float>& P, uint8_t*
                 for (int k = 0; k < 16; ++k) acc[0][dt][k] *= f;
         }
         weights(sc[0], a.c, run.off, run.l);
-        if (masked && P.odd_values(M.values_of(j)))
-#pragma unroll
-            for (int dt = 0; dt < 4; ++dt)
-                P.values_by_key(M.values_of(j), sc[0], acc[0][dt], dt, M.t_first + 32 * j, mylo, myhi, M.gm_of(j));
-        else P.template values<1>(M.values_of(j), sc, acc);
+        const uint8_t* vt = M.values_of(j);
+        if (masked && P.anew().odd_values(vt)) {
+            const Piece<float> A = P.anew();
+            A.template values<1, true>(vt, sc, acc);
+            int32_t lo, hi;
+            M.keys_seen(0, A.l32, lo, hi);
+            A.add_odd(vt, t0, lo, hi, M.gm_of(j), [&](int dt, int i, float x) { acc[0][dt][i] += x; });
+        } else P.template values<1>(vt, sc, acc);
     }
     const float l = xsum32(run.l);
 #pragma unroll
@@ -51,6 +60,6 @@ __device__ __forceinline__ void many_rows<float>(const Piece<float>& P, uint8_t*
     M.finish();
 }
 
-hipError_t launch_paged_f32(const AttnArgs& a, int64_t units, int64_t pieces, hipStream_t st) { return launch_paged<float>(a, units, pieces, st); }
+hipError_t launch_paged_f32(const AttnArgs& a, int64_t pieces, hipStream_t st) { return launch_paged<float>(a, pieces, st); }
 
 }  // namespace vr
