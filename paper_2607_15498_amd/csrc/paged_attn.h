@@ -32,11 +32,6 @@ struct AttnArgs {
 // rows of a bad page: 1 KB of zeros
 __device__ const uint4 pa_zeros[64] = {};
 
-// One direct-to-LDS load: 16 bytes per lane from base + off to LDS byte address dst + 16 lane.
-__device__ __forceinline__ void lds_load(const void* base, uint32_t off, uint32_t dst) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(dst)
-                 : "memory", "m0");
-}
 template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
@@ -59,6 +54,12 @@ __device__ __forceinline__ int64_t first_lane(int64_t v) {
     return (int64_t)((uint64_t)(uint32_t)first_lane((int32_t)(v >> 32)) << 32 | lo);
 }
 
+// One direct-to-LDS load: 16 bytes per lane from base + off to LDS byte address dst + 16 lane.
+__device__ __forceinline__ void lds_load(const void* base, uint32_t off, uint32_t dst) {
+    const uint64_t b = (uint64_t)first_lane((int64_t)base);      // scalars, wherever the compiler keeps them
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(b), "s"(first_lane((int)dst))
+                 : "memory", "m0");
+}
 __device__ __forceinline__ int64_t lane64(int64_t v, int lane) {
     return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 |
                      (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane));
@@ -82,69 +83,38 @@ __device__ __forceinline__ SeqRange load_range(const AttnArgs& a, int s) {
     if (s < a.S) r = seq_range(a.q_start[s], a.q_start[s + 1], a.kv_len[s], a.T, a.cap);
     return r;
 }
-// `first`: the first 64 sequences, kept for find_unit.  Counts are held to 2^24 a lane: more than PIECES_MAX
-// is enough to know.
-struct Plan { int32_t L, pieces; };
+// `first`: the first 64 sequences, kept for find_unit.
 __device__ __forceinline__ Plan wave_plan(const AttnArgs& a, const SeqRange& first) {
     const int lane = threadIdx.x & 63, n = a.S < 64 ? a.S : 64;
-    int64_t units = 0, work = 0, spans = 0;
-    int32_t longest = 0;
-    uint64_t many = 0;
-    for (int s0 = 0; s0 < a.S; s0 += 64) {
-        const SeqRange r = s0 ? load_range(a, s0 + lane) : first;
-        const int64_t t = (int64_t)seq_tiles(r, a.Hg) * a.G;
-        const int32_t span = seq_span(r, a.Hg, a.window);
-        units += t;
-        const int32_t c = key_cost(r, a.Hg, a.costs);
-        work += t * seq_mean(r, span, a.causal) * c;
-        spans += t * span * c;
-        if (t && span > longest) longest = span;
-        many |= __ballot(tile_rows(r, a.Hg) != ROWS_FEW);
-    }
-    longest = wave_most(longest, n);
-    units = wave_sum(units, n);
-    Plan best = {WHOLE, units < INT32_MAX ? (int32_t)units : INT32_MAX};
-    if (longest <= a.costs.lmin || units >= PIECES_MAX) return best;
-    work = wave_sum(work, n);
-    spans = wave_sum(spans, n);
-    int32_t L[CUTS], np[CUTS];
-    int64_t most[CUTS];
-#pragma unroll
-    for (int i = 0; i < CUTS; ++i) {
-        L[i] = cut_try(i, spans);
-        np[i] = 0;
-        most[i] = 0;
-    }
-    for (int s0 = 0; s0 < a.S; s0 += 64) {
-        const SeqRange r = s0 ? load_range(a, s0 + lane) : first;
-        const int32_t t = seq_tiles(r, a.Hg) * a.G, span = seq_span(r, a.Hg, a.window);       // t < PIECES_MAX
-        const int32_t c = key_cost(r, a.Hg, a.costs);
-#pragma unroll
-        for (int i = 0; i < CUTS; ++i) {
-            const int32_t m = seq_pieces(span, c, L[i], a.costs.lmin);
-            const int64_t len = t ? (int64_t)piece_len(span, m) * c : 0, sum = np[i] + (int64_t)t * m;
-            np[i] = sum < (1 << 24) ? (int32_t)sum : 1 << 24;
-            if (len > most[i]) most[i] = len;
-        }
-    }
+    Sums s;
+    for (int s0 = 0; s0 < a.S; s0 += 64)
+        sum_up(s, s0 ? load_range(a, s0 + lane) : first, a.G, a.Hg, a.causal, a.window, a.costs);
+    s.longest = wave_most(s.longest, n);
+    s.units = wave_sum(s.units, n);
+    if (!may_cut(s, a.costs)) return uncut(s);
+    s.work = wave_sum(s.work, n);
+    s.spans = wave_sum(s.spans, n);
+    s.many = __any(s.many);
+    CutSums t;
+    cut_begin(t, s.spans);
+    for (int s0 = 0; s0 < a.S; s0 += 64)
+        cut_up(t, s0 ? load_range(a, s0 + lane) : first, a.G, a.Hg, a.window, a.costs);
     for (int m = 1; m < n; m <<= 1)
 #pragma unroll
         for (int i = 0; i < CUTS; ++i) {
-            np[i] += __shfl_xor(np[i], m, WAVE);
-            const int64_t x = __shfl_xor(most[i], m, WAVE);
-            most[i] = x > most[i] ? x : most[i];
+            t.pieces[i] += __shfl_xor(t.pieces[i], m, WAVE);
+            t.partial[i] += __shfl_xor(t.partial[i], m, WAVE);
+            const int64_t x = __shfl_xor(t.most[i], m, WAVE);
+            t.most[i] = x > t.most[i] ? x : t.most[i];
         }
-    int64_t cost = INT64_MAX;
 #pragma unroll
     for (int i = 0; i < CUTS; ++i) {
-        const int32_t count = first_lane(np[i]);
-        const int64_t c = cut_cost(count, first_lane(most[i]), work, units, many == 0, a.costs);
-        if (c < cost) {
-            cost = c;
-            best = {L[i], count};
-        }
+        t.pieces[i] = first_lane(t.pieces[i]);
+        t.partial[i] = first_lane(t.partial[i]);
+        t.most[i] = first_lane(t.most[i]);
     }
-    return best;
+    const Plan p = pick(t, s, a.costs);
+    return Plan{first_lane(p.L), first_lane(p.pieces)};
 }
 // The sequence of number idx.  A sequence's pieces are (tile, piece, head) triples, heads innermost and the last
 // tile first (with causal rows it sees the most keys); JOIN: numbers count the second launch's work, (JOIN_ROWS rows,
@@ -287,7 +257,6 @@ struct Piece {
 #pragma unroll
         for (int k = 0; k < F::NF; ++k) qf[k] = load16(src + (2 * k + h) * 16);
     }
-    __device__ __forceinline__ int key_of(int i) const { return 8 * (i >> 2) + 4 * h + (i & 3); }
     // scores of NC blocks of 32 rows with 32 keys
     template <int NC>
     __device__ __forceinline__ void scores(const uint8_t* kt, const u32x4 (&qf)[NC][F::NF], f32x16 (&sc)[NC]) const {
@@ -310,14 +279,23 @@ struct Piece {
             }
         }
     }
-    // keys of a block from t0 on that the row with keys [mylo, myhi) does not see; gm: 16-key groups with a page
-    __device__ __forceinline__ bool sees(int32_t t, int32_t mylo, int32_t myhi, uint32_t gm_bit) const {
-        return t >= mylo && t < myhi && t >= lo && t < hi && gm_bit;
+    // The keys that a row sees of this piece, as the first and their number; gm: 16-key groups with a page.
+    struct Seen { int32_t lo, n; };
+    __device__ __forceinline__ Seen seen(int32_t row_lo, int32_t row_hi) const {
+        const int32_t b = row_lo > lo ? row_lo : lo, e = row_hi < hi ? row_hi : hi;
+        return Seen{b, e > b ? e - b : 0};
     }
-    __device__ __forceinline__ void mask(f32x16& sc, int32_t t0, int32_t mylo, int32_t myhi, uint32_t gm) const {
+    static __device__ __forceinline__ bool sees(int32_t t, Seen s) { return (uint32_t)(t - s.lo) < (uint32_t)s.n; }
+    __device__ __forceinline__ void mask(f32x16& sc, int32_t t0, Seen s, uint32_t gm) const {
+        if (gm != 3u) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (!(gm >> (i >> 3) & 1u)) sc[i] = -INFINITY;
+        }
+        const uint32_t at = (uint32_t)(t0 + 4 * h - s.lo);
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-            if (!sees(t0 + key_of(i), mylo, myhi, gm >> (i >> 3) & 1u)) sc[i] = -INFINITY;
+            if (at + 8 * (i >> 2) + (i & 3) >= (uint32_t)s.n) sc[i] = -INFINITY;
     }
     __device__ __forceinline__ float most(const f32x16& sc) const {
         float m = sc[0];
@@ -391,10 +369,10 @@ struct Piece {
     }
     // add(dt, i, x): x to the lane's sum of dim 32 dt + 8 (i / 4) + 4 h + i % 4
     template <typename A>
-    __device__ __forceinline__ void add_odd(const uint8_t* vt, int32_t t0, int32_t mylo, int32_t myhi, uint32_t gm, A&& add) const {
+    __device__ __forceinline__ void add_odd(const uint8_t* vt, int32_t t0, Seen s, uint32_t gm, A&& add) const {
 #pragma unroll 1
         for (int kk = 0; kk < 32; ++kk) {
-            const bool see = sees(t0 + kk, mylo, myhi, gm >> (kk >> 4) & 1u);
+            const bool see = sees(t0 + kk, s) && (gm >> (kk >> 4) & 1u);
             const int f = F::BF ? ((kk & 3) << 2) | ((kk >> 2) & 3) : ((kk >> 2) & 1) << 3;
 #pragma unroll
             for (int n = 0; n < 16; ++n) {                 // dims 8 n + 4 h ..
@@ -482,6 +460,7 @@ __device__ __forceinline__ void few_rows(const Piece<ET>& P, uint8_t* smem, int 
     const int myrow = l32 < rows ? l32 : 0, tok = myrow / Hg;
     int32_t mylo, myhi, firsthi, lastlo, x;
     row_keys(r, tok, a.causal, a.window, mylo, myhi);
+    const auto seen = P.seen(mylo, myhi);
     row_keys(r, 0, a.causal, a.window, x, firsthi);
     row_keys(r, (rows - 1) / Hg, a.causal, a.window, lastlo, x);
     u32x4 qf[1][F::NF];
@@ -535,7 +514,7 @@ __device__ __forceinline__ void few_rows(const Piece<ET>& P, uint8_t* smem, int 
         u32x4 p[1][2];
         auto softmax = [&]() {
             P.template scores<1>(kt, qf, sc);
-            if (masked) P.anew().mask(sc[0], t0, mylo, myhi, gm);
+            if (masked) P.anew().mask(sc[0], t0, seen, gm);
             const float mt = P.most(sc[0]);
             if (__any(mt > run.m + SLACK / a.c)) {
                 const float f = run.raise(mt, a.c);
@@ -581,7 +560,7 @@ __device__ __forceinline__ void few_rows(const Piece<ET>& P, uint8_t* smem, int 
             if (odd) P.anew().template values<1, true>(vt, sc, acc);
             else P.template values<1>(vt, sc, acc);
         }
-        if (odd) P.anew().add_odd(vt, t0, mylo, myhi, gm, [&](int dt, int i, float x) { acc[0][dt][i] += x; });
+        if (odd) P.anew().add_odd(vt, t0, seen, gm, [&](int dt, int i, float x) { acc[0][dt][i] += x; });
         if constexpr (!F::BF) {
             wait_lds();                                    // the values have been read
             if (more) {
@@ -700,10 +679,11 @@ struct Many {
         tok = row / P.a.Hg;
         head = P.g * P.a.Hg + row % P.a.Hg;
     }
-    __device__ __forceinline__ void keys_seen(int c, int l32, int32_t& lo, int32_t& hi) const {
-        int32_t tok, head;
-        row_of(c, l32, tok, head);
+    __device__ __forceinline__ typename Piece<ET>::Seen keys_seen(int c) const {
+        int32_t tok, head, lo, hi;
+        row_of(c, P.l32, tok, head);
         row_keys(P.r, tok, P.a.causal, P.a.window, lo, hi);
+        return P.seen(lo, hi);
     }
     __device__ __forceinline__ int32_t within(int32_t t) const { return (t < P.lo ? P.lo : t > P.hi ? P.hi : t) - t_first; }
     __device__ __forceinline__ int32_t window_key(int w) const { return t_first + 1024 * w + 16 * P.lane; }
@@ -732,6 +712,13 @@ struct Many {
     __device__ __forceinline__ void bring(int i) const {
         if (i < F::LPW) P.template bring1<false>(ksrc, adv, i, crow / 4, dst);
         else P.template bring1<true>(vsrc, adv, i - F::LPW, crow / 4, dst + F::STAGES * F::SB);
+    }
+    __device__ __forceinline__ void bring_half(bool keys) const {
+        const uint8_t* src = keys ? ksrc : vsrc;
+        const uint32_t to = keys ? dst : dst + F::STAGES * F::SB;
+        static_assert(F::BF || F::LPW == 2, "bf16 alone: both kinds of rows are laid out alike");
+#pragma unroll
+        for (int i = 0; i < F::LPW; ++i) P.template bring1<false>(src, adv, i, crow / 4, to);
     }
     __device__ __forceinline__ void issue(int s) {
         aim(s);

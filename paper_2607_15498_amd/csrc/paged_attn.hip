@@ -63,28 +63,20 @@ template <int A> __device__ __forceinline__ float agpr_get() {
 }
 // 19 wait states between the last product into a register and its use by anything else, and 4 before the next
 __device__ __forceinline__ void settle() { asm volatile("s_nop 15\n\ts_nop 3" ::: PA_AGPRS); }
-// A product may not follow within 2 wait states the vector instruction that wrote one of its operands.  The
-// interleaved steps read theirs from LDS or an iteration before (the test of the generated code looks for
-// that); elsewhere WAIT.
+// A product may not follow within 2 wait states the vector instruction that wrote one of its operands: they come
+// from LDS or from an iteration before (the test of the generated code looks for that).
 // s += K Q^T of fragment K, block C; K = 0 starts it
-template <int K, int C, bool WAIT = false> __device__ __forceinline__ void score(f32x16& s, const u32x4& f) {
+template <int K, int C> __device__ __forceinline__ void score(f32x16& s, const u32x4& f) {
     constexpr int q = QBASE + 4 * (8 * C + K);
-#define PA_SCORE(pre, c, o) \
-    asm volatile(pre "v_mfma_f32_32x32x16_bf16 %0, %1, a[%2:%3], " c : o(s) : "v"(f), "n"(q), "n"(q + 3) : PA_AGPRS)
-    if constexpr (K == 0 && WAIT) PA_SCORE("s_nop 3\n\t", "0", "=&v");
-    else if constexpr (K == 0) PA_SCORE("", "0", "=&v");
-    else if constexpr (WAIT) PA_SCORE("s_nop 3\n\t", "%0", "+v");
-    else PA_SCORE("", "%0", "+v");
-#undef PA_SCORE
+    if constexpr (K == 0)
+        asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, a[%2:%3], 0" : "=&v"(s) : "v"(f), "n"(q), "n"(q + 3) : PA_AGPRS);
+    else
+        asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, a[%2:%3], %0" : "+v"(s) : "v"(f), "n"(q), "n"(q + 3) : PA_AGPRS);
 }
 // sums of block C, dims 32 DT .. += V^T P^T
-template <int DT, int C, bool WAIT = false> __device__ __forceinline__ void value(const u32x4& f, const u32x4& p) {
+template <int DT, int C> __device__ __forceinline__ void value(const u32x4& f, const u32x4& p) {
     constexpr int o = 16 * (4 * C + DT);
-#define PA_VALUE(pre) \
-    asm volatile(pre "v_mfma_f32_32x32x16_bf16 a[%2:%3], %0, %1, a[%2:%3]" ::"v"(f), "v"(p), "n"(o), "n"(o + 15) : PA_AGPRS)
-    if constexpr (WAIT) PA_VALUE("s_nop 3\n\t");
-    else PA_VALUE("");
-#undef PA_VALUE
+    asm volatile("v_mfma_f32_32x32x16_bf16 a[%2:%3], %0, %1, a[%2:%3]" ::"v"(f), "v"(p), "n"(o), "n"(o + 15) : PA_AGPRS);
 }
 
 // bf16.  One wave has a SIMD to itself, so matrix and vector work overlap within it.  The iteration of step j
@@ -116,8 +108,11 @@ __device__ __forceinline__ void many_rows<uint16_t>(const Piece<uint16_t>& P, ui
         static_for<64>([&](auto i) { agpr_set<QBASE + i>(qf[i / 32][i / 4 % 8][i % 4]); });
     }
     settle();
+    const Piece<uint16_t>::Seen seen[2] = {M.keys_seen(0), M.keys_seen(1)};
     const float slack = SLACK / a.c;
     f32x16 sc[2][2];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sc[0][0][i] = sc[0][1][i] = sc[1][0][i] = sc[1][1][i] = -INFINITY;
     u32x4 p[2][2][2];
     float pend[2] = {1.f, 1.f}, limit[2] = {-INFINITY, -INFINITY};       // limit: scores above it raise the maximum
     float mx[2] = {-INFINITY, -INFINITY};                  // this lane's maxima of the last step's scores
@@ -204,41 +199,59 @@ __device__ __forceinline__ void many_rows<uint16_t>(const Piece<uint16_t>& P, ui
             __builtin_amdgcn_sched_barrier(0);
         });
     };
-    // any step
-    auto slow = [&](auto par, int j) {
-        constexpr int e = decltype(par)::value;
-        f32x16 &s0 = sc[e][0], &s1 = sc[e][1];
+    // any step, as an even one: sc[1] and p[0] are the steps before, and what it forms is moved there (one copy of
+    // the code: short prompts run little else, and fetching it is most of what it costs)
+    auto slow = [&](int j) {
+        f32x16 &s0 = sc[0][0], &s1 = sc[0][1];
+        const std::integral_constant<int, 0> par{};
         const uint8_t* vt = M.values_of(j - 2);
         const bool qk = j >= M.jf && j < M.jl, ex = j - 1 >= M.jf && j - 1 < M.jl, pv = j - 2 >= M.jf && j - 2 < M.jl;
         const Piece<uint16_t> L = P.anew();
+        u32x4 kf[8], vf[8];
+        if (qk)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) kf[k] = kfrag(j, k);
+        if (pv)
+#pragma unroll
+            for (int n = 0; n < 8; ++n) vf[n] = L.vfrag(vt, 16 * (n >> 2), n & 3);
         follow();
-        if (ex)
+        auto weights_of = [&](int k) {
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
+            for (int c = 0; c < 2; ++c) {
+                weigh(par, c, k);
+                pack(par, c, k);
+            }
+        };
+        if (qk) {
+            static_for<8>([&](auto k) {
+                score<k, 0>(s0, kf[k]);
+                score<k, 1>(s1, kf[k]);
+                weights_of(k);                             // of nothing for the first step: scores of -infinity
+            });
+            asm volatile("s_nop 15\n\ts_nop 3" : "+v"(s0), "+v"(s1));
+        } else if (ex) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    weigh(par, c, k);
-                    pack(par, c, k);
-                }
+            for (int k = 0; k < 8; ++k) weights_of(k);
+        }
         if (pv) {
-            settle();
             const bool odd = M.masked(j - 2) && L.odd_values(vt);
-            static_for<8>([&](auto n) {
-                u32x4 f = L.vfrag(vt, 16 * (n >> 2), n & 3);
-                if (odd)
+            if (odd) {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) f[k] = L.finite(f[k]);
-                value<n & 3, 0, true>(f, p[e][0][n >> 2]);
-                value<n & 3, 1, true>(f, p[e][1][n >> 2]);
+                for (int n = 0; n < 8; ++n)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) vf[n][k] = L.finite(vf[n][k]);
+                asm volatile("s_nop 3" : "+v"(vf[0]), "+v"(vf[1]), "+v"(vf[2]), "+v"(vf[3]), "+v"(vf[4]), "+v"(vf[5]), "+v"(vf[6]), "+v"(vf[7]));
+            }
+            static_for<8>([&](auto n) {
+                value<n & 3, 0>(vf[n], p[0][0][n >> 2]);
+                value<n & 3, 1>(vf[n], p[0][1][n >> 2]);
             });
             if (odd) {
                 settle();
                 static_for<2>([&](auto c) {
-                    int32_t lo, hi;
-                    M.keys_seen(c, L.l32, lo, hi);
                     f32x16 o[4];
                     static_for<64>([&](auto i) { o[i / 16][i % 16] = 0.f; });
-                    L.add_odd(vt, M.t_first + 32 * (j - 2), lo, hi, M.gm_of(j - 2),
+                    L.add_odd(vt, M.t_first + 32 * (j - 2), seen[c], M.gm_of(j - 2),
                               [&](int dt, int i, float x) { o[dt][i] += x; });
                     static_for<64>([&](auto i) { agpr_set<64 * c + i>(__float_as_uint(agpr_get<64 * c + i>() + o[i / 16][i % 16])); });
                 });
@@ -247,30 +260,25 @@ __device__ __forceinline__ void many_rows<uint16_t>(const Piece<uint16_t>& P, ui
         }
         mx[0] = mx[1] = -INFINITY;
         if (qk) {
-            static_for<8>([&](auto k) {
-                const u32x4 f = kfrag(j, k);
-                score<k, 0, true>(s0, f);
-                score<k, 1, true>(s1, f);
-            });
-            settle();
-            asm volatile("" : "+v"(s0), "+v"(s1));
             if (M.masked(j))
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    int32_t lo, hi;
-                    M.keys_seen(c, L.l32, lo, hi);
-                    L.mask(sc[e][c], M.t_first + 32 * j, lo, hi, M.gm_of(j));
-                }
+                for (int c = 0; c < 2; ++c) L.mask(sc[0][c], M.t_first + 32 * j, seen[c], M.gm_of(j));
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 mx[0] = fmaxf(mx[0], s0[i]);
                 mx[1] = fmaxf(mx[1], s1[i]);
             }
         }
-        if constexpr (e == 1) stage_ready(j);
-        if (e == 1 || j > 0)
+        if (j & 1) stage_ready(j);
+        if (j > 0) M.bring_half(j & 1);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) M.bring(4 * (1 - e) + i);
+        for (int c = 0; c < 2; ++c) {
+            sc[1][c] = sc[0][c];
+            p[0][c][0] = p[1][c][0];
+            p[0][c][1] = p[1][c][1];
+        }
+        // the copies are written well before the next step's products read them
+        asm volatile("s_nop 1" : "+v"(p[0][0][0]), "+v"(p[0][0][1]), "+v"(p[0][1][0]), "+v"(p[0][1][1]));
     };
     const std::integral_constant<int, 0> even{};
     const std::integral_constant<int, 1> odd{};
@@ -280,7 +288,7 @@ __device__ __forceinline__ void many_rows<uint16_t>(const Piece<uint16_t>& P, ui
     }
     const int32_t end = M.stages ? 2 * M.stages + 2 : 0;   // one stage's steps more: the last weights and values
     for (int j = 0; j < end;) {
-        if (j >= M.mf + 2 && j + 1 < M.ml && !M.bad) {
+        if (!(j & 1) && j >= M.mf + 2 && j + 1 < M.ml && !M.bad) {
             u32x4 kf[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) kf[k] = kfrag(j, k);
@@ -290,9 +298,8 @@ __device__ __forceinline__ void many_rows<uint16_t>(const Piece<uint16_t>& P, ui
                 j += 2;
             } while (j + 1 < M.ml && !M.bad);
         } else {
-            slow(even, j);
-            slow(odd, j + 1);
-            j += 2;
+            slow(j);
+            ++j;
         }
     }
     settle();

@@ -21,6 +21,7 @@ __device__ __forceinline__ void many_rows<float>(const Piece<float>& P, uint8_t*
     for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
         for (int k = 0; k < 16; ++k) acc[0][dt][k] = 0.f;
+    const auto seen = M.keys_seen(0);
     const float slack = SLACK / a.c;
     for (int j = 0; j < M.stages; ++j) {
         M.arrive(j);
@@ -30,12 +31,7 @@ __device__ __forceinline__ void many_rows<float>(const Piece<float>& P, uint8_t*
         P.template scores<1>(M.keys_of(j), qf, sc);
         const bool masked = M.masked(j);
         const int32_t t0 = M.t_first + 32 * j;
-        if (masked) {
-            const Piece<float> A = P.anew();
-            int32_t lo, hi;
-            M.keys_seen(0, A.l32, lo, hi);
-            A.mask(sc[0], t0, lo, hi, M.gm_of(j));
-        }
+        if (masked) P.anew().mask(sc[0], t0, seen, M.gm_of(j));
         const float mt = P.most(sc[0]);
         if (__any(mt > run.m + slack)) {
             const float f = run.raise(mt, a.c);
@@ -49,9 +45,7 @@ __device__ __forceinline__ void many_rows<float>(const Piece<float>& P, uint8_t*
         if (masked && P.anew().odd_values(vt)) {
             const Piece<float> A = P.anew();
             A.template values<1, true>(vt, sc, acc);
-            int32_t lo, hi;
-            M.keys_seen(0, A.l32, lo, hi);
-            A.add_odd(vt, t0, lo, hi, M.gm_of(j), [&](int dt, int i, float x) { acc[0][dt][i] += x; });
+            A.add_odd(vt, t0, seen, M.gm_of(j), [&](int dt, int i, float x) { acc[0][dt][i] += x; });
         } else P.template values<1>(vt, sc, acc);
     }
     const float l = xsum32(run.l);

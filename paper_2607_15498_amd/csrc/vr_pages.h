@@ -77,16 +77,21 @@ VR_HD int32_t seq_mean(SeqRange r, int32_t span, int causal) {
 
 // Costs, in units of 16 cycles of a workgroup, as measured: per key of a tile of few rows while all
 // workgroups read (the memory's share) and of one of many rows (the matrix cores'); of a piece's start
-// and end, and of the second launch.  A lone workgroup's few rows cost a quarter.
-struct Costs { int32_t few, many, piece, join, lmin; };      // lmin: shortest piece, keys
+// and end, and of the second launch, which besides reads what the first has written: JOIN_UNIT partial rows
+// (1040 bytes each, both ways) cost 1.  A lone workgroup's few rows cost a quarter.
+constexpr int JOIN_UNIT = 32;
+struct Costs { int32_t few, many, piece, join, lmin; };      // lmin: shortest piece, keys (a power of two)
 VR_HD Costs costs_of(bool bf16) {
-    return bf16 ? Costs{4, 3, 400, 600, 256} : Costs{8, 40, 400, 600, 128};
+    return bf16 ? Costs{4, 4, 400, 600, 256} : Costs{8, 45, 400, 600, 128};
 }
 VR_HD int32_t key_cost(SeqRange r, int Hg, Costs c) { return tile_rows(r, Hg) == ROWS_FEW ? c.few : c.many; }
-// pieces of a span of keys at `cost` each
+// pieces of a span of keys at `cost` each (32-bit divisions: the plan's code is run once, and what it costs is
+// fetching it)
 VR_HD int32_t seq_pieces(int32_t span, int32_t cost, int32_t L, int32_t lmin) {
     if (L == WHOLE || span <= lmin) return 1;
-    const int64_t n = ((int64_t)span * cost + L - 1) / L, most = (span + lmin - 1) / lmin;
+    const uint64_t all = (uint64_t)(uint32_t)span * (uint32_t)cost;
+    const uint32_t n = ((uint32_t)(all < (1u << 30) ? all : 1u << 30) + (uint32_t)L - 1) / (uint32_t)L;
+    const uint32_t most = ((uint32_t)span + (uint32_t)lmin - 1) >> __builtin_ctz((uint32_t)lmin);
     return (int32_t)(n < most ? n : most);
 }
 // keys of each of a span's np pieces
@@ -100,20 +105,69 @@ constexpr int CUTS = 6;
 constexpr int PIECES_MAX = 4 * SLOTS;          // of a cut call (an uncut one may have any number)
 // spans: sum of tiles x span x cost over sequences and heads
 VR_HD int32_t cut_try(int i, int64_t spans) {
-    if (i == 0) return WHOLE;
-    const int64_t n = (int64_t)(i == 1 ? 3 : 4 * (i - 1)) * (SLOTS / 4), L = (spans + n - 1) / n;
-    return L < 1 ? 1 : L < (1 << 30) ? (int32_t)L : 1 << 30;
+    const int64_t s = spans / SLOTS + 1;
+    const uint32_t slot = (uint32_t)(s < (1 << 28) ? s : 1 << 28);
+    return i == 0 ? WHOLE : (int32_t)(i == 1 ? slot * 4 / 3 : i == 2 ? slot : i == 3 ? slot / 2 : i == 4 ? slot / 3 : slot / 4) + 1;
 }
-// pieces: all of them; longest: the cost of the longest; work: of all; units: pieces of the uncut call; few: no
-// sequence has many rows
-VR_HD int64_t cut_cost(int64_t pieces, int64_t longest, int64_t work, int64_t units, bool few, Costs c) {
-    if (pieces > units && pieces > PIECES_MAX) return INT64_MAX;
+// What the estimate needs of the sequences: first these sums ...
+struct Sums { int64_t units = 0, work = 0, spans = 0; int32_t longest = 0; bool many = false; };
+VR_HD void sum_up(Sums& t, SeqRange r, int G, int Hg, int causal, int window, Costs c) {
+    const int64_t n = (int64_t)seq_tiles(r, Hg) * G;
+    const int32_t span = seq_span(r, Hg, window), cost = key_cost(r, Hg, c);
+    t.units += n;
+    t.work += n * seq_mean(r, span, causal) * cost;
+    t.spans += n * span * cost;
+    if (n && span > t.longest) t.longest = span;
+    t.many = t.many || tile_rows(r, Hg) != ROWS_FEW;
+}
+// ... then for every candidate these.  Counts stop at 2^24: more than PIECES_MAX is enough to know.
+struct CutSums {
+    int32_t L[CUTS], pieces[CUTS], partial[CUTS];      // partial: partial rows / JOIN_UNIT
+    int64_t most[CUTS];                                // cost of the longest piece
+};
+VR_HD void cut_begin(CutSums& t, int64_t spans) {
+    for (int i = 0; i < CUTS; ++i) {
+        t.L[i] = cut_try(i, spans);
+        t.pieces[i] = t.partial[i] = 0;
+        t.most[i] = 0;
+    }
+}
+VR_HD int32_t capped(int64_t v) { return v < (1 << 24) ? (int32_t)v : 1 << 24; }
+VR_HD void cut_up(CutSums& t, SeqRange r, int G, int Hg, int window, Costs c) {
+    const int64_t n = (int64_t)seq_tiles(r, Hg) * G;
+    const int32_t span = seq_span(r, Hg, window), cost = key_cost(r, Hg, c);
+    for (int i = 0; i < CUTS; ++i) {
+        const int32_t np = seq_pieces(span, cost, t.L[i], c.lmin);
+        const int64_t len = n ? (int64_t)piece_len(span, np) * cost : 0;
+        t.pieces[i] = capped(t.pieces[i] + n * np);
+        if (np > 1) t.partial[i] = capped(t.partial[i] + seq_rows(r, Hg) * G * np / JOIN_UNIT);
+        if (len > t.most[i]) t.most[i] = len;
+    }
+}
+VR_HD int64_t cut_cost(const CutSums& t, int i, const Sums& s, Costs c) {
+    const int64_t pieces = t.pieces[i], longest = t.most[i];
+    if (pieces > s.units && pieces > PIECES_MAX) return INT64_MAX;
     const int64_t rounds = (pieces + SLOTS - 1) / SLOTS;
-    int64_t t = rounds * longest;
-    if (few && pieces < SLOTS) t = longest * (pieces < SLOTS / 4 ? SLOTS / 4 : pieces) / SLOTS;
+    int64_t cost = rounds * longest;
+    if (!s.many && pieces < SLOTS) cost = longest * (pieces < SLOTS / 4 ? SLOTS / 4 : pieces) / SLOTS;
     // unlike pieces even out over several rounds (a sequence's longest come first)
-    if (rounds > 1 && t > work / SLOTS + longest) t = work / SLOTS + longest;
-    return t + rounds * c.piece + (pieces > units ? c.join : 0);
+    if (rounds > 1 && cost > s.work / SLOTS + longest) cost = s.work / SLOTS + longest;
+    return cost + rounds * c.piece + (pieces > s.units ? c.join + t.partial[i] : 0);
+}
+struct Plan { int32_t L, pieces; };
+VR_HD Plan uncut(const Sums& s) { return Plan{WHOLE, s.units < INT32_MAX ? (int32_t)s.units : INT32_MAX}; }
+VR_HD bool may_cut(const Sums& s, Costs c) { return s.longest > c.lmin && s.units < PIECES_MAX; }
+VR_HD Plan pick(const CutSums& t, const Sums& s, Costs c) {
+    int best = 0;
+    int64_t cost = cut_cost(t, 0, s, c);
+    for (int i = 1; i < CUTS; ++i) {
+        const int64_t x = cut_cost(t, i, s, c);
+        if (x < cost) {
+            cost = x;
+            best = i;
+        }
+    }
+    return Plan{t.L[best], t.pieces[best]};
 }
 
 // most (tile, head) pairs and pieces of any call with T rows and S sequences whose tables hold `cap` tokens
