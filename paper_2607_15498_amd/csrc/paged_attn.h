@@ -167,12 +167,7 @@ struct Form {
     static constexpr int NF = BF ? 8 : 16;                 // 16-byte fragments of a row per lane: pieces 2 k + h
     static constexpr int NC = BF ? 2 : 1;                  // many rows: blocks of 32 rows per wave
     static constexpr int WAVES = ROWS_MANY / (32 * NC);    // 4; fp32 8, two a SIMD
-    // few rows: for each of 4 waves a ring of NST 32-key tiles [K, V], brought in chunks of 4 KB
     static constexpr int KB = 32 * ROWB;
-    static constexpr int NST = BF ? 2 : 1;
-    static constexpr int RING = NST * 2 * KB;
-    static constexpr int CH = KB / 4096, CROWS = 4096 / ROWB;
-    static constexpr int JOIN = 4 * 32 * (132 + 2) * 4;
     // many rows: 4 stages of 16 KB of keys, then as many of values; every wave brings LPW KB of either
     static constexpr int SB = 16384;
     static constexpr int KT = SB / ROWB;                   // keys per stage: 64, fp32 32
@@ -181,7 +176,7 @@ struct Form {
     static constexpr int LPW = SB / 1024 / WAVES, WROWS = LPW * 1024 / ROWB;
     static constexpr size_t LDS = 128 * 1024;
     static_assert(SB == SPS * KB, "steps follow each other");
-    static_assert(4 * RING <= (int)LDS && JOIN <= (int)LDS && STAGES * 2 * SB <= (int)LDS, "the two forms share it");
+    static_assert(STAGES * 2 * SB <= (int)LDS, "of the largest");
 };
 
 // the call's L for the second launch, behind the partial rows
@@ -449,178 +444,7 @@ __device__ __forceinline__ void store4(ET* dst, float o0, float o1, float o2, fl
 
 // Few rows: rows 0 .. rows - 1 of the sequence's one tile.
 template <typename ET>
-__device__ __forceinline__ void few_rows(const Piece<ET>& P, uint8_t* smem, int rows, bool cut, int64_t rec_row) {
-    typedef Form<ET> F;
-    const AttnArgs& a = P.a;
-    const SeqRange& r = P.r;
-    const int wave = first_lane((int)(threadIdx.x >> 6)), lane = P.lane, l32 = P.l32, h = P.h;
-    const int Hg = a.Hg, g = P.g, lo = P.lo, hi = P.hi;
-    uint8_t* ring = smem + (wave & 3) * F::RING;
-    const uint32_t ring0 = first_lane((int)(uint32_t)(size_t)(__attribute__((address_space(3))) uint8_t*)ring);
-    const int myrow = l32 < rows ? l32 : 0, tok = myrow / Hg;
-    int32_t mylo, myhi, firsthi, lastlo, x;
-    row_keys(r, tok, a.causal, a.window, mylo, myhi);
-    const auto seen = P.seen(mylo, myhi);
-    row_keys(r, 0, a.causal, a.window, x, firsthi);
-    row_keys(r, (rows - 1) / Hg, a.causal, a.window, lastlo, x);
-    u32x4 qf[1][F::NF];
-    P.query(qf[0], r.q0 + tok, g * Hg + myrow % Hg);
-    Running run;
-    f32x16 acc[1][4], sc[1];
-#pragma unroll
-    for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) acc[0][dt][i] = 0.f;
-
-    // pages of the two 16-key groups of the wave's next 32 tiles, one a lane
-    constexpr int L = 4 * F::CH, step = 4 * 32;            // loads of a tile's keys (or values); keys to the next tile
-    int32_t window = 0, page[2];
-    int at = 32;
-    auto fetch = [&](int32_t t) {
-        if (at == 32) {
-            const int32_t tl = t + (lane >> 1) * step + (lane & 1) * 16;
-            window = P.page_of(P.raw_page(tl), tl);
-            at = 0;
-        }
-        page[0] = __builtin_amdgcn_readlane(window, 2 * at);
-        page[1] = __builtin_amdgcn_readlane(window, 2 * at + 1);
-        ++at;
-    };
-    auto bring = [&](auto values, const uint8_t* pool, int32_t t, uint32_t dst) {
-#pragma unroll
-        for (int c = 0; c < F::CH; ++c) {
-            const int32_t pg = page[c * F::CROWS / 16];
-            const uint8_t* src = P.rows_at(pool, pg, t + c * F::CROWS);
-#pragma unroll
-            for (int v = 0; v < 4; ++v) P.template bring1<values>(src, P.advance(pg), v, c * F::CROWS / 4, dst + c * 4096);
-        }
-    };
-    auto groups = [&]() { return (page[0] >= 0 ? 1u : 0u) | (page[1] >= 0 ? 2u : 0u); };
-    int32_t t0 = (lo & ~31) + 32 * wave;
-    uint32_t gm_in = 0;
-    if (wave >= 4) t0 = hi;                                // fp32: the other four have nothing to do here
-    if (t0 < hi) {
-        fetch(t0);
-        bring(std::false_type(), P.kbase, t0, ring0);
-        bring(std::true_type(), P.vbase, t0, ring0 + F::KB);
-        gm_in = groups();
-    }
-    for (int st = 0; t0 < hi; t0 += step) {
-        const uint32_t gm = gm_in;
-        uint8_t* kt = ring + st * 2 * F::KB;
-        const int32_t tn = t0 + step;
-        const bool more = tn < hi;
-        const bool masked = t0 < lastlo || t0 < lo || t0 + 32 > firsthi || t0 + 32 > hi || gm != 3u;
-        u32x4 p[1][2];
-        auto softmax = [&]() {
-            P.template scores<1>(kt, qf, sc);
-            if (masked) P.anew().mask(sc[0], t0, seen, gm);
-            const float mt = P.most(sc[0]);
-            if (__any(mt > run.m + SLACK / a.c)) {
-                const float f = run.raise(mt, a.c);
-#pragma unroll
-                for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[0][dt][i] *= f;
-            }
-            if constexpr (F::BF) weights(sc[0], a.c, run.off, p[0], run.l);
-            else weights(sc[0], a.c, run.off, run.l);
-        };
-        if constexpr (F::NST == 2) {
-            st ^= 1;
-            const uint32_t next = ring0 + st * 2 * F::KB;
-            wait_lds();                                    // the other tile has been read
-            if (more) {
-                fetch(tn);
-                bring(std::false_type(), P.kbase, tn, next);
-                bring(std::true_type(), P.vbase, tn, next + F::KB);
-                gm_in = groups();
-                wait_loads<3 * L>();
-            } else wait_loads<L>();
-            softmax();
-            if (more) wait_loads<2 * L>();
-            else wait_loads<0>();
-        } else {
-            wait_loads<L>();
-            softmax();
-            wait_lds();                                    // the keys have been read
-            if (more) {
-                fetch(tn);
-                bring(std::false_type(), P.kbase, tn, ring0);
-                wait_loads<L>();
-            } else wait_loads<0>();
-        }
-        uint8_t* vt = kt + F::KB;
-        P.clear_tail(t0, 0, 32, vt);
-        const bool odd = masked && P.anew().odd_values(vt);
-        if constexpr (F::BF) {
-            if (odd) P.anew().template values<1, true>(vt, p, acc);
-            else P.template values<1>(vt, p, acc);
-        } else {
-            if (odd) P.anew().template values<1, true>(vt, sc, acc);
-            else P.template values<1>(vt, sc, acc);
-        }
-        if (odd) P.anew().add_odd(vt, t0, seen, gm, [&](int dt, int i, float x) { acc[0][dt][i] += x; });
-        if constexpr (!F::BF) {
-            wait_lds();                                    // the values have been read
-            if (more) {
-                bring(std::true_type(), P.vbase, tn, ring0 + F::KB);
-                gm_in = groups();
-            }
-        }
-    }
-    run.l = xsum32(run.l);
-    __syncthreads();                                       // every wave is done with its ring
-    float* js = (float*)smem;                              // [4][32][132] sums
-    float* jm = js + 4 * 32 * 132;                         // [4][32][2]
-    if (wave < 4)
-#pragma unroll
-        for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-            for (int i = 0; i < 16; i += 4)
-                *reinterpret_cast<f32x4*>(js + (wave * 32 + l32) * 132 + 32 * dt + 2 * i + 4 * h) =
-                    f32x4{acc[0][dt][i], acc[0][dt][i + 1], acc[0][dt][i + 2], acc[0][dt][i + 3]};
-    if (wave < 4 && h == 0) *reinterpret_cast<float2*>(jm + (wave * 32 + l32) * 2) = float2{run.m, run.l};
-    __syncthreads();
-    const int row = threadIdx.x >> 3, d0 = 16 * (threadIdx.x & 7);
-    if (row < rows) {                                      // at most 32, a thread each 16 dims
-        float mw[4], lw[4], M = -INFINITY, Ls = 0.f, o[16];
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const float2 v = *reinterpret_cast<const float2*>(jm + (w * 32 + row) * 2);
-            mw[w] = v.x;
-            lw[w] = v.y;
-            M = fmaxf(M, v.x);
-        }
-        const float mu = M == -INFINITY ? 0.f : M;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[i] = 0.f;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const float f = __builtin_amdgcn_exp2f((mw[w] - mu) * a.c);
-            Ls = fmaf(f, lw[w], Ls);
-#pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-                const f32x4 v = *reinterpret_cast<const f32x4*>(js + (w * 32 + row) * 132 + d0 + i);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) o[i + k] = fmaf(f, v[k], o[i + k]);
-            }
-        }
-        if (cut) {
-            float* dst = a.rec + (rec_row + row) * D + d0;
-#pragma unroll
-            for (int i = 0; i < 16; i += 4) *reinterpret_cast<f32x4*>(dst + i) = f32x4{o[i], o[i + 1], o[i + 2], o[i + 3]};
-            if (d0 == 0) *reinterpret_cast<float2*>(a.rec + a.rec_rows * D + (rec_row + row) * 2) = float2{M, Ls};
-        } else {
-            const float inv = Ls == 0.f ? 0.f : 1.f / Ls;
-            ET* dst = (ET*)a.out + (int64_t)(r.q0 + row / Hg) * a.out_stride + (int64_t)(g * Hg + row % Hg) * D + d0;
-#pragma unroll
-            for (int i = 0; i < 16; i += 4) store4<ET>(dst + i, o[i] * inv, o[i + 1] * inv, o[i + 2] * inv, o[i + 3] * inv);
-        }
-    }
-    __syncthreads();                                       // the rings are free again
-}
-
+__device__ void few_rows(const Piece<ET>& P, uint8_t* smem, int rows, bool cut, int64_t rec_row);
 
 // Many rows, what bf16 and fp32 share: rows row0 .. row0 + rows - 1 of the sequence, 32 NC of them a wave,
 // the key stages and which steps of 32 keys the wave's rows see.

@@ -1,9 +1,218 @@
 // The fp32 kernel of the paged attention (paged_attn.hip).  Its products take 16 times as long as bf16's, so its
-// many-rows form goes one step after another, 32 rows a wave and two waves a SIMD: while one takes exponentials
-// or waits for a fragment, the other's products run.
+// forms go one step after another, with two waves a SIMD: while one takes exponentials or waits for a fragment, the
+// other's products run.  Many rows: 32 a wave.
 #include "paged_attn.h"
 
 namespace vr {
+
+__device__ __forceinline__ f32x4 mfma16(float a, float b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
+
+// Few rows: each of the 8 waves takes every eighth tile of 16 keys, keys and values 8 KB each of its own, and their
+// sums are joined at the end.  Products of 16 x 16: up to 16 rows (NB = 1) cost half as much as 32, and then
+// the matrix cores need 15 us of the 50 us that reading 32768 tokens of 8 heads takes.
+//   S^T = K Q^T: lane 16 q + i gives dims 16 c + 4 q + e of key i and of row i, product e of every c;
+//     receives keys 4 q + v of row i.
+//   O^T = V^T P^T: lane gives dim 64 half + 4 i + e of key 4 q + v (values of 16 bytes, a row's adjacent) and the
+//     weight that it holds; receives dims 64 half + 16 q + 4 v + e of row i.
+template <int NB>
+__device__ __forceinline__ void few_rows_of(const Piece<float>& P, uint8_t* smem, int rows, bool cut, int64_t rec_row) {
+    constexpr int NW = Form<float>::WAVES, ROWB = 512, TB = 16 * ROWB;
+    const AttnArgs& a = P.a;
+    const SeqRange& r = P.r;
+    const int wave = first_lane((int)(threadIdx.x >> 6)), lane = P.lane, i16 = lane & 15, q4 = lane >> 4;
+    const int Hg = a.Hg, g = P.g, lo = P.lo, hi = P.hi;
+    uint8_t* kt = smem + wave * 2 * TB;
+    uint8_t* vt = kt + TB;
+    const uint32_t kdst = first_lane((int)(uint32_t)(size_t)(__attribute__((address_space(3))) uint8_t*)kt);
+    int32_t firsthi, lastlo, x;
+    row_keys(r, 0, a.causal, a.window, x, firsthi);
+    row_keys(r, (rows - 1) / Hg, a.causal, a.window, lastlo, x);
+    typename Piece<float>::Seen seen[NB];
+    u32x4 qf[NB][8];
+    Running run[NB];
+    f32x4 acc[NB][2][4];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        const int row = 16 * b + i16 < rows ? 16 * b + i16 : 0, tok = row / Hg;
+        int32_t rlo, rhi;
+        row_keys(r, tok, a.causal, a.window, rlo, rhi);
+        seen[b] = P.seen(rlo, rhi);
+        const uint8_t* src = (const uint8_t*)((const float*)a.q + (int64_t)(r.q0 + tok) * a.q_stride + (int64_t)(g * Hg + row % Hg) * D);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) qf[b][c] = load16(src + (4 * c + q4) * 16);
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[b][half][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const uint32_t kaddr = (uint32_t)(i16 * ROWB + (q4 ^ (((i16 & 3) << 2) | (i16 >> 2))) * 16);
+    const float slack = SLACK / a.c;
+
+    // pages of the wave's next 64 tiles, one a lane
+    constexpr int L = TB / 1024, step = 16 * NW;
+    int32_t window = 0, page = -1;
+    int at = 64;
+    auto fetch = [&](int32_t t) {
+        if (at == 64) {
+            const int32_t tl = t + lane * step;
+            window = P.page_of(P.raw_page(tl), tl);
+            at = 0;
+        }
+        page = __builtin_amdgcn_readlane(window, at++);
+    };
+    auto bring_keys = [&](int32_t t) {
+        const uint8_t* src = P.rows_at(P.kbase, page, t);
+#pragma unroll
+        for (int v = 0; v < L; ++v) P.bring1<false>(src, P.advance(page), v, 0, kdst);
+    };
+    auto bring_values = [&](int32_t t) {
+        const uint8_t* src = P.rows_at(P.vbase, page, t);
+#pragma unroll
+        for (int v = 0; v < L; ++v) lds_load(src + v * P.advance(page), 16u * (uint32_t)lane, kdst + TB + v * 1024);
+    };
+    int32_t t0 = (lo & ~15) + 16 * wave;
+    if (t0 < hi) {
+        fetch(t0);
+        bring_keys(t0);
+        bring_values(t0);
+    }
+    for (; t0 < hi; t0 += step) {
+        const bool paged = page >= 0, more = t0 + step < hi;
+        const bool masked = t0 < lastlo || t0 < lo || t0 + 16 > firsthi || t0 + 16 > hi || !paged;
+        wait_loads<L>();
+        f32x4 sc[NB];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) sc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            const u32x4 f = *reinterpret_cast<const u32x4*>(kt + (kaddr ^ (64u * (c & 3))) + 256 * (c >> 2));
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int b = 0; b < NB; ++b) sc[b] = mfma16(__uint_as_float(f[e]), __uint_as_float(qf[b][c][e]), sc[b]);
+        }
+        wait_lds();                                        // the keys have been read
+        if (more) {
+            fetch(t0 + step);
+            bring_keys(t0 + step);
+        }
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            if (masked)
+#pragma unroll
+                for (int v = 0; v < 4; ++v)
+                    if (!paged || !P.sees(t0 + 4 * q4 + v, seen[b])) sc[b][v] = -INFINITY;
+            const float mt = fmaxf(fmaxf(sc[b][0], sc[b][1]), fmaxf(sc[b][2], sc[b][3]));
+            if (__any(mt > run[b].m + slack)) {
+                const float f = run[b].raise(xmax16(xmax32(mt)), a.c);
+#pragma unroll
+                for (int half = 0; half < 2; ++half)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) acc[b][half][e][v] *= f;
+            }
+#pragma unroll
+            for (int v = 0; v < 4; ++v) sc[b][v] = __builtin_amdgcn_exp2f(fmaf(sc[b][v], a.c, run[b].off));
+            run[b].l += (sc[b][0] + sc[b][1]) + (sc[b][2] + sc[b][3]);
+        }
+        if (more) wait_loads<L>();
+        else wait_loads<0>();
+        P.clear_tail(t0, 0, 16, vt);
+        bool odd = false;                                  // as Piece's: infinities and NaN among values of masked keys
+        if (masked) {
+            uint32_t bits = 0;
+            for (int i = lane; i < TB / 16; i += 64) {
+                const u32x4 w = *reinterpret_cast<const u32x4*>(vt + 16 * i);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) bits |= w[k] ^ P.finite(w[k]);
+            }
+            odd = __any(bits != 0);
+        }
+        auto products = [&](auto only_finite) {
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    u32x4 f = *reinterpret_cast<const u32x4*>(vt + (4 * q4 + v) * ROWB + 256 * half + 16 * i16);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if constexpr (only_finite) f[e] = P.finite(f[e]);
+#pragma unroll
+                        for (int b = 0; b < NB; ++b) acc[b][half][e] = mfma16(__uint_as_float(f[e]), sc[b][v], acc[b][half][e]);
+                    }
+                }
+        };
+        if (odd) {
+            products(std::true_type());
+#pragma unroll 1
+            for (int kk = 0; kk < 16; ++kk)
+#pragma unroll
+                for (int n = 0; n < 8; ++n) {              // dims 64 (n / 4) + 16 q + 4 (n % 4) ..
+                    const u32x4 w = *reinterpret_cast<const u32x4*>(vt + kk * ROWB + 256 * (n >> 2) + 64 * q4 + 16 * (n & 3));
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) {
+                        const bool see = paged && P.sees(t0 + kk, seen[b]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            acc[b][n >> 2][e][n & 3] += see ? __uint_as_float(w[e] ^ P.finite(w[e])) : 0.f;
+                    }
+                }
+        } else products(std::false_type());
+        wait_lds();                                        // the values have been read
+        if (more) bring_values(t0 + step);
+    }
+
+    float* js = (float*)smem;                              // [NW][16][132] sums
+    float* jm = js + NW * 16 * 132;                        // [NW][16][2]
+    static_assert(NW * 16 * 134 * 4 <= (int)Form<float>::LDS, "one block at a time");
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        const float l = xsum16(xsum32(run[b].l));
+        __syncthreads();                                   // every wave is done with what lies there
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+                *reinterpret_cast<f32x4*>(js + (wave * 16 + i16) * 132 + 64 * half + 16 * q4 + 4 * v) =
+                    f32x4{acc[b][half][0][v], acc[b][half][1][v], acc[b][half][2][v], acc[b][half][3][v]};
+        if (q4 == 0) *reinterpret_cast<float2*>(jm + (wave * 16 + i16) * 2) = float2{run[b].m, l};
+        __syncthreads();
+        const int in = threadIdx.x >> 5, row = 16 * b + in, d0 = 4 * (threadIdx.x & 31);
+        if (row < rows) {
+            float M = -INFINITY, Ls = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+            float2 ml[NW];
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                ml[w] = *reinterpret_cast<const float2*>(jm + (w * 16 + in) * 2);
+                M = fmaxf(M, ml[w].x);
+            }
+            const float mu = M == -INFINITY ? 0.f : M;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                const float f = __builtin_amdgcn_exp2f((ml[w].x - mu) * a.c);
+                const f32x4 v = *reinterpret_cast<const f32x4*>(js + (w * 16 + in) * 132 + d0);
+                Ls = fmaf(f, ml[w].y, Ls);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) o[k] = fmaf(f, v[k], o[k]);
+            }
+            if (cut) {
+                *reinterpret_cast<f32x4*>(a.rec + (rec_row + row) * D + d0) = f32x4{o[0], o[1], o[2], o[3]};
+                if (d0 == 0) *reinterpret_cast<float2*>(a.rec + a.rec_rows * D + (rec_row + row) * 2) = float2{M, Ls};
+            } else {
+                const float inv = Ls == 0.f ? 0.f : 1.f / Ls;
+                float* dst = (float*)a.out + (int64_t)(r.q0 + row / Hg) * a.out_stride + (int64_t)(g * Hg + row % Hg) * D + d0;
+                *reinterpret_cast<f32x4*>(dst) = f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+            }
+        }
+    }
+    __syncthreads();                                       // the waves' tiles are free again
+}
+template <>
+__device__ __forceinline__ void few_rows<float>(const Piece<float>& P, uint8_t* smem, int rows, bool cut, int64_t rec_row) {
+    if (rows <= 16) few_rows_of<1>(P, smem, rows, cut, rec_row);
+    else few_rows_of<2>(P, smem, rows, cut, rec_row);
+}
 
 template <>
 __device__ __forceinline__ void many_rows<float>(const Piece<float>& P, uint8_t* smem, int32_t row0, int32_t rows, bool cut,
