@@ -67,6 +67,7 @@ __device__ __forceinline__ int64_t lane64(int64_t v, int lane) {
 
 // ---- the call's cut, computed by every wave from the device lengths ----------------------------
 // Reductions over the first `n` lanes (the others hold nothing), to a scalar.
+__device__ __forceinline__ float first_lane(float v) { return __uint_as_float((uint32_t)first_lane((int32_t)__float_as_uint(v))); }
 template <typename V> __device__ __forceinline__ V wave_sum(V v, int n) {
     for (int m = 1; m < n; m <<= 1) v += __shfl_xor(v, m, WAVE);
     return first_lane(v);
@@ -95,32 +96,44 @@ __device__ __forceinline__ Plan wave_plan(const AttnArgs& a, const SeqRange& fir
     s.work = wave_sum(s.work, n);
     s.spans = wave_sum(s.spans, n);
     s.many = __any(s.many);
-    CutSums t;
-    cut_begin(t, s.spans);
-    for (int s0 = 0; s0 < a.S; s0 += 64)
-        cut_up(t, s0 ? load_range(a, s0 + lane) : first, a.G, a.Hg, a.window, a.costs);
-    for (int m = 1; m < n; m <<= 1)
-#pragma unroll
-        for (int i = 0; i < CUTS; ++i) {
-            t.pieces[i] += __shfl_xor(t.pieces[i], m, WAVE);
-            t.partial[i] += __shfl_xor(t.partial[i], m, WAVE);
-            const int64_t x = __shfl_xor(t.most[i], m, WAVE);
-            t.most[i] = x > t.most[i] ? x : t.most[i];
+    // lane 8 i + k: candidate i, every eighth sequence from k on (one copy of the code)
+    static_assert(CUTS <= 8, "a candidate is 8 lanes'");
+    const int cand = lane >> 3 < CUTS ? lane >> 3 : 0, slot = lane & 7;
+    Cut t = cut_begin(cand, s.spans);
+    for (int s0 = 0; s0 < a.S; s0 += 64) {
+        const SeqRange mine = s0 ? load_range(a, s0 + lane) : first;
+        const int here = a.S - s0 < 64 ? a.S - s0 : 64;
+#pragma unroll 1
+        for (int k = 0; k < here; k += 8) {
+            SeqRange r;
+            r.q0 = 0;
+            r.qlen = __shfl(mine.qlen, k + slot, WAVE);    // nothing behind the last
+            r.klen = __shfl(mine.klen, k + slot, WAVE);
+            cut_up(t, r, a.G, a.Hg, a.window, a.costs);
         }
-#pragma unroll
-    for (int i = 0; i < CUTS; ++i) {
-        t.pieces[i] = first_lane(t.pieces[i]);
-        t.partial[i] = first_lane(t.partial[i]);
-        t.most[i] = first_lane(t.most[i]);
     }
-    const Plan p = pick(t, s, a.costs);
-    return Plan{first_lane(p.L), first_lane(p.pieces)};
+    for (int m = 1; m < 8 && m < n; m <<= 1) {
+        t.pieces += __shfl_xor(t.pieces, m, WAVE);
+        t.partial += __shfl_xor(t.partial, m, WAVE);
+        t.most = fmaxf(t.most, __shfl_xor(t.most, m, WAVE));
+    }
+    const int cost = (int)__float_as_uint(cut_cost(t, s, a.costs));        // > 0: ordered as integers
+    int best = 0, least = first_lane(cost);
+#pragma unroll
+    for (int i = 1; i < CUTS; ++i) {
+        const int x = __builtin_amdgcn_readlane(cost, 8 * i);
+        if (x < least) {
+            least = x;
+            best = i;
+        }
+    }
+    if (best == 0) return uncut(s);
+    return Plan{__builtin_amdgcn_readlane(t.L, 8 * best), (int32_t)__builtin_amdgcn_readlane((int)t.pieces, 8 * best)};
 }
 // The sequence of number idx.  A sequence's pieces are (tile, piece, head) triples, heads innermost and the last
-// tile first (with causal rows it sees the most keys); JOIN: numbers count the second launch's work, (JOIN_ROWS rows,
+// tile first (with causal rows it sees the most keys); JOIN: numbers count the second launch's work, (join_rows rows,
 // head) pairs of cut sequences, of few rows (row, head) pairs.  base, end: the sequence's numbers; rec: its first row of
 // partial results.
-constexpr int JOIN_ROWS = 4;
 struct Unit { SeqRange r; int32_t s, np; int64_t base, end, rec; };
 template <bool JOIN>
 __device__ __forceinline__ bool find_unit(const AttnArgs& a, int32_t L, const SeqRange& first, int64_t idx, Unit& u) {
@@ -130,7 +143,7 @@ __device__ __forceinline__ bool find_unit(const AttnArgs& a, int32_t L, const Se
         const SeqRange r = s0 ? load_range(a, s0 + lane) : first;
         const int32_t np = seq_pieces(seq_span(r, a.Hg, a.window), key_cost(r, a.Hg, a.costs), L, a.costs.lmin);
         const int64_t t = (int64_t)seq_tiles(r, a.Hg) * a.G, nr = np > 1 ? t * np * tile_rows(r, a.Hg) : 0;
-        const int64_t rows = seq_rows(r, a.Hg), parts = rows <= ROWS_FEW ? rows : (rows + JOIN_ROWS - 1) / JOIN_ROWS;
+        const int64_t rows = seq_rows(r, a.Hg), parts = rows <= ROWS_FEW ? rows : (rows + join_rows(np) - 1) / join_rows(np);
         const int64_t n = JOIN ? (np > 1 ? parts * a.G : 0) : t * np;
         int64_t up = n, rup = nr;              // inclusive scans over the lanes
         for (int m = 1; m < lanes; m <<= 1) {
@@ -646,19 +659,66 @@ __global__ __launch_bounds__(64 * Form<ET>::WAVES, 1) void paged_attn_kernel(Att
     }
 }
 
-// Joins the pieces of cut sequences: a workgroup takes JOIN_ROWS rows of a head, a wave each, or of few rows one,
-// every fourth piece a wave.  A wave takes 8 pieces at a time with a running maximum, so that nothing waits for all
-// maxima first.  It is a chain of reads that the other dies have just written, about 2 us each: rows in parallel
-// are what helps (32 rows a workgroup: 126 us for 256 rows of 8 heads in 32 pieces; 4: 11 us).
+// One row's pieces p0, p0 + step, .. of np, for NR rows at once by a half wave, NP pieces at a time with a running
+// maximum, so that nothing waits for all maxima first.  at(n): the first of row n's partial rows; piece p's is p stride on.
+template <int NR, int NP, typename A>
+__device__ __forceinline__ void join_pieces(const AttnArgs& a, A&& at, int64_t stride, int p0, int step, int np, float (&M)[NR],
+                                            float (&l)[NR], f32x4 (&o)[NR]) {
+    const float* rec_ml = a.rec + a.rec_rows * D;
+    const int l32 = threadIdx.x & 31;
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+        M[n] = -INFINITY;
+        l[n] = 0.f;
+        o[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    for (int p = p0; p < np; p += NP * step) {
+        float2 ml[NR][NP];
+        f32x4 v[NR][NP];
+#pragma unroll
+        for (int n = 0; n < NR; ++n)
+#pragma unroll
+            for (int k = 0; k < NP; ++k) {
+                ml[n][k] = float2{-INFINITY, 0.f};
+                v[n][k] = f32x4{0.f, 0.f, 0.f, 0.f};
+                if (p + k * step < np) {
+                    const int64_t rr = at(n) + (p + k * step) * stride;
+                    ml[n][k] = *reinterpret_cast<const float2*>(rec_ml + rr * 2);
+                    v[n][k] = *reinterpret_cast<const f32x4*>(a.rec + rr * D + 4 * l32);
+                }
+            }
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+            float mn = M[n];
+#pragma unroll
+            for (int k = 0; k < NP; ++k) mn = fmaxf(mn, ml[n][k].x);
+            const float mu = mn == -INFINITY ? 0.f : mn, f0 = __builtin_amdgcn_exp2f((M[n] - mu) * a.c);
+            M[n] = mn;
+            l[n] *= f0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[n][e] *= f0;
+#pragma unroll
+            for (int k = 0; k < NP; ++k) {
+                const float f = __builtin_amdgcn_exp2f((ml[n][k].x - mu) * a.c);
+                l[n] = fmaf(f, ml[n][k].y, l[n]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[n][e] = fmaf(f, v[n][k][e], o[n][e]);
+            }
+        }
+    }
+}
+// Joins the pieces of cut sequences.  A half wave has a row, 16 bytes a lane.  Many rows: a workgroup takes join_rows rows
+// of a head; few: one row, every eighth piece a half wave.  It is a chain of reads that the other dies have just written,
+// about 2 us each: what helps is rows in parallel and loads that are all of use (1003 tokens of 32 heads in 2
+// pieces: 8 loads of one row's pieces a wave, 6 of them for nothing: 26 us; this: 12 us).
 template <typename ET>
 __global__ __launch_bounds__(256) void paged_join_kernel(AttnArgs a) {
-    __shared__ float so[4][D];
-    __shared__ float sl[4][2];
+    __shared__ __align__(16) float so[8][D];
+    __shared__ float sl[8][2];
     const SeqRange first = load_range(a, threadIdx.x & 63);
     const int32_t L = first_lane(*plan_of(a));
     if (L == WHOLE) return;
-    const int wave = first_lane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
-    const float* rec_ml = a.rec + a.rec_rows * D;
+    const int part = threadIdx.x >> 5, l32 = threadIdx.x & 31;     // half wave; its lane's dims are 4 l32 ..
     Unit u;
     u.base = u.end = 0;
     for (int64_t idx = blockIdx.x;; idx += gridDim.x) {
@@ -667,65 +727,56 @@ __global__ __launch_bounds__(256) void paged_join_kernel(AttnArgs a) {
         const uint32_t in = (uint32_t)(idx - u.base), G = (uint32_t)a.G;
         const int g = (int)(in % G), bm = tile_rows(r, a.Hg);
         const bool few = bm == ROWS_FEW;
-        const int64_t row = few ? in / G : (int64_t)(in / G) * JOIN_ROWS + wave;
-        const int tile = (int)(row / bm), i = (int)(row % bm);
+        const int32_t rows = (int32_t)seq_rows(r, a.Hg);
+        const int32_t row0 = (int32_t)(in / G) * (few ? 1 : join_rows(u.np));      // all in one tile
+        const int tile = row0 / bm, i0 = row0 % bm;
         const int64_t number = (int64_t)(seq_tiles(r, a.Hg) - 1 - tile) * u.np * G + g;      // of the tile's piece 0
         const int64_t rec0 = u.rec + number * bm, stride = (int64_t)G * bm;   // piece p's rows: rec0 + p stride
-        if (rec0 + (u.np - 1) * stride + bm > a.rec_rows) continue;           // as the first launch (few: uniform)
-        if (row < seq_rows(r, a.Hg)) {
-            float M = -INFINITY, o0 = 0.f, o1 = 0.f, l = 0.f;
-            const int p0 = few ? wave : 0, ps = few ? 4 : 1;
-            for (int p = p0; p < u.np; p += 8 * ps) {
-                float2 ml[8], v[8];
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {              // past the last piece: the last again, weight 0
-                    const int q = p + k * ps < u.np ? p + k * ps : u.np - 1;
-                    const int64_t rr = rec0 + q * stride + i;
-                    ml[k] = *reinterpret_cast<const float2*>(rec_ml + rr * 2);
-                    v[k] = *reinterpret_cast<const float2*>(a.rec + rr * D + 2 * lane);
-                }
-                float mn = M;
-#pragma unroll
-                for (int k = 0; k < 8; ++k) mn = fmaxf(mn, ml[k].x);
-                const float mu = mn == -INFINITY ? 0.f : mn, f0 = __builtin_amdgcn_exp2f((M - mu) * a.c);
-                M = mn;
-                l *= f0;
-                o0 *= f0;
-                o1 *= f0;
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    if (p + k * ps >= u.np) continue;
-                    const float f = __builtin_amdgcn_exp2f((ml[k].x - mu) * a.c);
-                    l = fmaf(f, ml[k].y, l);
-                    o0 = fmaf(f, v[k].x, o0);
-                    o1 = fmaf(f, v[k].y, o1);
-                }
-            }
-            if (few) {
-                __syncthreads();
-                so[wave][2 * lane] = o0;
-                so[wave][2 * lane + 1] = o1;
-                if (lane == 0) {
-                    sl[wave][0] = M;
-                    sl[wave][1] = l;
-                }
-                __syncthreads();
-                if (wave) continue;
-                M = fmaxf(fmaxf(sl[0][0], sl[1][0]), fmaxf(sl[2][0], sl[3][0]));
-                const float mu = M == -INFINITY ? 0.f : M;
-                o0 = o1 = l = 0.f;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float f = __builtin_amdgcn_exp2f((sl[k][0] - mu) * a.c);
-                    l = fmaf(f, sl[k][1], l);
-                    o0 = fmaf(f, so[k][2 * lane], o0);
-                    o1 = fmaf(f, so[k][2 * lane + 1], o1);
-                }
-            }
+        if (rec0 + (u.np - 1) * stride + bm > a.rec_rows) continue;           // as the first launch (uniform)
+        auto put = [&](int32_t row, float l, const f32x4& o) {
             const float inv = l == 0.f ? 0.f : 1.f / l;
-            ET* dst = (ET*)a.out + (r.q0 + row / a.Hg) * a.out_stride + (g * a.Hg + row % a.Hg) * D + 2 * lane;
-            if constexpr (sizeof(ET) == 2) *reinterpret_cast<uint32_t*>(dst) = cvt_bf16x2(o0 * inv, o1 * inv);
-            else *reinterpret_cast<float2*>(dst) = float2{o0 * inv, o1 * inv};
+            ET* dst = (ET*)a.out + (int64_t)(r.q0 + row / a.Hg) * a.out_stride + (int64_t)(g * a.Hg + row % a.Hg) * D + 4 * l32;
+            store4<ET>(dst, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+        };
+        if (few) {
+            float M[1], l[1];
+            f32x4 o[1];
+            join_pieces<1, 8>(a, [&](int) { return rec0 + i0; }, stride, part, 8, u.np, M, l, o);
+            __syncthreads();
+            *reinterpret_cast<f32x4*>(&so[part][4 * l32]) = o[0];
+            if (l32 == 0) {
+                sl[part][0] = M[0];
+                sl[part][1] = l[0];
+            }
+            __syncthreads();
+            if (part) continue;
+            float mx = sl[0][0], ls = 0.f;
+            f32x4 os = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 1; k < 8; ++k) mx = fmaxf(mx, sl[k][0]);
+            const float mu = mx == -INFINITY ? 0.f : mx;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float f = __builtin_amdgcn_exp2f((sl[k][0] - mu) * a.c);
+                const f32x4 v = *reinterpret_cast<const f32x4*>(&so[k][4 * l32]);
+                ls = fmaf(f, sl[k][1], ls);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) os[e] = fmaf(f, v[e], os[e]);
+            }
+            put(row0, ls, os);
+        } else if (u.np <= 4) {
+            float M[2], l[2];
+            f32x4 o[2];
+            const int32_t mine = row0 + 2 * part;
+            join_pieces<2, 4>(a, [&](int n) { return rec0 + i0 + 2 * part + n; }, stride, 0, 1, u.np, M, l, o);
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+                if (mine + n < rows) put(mine + n, l[n], o[n]);
+        } else {
+            float M[1], l[1];
+            f32x4 o[1];
+            join_pieces<1, 8>(a, [&](int) { return rec0 + i0 + part; }, stride, 0, 1, u.np, M, l, o);
+            if (row0 + part < rows) put(row0 + part, l[0], o[0]);
         }
     }
 }

@@ -104,71 +104,54 @@ VR_HD int32_t piece_len(int32_t span, int np) {
 constexpr int CUTS = 6;
 constexpr int PIECES_MAX = 4 * SLOTS;          // of a cut call (an uncut one may have any number)
 // spans: sum of tiles x span x cost over sequences and heads
-VR_HD int32_t cut_try(int i, int64_t spans) {
-    const int64_t s = spans / SLOTS + 1;
-    const uint32_t slot = (uint32_t)(s < (1 << 28) ? s : 1 << 28);
-    return i == 0 ? WHOLE : (int32_t)(i == 1 ? slot * 4 / 3 : i == 2 ? slot : i == 3 ? slot / 2 : i == 4 ? slot / 3 : slot / 4) + 1;
+VR_HD int32_t cut_try(int i, float spans) {
+    if (i == 0) return WHOLE;
+    const float slot = spans * (1.f / SLOTS);
+    const float x = i == 1 ? slot * 4.f / 3.f : slot / (float)(i - 1);
+    return x < 1e9f ? (int32_t)x + 1 : 1000000000;
 }
-// What the estimate needs of the sequences: first these sums ...
-struct Sums { int64_t units = 0, work = 0, spans = 0; int32_t longest = 0; bool many = false; };
+// What the estimate needs of the sequences: first these sums (in floats: one instruction each, and only the
+// choice hangs on them) ...
+struct Sums { int64_t units = 0; float work = 0.f, spans = 0.f; int32_t longest = 0; bool many = false; };
 VR_HD void sum_up(Sums& t, SeqRange r, int G, int Hg, int causal, int window, Costs c) {
     const int64_t n = (int64_t)seq_tiles(r, Hg) * G;
-    const int32_t span = seq_span(r, Hg, window), cost = key_cost(r, Hg, c);
+    const int32_t span = seq_span(r, Hg, window);
+    const float cost = (float)n * (float)key_cost(r, Hg, c);
     t.units += n;
-    t.work += n * seq_mean(r, span, causal) * cost;
-    t.spans += n * span * cost;
+    t.work += cost * (float)seq_mean(r, span, causal);
+    t.spans += cost * (float)span;
     if (n && span > t.longest) t.longest = span;
     t.many = t.many || tile_rows(r, Hg) != ROWS_FEW;
 }
-// ... then for every candidate these.  Counts stop at 2^24: more than PIECES_MAX is enough to know.
-struct CutSums {
-    int32_t L[CUTS], pieces[CUTS], partial[CUTS];      // partial: partial rows / JOIN_UNIT
-    int64_t most[CUTS];                                // cost of the longest piece
-};
-VR_HD void cut_begin(CutSums& t, int64_t spans) {
-    for (int i = 0; i < CUTS; ++i) {
-        t.L[i] = cut_try(i, spans);
-        t.pieces[i] = t.partial[i] = 0;
-        t.most[i] = 0;
-    }
+// ... then for every candidate these (counts up to 2^24 are exact, and PIECES_MAX is the most that is taken).
+struct Cut { int32_t L; float pieces, partial, most; };   // partial: partial rows / JOIN_UNIT; most: cost of the longest piece
+VR_HD Cut cut_begin(int i, float spans) { return Cut{cut_try(i, spans), 0.f, 0.f, 0.f}; }
+VR_HD void cut_up(Cut& t, SeqRange r, int G, int Hg, int window, Costs c) {
+    const int32_t tiles = seq_tiles(r, Hg), span = seq_span(r, Hg, window), cost = key_cost(r, Hg, c);
+    const int32_t np = seq_pieces(span, cost, t.L, c.lmin);
+    const float all = (float)G * (float)np, len = tiles ? (float)piece_len(span, np) * (float)cost : 0.f;
+    t.pieces += all * (float)tiles;
+    if (np > 1) t.partial += all * (float)seq_rows(r, Hg) * (1.f / JOIN_UNIT);
+    if (len > t.most) t.most = len;
 }
-VR_HD int32_t capped(int64_t v) { return v < (1 << 24) ? (int32_t)v : 1 << 24; }
-VR_HD void cut_up(CutSums& t, SeqRange r, int G, int Hg, int window, Costs c) {
-    const int64_t n = (int64_t)seq_tiles(r, Hg) * G;
-    const int32_t span = seq_span(r, Hg, window), cost = key_cost(r, Hg, c);
-    for (int i = 0; i < CUTS; ++i) {
-        const int32_t np = seq_pieces(span, cost, t.L[i], c.lmin);
-        const int64_t len = n ? (int64_t)piece_len(span, np) * cost : 0;
-        t.pieces[i] = capped(t.pieces[i] + n * np);
-        if (np > 1) t.partial[i] = capped(t.partial[i] + seq_rows(r, Hg) * G * np / JOIN_UNIT);
-        if (len > t.most[i]) t.most[i] = len;
-    }
-}
-VR_HD int64_t cut_cost(const CutSums& t, int i, const Sums& s, Costs c) {
-    const int64_t pieces = t.pieces[i], longest = t.most[i];
-    if (pieces > s.units && pieces > PIECES_MAX) return INT64_MAX;
-    const int64_t rounds = (pieces + SLOTS - 1) / SLOTS;
-    int64_t cost = rounds * longest;
-    if (!s.many && pieces < SLOTS) cost = longest * (pieces < SLOTS / 4 ? SLOTS / 4 : pieces) / SLOTS;
+VR_HD float cut_cost(const Cut& t, const Sums& s, Costs c) {
+    const float units = (float)s.units;
+    if (t.pieces > units && t.pieces > (float)PIECES_MAX) return 1e30f;
+    const float rounds = (float)(((int32_t)t.pieces + SLOTS - 1) / SLOTS);
+    float cost = rounds * t.most;
+    if (!s.many && t.pieces < (float)SLOTS) cost = t.most * (t.pieces < SLOTS / 4 ? SLOTS / 4 : t.pieces) * (1.f / SLOTS);
     // unlike pieces even out over several rounds (a sequence's longest come first)
-    if (rounds > 1 && cost > s.work / SLOTS + longest) cost = s.work / SLOTS + longest;
-    return cost + rounds * c.piece + (pieces > s.units ? c.join + t.partial[i] : 0);
+    const float even = s.work * (1.f / SLOTS) + t.most;
+    if (rounds > 1.f && cost > even) cost = even;
+    return cost + rounds * (float)c.piece + (t.pieces > units ? (float)c.join + t.partial : 0.f);
 }
 struct Plan { int32_t L, pieces; };
 VR_HD Plan uncut(const Sums& s) { return Plan{WHOLE, s.units < INT32_MAX ? (int32_t)s.units : INT32_MAX}; }
 VR_HD bool may_cut(const Sums& s, Costs c) { return s.longest > c.lmin && s.units < PIECES_MAX; }
-VR_HD Plan pick(const CutSums& t, const Sums& s, Costs c) {
-    int best = 0;
-    int64_t cost = cut_cost(t, 0, s, c);
-    for (int i = 1; i < CUTS; ++i) {
-        const int64_t x = cut_cost(t, i, s, c);
-        if (x < cost) {
-            cost = x;
-            best = i;
-        }
-    }
-    return Plan{t.L[best], t.pieces[best]};
-}
+
+// Rows of many that a workgroup of the second launch joins: a half wave has 8 loads under way, of 4 rows' pieces or of 8
+// pieces' rows.
+VR_HD int join_rows(int np) { return np <= 4 ? 16 : 8; }
 
 // most (tile, head) pairs and pieces of any call with T rows and S sequences whose tables hold `cap` tokens
 VR_HD int64_t max_units(int64_t T, int S, int G, int Hg) { return G * (T * Hg / ROWS_MANY + (S < T ? S : T)); }
