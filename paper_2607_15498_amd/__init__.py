@@ -536,6 +536,8 @@ class PagedCache:
 
 
 def new_pages(n_pages: int, G: int, page: int = 64, dtype: str = "bf16", device="cuda") -> PagedCache:
+    if dtype not in ("bf16", "f32"):
+        _einval(f"dtype {dtype!r} is neither 'bf16' nor 'f32'")
     dt = torch.bfloat16 if dtype == "bf16" else torch.float32
     k, v = (torch.zeros((n_pages, G, page, HEAD_DIM), dtype=dt, device=device) for _ in range(2))
     return PagedCache(k, v)
@@ -581,12 +583,16 @@ def _rows(t: torch.Tensor, dtype, T: Optional[int], heads: Optional[int], device
     return t.data_ptr(), (s0 if n > 1 else h * d)
 
 
+_raw_stream = torch._C._cuda_getCurrentRawStream      # the stream's handle without a Stream object (2 us a call)
+
+
 def _launch(device: torch.device, call, *args):
-    if torch.cuda.current_device() == device.index:
-        rc = call(*args, torch.cuda.current_stream(device).cuda_stream)
+    i = device.index
+    if torch.cuda.current_device() == i:
+        rc = call(*args, _raw_stream(i))
     else:
         with torch.cuda.device(device):
-            rc = call(*args, torch.cuda.current_stream(device).cuda_stream)
+            rc = call(*args, _raw_stream(i))
     if rc:
         _check(rc)
 
@@ -597,6 +603,27 @@ def _f32(t: Optional[torch.Tensor], shapes, device, name: str) -> int:
     if t.dtype != torch.float32 or t.device != device or tuple(t.shape) not in shapes or not t.is_contiguous():
         _einval(f"{name} must be a contiguous float32 tensor of shape {' or '.join(map(str, shapes))} on {device}")
     return t.data_ptr()
+
+
+_THETA = ((HEAD_DIM // 2,),)
+
+
+def _normed(x, w, out, T: int, dt, dev, name: str):
+    """One side of norm_rotate: the output, then address, stride and heads of x, address and stride of
+    its weights, address and stride of the output."""
+    if x is None:
+        if w is not None or out is not None:
+            _einval(f"w{name} or {name}_out without {name}")
+        return None, 0, 0, 0, 0, 0, 0, 0
+    px, sx = _rows(x, dt, T, None, dev, name)
+    heads = int(x.shape[1])
+    pw = _f32(w, ((HEAD_DIM,), (heads, HEAD_DIM)), dev, "w" + name) if w is not None else 0
+    if out is None:
+        out = torch.empty((T, heads, HEAD_DIM), dtype=dt, device=dev)
+        po, so = out.data_ptr(), heads * HEAD_DIM
+    else:
+        po, so = _rows(out, dt, T, heads, dev, name + "_out")
+    return out, px, sx, heads, pw, HEAD_DIM if pw and w.dim() == 2 else 0, po, so
 
 
 def norm_rotate(q: Optional[torch.Tensor], k: Optional[torch.Tensor] = None, pos: Optional[torch.Tensor] = None,
@@ -613,31 +640,19 @@ def norm_rotate(q: Optional[torch.Tensor], k: Optional[torch.Tensor] = None, pos
     if not some.is_cuda or dt not in _DTYPES:
         _einval("q and k must be bf16 or fp32 device tensors")
     T = int(some.shape[0])
-    side = []
-    for x, w, o, name in ((q, wq, q_out, "q"), (k, wk, k_out, "k")):
-        if x is None:
-            if w is not None or o is not None:
-                _einval(f"w{name} or {name}_out without {name}")
-            side.append((0, 0, 0, 0, 0, 0, 0, None))
-            continue
-        px, sx = _rows(x, dt, T, None, dev, name)
-        heads = int(x.shape[1])
-        pw = _f32(w, ((HEAD_DIM,), (heads, HEAD_DIM)), dev, "w" + name)
-        if o is None:
-            o = torch.empty((T, heads, HEAD_DIM), dtype=dt, device=dev)
-        po, so = _rows(o, dt, T, heads, dev, name + "_out")
-        side.append((px, sx, heads, pw, HEAD_DIM if w is not None and w.dim() == 2 else 0, po, so, o))
-    if theta is not None and pos is None:
-        _einval("rotation needs pos")
-    pp = 0
     if theta is not None:
-        pp = _i32(pos, 1, "pos")
+        if pos is None:
+            _einval("rotation needs pos")
+        pp, pt = _i32(pos, 1, "pos"), _f32(theta, _THETA, dev, "theta")
         if pos.shape[0] != T or pos.device != dev:
             _einval(f"pos must have {T} entries on {dev}")
-    a, b = side
-    _launch(dev, library().varrate_norm_rotate, _DTYPES[dt], T, a[0], a[1], a[2], b[0], b[1], b[2], pp,
-            _f32(theta, ((HEAD_DIM // 2,),), dev, "theta"), a[3], a[4], b[3], b[4], eps, a[5], a[6], b[5], b[6])
-    return a[7], b[7]
+    else:
+        pp = pt = 0
+    q_out, qx, qs, H, qw, qws, qo, qos = _normed(q, wq, q_out, T, dt, dev, "q")
+    k_out, kx, ks, G, kw, kws, ko, kos = _normed(k, wk, k_out, T, dt, dev, "k")
+    _launch(dev, library().varrate_norm_rotate, _DTYPES[dt], T, qx, qs, H, kx, ks, G, pp, pt, qw, qws, kw, kws, eps,
+            qo, qos, ko, kos)
+    return q_out, k_out
 
 
 def paged_append(pages: PagedCache, batch: PagedBatch, k: torch.Tensor, v: torch.Tensor,
@@ -651,7 +666,7 @@ def paged_append(pages: PagedCache, batch: PagedBatch, k: torch.Tensor, v: torch
     if batch.table.device != dev:
         _einval(f"the batch must be on {dev}")
     _launch(dev, library().varrate_paged_append, pages.c(), batch.c(T), pk, sk, pv, sv,
-            _f32(theta, ((HEAD_DIM // 2,),), dev, "theta"))
+            _f32(theta, _THETA, dev, "theta"))
     return pages
 
 
@@ -673,12 +688,19 @@ def paged_attn(pages: PagedCache, batch: PagedBatch, q: torch.Tensor, causal: bo
         _einval(f"the batch must be on {dev}")
     if out is None:
         out = torch.empty((T, H, HEAD_DIM), dtype=q.dtype, device=dev)
-    po, so = _rows(out, q.dtype, T, H, dev, "out")
-    ws = workspace if workspace is not None else paged_attn_workspace(pages, batch, T, H)
-    if not ws.is_cuda or ws.device != dev or not ws.is_contiguous():
+        po, so = out.data_ptr(), H * HEAD_DIM
+    else:
+        po, so = _rows(out, q.dtype, T, H, dev, "out")
+    L, pc, bc = library(), pages.c(), batch.c(T)
+    if workspace is None:
+        nbytes = L.varrate_paged_attn_workspace_bytes(pc, bc, H)
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+    elif workspace.device != dev or not workspace.is_contiguous():
         _einval(f"workspace must be a contiguous tensor on {dev}")
-    _launch(dev, library().varrate_paged_attn, pages.c(), batch.c(T), pq, sq, H, 1 if causal else 0, int(window),
-            HEAD_DIM ** -0.5 if scale is None else scale, po, so, ws.data_ptr(), ws.numel() * ws.element_size())
+    else:
+        nbytes = workspace.numel() * workspace.element_size()
+    _launch(dev, L.varrate_paged_attn, pc, bc, pq, sq, H, 1 if causal else 0, int(window),
+            HEAD_DIM ** -0.5 if scale is None else scale, po, so, workspace.data_ptr() if nbytes else 0, nbytes)
     return out
 
 
@@ -692,12 +714,11 @@ def paged_gather(pages: PagedCache, table: torch.Tensor, n: int, K: Optional[tor
         _einval(f"table must be on {dev}")
     if n < 0:
         _einval(f"n={n} is negative")
-    outs = []
+    shape, dt = (n, pages.G, HEAD_DIM), pages.k.dtype
     for x, name in ((K, "K"), (V, "V")):
-        if x is None:
-            x = torch.empty((n, pages.G, HEAD_DIM), dtype=pages.k.dtype, device=dev)
-        elif x.device != dev or tuple(x.shape) != (n, pages.G, HEAD_DIM):
-            _einval(f"{name} must be [{n}][{pages.G}][{HEAD_DIM}] on {dev}")
-        outs.append((x, _dev_ptr(x, pages.k.dtype, name)))
-    _launch(dev, library().varrate_paged_gather, pages.c(), pt, int(table.shape[0]), n, outs[0][1], outs[1][1])
-    return outs[0][0], outs[1][0]
+        if x is not None and (x.device != dev or x.dtype != dt or x.shape != shape or not x.is_contiguous()):
+            _einval(f"{name} must be a contiguous {dt} tensor {list(shape)} on {dev}")
+    K = torch.empty(shape, dtype=dt, device=dev) if K is None else K
+    V = torch.empty(shape, dtype=dt, device=dev) if V is None else V
+    _launch(dev, library().varrate_paged_gather, pages.c(), pt, int(table.shape[0]), n, K.data_ptr(), V.data_ptr())
+    return K, V
