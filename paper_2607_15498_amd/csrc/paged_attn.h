@@ -32,6 +32,14 @@ struct AttnArgs {
 // rows of a bad page: 1 KB of zeros
 __device__ const uint4 pa_zeros[64] = {};
 
+// The lane's number, formed where it is used: what is derived from it is not kept for a whole loop.  (A register
+// that is spilt there costs more than its load: the wait for it is one for all of the stages that are under way.)
+__device__ __forceinline__ int lane_now() {
+    int l;
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
+    return l;
+}
+
 template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
@@ -219,7 +227,11 @@ struct Piece {
         h = lane >> 5;
         const int lrow = lane / F::PPR;                    // the row that this lane loads of a 1 KB piece
         off0 = (uint32_t)(lrow * F::ROWB + ((lane % F::PPR) ^ ((lrow & 3) << 2)) * 16);
-        kaddr = (uint32_t)(l32 * F::ROWB + (h ^ (((l32 & 3) << 2) | ((l32 >> 2) & 3))) * 16);
+        kaddr = key_addr(lane);
+    }
+    static __device__ __forceinline__ uint32_t key_addr(int ln) {
+        const int row = ln & 31;
+        return (uint32_t)(row * F::ROWB + ((ln >> 5) ^ (((row & 3) << 2) | ((row >> 2) & 3))) * 16);
     }
     // the same piece with the lane's numbers anew: what the rare masked steps derive from them is not kept in
     // registers for the whole loop
@@ -246,11 +258,11 @@ struct Piece {
     // 1 KB number v of them into LDS at dst (of number 0); row 0 of number 0 is row 4 `quad` of its block
     template <bool VALUES>
     __device__ __forceinline__ void bring1(const uint8_t* src, int adv, int v, int quad, uint32_t dst) const {
-        // rows 4 v + .. (bf16) or 2 v + .. (fp32): the rest of f(row)
+        // rows 4 v + .. (bf16) or 2 v + .. (fp32): the rest of f(row); fp32 values are read a row at a time as they are
         if constexpr (F::BF) lds_load(src + v * adv, off0 ^ (((uint32_t)(quad + v) & 3u) << 4), dst + v * 1024);
         else if constexpr (!VALUES)
             lds_load(src + v * adv, off0 ^ ((uint32_t)((v & 1) << 3 | ((quad + (v >> 1)) & 3)) << 4), dst + v * 1024);
-        else lds_load(src + v * adv, (16u * (uint32_t)lane) ^ (((uint32_t)(quad + (v >> 1)) & 1u) << 7), dst + v * 1024);
+        else lds_load(src + v * adv, 16u * (uint32_t)lane, dst + v * 1024);
     }
     // values behind the end in the rows [r0, r1) of a tile of keys from t0 on: not read as data
     __device__ __forceinline__ void clear_tail(int32_t t0, int32_t r0, int32_t r1, uint8_t* vt) const {
@@ -272,18 +284,28 @@ struct Piece {
         for (int c = 0; c < NC; ++c)
 #pragma unroll
             for (int i = 0; i < 16; ++i) sc[c][i] = 0.f;
+        if constexpr (F::BF) {
 #pragma unroll
-        for (int k = 0; k < F::NF; ++k) {
-            const u32x4 f = *reinterpret_cast<const u32x4*>(kt + (kaddr ^ (32u * (k & 7))) + 256 * (k >> 3));
-            if constexpr (F::BF) {
+            for (int k = 0; k < F::NF; ++k) {
+                const u32x4 f = *reinterpret_cast<const u32x4*>(kt + (kaddr ^ (32u * k)));
 #pragma unroll
                 for (int c = 0; c < NC; ++c) sc[c] = mfma32(f, qf[c][k], sc[c]);
-            } else {
+            }
+        } else {
+            const uint32_t ka = key_addr(lane_now());
+            u32x4 f[2];
+            f[0] = *reinterpret_cast<const u32x4*>(kt + ka);
+#pragma unroll
+            for (int k = 0; k < F::NF; ++k) {              // the next fragment is read before the products of this one
+                if (k + 1 < F::NF)
+                    f[(k + 1) & 1] = *reinterpret_cast<const u32x4*>(kt + (ka ^ (32u * ((k + 1) & 7))) + 256 * ((k + 1) >> 3));
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
 #pragma unroll
                     for (int c = 0; c < NC; ++c)
-                        sc[c] = mfma32(__uint_as_float(f[e]), __uint_as_float(qf[c][k][e]), sc[c]);
+                        sc[c] = mfma32(__uint_as_float(f[k & 1][e]), __uint_as_float(qf[c][k][e]), sc[c]);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
     }
@@ -326,12 +348,6 @@ struct Piece {
         }
         return f;
     }
-    // fp32: key r0 + 4 h (bit 2 of r0 is 0), dim 32 dt + l32: 128 bytes of each of two rows, h of them in the other
-    // half of the banks
-    __device__ __forceinline__ float vfrag32(const uint8_t* vt, int r0, int dt) const {
-        const int at = 4 * h * F::ROWB + (dt & 1 ? -128 * h : 128 * h) + 4 * l32;
-        return *reinterpret_cast<const float*>(vt + r0 * F::ROWB + 128 * dt + at);
-    }
     // x with infinities and NaN made 0: one fp32, or a bf16 pair
     static __device__ __forceinline__ uint32_t finite(uint32_t x) {
         if constexpr (F::BF) return x & ~((((x & 0x7F807F80u) + 0x00800080u) >> 15 & 0x00010001u) * 0xFFFFu);
@@ -352,17 +368,24 @@ struct Piece {
                 for (int c = 0; c < NC; ++c) acc[c][dt] = mfma32(f, p[c][mm], acc[c][dt]);
             }
     }
-    template <int NC, bool FINITE = false>
-    __device__ __forceinline__ void values(const uint8_t* vt, const f32x16 (&p)[NC], f32x16 (&acc)[NC][4]) const {
+    // fp32: a lane reads dims 4 l32 .. of key 8 (i / 4) + 4 h + i % 4, one for each of acc, and the next key's before
+    // its products: acc[e][n] is dim 4 (8 (n / 4) + 4 h + n % 4) + e.  odd: finite values alone.
+    __device__ __forceinline__ void values(const uint8_t* vt, const f32x16& p, f32x16 (&acc)[4], bool odd) const {
+        const int ln = lane_now();
+        const uint8_t* row = vt + 4 * (ln >> 5) * F::ROWB + 16 * (ln & 31);
+        u32x4 f[2];
+        f[0] = *reinterpret_cast<const u32x4*>(row);
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
+        for (int i = 0; i < 16; ++i) {
+            if (i < 15) f[(i + 1) & 1] = *reinterpret_cast<const u32x4*>(row + (8 * ((i + 1) >> 2) + ((i + 1) & 3)) * F::ROWB);
+            __builtin_amdgcn_sched_barrier(0);
+            if (odd)
 #pragma unroll
-            for (int dt = 0; dt < 4; ++dt) {
-                float f = vfrag32(vt, 8 * (i >> 2) + (i & 3), dt);
-                if constexpr (FINITE) f = __uint_as_float(finite(__float_as_uint(f)));
+                for (int e = 0; e < 4; ++e) f[i & 1][e] = finite(f[i & 1][e]);
 #pragma unroll
-                for (int c = 0; c < NC; ++c) acc[c][dt] = mfma32(f, p[c][i], acc[c][dt]);
-            }
+            for (int e = 0; e < 4; ++e) acc[e] = mfma32(__uint_as_float(f[i & 1][e]), p[i], acc[e]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     }
     // A masked block whose values hold infinities or NaN: 0 x inf is not 0, so a row must not meet the values of keys
     // that it does not see.  The products take the finite values, and every row adds the others of the keys that it sees.
@@ -375,16 +398,16 @@ struct Piece {
         }
         return __ballot(odd != 0) != 0;
     }
-    // add(dt, i, x): x to the lane's sum of dim 32 dt + 8 (i / 4) + 4 h + i % 4
+    // add(dt, i, x): x to the lane's sum of dim 32 dt + 8 (i / 4) + 4 h + i % 4, fp32 32 dt + 16 h + i
     template <typename A>
     __device__ __forceinline__ void add_odd(const uint8_t* vt, int32_t t0, Seen s, uint32_t gm, A&& add) const {
 #pragma unroll 1
         for (int kk = 0; kk < 32; ++kk) {
             const bool see = sees(t0 + kk, s) && (gm >> (kk >> 4) & 1u);
-            const int f = F::BF ? ((kk & 3) << 2) | ((kk >> 2) & 3) : ((kk >> 2) & 1) << 3;
+            const int f = F::BF ? ((kk & 3) << 2) | ((kk >> 2) & 3) : 0;
 #pragma unroll
-            for (int n = 0; n < 16; ++n) {                 // dims 8 n + 4 h ..
-                const int byte = (8 * n + 4 * h) * (int)sizeof(ET);
+            for (int n = 0; n < 16; ++n) {                 // four dims
+                const int byte = (F::BF ? 8 * n + 4 * h : 32 * (n >> 2) + 16 * h + 4 * (n & 3)) * (int)sizeof(ET);
                 const uint8_t* at = vt + kk * F::ROWB + (((byte >> 4) ^ f) << 4) + (byte & 15);
                 float x[4];
                 if constexpr (F::BF) {
@@ -584,24 +607,26 @@ struct Many {
     __device__ __forceinline__ uint8_t* keys_of(int j) const { return smem + ((uint32_t)j * F::KB & (F::STAGES * F::SB - 1)); }
     __device__ __forceinline__ uint8_t* values_of(int j) const { return keys_of(j) + F::STAGES * F::SB; }
     __device__ __forceinline__ bool masked(int j) const { return j < mf || j >= ml || gm_of(j) != 3u; }
-    // block c's rows: sums (of 32 dims dt) and, with `last`, maximum and sum
+    // block c's rows: sums (of 32 dims dt, four at a time as the products leave them) and, with `last`, maximum and sum
     __device__ __forceinline__ void put(int c, int dt, const f32x16& o, const Running& run, float l, bool cut, int64_t rec_row,
                                         bool last) const {
         const AttnArgs& a = P.a;
         const int i0 = wrow + 32 * c + P.l32;
         if (i0 >= rows) return;
+        const int first = 32 * dt + (F::BF ? 4 : 16) * P.h;
+        constexpr int next = F::BF ? 2 : 1;
         if (cut) {
-            float* dst = a.rec + (rec_row + i0) * D + 32 * dt + 4 * P.h;
+            float* dst = a.rec + (rec_row + i0) * D + first;
 #pragma unroll
-            for (int i = 0; i < 16; i += 4) *reinterpret_cast<f32x4*>(dst + 2 * i) = f32x4{o[i], o[i + 1], o[i + 2], o[i + 3]};
+            for (int i = 0; i < 16; i += 4) *reinterpret_cast<f32x4*>(dst + next * i) = f32x4{o[i], o[i + 1], o[i + 2], o[i + 3]};
             if (last && P.h == 0) *reinterpret_cast<float2*>(a.rec + a.rec_rows * D + (rec_row + i0) * 2) = float2{run.m, l};
         } else {
             const float inv = l == 0.f ? 0.f : 1.f / l;
             int32_t tok, head;
             row_of(c, P.l32, tok, head);
-            ET* dst = (ET*)a.out + (int64_t)(P.r.q0 + tok) * a.out_stride + (int64_t)head * D + 32 * dt + 4 * P.h;
+            ET* dst = (ET*)a.out + (int64_t)(P.r.q0 + tok) * a.out_stride + (int64_t)head * D + first;
 #pragma unroll
-            for (int i = 0; i < 16; i += 4) store4<ET>(dst + 2 * i, o[i] * inv, o[i + 1] * inv, o[i + 2] * inv, o[i + 3] * inv);
+            for (int i = 0; i < 16; i += 4) store4<ET>(dst + next * i, o[i] * inv, o[i + 1] * inv, o[i + 2] * inv, o[i + 3] * inv);
         }
     }
 };

@@ -83,13 +83,18 @@ __device__ __forceinline__ void few_rows_of(const Piece<float>& P, uint8_t* smem
         f32x4 sc[NB];
 #pragma unroll
         for (int b = 0; b < NB; ++b) sc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+        auto kfrag = [&](int c) { return *reinterpret_cast<const u32x4*>(kt + (kaddr ^ (64u * (c & 3))) + 256 * (c >> 2)); };
+        u32x4 kf[2] = {kfrag(0)};
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
-            const u32x4 f = *reinterpret_cast<const u32x4*>(kt + (kaddr ^ (64u * (c & 3))) + 256 * (c >> 2));
+        for (int c = 0; c < 8; ++c) {                      // the next fragment is read before the products of this one
+            if (c < 7) kf[(c + 1) & 1] = kfrag(c + 1);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
 #pragma unroll
-                for (int b = 0; b < NB; ++b) sc[b] = mfma16(__uint_as_float(f[e]), __uint_as_float(qf[b][c][e]), sc[b]);
+                for (int b = 0; b < NB; ++b)
+                    sc[b] = mfma16(__uint_as_float(kf[c & 1][e]), __uint_as_float(qf[b][c][e]), sc[b]);
+            __builtin_amdgcn_sched_barrier(0);
         }
         wait_lds();                                        // the keys have been read
         if (more) {
@@ -129,22 +134,24 @@ __device__ __forceinline__ void few_rows_of(const Piece<float>& P, uint8_t* smem
             }
             odd = __any(bits != 0);
         }
-        auto products = [&](auto only_finite) {
+        // four rows' fragments, the next before the products of these
+        auto vfrag = [&](int n) { return *reinterpret_cast<const u32x4*>(vt + (4 * q4 + (n >> 1)) * ROWB + 256 * (n & 1) + 16 * i16); };
+        u32x4 f[2] = {vfrag(0)};
 #pragma unroll
-            for (int v = 0; v < 4; ++v)
+        for (int n = 0; n < 8; ++n) {
+            if (n < 7) f[(n + 1) & 1] = vfrag(n + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            if (odd)
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    u32x4 f = *reinterpret_cast<const u32x4*>(vt + (4 * q4 + v) * ROWB + 256 * half + 16 * i16);
+                for (int e = 0; e < 4; ++e) f[n & 1][e] = P.finite(f[n & 1][e]);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if constexpr (only_finite) f[e] = P.finite(f[e]);
+            for (int e = 0; e < 4; ++e)
 #pragma unroll
-                        for (int b = 0; b < NB; ++b) acc[b][half][e] = mfma16(__uint_as_float(f[e]), sc[b][v], acc[b][half][e]);
-                    }
-                }
-        };
+                for (int b = 0; b < NB; ++b)
+                    acc[b][n & 1][e] = mfma16(__uint_as_float(f[n & 1][e]), sc[b][n >> 1], acc[b][n & 1][e]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
         if (odd) {
-            products(std::true_type());
 #pragma unroll 1
             for (int kk = 0; kk < 16; ++kk)
 #pragma unroll
@@ -158,7 +165,7 @@ __device__ __forceinline__ void few_rows_of(const Piece<float>& P, uint8_t* smem
                             acc[b][n >> 2][e][n & 3] += see ? __uint_as_float(w[e] ^ P.finite(w[e])) : 0.f;
                     }
                 }
-        } else products(std::false_type());
+        }
         wait_lds();                                        // the values have been read
         if (more) bring_values(t0 + step);
     }
@@ -222,14 +229,14 @@ __device__ __forceinline__ void many_rows<float>(const Piece<float>& P, uint8_t*
     if (M.stages) M.begin();
     Running run;
     u32x4 qf[1][16];
-    f32x16 acc[1][4];
+    f32x16 acc[4];
     int32_t tok, head;
     M.row_of(0, P.l32, tok, head);
     P.query(qf[0], P.r.q0 + tok, head);
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
-        for (int k = 0; k < 16; ++k) acc[0][dt][k] = 0.f;
+        for (int k = 0; k < 16; ++k) acc[dt][k] = 0.f;
     const auto seen = M.keys_seen(0);
     const float slack = SLACK / a.c;
     for (int j = 0; j < M.stages; ++j) {
@@ -247,19 +254,23 @@ __device__ __forceinline__ void many_rows<float>(const Piece<float>& P, uint8_t*
 #pragma unroll
             for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
-                for (int k = 0; k < 16; ++k) acc[0][dt][k] *= f;
+                for (int k = 0; k < 16; ++k) acc[dt][k] *= f;
         }
         weights(sc[0], a.c, run.off, run.l);
         const uint8_t* vt = M.values_of(j);
-        if (masked && P.anew().odd_values(vt)) {
-            const Piece<float> A = P.anew();
-            A.template values<1, true>(vt, sc, acc);
-            A.add_odd(vt, t0, seen, M.gm_of(j), [&](int dt, int i, float x) { acc[0][dt][i] += x; });
-        } else P.template values<1>(vt, sc, acc);
+        const bool odd = masked && P.anew().odd_values(vt);
+        P.values(vt, sc[0], acc, odd);
+        if (odd)
+            P.anew().add_odd(vt, t0, seen, M.gm_of(j), [&](int dt, int i, float x) { acc[i & 3][4 * dt + (i >> 2)] += x; });
     }
     const float l = xsum32(run.l);
 #pragma unroll
-    for (int dt = 0; dt < 4; ++dt) M.put(0, dt, acc[0][dt], run, l, cut, rec_row, dt == 3);
+    for (int dt = 0; dt < 4; ++dt) {
+        f32x16 o;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[i] = acc[i & 3][4 * dt + (i >> 2)];
+        M.put(0, dt, o, run, l, cut, rec_row, dt == 3);
+    }
     M.finish();
 }
 

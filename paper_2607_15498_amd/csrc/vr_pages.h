@@ -82,7 +82,7 @@ VR_HD int32_t seq_mean(SeqRange r, int32_t span, int causal) {
 constexpr int JOIN_UNIT = 32;
 struct Costs { int32_t few, many, piece, join, lmin; };      // lmin: shortest piece, keys (a power of two)
 VR_HD Costs costs_of(bool bf16) {
-    return bf16 ? Costs{4, 4, 400, 600, 256} : Costs{8, 45, 400, 600, 128};
+    return bf16 ? Costs{4, 4, 400, 600, 256} : Costs{7, 36, 400, 600, 128};
 }
 VR_HD int32_t key_cost(SeqRange r, int Hg, Costs c) { return tile_rows(r, Hg) == ROWS_FEW ? c.few : c.many; }
 // pieces of a span of keys at `cost` each (32-bit divisions: the plan's code is run once, and what it costs is
