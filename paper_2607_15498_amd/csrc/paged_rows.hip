@@ -87,87 +87,99 @@ template <typename ET, bool PAGED>
 __global__ __launch_bounds__(256) void row_kernel(RowArgs p) {
     __shared__ float2 cs[TPB_MAX][64];
     __shared__ int64_t slot[TPB_MAX];        // PAGED: page x G x page size + slot, -1: none
-    const int32_t t0 = (int32_t)blockIdx.x * p.tpb;
-    const int nt = p.T - t0 < p.tpb ? p.T - t0 : p.tpb;
     const int h0 = (int)blockIdx.y * p.hpb, Hs = p.Ha + p.Hb;
     const int nh = Hs - h0 < p.hpb ? Hs - h0 : p.hpb;
-    if (PAGED || p.theta) {
-        for (int i = threadIdx.x; i < nt * 64; i += 256) {
-            const int t = i >> 6;
-            int32_t at = -1;
+    const int64_t step = (int64_t)gridDim.x * p.tpb;
+    for (int64_t at0 = (int64_t)blockIdx.x * p.tpb; at0 < p.T; at0 += step) {
+        const int32_t t0 = (int32_t)at0;
+        const int nt = p.T - t0 < p.tpb ? p.T - t0 : p.tpb;
+        if (PAGED || p.theta) {
+            for (int i = threadIdx.x; i < nt * 64; i += 256) {
+                const int t = i >> 6;
+                int32_t at = -1;
+                if constexpr (PAGED) {
+                    const int s = find_seq(p.q_start, p.S, t0 + t);
+                    if (s >= 0) {
+                        const SeqRange r = seq_range(p.q_start[s], p.q_start[s + 1], p.kv_len[s], p.T, p.cap);
+                        at = r.klen - r.qlen + (t0 + t - r.q0);
+                        // a length beyond the table would move the rows: nothing is written for it
+                        if (p.kv_len[s] > p.cap || p.kv_len[s] < 0) at = -1;
+                    }
+                    if ((i & 63) == 0) {
+                        const int32_t pg = at < 0 ? -1 : good_page(p.table[s * p.table_stride + (at >> p.shift)], p.n_pages);
+                        slot[t] = pg < 0 ? -1 : (((int64_t)pg * p.Ha) << p.shift) + (at & ((1 << p.shift) - 1));
+                    }
+                } else at = p.pos[t0 + t];
+                if (p.theta) cs[t][i & 63] = turn_of(at, p.theta[i & 63]);
+            }
+            __syncthreads();
+        }
+        const int j = threadIdx.x & 7;
+        for (int i = threadIdx.x >> 3; i < nt * nh; i += 32) {
+            // norm and rotation: in the order of the rows; append: a head's tokens together, as they lie in its page
+            const int t = PAGED ? i % nt : i / nh, hd = h0 + (PAGED ? i / nt : i % nh);
+            const bool second = hd >= p.Ha;
+            const int hh = second ? hd - p.Ha : hd;
+            const ET* src = (second ? (const ET*)p.b + (int64_t)(t0 + t) * p.b_stride
+                                    : (const ET*)p.a + (int64_t)(t0 + t) * p.a_stride) + (int64_t)hh * D + 8 * j;
+            ET* dst;
             if constexpr (PAGED) {
-                const int s = find_seq(p.q_start, p.S, t0 + t);
-                if (s >= 0) {
-                    const SeqRange r = seq_range(p.q_start[s], p.q_start[s + 1], p.kv_len[s], p.T, p.cap);
-                    at = r.klen - r.qlen + (t0 + t - r.q0);
-                    // a length beyond the table would move the rows: nothing is written for it
-                    if (p.kv_len[s] > p.cap || p.kv_len[s] < 0) at = -1;
-                }
-                if ((i & 63) == 0) {
-                    const int32_t pg = at < 0 ? -1 : good_page(p.table[s * p.table_stride + (at >> p.shift)], p.n_pages);
-                    slot[t] = pg < 0 ? -1 : (((int64_t)pg * p.Ha) << p.shift) + (at & ((1 << p.shift) - 1));
-                }
-            } else at = p.pos[t0 + t];
-            if (p.theta) cs[t][i & 63] = turn_of(at, p.theta[i & 63]);
-        }
-        __syncthreads();
-    }
-    const int j = threadIdx.x & 7;
-    for (int i = threadIdx.x >> 3; i < nt * nh; i += 32) {
-        const int t = i / nh, hd = h0 + i % nh;
-        const bool second = hd >= p.Ha;
-        const int hh = second ? hd - p.Ha : hd;
-        const ET* src = (second ? (const ET*)p.b + (int64_t)(t0 + t) * p.b_stride
-                                : (const ET*)p.a + (int64_t)(t0 + t) * p.a_stride) + (int64_t)hh * D + 8 * j;
-        ET* dst;
-        if constexpr (PAGED) {
-            if (slot[t] < 0) continue;
-            dst = (ET*)(second ? p.bo : p.ao) + (slot[t] + ((int64_t)hh << p.shift)) * D + 8 * j;
-        } else {
-            dst = (second ? (ET*)p.bo + (int64_t)(t0 + t) * p.bo_stride
-                          : (ET*)p.ao + (int64_t)(t0 + t) * p.ao_stride) + (int64_t)hh * D + 8 * j;
-        }
-        Half8 x0 = load8(src), x1 = load8(src + 64);
-        if constexpr (!PAGED) {
-            const float* w = second ? p.wb : p.wa;
-            if (w) {                         // the same for the 8 lanes of a row
-                w += hh * (second ? p.wb_stride : p.wa_stride) + 8 * j;
-                const Half8 w0 = load8(w), w1 = load8(w + 64);
-                float sq = 0.f;
+                if (slot[t] < 0) continue;
+                dst = (ET*)(second ? p.bo : p.ao) + (slot[t] + ((int64_t)hh << p.shift)) * D + 8 * j;
+            } else {
+                dst = (second ? (ET*)p.bo + (int64_t)(t0 + t) * p.bo_stride
+                              : (ET*)p.ao + (int64_t)(t0 + t) * p.ao_stride) + (int64_t)hh * D + 8 * j;
+            }
+            Half8 x0 = load8(src), x1 = load8(src + 64);
+            if constexpr (!PAGED) {
+                const float* w = second ? p.wb : p.wa;
+                if (w) {                         // the same for the 8 lanes of a row
+                    w += hh * (second ? p.wb_stride : p.wa_stride) + 8 * j;
+                    const Half8 w0 = load8(w), w1 = load8(w + 64);
+                    float sq = 0.f;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) sq = fmaf(x0.x[k], x0.x[k], fmaf(x1.x[k], x1.x[k], sq));
-                sq += shfl_xor_f(sq, 1);
-                sq += shfl_xor_f(sq, 2);
-                sq += shfl_xor_f(sq, 4);
-                const float r = 1.0f / sqrtf(sq * (1.0f / D) + p.eps);
+                    for (int k = 0; k < 8; ++k) sq = fmaf(x0.x[k], x0.x[k], fmaf(x1.x[k], x1.x[k], sq));
+                    sq += shfl_xor_f(sq, 1);
+                    sq += shfl_xor_f(sq, 2);
+                    sq += shfl_xor_f(sq, 4);
+                    const float r = 1.0f / sqrtf(sq * (1.0f / D) + p.eps);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        x0.x[k] *= r * w0.x[k];
+                        x1.x[k] *= r * w1.x[k];
+                    }
+                }
+            }
+            if (p.theta && !(PAGED && second)) {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
-                    x0.x[k] *= r * w0.x[k];
-                    x1.x[k] *= r * w1.x[k];
+                    const float2 q = cs[t][8 * j + k];
+                    const float u = x0.x[k], v = x1.x[k];
+                    x0.x[k] = u * q.x - v * q.y;
+                    x1.x[k] = u * q.y + v * q.x;
                 }
             }
+            store8(dst, x0);
+            store8(dst + 64, x1);
         }
-        if (p.theta && !(PAGED && second)) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const float2 q = cs[t][8 * j + k];
-                const float u = x0.x[k], v = x1.x[k];
-                x0.x[k] = u * q.x - v * q.y;
-                x1.x[k] = u * q.y + v * q.x;
-            }
-        }
-        store8(dst, x0);
-        store8(dst + 64, x1);
+        if (at0 + step < p.T) __syncthreads();             // the tables are written again
     }
 }
 
+// Few rows: a token and 32 of its rows a workgroup, so that they spread over the card.  Many: about 128 rows a workgroup
+// share their tokens' angles; append's workgroups find their slots first, and more that are smaller hide that
+// better.  Rows a workgroup 64 / 128 / 256: norm and rotation of 16384 tokens of 28 + 4 heads 47.5 / 45.8 / 50 us (5.8 TB/s
+// of reading and writing); append of 32768 tokens of 8 + 8 heads 51.3 / 54.4 / 60 us (5.2 TB/s), 53.6 / 57 / 60 with a token's
+// heads together instead.
 template <typename ET, bool PAGED>
 hipError_t launch_rows(RowArgs p, hipStream_t st) {
     const int Hs = p.Ha + p.Hb;
     const bool many = (int64_t)p.T * Hs >= 32 * 1024;
-    p.tpb = many ? (Hs >= 128 ? 1 : (128 + Hs - 1) / Hs < TPB_MAX ? (128 + Hs - 1) / Hs : TPB_MAX) : 1;
+    constexpr int per = PAGED ? 64 : 128;
+    p.tpb = !many ? 1 : (per + Hs - 1) / Hs < TPB_MAX ? (per + Hs - 1) / Hs : TPB_MAX;
     p.hpb = many ? Hs : Hs < 32 ? Hs : 32;
-    const dim3 grid((unsigned)((p.T + p.tpb - 1) / p.tpb), (unsigned)((Hs + p.hpb - 1) / p.hpb));
+    const int64_t blocks = ((int64_t)p.T + p.tpb - 1) / p.tpb;
+    const dim3 grid((unsigned)(blocks < 1 << 20 ? blocks : 1 << 20), (unsigned)((Hs + p.hpb - 1) / p.hpb));
     row_kernel<ET, PAGED><<<grid, 256, 0, st>>>(p);
     return hipGetLastError();
 }
