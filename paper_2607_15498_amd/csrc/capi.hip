@@ -26,11 +26,15 @@ hipError_t ensure_lds_limit(const void* fn, size_t bytes) {
     int dev = 0;
     hipError_t e = hipGetDevice(&dev);
     if (e != hipSuccess) return e;
-    std::lock_guard<std::mutex> lock(mu);
-    size_t& have = raised[{fn, dev}];
-    if (bytes <= have) return hipSuccess;
-    e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-    if (e == hipSuccess) have = bytes;
+    try {                                                  // nothing is thrown through a C entry
+        std::lock_guard<std::mutex> lock(mu);
+        size_t& have = raised[{fn, dev}];
+        if (bytes <= have) return hipSuccess;
+        e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+        if (e == hipSuccess) have = bytes;
+    } catch (...) {
+        return hipErrorOutOfMemory;
+    }
     return e;
 }
 
@@ -47,7 +51,10 @@ int fail(int code, const char* fmt, ...) {
     va_start(ap, fmt);
     vsnprintf(buf, sizeof buf, fmt, ap);
     va_end(ap);
-    g_err = buf;
+    try {
+        g_err = buf;
+    } catch (...) {                                        // no memory for the text: the code stands
+    }
     return code;
 }
 
@@ -736,7 +743,7 @@ int varrate_paged_attn(const varrate_pages* pg, const varrate_batch* b, const vo
     if (causal != 0 && causal != 1) return fail(VARRATE_EINVAL, "causal=%d outside {0, 1}", causal);
     if (window < 0 || window > (1 << 30)) return fail(VARRATE_EINVAL, "window=%d outside [0, 2^30]", window);
     if (window && !causal) return fail(VARRATE_EUNSUPPORTED, "a window without causal order");
-    if (!(scale > 0.f) || !std::isfinite(scale)) return fail(VARRATE_EINVAL, "scale must be finite and > 0");
+    if (!(scale >= 0x1p-100f && scale <= 0x1p100f)) return fail(VARRATE_EINVAL, "scale outside [2^-100, 2^100]");
     if (b->T == 0) return VARRATE_OK;
     if ((rc = check_rows(q, q_stride, b->T, H, pg->dtype, false, "q")) ||
         (rc = check_rows(out, out_stride, b->T, H, pg->dtype, true, "out"))) return rc;

@@ -142,13 +142,18 @@ __device__ __forceinline__ Plan wave_plan(const AttnArgs& a, const SeqRange& fir
 // tile first (with causal rows it sees the most keys); JOIN: numbers count the second launch's work, (join_rows rows,
 // head) pairs of cut sequences, of few rows (row, head) pairs.  base, end: the sequence's numbers; rec: its first row of
 // partial results.
-struct Unit { SeqRange r; int32_t s, np; int64_t base, end, rec; };
+// at, before, rbefore: the 64 sequences that it was found among, and the numbers and rows before them; a search for a
+// number behind goes on from there.
+struct Unit { SeqRange r; int32_t s, np, at; int64_t base, end, rec, before, rbefore; };
 template <bool JOIN>
 __device__ __forceinline__ bool find_unit(const AttnArgs& a, int32_t L, const SeqRange& first, int64_t idx, Unit& u) {
     const int lane = threadIdx.x & 63, lanes = a.S < 64 ? a.S : 64;
-    int64_t before = 0, rbefore = 0;
-    for (int s0 = 0; s0 < a.S; s0 += 64) {
-        const SeqRange r = s0 ? load_range(a, s0 + lane) : first;
+    if (idx < u.before) {
+        u.at = 0;
+        u.before = u.rbefore = 0;
+    }
+    while (u.at < a.S) {
+        const SeqRange r = u.at ? load_range(a, u.at + lane) : first;
         const int32_t np = seq_pieces(seq_span(r, a.Hg, a.window), key_cost(r, a.Hg, a.costs), L, a.costs.lmin);
         const int64_t t = (int64_t)seq_tiles(r, a.Hg) * a.G, nr = np > 1 ? t * np * tile_rows(r, a.Hg) : 0;
         const int64_t rows = seq_rows(r, a.Hg), parts = rows <= ROWS_FEW ? rows : (rows + join_rows(np) - 1) / join_rows(np);
@@ -161,22 +166,24 @@ __device__ __forceinline__ bool find_unit(const AttnArgs& a, int32_t L, const Se
                 rup += y;
             }
         }
-        const uint64_t hit = __ballot(lane < lanes && before + up > idx);
+        const uint64_t hit = __ballot(lane < lanes && u.before + up > idx);
         if (hit) {
             const int l = __builtin_ctzll(hit);
             u.r.q0 = __builtin_amdgcn_readlane(r.q0, l);
             u.r.qlen = __builtin_amdgcn_readlane(r.qlen, l);
             u.r.klen = __builtin_amdgcn_readlane(r.klen, l);
             u.np = __builtin_amdgcn_readlane(np, l);
-            u.base = before + lane64(up - n, l);
-            u.end = before + lane64(up, l);
-            u.rec = rbefore + lane64(rup - nr, l);
-            u.s = s0 + l;
+            u.base = u.before + lane64(up - n, l);
+            u.end = u.before + lane64(up, l);
+            u.rec = u.rbefore + lane64(rup - nr, l);
+            u.s = u.at + l;
             return true;
         }
-        before += lane64(up, lanes - 1);
-        rbefore += lane64(rup, lanes - 1);
+        u.before += lane64(up, lanes - 1);
+        u.rbefore += lane64(rup, lanes - 1);
+        u.at += 64;
     }
+    u.base = u.end = 0;                        // behind the last: not found, nor what comes behind it
     return false;
 }
 
@@ -634,10 +641,10 @@ struct Many {
 template <typename ET>
 __device__ void many_rows(const Piece<ET>& P, uint8_t* smem, int32_t row0, int32_t rows, bool cut, int64_t rec_row);
 
-// grid: at most one workgroup per slot, a multiple of 8.  Workgroup b takes one piece number of every round of
-// gridDim: b, then in turned order (the pieces of a sequence shrink along its numbers; turning gives every
-// workgroup long and short ones), b % 8 kept: heads stay on their XCD's L2.  Half of the workgroups go through
-// the rounds backwards, so that the single tokens' reads and the chunks' products overlap.
+// grid: at most one workgroup per slot, a multiple of 8.  A workgroup takes one piece of every round of gridDim.  Half of
+// them go through the rounds backwards, so that the single tokens' reads and the chunks' products overlap
+// (1003 tokens beside 16 single ones: 240 us all forwards, 199 so); of more than 64 sequences none, so that they are looked
+// through once.
 template <typename ET>
 __global__ __launch_bounds__(64 * Form<ET>::WAVES, 1) void paged_attn_kernel(AttnArgs a) {
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -647,15 +654,10 @@ __global__ __launch_bounds__(64 * Form<ET>::WAVES, 1) void paged_attn_kernel(Att
     const int32_t L = plan.L;
     const uint32_t b = blockIdx.x, n = gridDim.x;
     const int rounds = (int)(((uint32_t)plan.pieces + n - 1) / n);
-    Unit u;
-    u.base = u.end = 0;
+    Unit u = {};
     for (int k = 0; k < rounds; ++k) {
-        const int round = b & 8 ? rounds - 1 - k : k;
-        const int64_t idx = (int64_t)round * n + (round & 1 ? ((n - 1 - b) & ~7u) | (b & 7u) : b);
-        if ((idx >= u.end || idx < u.base) && !find_unit<false>(a, L, first, idx, u)) {
-            u.base = u.end = 0;
-            continue;                                      // behind the last piece
-        }
+        const int64_t idx = piece_number(b, n, b & 8 && a.S <= 64 ? rounds - 1 - k : k);
+        if ((idx >= u.end || idx < u.base) && !find_unit<false>(a, L, first, idx, u)) continue;   // behind the last piece
         const SeqRange r = u.r;
         const uint32_t in = (uint32_t)(idx - u.base), G = (uint32_t)a.G;
         const int g = (int)(in % G), piece = (int)(in / G % (uint32_t)u.np);
@@ -663,17 +665,9 @@ __global__ __launch_bounds__(64 * Form<ET>::WAVES, 1) void paged_attn_kernel(Att
         const int bm = tile_rows(r, a.Hg);
         const int32_t row0 = tile * bm;
         const int32_t rows = (int32_t)(seq_rows(r, a.Hg) - row0 < bm ? seq_rows(r, a.Hg) - row0 : bm);
-        // keys that the tile's rows see, and of them this piece
-        int32_t lo, hi, x;
-        row_keys(r, row0 / a.Hg, a.causal, a.window, lo, x);
-        row_keys(r, (row0 + rows - 1) / a.Hg, a.causal, a.window, x, hi);
+        int32_t lo, hi;
+        piece_keys(r, row0, rows, piece, u.np, a.Hg, a.causal, a.window, lo, hi);
         const bool cut = u.np > 1;
-        if (cut) {
-            const int32_t len = piece_len(seq_span(r, a.Hg, a.window), u.np);
-            const int64_t p0 = (lo & ~63) + (int64_t)piece * len;
-            if (lo < p0) lo = (int32_t)(p0 < r.klen ? p0 : r.klen);
-            if (hi > p0 + len) hi = (int32_t)(p0 + len);
-        }
         lo = first_lane(lo);
         hi = first_lane(hi > lo ? hi : lo);                // an empty piece: no keys, weight 0
         const int64_t rec_row = u.rec + (int64_t)in * bm;
@@ -744,8 +738,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(AttnArgs a) {
     const int32_t L = first_lane(*plan_of(a));
     if (L == WHOLE) return;
     const int part = threadIdx.x >> 5, l32 = threadIdx.x & 31;     // half wave; its lane's dims are 4 l32 ..
-    Unit u;
-    u.base = u.end = 0;
+    Unit u = {};
     for (int64_t idx = blockIdx.x;; idx += gridDim.x) {
         if (idx >= u.end && !find_unit<true>(a, L, first, idx, u)) break;
         const SeqRange r = u.r;

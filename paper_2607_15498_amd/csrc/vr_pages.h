@@ -168,12 +168,30 @@ VR_HD int64_t max_records(int64_t T, int S, int G, int Hg, int64_t cap, int lmin
     return (p < PIECES_MAX ? p : PIECES_MAX) * (T * Hg <= ROWS_FEW ? ROWS_FEW : ROWS_MANY);
 }
 
-// Keys [lo, hi) that row `row` of the sequence sees (none when hi <= lo).
+// Keys [lo, hi) that the sequence's new token i sees (none when hi <= lo).
 VR_HD void row_keys(SeqRange r, int32_t i, int causal, int window, int32_t& lo, int32_t& hi) {
     const int32_t pos = r.klen - r.qlen + i;
     hi = causal ? (pos + 1 < r.klen ? pos + 1 : r.klen) : r.klen;
     if (hi < 0) hi = 0;
     lo = window && pos - window + 1 > 0 ? pos - window + 1 : 0;
+}
+// Keys [lo, hi) of piece number `piece` of the np of the tile of rows row0 .. row0 + rows - 1 (none when hi <= lo): pieces start
+// at multiples of 64, the first at the one before the tile's first key.
+VR_HD void piece_keys(SeqRange r, int32_t row0, int32_t rows, int32_t piece, int32_t np, int Hg, int causal, int window,
+                      int32_t& lo, int32_t& hi) {
+    int32_t x;
+    row_keys(r, row0 / Hg, causal, window, lo, x);
+    row_keys(r, (row0 + rows - 1) / Hg, causal, window, x, hi);
+    if (np == 1) return;
+    const int32_t len = piece_len(seq_span(r, Hg, window), np);
+    const int64_t p0 = (lo & ~63) + (int64_t)piece * len;
+    if (lo < p0) lo = (int32_t)(p0 < r.klen ? p0 : r.klen);
+    if (hi > p0 + len) hi = (int32_t)(p0 + len);
+}
+// The piece that workgroup b of n (a multiple of 8) takes in a round: b, then in turned order (the pieces of a sequence
+// shrink along its numbers; turning gives every workgroup long and short ones), b % 8 kept: heads stay on their XCD's L2.
+VR_HD int64_t piece_number(uint32_t b, uint32_t n, int round) {
+    return (int64_t)round * n + (round & 1 ? ((n - 1 - b) & ~7u) | (b & 7u) : b);
 }
 
 }  // namespace vr
