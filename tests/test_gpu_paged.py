@@ -612,3 +612,138 @@ def test_two_streams_at_once(vr):
                 got[i].append(vr.paged_attn(pages, batch, qs[i]))
     torch.cuda.synchronize()
     assert all(torch.equal(o, want[i]) for i in range(2) for o in got[i])
+
+
+# ---- the far ends of the ranges, and what the binding refuses --------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m", [1, 5, 8, 70])
+def test_attn_seen_infinities(vr, dtype, m):
+    """Infinite values reach the rows that see them, in their own dims and heads, and nothing else: rows of
+    one token, of up to 16, of up to 32 and many."""
+    import torch
+    n, G, H = 333, 2, 8
+    pool = Pool([n], G, 16, dtype, seed=41)
+    q = torch.randn((m, H, D), generator=torch.Generator().manual_seed(42)).to(tdt(dtype))
+    ref, tol = attn_ref(pool, q, [m], H)
+    t = n - m + m // 2
+    p, i = int(pool.table[0, t // 16]), t % 16
+    up, down = [0, 7, 33, 64, 100, 127], [1, 18, 31, 47, 95, 126]
+    pool.v[p, 1, i, up] = float("inf")
+    pool.v[p, 1, i, down] = float("-inf")
+    pages, batch = pool.device(vr, [m])
+    out = vr.paged_attn(pages, batch, q.cuda()).cpu().double()
+    hit = torch.zeros((m, H, D), dtype=torch.bool)
+    hit[m // 2:, 4:, up + down] = True
+    assert (out[m // 2:, 4:][..., up] == float("inf")).all() and (out[m // 2:, 4:][..., down] == float("-inf")).all()
+    within(out[~hit], ref[~hit], tol[~hit], "the others")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attn_many_sequences_some_cut(vr, dtype):
+    """150 sequences with long ones and chunks among the first and the last 64."""
+    kv = [1 + (37 * s) % 211 for s in range(150)]
+    q = [1] * 150
+    for s, (m, n) in {2: (1, 3000), 5: (90, 700), 63: (1, 1200), 64: (3, 900), 100: (70, 70), 127: (0, 50), 149: (1, 2500)}.items():
+        q[s], kv[s] = m, n
+    check_attn(vr, q, kv, 1, 4, 16, dtype, seed=19)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attn_many_heads(vr, dtype):
+    """One KV head with more query heads than a tile has rows; scales at the lower end."""
+    check_attn(vr, [1, 2], [300, 50], 1, 300, 16, dtype, seed=23)
+    check_attn(vr, [1, 20], [300, 50], 1, 4, 16, dtype, seed=24, scale=2.0 ** -100)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_offsets_beyond_32_bits(vr, dtype):
+    """Pools of more than 2^32 bytes and 2^31 elements: the last pages give what the first give."""
+    import torch
+    G, H, page = 8, 32, 64
+    n_pages = (1 << 31) // (G * page * D) + 40
+    lens, q_len = [500, 90, 700], [1, 90, 33]
+    pool = Pool(lens, G, page, dtype, seed=29)
+    small, batch = pool.device(vr, q_len)
+    far = vr.PagedCache(*(torch.empty((n_pages, G, page, D), dtype=tdt(dtype), device="cuda") for _ in range(2)))
+    assert far.k.numel() > 1 << 31 and far.k.numel() * far.k.element_size() > 1 << 32
+    shift = n_pages - pool.k.shape[0]
+    far.k[shift:], far.v[shift:] = small.k, small.v
+    ftab = torch.where(pool.table >= 0, pool.table + shift, pool.table).cuda()
+    fbatch = vr.PagedBatch(ftab, batch.kv_len, batch.q_start)
+    gen = torch.Generator().manual_seed(5)
+    q, k, v = (torch.randn((sum(q_len), h, D), generator=gen).to(tdt(dtype)).cuda() for h in (H, G, G))
+    theta = theta_of().cuda()
+    vr.paged_append(small, batch, k, v, theta)
+    vr.paged_append(far, fbatch, k, v, theta)
+    same = lambda a, b: torch.equal(a.view(torch.uint8), b.view(torch.uint8))      # unused slots hold NaN
+    assert same(far.k[shift:], small.k) and same(far.v[shift:], small.v)
+    assert torch.equal(vr.paged_attn(far, fbatch, q), vr.paged_attn(small, batch, q))
+    for s, n in enumerate(lens):
+        a, b = vr.paged_gather(far, ftab[s], n), vr.paged_gather(small, batch.table[s], n)
+        assert same(a[0], b[0]) and same(a[1], b[1])
+
+
+def test_norm_rotate_more_blocks_than_the_grid(vr):
+    """2^24 + 5 rows of one head: the workgroups go round, and the last rows are right."""
+    import torch
+    T = (1 << 24) + 5
+    x = torch.zeros((T, 1, D), dtype=torch.bfloat16, device="cuda")
+    pos = torch.zeros(T, dtype=torch.int32, device="cuda")
+    theta = theta_of().cuda()
+    gen = torch.Generator().manual_seed(3)
+    parts = [slice(0, 40), slice((1 << 24) - 20, T), slice(1 << 23, (1 << 23) + 30)]
+    for s in parts:
+        x[s] = torch.randn((s.stop - s.start, 1, D), generator=gen).bfloat16().cuda()
+        pos[s] = torch.randint(0, 1 << 20, (s.stop - s.start,), generator=gen, dtype=torch.int32).cuda()
+    out = vr.norm_rotate(x, pos=pos, theta=theta)[0]
+    for s in parts:
+        ref, tol = norm_ref(x[s].cpu(), None, pos[s].cpu(), theta.cpu(), 0, "bf16")
+        within(out[s], ref, tol, str(s))
+
+
+def test_binding_refuses(vr):
+    """Wrong types, shapes, strides and devices raise before anything is enqueued; nothing is written."""
+    import torch
+    G, H, page, T = 2, 4, 16, 3
+    pages = vr.new_pages(4, G, page)
+    i32 = lambda *a: torch.tensor(a, dtype=torch.int32, device="cuda")
+    batch = vr.PagedBatch(i32(0, 1).view(1, 2), i32(20), i32(0, T))
+    q, k, v = (torch.ones((T, h, D), dtype=torch.bfloat16, device="cuda") for h in (H, G, G))
+    th, pos = theta_of().cuda(), i32(0, 1, 2)
+    wide = torch.ones((T, H, 2 * D), dtype=torch.bfloat16, device="cuda")
+    bad = [
+        lambda: vr.PagedCache(pages.k, pages.v[:2]), lambda: vr.PagedCache(pages.k, pages.v.float()),
+        lambda: vr.PagedCache(pages.k.half(), pages.v.half()), lambda: vr.PagedCache(pages.k.transpose(1, 2), pages.v.transpose(1, 2)),
+        lambda: vr.PagedCache(pages.k.cpu(), pages.v.cpu()), lambda: vr.new_pages(4, G, 24) and vr.paged_gather(vr.new_pages(4, G, 24), i32(0), 1),
+        lambda: vr.PagedBatch(i32(0, 1), i32(20), i32(0, 3)), lambda: vr.PagedBatch(i32(0, 1).view(1, 2).long(), i32(20), i32(0, 3)),
+        lambda: vr.PagedBatch(i32(0, 1).view(1, 2), i32(20, 20), i32(0, 3)), lambda: vr.PagedBatch(i32(0, 1).view(1, 2), i32(20), i32(0)),
+        lambda: vr.PagedBatch(i32(0, 1).view(1, 2), i32(20).cpu(), i32(0, 3)),
+        lambda: vr.PagedBatch(i32(0, 1, 2, 3).view(1, 4)[:, ::2], i32(20), i32(0, 3)),
+        lambda: vr.norm_rotate(None), lambda: vr.norm_rotate(q, theta=th), lambda: vr.norm_rotate(q, pos=pos.long(), theta=th),
+        lambda: vr.norm_rotate(q, pos=pos[:2], theta=th), lambda: vr.norm_rotate(q, pos=pos, theta=th[:32]),
+        lambda: vr.norm_rotate(q, pos=pos, theta=th.double()), lambda: vr.norm_rotate(q.half()), lambda: vr.norm_rotate(q, k.float()),
+        lambda: vr.norm_rotate(q, k[:2]), lambda: vr.norm_rotate(q, wq=th), lambda: vr.norm_rotate(q, wk=torch.ones(D, device="cuda")),
+        lambda: vr.norm_rotate(q, wq=torch.ones((G, D), device="cuda")), lambda: vr.norm_rotate(wide[..., ::2]),
+        lambda: vr.norm_rotate(q, q_out=k), lambda: vr.norm_rotate(q, q_out=q.float()), lambda: vr.norm_rotate(q, eps=-1.0),
+        lambda: vr.norm_rotate(q[..., :64]), lambda: vr.norm_rotate(wide.view(-1)[4:4 + T * H * D].view(T, H, D)),
+        lambda: vr.paged_append(pages, batch, k.float(), v), lambda: vr.paged_append(pages, batch, k, v[:2]),
+        lambda: vr.paged_append(pages, batch, q, v), lambda: vr.paged_append(pages, batch, k.cpu(), v),
+        lambda: vr.paged_append(pages, batch, k, v, theta=th[1:33]), lambda: vr.paged_attn(pages, batch, q.float()),
+        lambda: vr.paged_attn(pages, batch, q[0]), lambda: vr.paged_attn(pages, batch, q[:, :3]), lambda: vr.paged_attn(pages, batch, q, out=k),
+        lambda: vr.paged_attn(pages, batch, q, out=q), lambda: vr.paged_attn(pages, batch, q, window=-1),
+        lambda: vr.paged_attn(pages, batch, q, causal=False, window=4), lambda: vr.paged_attn(pages, batch, q, scale=0.0),
+        lambda: vr.paged_attn(pages, batch, q, scale=float("nan")), lambda: vr.paged_attn(pages, batch, q, out=q.cpu()),
+        lambda: vr.paged_attn(pages, vr.PagedBatch(i32(*range(40)).view(1, 40), i32(20), i32(0, T)), q,
+                              workspace=torch.empty(64, dtype=torch.uint8, device="cuda")),
+        lambda: vr.paged_gather(pages, i32(0, 1), -1), lambda: vr.paged_gather(pages, i32(0, 1), 33),
+        lambda: vr.paged_gather(pages, i32(0, 1).view(1, 2), 3), lambda: vr.paged_gather(pages, i32(0, 1).cpu(), 3),
+        lambda: vr.paged_gather(pages, i32(0, 1), 3, K=k[:2]), lambda: vr.paged_gather(pages, i32(0, 1), 3, V=v.float()),
+        lambda: vr.paged_gather(pages, i32(0, 1), 3, K=wide[:, :G, ::2]),
+    ]
+    for i, call in enumerate(bad):
+        with pytest.raises(vr.VarRateError):
+            call()
+            say(f"call {i} was not refused")
+    torch.cuda.synchronize()
+    assert (pages.k == 0).all() and (pages.v == 0).all() and (q == 1).all() and (k == 1).all()
