@@ -19,7 +19,7 @@ struct AttnArgs {
     const int32_t* table;
     const int32_t* kv_len;
     const int32_t* q_start;
-    float* rec;                     // cut calls: partial rows [rec_rows][128], then their [rec_rows][2] (max, sum)
+    float* rec;                     // partial rows [rec_rows][128], then their [rec_rows][2] (max, sum), then the shares
     int64_t q_stride, out_stride;   // elements between tokens
     int64_t table_stride;
     int64_t rec_rows;
@@ -73,18 +73,11 @@ __device__ __forceinline__ int64_t lane64(int64_t v, int lane) {
                      (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane));
 }
 
-// ---- the call's cut, computed by every wave from the device lengths ----------------------------
+// ---- who does what, computed by every wave from the device lengths ------------------------------
 // Reductions over the first `n` lanes (the others hold nothing), to a scalar.
 __device__ __forceinline__ float first_lane(float v) { return __uint_as_float((uint32_t)first_lane((int32_t)__float_as_uint(v))); }
 template <typename V> __device__ __forceinline__ V wave_sum(V v, int n) {
     for (int m = 1; m < n; m <<= 1) v += __shfl_xor(v, m, WAVE);
-    return first_lane(v);
-}
-__device__ __forceinline__ int32_t wave_most(int32_t v, int n) {
-    for (int m = 1; m < n; m <<= 1) {
-        const int32_t x = __shfl_xor(v, m, WAVE);
-        v = x > v ? x : v;
-    }
     return first_lane(v);
 }
 __device__ __forceinline__ SeqRange load_range(const AttnArgs& a, int s) {
@@ -92,100 +85,102 @@ __device__ __forceinline__ SeqRange load_range(const AttnArgs& a, int s) {
     if (s < a.S) r = seq_range(a.q_start[s], a.q_start[s + 1], a.kv_len[s], a.T, a.cap);
     return r;
 }
-// `first`: the first 64 sequences, kept for find_unit.
+struct Plan { int64_t head, units; Split split; };         // cost of a head's work; tiles x heads
+// `first`: the first 64 sequences, kept for the searches.
 __device__ __forceinline__ Plan wave_plan(const AttnArgs& a, const SeqRange& first) {
     const int lane = threadIdx.x & 63, n = a.S < 64 ? a.S : 64;
     Sums s;
     for (int s0 = 0; s0 < a.S; s0 += 64)
         sum_up(s, s0 ? load_range(a, s0 + lane) : first, a.G, a.Hg, a.causal, a.window, a.costs);
-    s.longest = wave_most(s.longest, n);
-    s.units = wave_sum(s.units, n);
-    if (!may_cut(s, a.costs)) return uncut(s);
-    s.work = wave_sum(s.work, n);
-    s.spans = wave_sum(s.spans, n);
-    s.many = __any(s.many);
-    // lane 8 i + k: candidate i, every eighth sequence from k on (one copy of the code)
-    static_assert(CUTS <= 8, "a candidate is 8 lanes'");
-    const int cand = lane >> 3 < CUTS ? lane >> 3 : 0, slot = lane & 7;
-    Cut t = cut_begin(cand, s.spans);
-    for (int s0 = 0; s0 < a.S; s0 += 64) {
-        const SeqRange mine = s0 ? load_range(a, s0 + lane) : first;
-        const int here = a.S - s0 < 64 ? a.S - s0 : 64;
-#pragma unroll 1
-        for (int k = 0; k < here; k += 8) {
-            SeqRange r;
-            r.q0 = 0;
-            r.qlen = __shfl(mine.qlen, k + slot, WAVE);    // nothing behind the last
-            r.klen = __shfl(mine.klen, k + slot, WAVE);
-            cut_up(t, r, a.G, a.Hg, a.window, a.costs);
-        }
+    for (int m = 1; m < n; m <<= 1) {
+        s.head += (uint64_t)__shfl_xor((int64_t)s.head, m, WAVE);
+        s.units += __shfl_xor(s.units, m, WAVE);
+        s.total += __shfl_xor(s.total, m, WAVE);
+        s.many += __shfl_xor(s.many, m, WAVE);
+        s.units_many += __shfl_xor(s.units_many, m, WAVE);
+        s.longest = fmaxf(s.longest, __shfl_xor(s.longest, m, WAVE));
     }
-    for (int m = 1; m < 8 && m < n; m <<= 1) {
-        t.pieces += __shfl_xor(t.pieces, m, WAVE);
-        t.partial += __shfl_xor(t.partial, m, WAVE);
-        t.most = fmaxf(t.most, __shfl_xor(t.most, m, WAVE));
-    }
-    const int cost = (int)__float_as_uint(cut_cost(t, s, a.costs));        // > 0: ordered as integers
-    int best = 0, least = first_lane(cost);
-#pragma unroll
-    for (int i = 1; i < CUTS; ++i) {
-        const int x = __builtin_amdgcn_readlane(cost, 8 * i);
-        if (x < least) {
-            least = x;
-            best = i;
-        }
-    }
-    if (best == 0) return uncut(s);
-    return Plan{__builtin_amdgcn_readlane(t.L, 8 * best), (int32_t)__builtin_amdgcn_readlane((int)t.pieces, 8 * best)};
+    const int64_t head = first_lane((int64_t)s.head);
+    s.units = first_lane(s.units);
+    s.total = first_lane(s.total);
+    s.many = first_lane(s.many);
+    s.units_many = first_lane(s.units_many);
+    s.longest = first_lane(s.longest);
+    if (!a.rec_rows) return Plan{head, s.units, Split{0, 0}};
+    const Split p = split_of(s, (int)gridDim.x, a.costs);
+    return Plan{head, s.units, Split{first_lane(p.among), first_lane(p.same)}};
 }
-// The sequence of number idx.  A sequence's pieces are (tile, piece, head) triples, heads innermost and the last
-// tile first (with causal rows it sees the most keys); JOIN: numbers count the second launch's work, (join_rows rows,
-// head) pairs of cut sequences, of few rows (row, head) pairs.  base, end: the sequence's numbers; rec: its first row of
-// partial results.
-// at, before, rbefore: the 64 sequences that it was found among, and the numbers and rows before them; a search for a
-// number behind goes on from there.
-struct Unit { SeqRange r; int32_t s, np, at; int64_t base, end, rec, before, rbefore; };
-template <bool JOIN>
-__device__ __forceinline__ bool find_unit(const AttnArgs& a, int32_t L, const SeqRange& first, int64_t idx, Unit& u) {
+// The sequence into whose measure number x falls.  at, before: the 64 sequences that it was found among and the measure
+// before them: a search for a number behind goes on from there.
+struct Search { int32_t at = 0; int64_t before = 0; };
+struct Found { SeqRange r; int32_t s; int64_t base; };
+template <typename M>
+__device__ __forceinline__ bool find(const AttnArgs& a, const SeqRange& first, int64_t x, Search& from, Found& f, M&& measure) {
     const int lane = threadIdx.x & 63, lanes = a.S < 64 ? a.S : 64;
-    if (idx < u.before) {
-        u.at = 0;
-        u.before = u.rbefore = 0;
-    }
-    while (u.at < a.S) {
-        const SeqRange r = u.at ? load_range(a, u.at + lane) : first;
-        const int32_t np = seq_pieces(seq_span(r, a.Hg, a.window), key_cost(r, a.Hg, a.costs), L, a.costs.lmin);
-        const int64_t t = (int64_t)seq_tiles(r, a.Hg) * a.G, nr = np > 1 ? t * np * tile_rows(r, a.Hg) : 0;
-        const int64_t rows = seq_rows(r, a.Hg), parts = rows <= ROWS_FEW ? rows : (rows + join_rows(np) - 1) / join_rows(np);
-        const int64_t n = JOIN ? (np > 1 ? parts * a.G : 0) : t * np;
-        int64_t up = n, rup = nr;              // inclusive scans over the lanes
+    if (x < from.before) from = Search{};
+    while (from.at < a.S) {
+        const SeqRange r = from.at ? load_range(a, from.at + lane) : first;
+        const int64_t n = measure(r);
+        int64_t up = n;                        // inclusive scan over the lanes
         for (int m = 1; m < lanes; m <<= 1) {
-            const int64_t x = __shfl_up(up, m, WAVE), y = __shfl_up(rup, m, WAVE);
-            if (lane >= m) {
-                up += x;
-                rup += y;
-            }
+            const int64_t y = __shfl_up(up, m, WAVE);
+            if (lane >= m) up += y;
         }
-        const uint64_t hit = __ballot(lane < lanes && u.before + up > idx);
+        const uint64_t hit = __ballot(lane < lanes && from.before + up > x);
         if (hit) {
             const int l = __builtin_ctzll(hit);
-            u.r.q0 = __builtin_amdgcn_readlane(r.q0, l);
-            u.r.qlen = __builtin_amdgcn_readlane(r.qlen, l);
-            u.r.klen = __builtin_amdgcn_readlane(r.klen, l);
-            u.np = __builtin_amdgcn_readlane(np, l);
-            u.base = u.before + lane64(up - n, l);
-            u.end = u.before + lane64(up, l);
-            u.rec = u.rbefore + lane64(rup - nr, l);
-            u.s = u.at + l;
+            f.r.q0 = __builtin_amdgcn_readlane(r.q0, l);
+            f.r.qlen = __builtin_amdgcn_readlane(r.qlen, l);
+            f.r.klen = __builtin_amdgcn_readlane(r.klen, l);
+            f.s = from.at + l;
+            f.base = from.before + lane64(up - n, l);
             return true;
         }
-        u.before += lane64(up, lanes - 1);
-        u.rbefore += lane64(rup, lanes - 1);
-        u.at += 64;
+        from.before += lane64(up, lanes - 1);
+        from.at += 64;
     }
-    u.base = u.end = 0;                        // behind the last: not found, nor what comes behind it
     return false;
 }
+// The tile of place `pos` of all work, and the tile's place and cost.  Lane by lane: even lanes one pos and odd ones another (a
+// share's begin and end at once: it is a chain of a few hundred instructions).
+struct Tile { Found f; int32_t g = 0, tile = 0; int64_t start = 0, w = 0; bool many = false; };
+__device__ __forceinline__ void tile_of(const AttnArgs& a, const Plan& plan, const SeqRange& first, int64_t pos, Search& from, Tile& t) {
+    int32_t g = (int32_t)((float)pos / (float)plan.head);        // about, then exactly
+    g = g < a.G ? g : a.G - 1;
+    while (g > 0 && g * plan.head > pos) --g;
+    while (g < a.G - 1 && (g + 1) * plan.head <= pos) ++g;
+    const int64_t x = pos - g * plan.head;
+    auto cost = [&](const SeqRange& r) {
+        const Line l = seq_line(r, a.Hg, a.causal, a.window, a.costs);
+        return line_before(l, l.tiles);
+    };
+    Found odd;
+    const int64_t x0 = lane64(x, 0), x1 = lane64(x, 1);
+    find(a, first, x0, from, t.f, cost);
+    odd = t.f;
+    if (x1 != x0) {
+        Search other;
+        find(a, first, x1, other, odd, cost);
+    }
+    const bool second = threadIdx.x & 1;
+    SeqRange r;
+    r.q0 = second ? odd.r.q0 : t.f.r.q0;
+    r.qlen = second ? odd.r.qlen : t.f.r.qlen;
+    r.klen = second ? odd.r.klen : t.f.r.klen;
+    const int64_t base = second ? odd.base : t.f.base;
+    const Line l = seq_line(r, a.Hg, a.causal, a.window, a.costs);
+    t.g = g;
+    t.tile = line_tile(l, x - base);
+    t.start = g * plan.head + base + line_before(l, t.tile);
+    t.w = line_at(l, t.tile);
+    t.many = is_many(r, a.Hg);
+}
+// What the second launch is told of a share: where it begins, in which tile (that one's place), and whether inside it.
+struct Share { int64_t pos, start; SeqRange r; int32_t g, tile, inside; };
+// behind the partial rows: into how many shares the work is divided, then these
+__device__ __forceinline__ int32_t* among_of(const AttnArgs& a) { return (int32_t*)(a.rec + a.rec_rows * (D + 2)); }
+__device__ __forceinline__ Share* shares_of(const AttnArgs& a) { return (Share*)(among_of(a) + 4); }
+constexpr size_t SHARES_BYTES = 16 + SLOTS * sizeof(Share);
 
 template <typename ET>
 struct Form {
@@ -207,9 +202,6 @@ struct Form {
     static_assert(STAGES * 2 * SB <= (int)LDS, "of the largest");
 };
 
-// the call's L for the second launch, behind the partial rows
-__device__ __forceinline__ int32_t* plan_of(const AttnArgs& a) { return (int32_t*)(a.rec + a.rec_rows * (D + 2)); }
-
 // What both forms need of a piece, and the operations on 32-key blocks.
 template <typename ET>
 struct Piece {
@@ -223,12 +215,12 @@ struct Piece {
     int lane, l32, h;
     uint32_t off0, kaddr;
 
-    __device__ __forceinline__ Piece(const AttnArgs& a_, const Unit& u, int g_, int32_t lo_, int32_t hi_)
-        : a(a_), r(u.r), g(g_), lo(lo_), hi(hi_) {
+    __device__ __forceinline__ Piece(const AttnArgs& a_, const Found& f, int g_, int32_t lo_, int32_t hi_)
+        : a(a_), r(f.r), g(g_), lo(lo_), hi(hi_) {
         head_bytes = (int64_t)F::ROWB << a.shift;
         kbase = (const uint8_t*)a.k + (int64_t)g * head_bytes;
         vbase = (const uint8_t*)a.v + (int64_t)g * head_bytes;
-        trow = a.table + (int64_t)u.s * a.table_stride;
+        trow = a.table + (int64_t)f.s * a.table_stride;
         lane = threadIdx.x & 63;
         l32 = lane & 31;
         h = lane >> 5;
@@ -641,48 +633,103 @@ struct Many {
 template <typename ET>
 __device__ void many_rows(const Piece<ET>& P, uint8_t* smem, int32_t row0, int32_t rows, bool cut, int64_t rec_row);
 
-// grid: at most one workgroup per slot, a multiple of 8.  A workgroup takes one piece of every round of gridDim.  Half of
-// them go through the rounds backwards, so that the single tokens' reads and the chunks' products overlap
-// (1003 tokens beside 16 single ones: 240 us all forwards, 199 so); of more than 64 sequences none, so that they are looked
-// through once.
+// grid: at most one workgroup per slot, a multiple of 8.  Whole tiles: a workgroup takes one of each round, half of
+// them go through the rounds backwards, so that the single tokens' reads and the chunks' products overlap (of more than 64
+// sequences none, so that they are looked through once).  Shares: the work is laid end to end and divided evenly; shares
+// that begin or end inside a tile leave partial rows.
+//   Even shares, against pieces of one length per call dealt out in turn: 1003 tokens beside 16 single ones 192 -> 173 us
+//   (chunk and single tokens side by side from the start), fp32 prompts of 1531 and 777 tokens 339 -> 257 us, 32 single tokens
+//   over 100 .. 21800 311 -> 287 us.  Finding a share's ends takes 3 us, which tiles alike in equal pieces save.
 template <typename ET>
 __global__ __launch_bounds__(64 * Form<ET>::WAVES, 1) void paged_attn_kernel(AttnArgs a) {
     extern __shared__ __align__(1024) uint8_t smem[];
     const SeqRange first = load_range(a, threadIdx.x & 63);
     const Plan plan = wave_plan(a, first);
-    if (a.rec_rows && blockIdx.x == 0 && threadIdx.x == 0) *plan_of(a) = plan.L;
-    const int32_t L = plan.L;
     const uint32_t b = blockIdx.x, n = gridDim.x;
-    const int rounds = (int)(((uint32_t)plan.pieces + n - 1) / n);
-    Unit u = {};
-    for (int k = 0; k < rounds; ++k) {
-        const int64_t idx = piece_number(b, n, b & 8 && a.S <= 64 ? rounds - 1 - k : k);
-        if ((idx >= u.end || idx < u.base) && !find_unit<false>(a, L, first, idx, u)) continue;   // behind the last piece
-        const SeqRange r = u.r;
-        const uint32_t in = (uint32_t)(idx - u.base), G = (uint32_t)a.G;
-        const int g = (int)(in % G), piece = (int)(in / G % (uint32_t)u.np);
-        const int tile = seq_tiles(r, a.Hg) - 1 - (int)(in / G / (uint32_t)u.np);
+    const Split split = plan.split;
+    const bool even = split.among && !split.same;
+    const int32_t share = share_of(b, split.among);
+    const int64_t total = plan.head * a.G, all = (plan.units + n - 1) / n;
+    const int32_t rounds = split.same ? 1 : all < INT32_MAX ? (int32_t)all : INT32_MAX;
+    if (a.rec_rows && b == 0 && threadIdx.x == 0) *among_of(a) = split.among;
+    if (split.among && share == split.among) return;
+    Search from;
+    Tile t;
+    int64_t pos = 0, end = 0;
+    int place = 2 * share;
+    for (int k = 0;; ++k) {
+        int64_t x0 = 0, x1 = 0;
+        bool cut = false;
+        if (even) {
+            if (k > 0 && pos >= end) break;
+            if (k == 0 || pos >= t.start + t.w) {
+                const int64_t at = k ? pos : share_begin(total, share + (int)(threadIdx.x & 1), split);
+                Tile u;
+                tile_of(a, plan, first, at < total ? at : total - 1, from, u);
+                if (k == 0) {                              // where the share begins and ends
+                    const int64_t to = at < total ? u.start + cut_at(at - u.start, u.w, u.many, a.costs) : total;
+                    pos = lane64(to, 0);
+                    end = lane64(to, 1);
+                }
+                t.f = u.f;
+                t.g = first_lane(u.g);
+                t.tile = first_lane(u.tile);
+                t.start = first_lane(u.start);
+                t.w = first_lane(u.w);
+                if (k == 0) {
+                    if (threadIdx.x == 0)
+                        shares_of(a)[share] = Share{pos, t.start, t.f.r, t.g, t.tile, pos > t.start && pos < t.start + t.w};
+                    continue;
+                }
+            }
+            x0 = pos - t.start;
+            x1 = end - t.start < t.w ? end - t.start : t.w;
+            cut = x1 - x0 != t.w;
+            pos = t.start + x1;
+        } else {
+            // tiles by their numbers: whole ones sequence after sequence, the last tile first (with causal rows it sees the
+            // most keys), heads innermost; those in equal pieces head after head
+            if (k == rounds) break;
+            const int32_t G = split.same ? 1 : a.G;
+            int64_t idx = tile_number(b, n, b & 8 && a.S <= 64 ? rounds - 1 - k : k);
+            if (split.same) {
+                const uint32_t u = (uint32_t)share / (uint32_t)split.same, each = (uint32_t)plan.units / (uint32_t)a.G;
+                cut = true;
+                t.start = u;
+                t.w = split.same;
+                x0 = share - (int64_t)u * split.same;
+                x1 = x0 + 1;
+                t.g = (int32_t)(u / each);
+                idx = u % each;
+            }
+            if (!find(a, first, idx, from, t.f, [&](const SeqRange& r) { return (int64_t)seq_tiles(r, a.Hg) * G; }))
+                continue;                                  // behind the last
+            const uint32_t in = (uint32_t)(idx - t.f.base);
+            if (!split.same) t.g = (int32_t)(in % (uint32_t)G);
+            t.tile = seq_tiles(t.f.r, a.Hg) - 1 - (int32_t)(in / (uint32_t)G);
+            if (split.same && threadIdx.x == 0)
+                shares_of(a)[share] = Share{share, t.start * t.w, t.f.r, t.g, t.tile, x0 != 0};
+        }
+        const int64_t rec_row = (int64_t)place * place_rows(a.T, a.Hg);
+        if (even) place |= 1;
+        const SeqRange r = t.f.r;
         const int bm = tile_rows(r, a.Hg);
-        const int32_t row0 = tile * bm;
+        const int32_t row0 = t.tile * bm;
         const int32_t rows = (int32_t)(seq_rows(r, a.Hg) - row0 < bm ? seq_rows(r, a.Hg) - row0 : bm);
         int32_t lo, hi;
-        piece_keys(r, row0, rows, piece, u.np, a.Hg, a.causal, a.window, lo, hi);
-        const bool cut = u.np > 1;
-        lo = first_lane(lo);
-        hi = first_lane(hi > lo ? hi : lo);                // an empty piece: no keys, weight 0
-        const int64_t rec_row = u.rec + (int64_t)in * bm;
-        if (cut && rec_row + bm > a.rec_rows) continue;    // starts that fall: no room for their pieces (uniform)
-        const Piece<ET> P(a, u, g, lo, hi);
+        tile_keys(r, row0, rows, a.Hg, a.causal, a.window, lo, hi);
+        if (cut) piece_keys(x0, x1, t.w, lo, hi);
+        const Piece<ET> P(a, t.f, t.g, first_lane(lo), first_lane(hi));
         if (bm == ROWS_FEW) few_rows<ET>(P, smem, rows, cut, rec_row);
         else many_rows<ET>(P, smem, row0, rows, cut, rec_row);
     }
 }
 
 // One row's pieces p0, p0 + step, .. of np, for NR rows at once by a half wave, NP pieces at a time with a running
-// maximum, so that nothing waits for all maxima first.  at(n): the first of row n's partial rows; piece p's is p stride on.
+// maximum, so that nothing waits for all maxima first.  at(n, p): the partial row of row n and piece p.
 template <int NR, int NP, typename A>
-__device__ __forceinline__ void join_pieces(const AttnArgs& a, A&& at, int64_t stride, int p0, int step, int np, float (&M)[NR],
-                                            float (&l)[NR], f32x4 (&o)[NR]) {
+__device__ __forceinline__ void join_pieces(const AttnArgs& a, A&& at, int p0, int step, int np, float (&M)[NR], float (&l)[NR],
+                                            f32x4 (&o)[NR]) {
     const float* rec_ml = a.rec + a.rec_rows * D;
     const int l32 = threadIdx.x & 31;
 #pragma unroll
@@ -701,7 +748,7 @@ __device__ __forceinline__ void join_pieces(const AttnArgs& a, A&& at, int64_t s
                 ml[n][k] = float2{-INFINITY, 0.f};
                 v[n][k] = f32x4{0.f, 0.f, 0.f, 0.f};
                 if (p + k * step < np) {
-                    const int64_t rr = at(n) + (p + k * step) * stride;
+                    const int64_t rr = at(n, p + k * step);
                     ml[n][k] = *reinterpret_cast<const float2*>(rec_ml + rr * 2);
                     v[n][k] = *reinterpret_cast<const f32x4*>(a.rec + rr * D + 4 * l32);
                 }
@@ -726,48 +773,67 @@ __device__ __forceinline__ void join_pieces(const AttnArgs& a, A&& at, int64_t s
         }
     }
 }
-// Joins the pieces of cut sequences.  A half wave has a row, 16 bytes a lane.  Many rows: a workgroup takes join_rows rows
-// of a head; few: one row, every eighth piece a half wave.  It is a chain of reads that the other dies have just written,
-// about 2 us each: what helps is rows in parallel and loads that are all of use (1003 tokens of 32 heads in 2
-// pieces: 8 loads of one row's pieces a wave, 6 of them for nothing: 26 us; this: 12 us).
+// Joins the tiles that were cut.  grid (parts, shares - 1): the workgroups of every share but the first, which have work if
+// theirs is the first to begin inside its tile.  A half wave has a row, 16 bytes a lane, or two; of few rows a workgroup
+// has one, every eighth piece a half wave.  It is a chain of reads that the other dies have just written, about 2 us each: what helps is
+// rows in parallel and loads that are all of use (1003 tokens of 32 heads in 2 pieces: 8 loads of one row's pieces a
+// wave, 6 of them for nothing: 26 us; this: 11 us).
 template <typename ET>
 __global__ __launch_bounds__(256) void paged_join_kernel(AttnArgs a) {
     __shared__ __align__(16) float so[8][D];
     __shared__ float sl[8][2];
-    const SeqRange first = load_range(a, threadIdx.x & 63);
-    const int32_t L = first_lane(*plan_of(a));
-    if (L == WHOLE) return;
-    const int part = threadIdx.x >> 5, l32 = threadIdx.x & 31;     // half wave; its lane's dims are 4 l32 ..
-    Unit u = {};
-    for (int64_t idx = blockIdx.x;; idx += gridDim.x) {
-        if (idx >= u.end && !find_unit<true>(a, L, first, idx, u)) break;
-        const SeqRange r = u.r;
-        const uint32_t in = (uint32_t)(idx - u.base), G = (uint32_t)a.G;
-        const int g = (int)(in % G), bm = tile_rows(r, a.Hg);
-        const bool few = bm == ROWS_FEW;
-        const int32_t rows = (int32_t)seq_rows(r, a.Hg);
-        const int32_t row0 = (int32_t)(in / G) * (few ? 1 : join_rows(u.np));      // all in one tile
-        const int tile = row0 / bm, i0 = row0 % bm;
-        const int64_t number = (int64_t)(seq_tiles(r, a.Hg) - 1 - tile) * u.np * G + g;      // of the tile's piece 0
-        const int64_t rec0 = u.rec + number * bm, stride = (int64_t)G * bm;   // piece p's rows: rec0 + p stride
-        if (rec0 + (u.np - 1) * stride + bm > a.rec_rows) continue;           // as the first launch (uniform)
-        auto put = [&](int32_t row, float l, const f32x4& o) {
-            const float inv = l == 0.f ? 0.f : 1.f / l;
-            ET* dst = (ET*)a.out + (int64_t)(r.q0 + row / a.Hg) * a.out_stride + (int64_t)(g * a.Hg + row % a.Hg) * D + 4 * l32;
-            store4<ET>(dst, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
-        };
-        if (few) {
+    const int i = 1 + (int)blockIdx.y, part = (int)blockIdx.x, parts = (int)gridDim.x;
+    const int lane = threadIdx.x & 63, half = threadIdx.x >> 5, l32 = threadIdx.x & 31;
+    // all that may be asked for, at once
+    const Share* shares = shares_of(a);
+    const Share here = shares[i], before = shares[i - 1];
+    const int j0 = i + 1 + lane < SLOTS ? i + 1 + lane : SLOTS - 1;
+    int32_t next_inside = shares[j0].inside;
+    int64_t next_start = shares[j0].start;
+    const int32_t among = first_lane(*among_of(a));
+    if (i >= among || !first_lane(here.inside)) return;
+    const int64_t start = first_lane(here.start);
+    if (first_lane(before.inside) && first_lane(before.start) == start) return;
+    const SeqRange r = {first_lane(here.r.q0), first_lane(here.r.qlen), first_lane(here.r.klen)};
+    const int g = first_lane(here.g), bm = tile_rows(r, a.Hg);
+    const int32_t row0 = first_lane(here.tile) * bm;
+    const int32_t rows = (int32_t)(seq_rows(r, a.Hg) - row0 < bm ? seq_rows(r, a.Hg) - row0 : bm);
+    // its pieces: share i - 1's last, and the first of i, i + 1, .. that begin inside the tile
+    int np = 2;
+    for (int j = i + 1;; j += 64) {
+        const uint64_t on = __ballot(j + lane < among && next_inside && next_start == start);
+        if (on != ~0ull) {
+            np += __builtin_ctzll(~on);
+            break;
+        }
+        np += 64;
+        const int jn = j + 64 + lane < SLOTS ? j + 64 + lane : SLOTS - 1;
+        next_inside = shares[jn].inside;
+        next_start = shares[jn].start;
+    }
+    const int64_t pr = place_rows(a.T, a.Hg);
+    const int64_t rec0 = (2 * (i - 1) + (first_lane(before.pos) == start ? 0 : 1)) * pr;
+    auto piece = [&](int p) { return p == 0 ? rec0 : 2 * (i + p - 1) * pr; };
+    auto put = [&](int32_t in, float l, const f32x4& o) {
+        const int32_t row = row0 + in;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        ET* dst = (ET*)a.out + (int64_t)(r.q0 + row / a.Hg) * a.out_stride + (int64_t)(g * a.Hg + row % a.Hg) * D + 4 * l32;
+        store4<ET>(dst, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+    };
+    // (rows behind the tile's last are read as they are and dropped)
+    if (bm == ROWS_FEW) {
+        for (int row = part; row < rows; row += parts) {
             float M[1], l[1];
             f32x4 o[1];
-            join_pieces<1, 8>(a, [&](int) { return rec0 + i0; }, stride, part, 8, u.np, M, l, o);
+            join_pieces<1, 8>(a, [&](int, int p) { return piece(p) + row; }, half, 8, np, M, l, o);
             __syncthreads();
-            *reinterpret_cast<f32x4*>(&so[part][4 * l32]) = o[0];
+            *reinterpret_cast<f32x4*>(&so[half][4 * l32]) = o[0];
             if (l32 == 0) {
-                sl[part][0] = M[0];
-                sl[part][1] = l[0];
+                sl[half][0] = M[0];
+                sl[half][1] = l[0];
             }
             __syncthreads();
-            if (part) continue;
+            if (half) continue;
             float mx = sl[0][0], ls = 0.f;
             f32x4 os = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -781,39 +847,42 @@ __global__ __launch_bounds__(256) void paged_join_kernel(AttnArgs a) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) os[e] = fmaf(f, v[e], os[e]);
             }
-            put(row0, ls, os);
-        } else if (u.np <= 4) {
+            put(row, ls, os);
+        }
+    } else if (np <= 4) {
+        for (int mine = 16 * part + 2 * half; mine < rows; mine += 16 * parts) {
             float M[2], l[2];
             f32x4 o[2];
-            const int32_t mine = row0 + 2 * part;
-            join_pieces<2, 4>(a, [&](int n) { return rec0 + i0 + 2 * part + n; }, stride, 0, 1, u.np, M, l, o);
-#pragma unroll
-            for (int n = 0; n < 2; ++n)
-                if (mine + n < rows) put(mine + n, l[n], o[n]);
-        } else {
+            join_pieces<2, 4>(a, [&](int n, int p) { return piece(p) + mine + n; }, 0, 1, np, M, l, o);
+            put(mine, l[0], o[0]);
+            if (mine + 1 < rows) put(mine + 1, l[1], o[1]);
+        }
+    } else {
+        for (int mine = 8 * part + half; mine < rows; mine += 8 * parts) {
             float M[1], l[1];
             f32x4 o[1];
-            join_pieces<1, 8>(a, [&](int) { return rec0 + i0 + part; }, stride, 0, 1, u.np, M, l, o);
-            if (row0 + part < rows) put(row0 + part, l[0], o[0]);
+            join_pieces<1, 8>(a, [&](int, int p) { return piece(p) + mine; }, 0, 1, np, M, l, o);
+            put(mine, l[0], o[0]);
         }
     }
 }
 
-// SLOTS workgroups, and the second launch unless the tables are too short for a cut
+// the second launch follows unless the tables are too short for a cut
 template <typename ET>
-hipError_t launch_paged(const AttnArgs& a, int64_t pieces, hipStream_t st) {
+hipError_t launch_paged(const AttnArgs& a, int groups, hipStream_t st) {
     const void* fn = (const void*)paged_attn_kernel<ET>;
     hipError_t e = ensure_lds_limit(fn, Form<ET>::LDS);
     if (e != hipSuccess) return e;
-    const unsigned grid = pieces < SLOTS ? ((unsigned)pieces + 7) & ~7u : SLOTS;
-    paged_attn_kernel<ET><<<grid, 64 * Form<ET>::WAVES, Form<ET>::LDS, st>>>(a);
+    paged_attn_kernel<ET><<<groups, 64 * Form<ET>::WAVES, Form<ET>::LDS, st>>>(a);
     if ((e = hipGetLastError()) != hipSuccess || !a.rec_rows) return e;
-    const int64_t rows = (int64_t)a.T * a.G * a.Hg;
-    paged_join_kernel<ET><<<(unsigned)(rows < 2048 ? rows : 2048), 256, 0, st>>>(a);
+    // about 2048 workgroups that have work: many for each of few tiles, of many tiles a few
+    const int64_t units = max_units(a.T, a.S, a.G, a.Hg), each = 2048 / (units ? units : 1);
+    const unsigned parts = place_rows(a.T, a.Hg) == ROWS_FEW ? (unsigned)(a.T * a.Hg) : each < 8 ? 8 : each < 32 ? (unsigned)each : 32;
+    paged_join_kernel<ET><<<dim3(parts, (unsigned)groups - 1), 256, 0, st>>>(a);
     return hipGetLastError();
 }
 
-hipError_t launch_paged_bf16(const AttnArgs& a, int64_t pieces, hipStream_t st);
-hipError_t launch_paged_f32(const AttnArgs& a, int64_t pieces, hipStream_t st);
+hipError_t launch_paged_bf16(const AttnArgs& a, int groups, hipStream_t st);
+hipError_t launch_paged_f32(const AttnArgs& a, int groups, hipStream_t st);
 
 }  // namespace vr

@@ -466,12 +466,12 @@ __device__ __forceinline__ void many_rows<uint16_t>(const Piece<uint16_t>& P, ui
     M.finish();
 }
 
-hipError_t launch_paged_bf16(const AttnArgs& a, int64_t pieces, hipStream_t st) { return launch_paged<uint16_t>(a, pieces, st); }
+hipError_t launch_paged_bf16(const AttnArgs& a, int groups, hipStream_t st) { return launch_paged<uint16_t>(a, groups, st); }
 
 // ---- host ------------------------------------------------------------------------------------
 size_t paged_attn_ws_bytes(int64_t T, int S, int G, int H, int dtype, int64_t cap) {
     const int64_t rows = max_records(T, S, G, H / G, cap, costs_of(dtype == VARRATE_BF16).lmin);
-    return rows ? (size_t)rows * (D + 2) * 4 + 16 : 0;
+    return rows ? (size_t)rows * (D + 2) * 4 + SHARES_BYTES : 0;
 }
 
 hipError_t launch_paged_attn(const varrate_pages& pg, const varrate_batch& b, const void* q, int64_t q_stride, int H,
@@ -500,8 +500,8 @@ hipError_t launch_paged_attn(const varrate_pages& pg, const varrate_batch& b, co
     a.costs = costs_of(pg.dtype == VARRATE_BF16);
     a.c = scale * 1.4426950408889634f;
     a.rec_rows = max_records(b.T, b.S, pg.G, a.Hg, a.cap, a.costs.lmin);
-    const int64_t pieces = max_pieces(b.T, b.S, pg.G, a.Hg, a.cap, a.costs.lmin);
-    return pg.dtype == VARRATE_BF16 ? launch_paged_bf16(a, pieces, st) : launch_paged_f32(a, pieces, st);
+    const int groups = max_groups(b.T, b.S, pg.G, a.Hg, a.cap, a.costs.lmin);
+    return pg.dtype == VARRATE_BF16 ? launch_paged_bf16(a, groups, st) : launch_paged_f32(a, groups, st);
 }
 
 }  // namespace vr

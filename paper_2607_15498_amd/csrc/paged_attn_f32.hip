@@ -274,6 +274,6 @@ __device__ __forceinline__ void many_rows<float>(const Piece<float>& P, uint8_t*
     M.finish();
 }
 
-hipError_t launch_paged_f32(const AttnArgs& a, int64_t pieces, hipStream_t st) { return launch_paged<float>(a, pieces, st); }
+hipError_t launch_paged_f32(const AttnArgs& a, int groups, hipStream_t st) { return launch_paged<float>(a, groups, st); }
 
 }  // namespace vr

@@ -3,6 +3,7 @@
 // page numbers) goes through here and is brought into range first: a bad entry costs its own
 // tokens, never an access outside the buffers.
 #pragma once
+#include <math.h>
 #include <stdint.h>
 
 #if defined(__HIPCC__)
@@ -49,13 +50,13 @@ VR_HD int32_t good_page(int32_t page, int32_t n_pages) { return page >= 0 && pag
 // ---- how the attention is cut ----------------------------------------------------------------
 // The rows of one (sequence, KV head) are its qlen x Hg (new token, query head) pairs, token-major.
 // Up to ROWS_FEW of them make one tile, whose keys a workgroup's waves divide among themselves; more
-// are cut into tiles of ROWS_MANY rows, which the waves divide.  The keys that a
-// tile sees are cut into pieces, the same number and length for all tiles of a sequence, of a cost of
-// about L at most: one number for the whole call, so that long sequences get more pieces.  (Tiles that
-// see fewer keys have empty pieces at the end.)
+// are cut into tiles of ROWS_MANY rows, which the waves divide.  A call is shared out in one of three ways:
+// whole tiles, one of each round of workgroups to each; every tile in the same number of pieces, one a workgroup; or all
+// work laid end to end (head after head, its sequences, their tiles, a tile's keys) and divided evenly, so that a
+// workgroup has the end of one tile, whole tiles and the beginning of another.  The second launch joins the tiles
+// that were cut.
 constexpr int ROWS_FEW = 32, ROWS_MANY = 256;
 constexpr int SLOTS = 256;                     // workgroups that the card holds at once (one per CU)
-constexpr int32_t WHOLE = INT32_MAX;           // L of a call that is not cut
 
 VR_HD int64_t seq_rows(SeqRange r, int Hg) { return (int64_t)r.qlen * Hg; }
 VR_HD int tile_rows(SeqRange r, int Hg) { return seq_rows(r, Hg) <= ROWS_FEW ? ROWS_FEW : ROWS_MANY; }
@@ -69,103 +70,145 @@ VR_HD int32_t seq_span(SeqRange r, int Hg, int window) {
     const int64_t n = window + 63 + (tile_rows(r, Hg) + Hg - 2) / Hg;     // the tile's last token is that far from its first
     return n < r.klen ? (int32_t)n : r.klen;
 }
-// the keys that its tiles see on average
-VR_HD int32_t seq_mean(SeqRange r, int32_t span, int causal) {
-    const int32_t first = r.klen - r.qlen > 0 ? r.klen - r.qlen : 0;       // keys before the new tokens
-    return causal && span == r.klen ? first + (r.klen - first) / 2 + 1 : span;
-}
-
-// Costs, in units of 16 cycles of a workgroup, as measured: per key of a tile of few rows while all
+// Costs, in units of 8 cycles of a workgroup, as measured: per key of a tile of few rows while all
 // workgroups read (the memory's share) and of one of many rows (the matrix cores'); of a piece's start
-// and end, and of the second launch, which besides reads what the first has written: JOIN_UNIT partial rows
-// (1040 bytes each, both ways) cost 1.  A lone workgroup's few rows cost a quarter.
-constexpr int JOIN_UNIT = 32;
-struct Costs { int32_t few, many, piece, join, lmin; };      // lmin: shortest piece, keys (a power of two)
+// and end, of few rows and of many; and of joining tiles in the second launch (what it takes beyond being there),
+// which besides reads what the first has written: JOIN_UNIT partial rows (1040 bytes each, both ways) cost 1.
+constexpr int JOIN_UNIT = 16;
+struct Costs { int32_t few, many, piece_few, piece_many, join, lmin; };      // lmin: shortest piece, keys
 VR_HD Costs costs_of(bool bf16) {
-    return bf16 ? Costs{4, 4, 400, 600, 256} : Costs{7, 36, 400, 600, 128};
+    return bf16 ? Costs{5, 8, 600, 4400, 400, 256} : Costs{12, 72, 600, 1800, 400, 128};
 }
-VR_HD int32_t key_cost(SeqRange r, int Hg, Costs c) { return tile_rows(r, Hg) == ROWS_FEW ? c.few : c.many; }
-// pieces of a span of keys at `cost` each (32-bit divisions: the plan's code is run once, and what it costs is
-// fetching it)
-VR_HD int32_t seq_pieces(int32_t span, int32_t cost, int32_t L, int32_t lmin) {
-    if (L == WHOLE || span <= lmin) return 1;
-    const uint64_t all = (uint64_t)(uint32_t)span * (uint32_t)cost;
-    const uint32_t n = ((uint32_t)(all < (1u << 30) ? all : 1u << 30) + (uint32_t)L - 1) / (uint32_t)L;
-    const uint32_t most = ((uint32_t)span + (uint32_t)lmin - 1) >> __builtin_ctz((uint32_t)lmin);
-    return (int32_t)(n < most ? n : most);
+VR_HD bool is_many(SeqRange r, int Hg) { return seq_rows(r, Hg) > ROWS_FEW; }
+VR_HD int32_t key_cost(SeqRange r, int Hg, Costs c) { return is_many(r, Hg) ? c.many : c.few; }
+
+// The cost of a sequence's tiles for one head: a + b (t + 1) for tile t.  (Tiles of causal chunks see 256 / Hg keys more
+// one after another; what is rounded in b shifts a little work, and nothing else hangs on it.)
+struct Line { int64_t a, b; int32_t tiles; };
+VR_HD Line seq_line(SeqRange r, int Hg, int causal, int window, Costs c) {
+    const int32_t tiles = seq_tiles(r, Hg), first = r.klen - r.qlen;       // keys before the new tokens
+    const bool many = is_many(r, Hg);
+    const int64_t piece = many ? c.piece_many : c.piece_few, cost = many ? c.many : c.few;
+    if (many && causal && !window && first >= 0) return Line{piece + cost * first, ROWS_MANY * cost / Hg, tiles};
+    return Line{piece + cost * seq_span(r, Hg, window), 0, tiles};
 }
-// keys of each of a span's np pieces
-VR_HD int32_t piece_len(int32_t span, int np) {
-    return np == 1 ? span : (int32_t)((((uint32_t)span + (uint32_t)np - 1) / (uint32_t)np + 63) & ~63u);
+// cost of the tiles before tile t
+VR_HD int64_t line_before(const Line& l, int64_t t) { return t * l.a + l.b * (t * (t + 1) / 2); }
+VR_HD int64_t line_at(const Line& l, int64_t t) { return l.a + l.b * (t + 1); }
+// the tile that `x` (of all tiles' cost) falls into: about, then exactly
+VR_HD int32_t line_tile(const Line& l, int64_t x) {
+    if (l.tiles <= 1) return 0;
+    float t;
+    if (l.b == 0) t = (float)x / (float)l.a;
+    else {
+        const float m = (float)l.a + 0.5f * (float)l.b;
+        t = (sqrtf(m * m + 2.f * (float)l.b * (float)x) - m) / (float)l.b;
+    }
+    int64_t i = t < (float)l.tiles ? (int64_t)t : l.tiles;
+    if (i > l.tiles - 1) i = l.tiles - 1;
+    while (i > 0 && line_before(l, i) > x) --i;
+    while (i < l.tiles - 1 && line_before(l, i + 1) <= x) ++i;
+    return (int32_t)i;
+}
+// A cut at x of a tile of cost w: where it leaves too little on either side (few rows: the shortest piece; many: 64 keys, and
+// what a piece's start and end cost), at the nearer end instead.
+VR_HD int64_t cut_at(int64_t x, int64_t w, bool many, Costs c) {
+    const int64_t keys = many ? 64 * (int64_t)c.many : (int64_t)c.lmin * c.few;
+    const int64_t least = many && keys < c.piece_many ? c.piece_many : keys;
+    return x >= least && w - x >= least ? x : 2 * x < w ? 0 : w;
+}
+// ... and how many of the tile's `all` keys lie before it
+VR_HD int32_t cut_key(int64_t x, int64_t w, int32_t all) {
+    if (x >= w) return all;
+    const float k = (float)all * ((float)x / (float)w) + 32.f;
+    return k < (float)all ? (int32_t)k & ~63 : all & ~63;
 }
 
-// How many pieces: the cut with the shortest estimated time.  Candidate 0 is uncut; the others aim at 3/4
-// of a piece for every slot (room for what rounding up adds), at 1, 2, 3 and 4.
-constexpr int CUTS = 6;
-constexpr int PIECES_MAX = 4 * SLOTS;          // of a cut call (an uncut one may have any number)
-// spans: sum of tiles x span x cost over sequences and heads
-VR_HD int32_t cut_try(int i, float spans) {
-    if (i == 0) return WHOLE;
-    const float slot = spans * (1.f / SLOTS);
-    const float x = i == 1 ? slot * 4.f / 3.f : slot / (float)(i - 1);
-    return x < 1e9f ? (int32_t)x + 1 : 1000000000;
-}
-// What the estimate needs of the sequences: first these sums (in floats: one instruction each, and only the
-// choice hangs on them) ...
-struct Sums { int64_t units = 0; float work = 0.f, spans = 0.f; int32_t longest = 0; bool many = false; };
+// What the choice needs of the sequences.  The floats bound sums that could overflow (of starts that fall).
+struct Sums {
+    uint64_t head = 0;                         // cost of one head's work
+    int64_t units = 0;                         // tiles x heads
+    float total = 0.f, many = 0.f, units_many = 0.f, longest = 0.f;
+};
 VR_HD void sum_up(Sums& t, SeqRange r, int G, int Hg, int causal, int window, Costs c) {
-    const int64_t n = (int64_t)seq_tiles(r, Hg) * G;
-    const int32_t span = seq_span(r, Hg, window);
-    const float cost = (float)n * (float)key_cost(r, Hg, c);
-    t.units += n;
-    t.work += cost * (float)seq_mean(r, span, causal);
-    t.spans += cost * (float)span;
-    if (n && span > t.longest) t.longest = span;
-    t.many = t.many || tile_rows(r, Hg) != ROWS_FEW;
+    const Line l = seq_line(r, Hg, causal, window, c);
+    const int64_t all = line_before(l, l.tiles);
+    t.head += (uint64_t)all;
+    t.units += (int64_t)l.tiles * G;
+    t.total += (float)all * (float)G;
+    if (is_many(r, Hg)) {
+        t.many += (float)all * (float)G;
+        t.units_many += (float)l.tiles * (float)G;
+    }
+    const float last = l.tiles ? (float)line_at(l, l.tiles - 1) : 0.f;
+    if (last > t.longest) t.longest = last;
 }
-// ... then for every candidate these (counts up to 2^24 are exact, and PIECES_MAX is the most that is taken).
-struct Cut { int32_t L; float pieces, partial, most; };   // partial: partial rows / JOIN_UNIT; most: cost of the longest piece
-VR_HD Cut cut_begin(int i, float spans) { return Cut{cut_try(i, spans), 0.f, 0.f, 0.f}; }
-VR_HD void cut_up(Cut& t, SeqRange r, int G, int Hg, int window, Costs c) {
-    const int32_t tiles = seq_tiles(r, Hg), span = seq_span(r, Hg, window), cost = key_cost(r, Hg, c);
-    const int32_t np = seq_pieces(span, cost, t.L, c.lmin);
-    const float all = (float)G * (float)np, len = tiles ? (float)piece_len(span, np) * (float)cost : 0.f;
-    t.pieces += all * (float)tiles;
-    if (np > 1) t.partial += all * (float)seq_rows(r, Hg) * (1.f / JOIN_UNIT);
-    if (len > t.most) t.most = len;
+// How n workgroups share the work out: into `among` shares (0: whole tiles), `same` to every tile (0: even ones).
+struct Split { int32_t among, same; };
+VR_HD Split split_of(const Sums& s, int n, Costs c) {
+    const Split tiles = {0, 0};
+    if (!(s.total > 0.f && s.total < 1e18f)) return tiles;
+    const float units = (float)s.units, all = (float)n, turns = units / all, mean = s.total / units;
+    const float piece = (float)(s.many > 0.f ? c.piece_many : c.piece_few), tile = (float)(ROWS_MANY / JOIN_UNIT);
+    // one round of `pieces` whose longest is `x`: few rows share the memory, down to about half of the cost for a lone one
+    // (1024 instead of 256 keys: 12.5 ns a key)
+    auto round_of = [&](float pieces, float x) {
+        const float load = s.many > 0.f ? 1.f : pieces < 0.55f * all ? 0.55f : pieces / all;
+        return (x - piece) * load + piece;
+    };
+    const float rounds = (float)((s.units + n - 1) / n);
+    float least_time = round_of(units, s.longest);
+    if (rounds > 1.f) {                        // tiles one to each, in turned order: what the last round lacks
+        least_time = s.total / all + (rounds - turns) * mean;
+        const float odd = s.total / all + 0.5f * (s.longest - mean);
+        if (((int64_t)rounds & 1) && least_time < odd) least_time = odd;
+    }
+    Split best = tiles;
+    // shares no shorter than a shortest piece on average
+    const float shortest = (float)((s.many > 0.f ? c.many : c.few) * c.lmin);
+    const float among = s.total < (shortest + piece) * all ? (float)(int32_t)(s.total / (shortest + piece)) : all;
+    if (among >= 2.f) {
+        const float cuts = among * (s.many / s.total);
+        const float x = round_of(among, s.total / among) + piece + (float)c.join +
+                        tile * (cuts + (s.units_many < cuts ? s.units_many : cuts));
+        if (x < least_time) {
+            least_time = x;
+            best.among = (int32_t)among;
+        }
+    }
+    // every tile in the same number of pieces
+    const float fit = (s.longest - piece) / shortest;
+    int32_t same = s.units < n ? n / (int32_t)s.units : 0;
+    if (fit < (float)same) same = (int32_t)fit;
+    if (same > 1) {
+        const float x = round_of(units * (float)same, (s.longest - piece) / (float)same + piece) + (float)c.join +
+                        tile * s.units_many * (float)same;
+        if (x < least_time) best = Split{(int32_t)s.units * same, same};
+    }
+    return best;
 }
-VR_HD float cut_cost(const Cut& t, const Sums& s, Costs c) {
-    const float units = (float)s.units;
-    if (t.pieces > units && t.pieces > (float)PIECES_MAX) return 1e30f;
-    const float rounds = (float)(((int32_t)t.pieces + SLOTS - 1) / SLOTS);
-    float cost = rounds * t.most;
-    if (!s.many && t.pieces < (float)SLOTS) cost = t.most * (t.pieces < SLOTS / 4 ? SLOTS / 4 : t.pieces) * (1.f / SLOTS);
-    // unlike pieces even out over several rounds (a sequence's longest come first)
-    const float even = s.work * (1.f / SLOTS) + t.most;
-    if (rounds > 1.f && cost > even) cost = even;
-    return cost + rounds * (float)c.piece + (t.pieces > units ? (float)c.join + t.partial : 0.f);
+// where share i begins (that all workgroups get the same number is what counts)
+VR_HD int64_t share_begin(int64_t total, int32_t i, Split p) {
+    return i >= p.among ? total : (int64_t)((float)total * ((float)i / (float)p.among));
 }
-struct Plan { int32_t L, pieces; };
-VR_HD Plan uncut(const Sums& s) { return Plan{WHOLE, s.units < INT32_MAX ? (int32_t)s.units : INT32_MAX}; }
-VR_HD bool may_cut(const Sums& s, Costs c) { return s.longest > c.lmin && s.units < PIECES_MAX; }
+// Workgroup b's share (`among`: none).  Workgroups b, b + 8, .. run on one die, whose L2 they share, and get shares side
+// by side, so that a head's keys are read into few dies' caches.
+VR_HD int32_t share_of(uint32_t b, int32_t among) {
+    const int32_t each = (among + 7) >> 3, i = (int32_t)(b >> 3);
+    const int32_t share = (int32_t)(b & 7u) * each + i;
+    return i < each && share < among ? share : among;
+}
 
-// Rows of many that a workgroup of the second launch joins: a half wave has 8 loads under way, of 4 rows' pieces or of 8
-// pieces' rows.
-VR_HD int join_rows(int np) { return np <= 4 ? 16 : 8; }
-
-// most (tile, head) pairs and pieces of any call with T rows and S sequences whose tables hold `cap` tokens
+// most (tile, head) pairs of any call with T rows and S sequences; workgroups that a call whose tables hold `cap` tokens can use
 VR_HD int64_t max_units(int64_t T, int S, int G, int Hg) { return G * (T * Hg / ROWS_MANY + (S < T ? S : T)); }
-VR_HD int64_t max_pieces(int64_t T, int S, int G, int Hg, int64_t cap, int lmin) {
-    const int64_t units = max_units(T, S, G, Hg);
-    const int64_t most = units * ((cap + lmin - 1) / lmin);
-    const int64_t cut = most < PIECES_MAX ? most : PIECES_MAX;
-    return units > cut ? units : cut;
+VR_HD int max_groups(int64_t T, int S, int G, int Hg, int64_t cap, int lmin) {
+    const int64_t n = max_units(T, S, G, Hg) * ((cap + lmin - 1) / lmin);
+    return n < SLOTS ? (int)((n + 7) & ~(int64_t)7) : SLOTS;
 }
-// most rows of partial results
+// Partial results: a workgroup has two places, for a tile that it begins with and for one that it ends with.
+VR_HD int place_rows(int64_t T, int Hg) { return T * Hg <= ROWS_FEW ? ROWS_FEW : ROWS_MANY; }
 VR_HD int64_t max_records(int64_t T, int S, int G, int Hg, int64_t cap, int lmin) {
-    if (cap <= lmin) return 0;
-    const int64_t p = max_pieces(T, S, G, Hg, cap, lmin);
-    return (p < PIECES_MAX ? p : PIECES_MAX) * (T * Hg <= ROWS_FEW ? ROWS_FEW : ROWS_MANY);
+    return cap <= 2 * lmin ? 0 : (int64_t)2 * max_groups(T, S, G, Hg, cap, lmin) * place_rows(T, Hg);
 }
 
 // Keys [lo, hi) that the sequence's new token i sees (none when hi <= lo).
@@ -175,22 +218,25 @@ VR_HD void row_keys(SeqRange r, int32_t i, int causal, int window, int32_t& lo, 
     if (hi < 0) hi = 0;
     lo = window && pos - window + 1 > 0 ? pos - window + 1 : 0;
 }
-// Keys [lo, hi) of piece number `piece` of the np of the tile of rows row0 .. row0 + rows - 1 (none when hi <= lo): pieces start
-// at multiples of 64, the first at the one before the tile's first key.
-VR_HD void piece_keys(SeqRange r, int32_t row0, int32_t rows, int32_t piece, int32_t np, int Hg, int causal, int window,
-                      int32_t& lo, int32_t& hi) {
+// Keys [lo, hi) of a tile's rows row0 .. row0 + rows - 1 ...
+VR_HD void tile_keys(SeqRange r, int32_t row0, int32_t rows, int Hg, int causal, int window, int32_t& lo, int32_t& hi) {
     int32_t x;
     row_keys(r, row0 / Hg, causal, window, lo, x);
     row_keys(r, (row0 + rows - 1) / Hg, causal, window, x, hi);
-    if (np == 1) return;
-    const int32_t len = piece_len(seq_span(r, Hg, window), np);
-    const int64_t p0 = (lo & ~63) + (int64_t)piece * len;
-    if (lo < p0) lo = (int32_t)(p0 < r.klen ? p0 : r.klen);
-    if (hi > p0 + len) hi = (int32_t)(p0 + len);
+    if (hi < lo) hi = lo;
 }
-// The piece that workgroup b of n (a multiple of 8) takes in a round: b, then in turned order (the pieces of a sequence
-// shrink along its numbers; turning gives every workgroup long and short ones), b % 8 kept: heads stay on their XCD's L2.
-VR_HD int64_t piece_number(uint32_t b, uint32_t n, int round) {
+// ... and of them those of the piece [x0, x1) of its cost w: cuts lie at multiples of 64 keys
+VR_HD void piece_keys(int64_t x0, int64_t x1, int64_t w, int32_t& lo, int32_t& hi) {
+    const int32_t from = lo & ~63, all = hi - from;
+    const int32_t k0 = from + cut_key(x0, w, all), k1 = from + cut_key(x1, w, all);
+    if (k0 > lo) lo = k0;
+    if (k1 < hi) hi = k1;
+    if (hi < lo) hi = lo;
+}
+// Whole tiles: the number of the (tile, head) pair that workgroup b of n (a multiple of 8) takes in a round: b, then in
+// turned order (a sequence's tiles shrink along its numbers; turning gives every workgroup long and short
+// ones), b % 8 kept: heads stay on their die's L2.
+VR_HD int64_t tile_number(uint32_t b, uint32_t n, int round) {
     return (int64_t)round * n + (round & 1 ? ((n - 1 - b) & ~7u) | (b & 7u) : b);
 }
 

@@ -126,7 +126,7 @@ def test_batches_refused(L, kw, code):
     (dict(ws=A + 4), EINVAL),
 ])
 def test_attn_refused(L, kw, code):
-    assert attn(L, None, batch(width=8), **kw) == code and L.varrate_last_error()     # 512 keys: may be cut
+    assert attn(L, None, batch(width=16), **kw) == code and L.varrate_last_error()    # 1024 keys: may be cut
 
 
 @pytest.mark.parametrize("kw,code", [
@@ -172,9 +172,9 @@ def test_nothing_to_do(L):
 def test_workspace_follows_the_table(L):
     """A table too short for a cut needs none; what a call may need grows with rows and table up to a bound."""
     need = lambda T, S, width, H=4, **kw: L.varrate_paged_attn_workspace_bytes(pages(**kw), batch(T=T, S=S, width=width), H)
-    assert need(1, 1, 4) == 0 and need(1, 1, 2, dtype=0) == 0
-    assert 0 < need(1, 1, 5) < need(1, 1, 64) < need(4, 4, 64) <= need(4, 4, 1 << 20)
-    assert need(1 << 20, 1, 1 << 20) == need(1 << 22, 1, 1 << 20) == 1024 * 256 * 130 * 4 + 16
+    assert need(1, 1, 8) == 0 and need(1, 1, 4, dtype=0) == 0
+    assert 0 < need(1, 1, 9) <= need(1, 1, 64) < need(4, 4, 64) <= need(4, 4, 1 << 20)
+    assert need(1 << 20, 1, 1 << 20) == need(1 << 22, 1, 1 << 20) == 2 * 256 * 256 * 130 * 4 + 16 + 256 * 40
 
 
 def test_binding_refuses_before_the_library(L):
@@ -214,46 +214,145 @@ using namespace vr;
 static std::mt19937 gen(7);
 static int32_t pick_of(int32_t lo, int32_t hi) { return lo + (int32_t)(gen() % (uint32_t)(hi - lo + 1)); }
 
-static void one_cut(const std::vector<SeqRange>& r, int32_t L, int G, int Hg, int causal, int window, Costs c, bool rising,
-                    int64_t T, int64_t cap, bool taken) {
-    int64_t pieces = 0, units = 0, recs = 0;
-    for (SeqRange s : r) {
-        const int64_t rows = seq_rows(s, Hg);
-        const int bm = tile_rows(s, Hg), tiles = seq_tiles(s, Hg);
-        CHECK((int64_t)tiles * bm >= rows && (int64_t)(tiles - 1) * bm < rows + (rows == 0));
-        const int32_t span = seq_span(s, Hg, window), np = seq_pieces(span, key_cost(s, Hg, c), L, c.lmin);
-        CHECK(np >= 1);
-        pieces += (int64_t)tiles * np * G;
-        units += (int64_t)tiles * G;
-        if (np > 1) recs += (int64_t)tiles * np * G * bm;
-        for (int tile = 0; tile < tiles; ++tile) {
-            const int32_t row0 = tile * bm, n = (int32_t)std::min<int64_t>(bm, rows - row0);
-            int32_t first = 0, last = 0, at = -1;
-            for (int i = 0; i < n; ++i) {
-                int32_t lo, hi;
-                row_keys(s, (row0 + i) / Hg, causal, window, lo, hi);
-                CHECK(lo >= 0 && hi >= 0 && hi <= s.klen);
-                if (i == 0) first = lo;
-                CHECK(lo >= first && hi >= last);           // both grow along the rows
-                last = hi;
+struct Tile { int s = -1, g = 0, tile = 0; int64_t start = 0, w = 0; };
+struct Share { int64_t pos; Tile t; bool inside; };
+struct Piece { int s, g, tile; int32_t lo, hi; bool cut; int place; };
+
+struct Call {
+    std::vector<SeqRange> r;
+    int G, Hg, causal, window;
+    Costs c;
+    Split split;
+    int64_t head = 0;
+    Line line(int s) const { return seq_line(r[s], Hg, causal, window, c); }
+    Tile tile_of(int64_t pos) const {
+        Tile t;
+        t.g = (int)(pos / head);
+        int64_t x = pos % head, base = t.g * head;
+        for (int s = 0; s < (int)r.size(); ++s) {
+            const Line l = line(s);
+            const int64_t all = line_before(l, l.tiles);
+            if (x < all) {
+                t.s = s;
+                t.tile = line_tile(l, x);
+                CHECK(t.tile >= 0 && t.tile < l.tiles && line_before(l, t.tile) <= x && x < line_before(l, t.tile + 1));
+                t.start = base + line_before(l, t.tile);
+                t.w = line_at(l, t.tile);
+                CHECK(t.w > 0 && t.start + t.w == base + line_before(l, t.tile + 1));
+                return t;
             }
-            for (int p = 0; p < np; ++p) {
-                int32_t lo, hi;
-                piece_keys(s, row0, n, p, np, Hg, causal, window, lo, hi);
-                if (hi <= lo) continue;
-                CHECK(lo >= 0 && hi <= s.klen);
-                if (at < 0) CHECK(lo == first);
-                else CHECK(lo == at && lo % 64 == 0);       // pieces follow each other
-                at = hi;
-            }
-            CHECK(at == last || (at < 0 && last <= first));
+            x -= all;
+            base += all;
+        }
+        CHECK(!"found");
+        return t;
+    }
+    int64_t share_at(int i, Tile& t) const {
+        const int64_t total = head * G, pos = share_begin(total, i, split);
+        CHECK(pos >= 0 && pos <= total);
+        if (pos >= total) return total;
+        t = tile_of(pos);
+        return t.start + cut_at(pos - t.start, t.w, is_many(r[t.s], Hg), c);
+    }
+};
+
+// every tile's keys are some share's exactly once, and the second launch finds the pieces of those that were cut
+static void shares_of(Call k, Split split) {
+    const int among = split.among;
+    k.split = split;
+    k.head = 0;
+    for (int s = 0; s < (int)k.r.size(); ++s) k.head += line_before(k.line(s), k.line(s).tiles);
+    std::vector<Share> shares(among);
+    std::vector<Piece> all;
+    for (int i = 0; split.same && i < among; ++i) {        // every tile in equal pieces
+        int u = i / split.same, x = i % split.same, each = among / split.same / k.G, in = u % each;
+        Tile t;
+        t.g = u / each;
+        for (t.s = 0; in >= seq_tiles(k.r[t.s], k.Hg); ++t.s) in -= seq_tiles(k.r[t.s], k.Hg);
+        const SeqRange r = k.r[t.s];
+        t.tile = seq_tiles(r, k.Hg) - 1 - in;
+        t.start = (int64_t)u * split.same;
+        const int bm = tile_rows(r, k.Hg);
+        const int32_t row0 = t.tile * bm, rows = (int32_t)std::min<int64_t>(bm, seq_rows(r, k.Hg) - row0);
+        int32_t lo, hi;
+        tile_keys(r, row0, rows, k.Hg, k.causal, k.window, lo, hi);
+        piece_keys(x, x + 1, split.same, lo, hi);
+        shares[i] = Share{i, t, x != 0};
+        all.push_back(Piece{t.s, t.g, t.tile, lo, hi, true, 2 * i});
+    }
+    auto order = [](const Piece& a, const Piece& b) {
+        return a.g != b.g ? a.g < b.g : a.s != b.s ? a.s < b.s : a.tile < b.tile;
+    };
+    std::stable_sort(all.begin(), all.end(), order);
+    for (int i = 0; !split.same && i < among; ++i) {
+        Tile t, last;
+        const int64_t end = k.share_at(i + 1, last);
+        int64_t pos = k.share_at(i, t);
+        CHECK(i == 0 ? pos == 0 : pos <= end);
+        shares[i] = Share{pos, t, pos > t.start && pos < t.start + t.w};
+        for (int place = 2 * i; pos < end; place |= 1) {
+            if (pos >= t.start + t.w) t = k.tile_of(pos);
+            const int64_t x0 = pos - t.start, x1 = std::min(end - t.start, t.w);
+            const SeqRange r = k.r[t.s];
+            const int bm = tile_rows(r, k.Hg);
+            const int32_t row0 = t.tile * bm, rows = (int32_t)std::min<int64_t>(bm, seq_rows(r, k.Hg) - row0);
+            int32_t lo, hi;
+            CHECK(rows > 0);
+            tile_keys(r, row0, rows, k.Hg, k.causal, k.window, lo, hi);
+            const bool cut = x1 - x0 != t.w;
+            if (cut) piece_keys(x0, x1, t.w, lo, hi);
+            CHECK(lo >= 0 && lo <= hi && hi <= (r.klen > lo ? r.klen : lo));
+            all.push_back(Piece{t.s, t.g, t.tile, lo, hi, cut, place});
+            pos = t.start + x1;
         }
     }
-    if (taken && rising) {
-        CHECK(units <= max_units(T, (int)r.size(), G, Hg));
-        CHECK(pieces <= max_pieces(T, (int)r.size(), G, Hg, cap, c.lmin));
-        CHECK(recs <= max_records(T, (int)r.size(), G, Hg, cap, c.lmin));
+    // in the order of the shares a tile's pieces follow each other
+    size_t at = 0, cuts = 0, joined = 0;
+    for (int g = 0; g < k.G; ++g)
+        for (int s = 0; s < (int)k.r.size(); ++s)
+            for (int tile = 0; tile < seq_tiles(k.r[s], k.Hg); ++tile) {
+                const SeqRange r = k.r[s];
+                const int bm = tile_rows(r, k.Hg);
+                const int32_t row0 = tile * bm, rows = (int32_t)std::min<int64_t>(bm, seq_rows(r, k.Hg) - row0);
+                int32_t lo, hi, from = 0;
+                tile_keys(r, row0, rows, k.Hg, k.causal, k.window, lo, hi);
+                for (int i = 0; i < rows; i += rows > 40 ? 13 : 1) {       // no row sees keys outside
+                    int32_t a, b;
+                    row_keys(r, (row0 + i) / k.Hg, k.causal, k.window, a, b);
+                    CHECK(b <= a || (a >= lo && b <= hi));
+                }
+                bool some = false;
+                size_t n = 0;
+                for (; at < all.size() && all[at].s == s && all[at].g == g && all[at].tile == tile; ++at, ++n) {
+                    if (all[at].hi > all[at].lo) {
+                        CHECK(all[at].lo == (some ? from : lo) && (!some || from % 64 == 0));
+                        from = all[at].hi;
+                        some = true;
+                    }
+                    CHECK(n == 0 || all[at].cut);
+                }
+                CHECK(n >= 1 && (hi <= lo || (some && from == hi)));
+                CHECK((n > 1) == all[at - 1].cut);
+                cuts += n > 1;
+            }
+    CHECK(at == all.size());
+    for (int i = 1; i < among; ++i) {
+        if (!shares[i].inside || (shares[i - 1].inside && shares[i - 1].t.start == shares[i].t.start)) continue;
+        const Tile t = shares[i].t;
+        int np = 2;
+        while (i + np - 1 < among && shares[i + np - 1].inside && shares[i + np - 1].t.start == t.start) ++np;
+        std::vector<int> places = {2 * (i - 1) + (shares[i - 1].pos == t.start ? 0 : 1)}, want;
+        for (int p = 1; p < np; ++p) places.push_back(2 * (i + p - 1));
+        for (const Piece& p : all)
+            if (p.s == t.s && p.g == t.g && p.tile == t.tile) want.push_back(p.place);
+        CHECK(places == want);
+        ++joined;
     }
+    CHECK(joined == cuts);
+    std::vector<int> used;
+    for (const Piece& p : all) if (p.cut) used.push_back(p.place);
+    std::sort(used.begin(), used.end());
+    CHECK(std::adjacent_find(used.begin(), used.end()) == used.end() && (used.empty() || used.back() < 2 * among));
 }
 
 int main() {
@@ -283,47 +382,54 @@ int main() {
             else CHECK(q < S && start[q] <= t && t < start[q + 1]);
             if (q >= 0) CHECK(t >= r[q].q0 && t < r[q].q0 + r[q].qlen);
         }
-        float best = 0.f;
-        Cut kept = {};
-        for (int i = 0; i < CUTS; ++i) {
-            Cut t = cut_begin(i, s.spans);
-            CHECK(t.L >= 1);
-            for (SeqRange x : r) cut_up(t, x, G, Hg, window, c);
-            const float cost = cut_cost(t, s, c);
-            CHECK(cost >= 0.f && cost <= 1e30f);
-            if (i == 0 || cost < best) {
-                best = cost;
-                kept = t;
-            }
-            const bool taken = i == 0 || cost < 1e30f;
-            int64_t pieces = 0;
-            for (SeqRange x : r)
-                pieces += (int64_t)seq_tiles(x, Hg) * G * seq_pieces(seq_span(x, Hg, window), key_cost(x, Hg, c), t.L, c.lmin);
-            CHECK((float)pieces == t.pieces);
-            one_cut(r, t.L, G, Hg, causal, window, c, rising, T, cap, taken && may_cut(s, c));
+        Call k{r, G, Hg, causal, window, c, Split{0, 0}, 0};
+        const int n = max_groups(T, S, G, Hg, cap, c.lmin);
+        const Split split = n ? split_of(s, n, c) : Split{0, 0};
+        CHECK(n % 8 == 0 && n >= 0 && n <= SLOTS && split.among >= 0 && split.among <= n && split.among != 1);
+        CHECK(split.same == 0 || (split.same > 1 && split.among == s.units * split.same));
+        const int64_t records = max_records(T, S, G, Hg, cap, c.lmin);
+        CHECK(records == 0 || (records == 2 * n * place_rows(T, Hg) && records <= 2 * SLOTS * ROWS_MANY));
+        for (const SeqRange& x : r) CHECK(T * Hg > ROWS_FEW || seq_rows(x, Hg) <= ROWS_FEW || !rising);
+        if (s.head > 0 && s.units < 20000) {
+            if (split.among) shares_of(k, split);
+            shares_of(k, Split{pick_of(2, 256), 0});
+            shares_of(k, Split{2, 0});
+            if (s.units <= 128) shares_of(k, Split{(int32_t)s.units * 2, 2});
+            if (s.units <= 36) shares_of(k, Split{(int32_t)s.units * 7, 7});
         }
-        one_cut(r, pick_of(1, 5000), G, Hg, causal, window, c, rising, T, cap, false);
         if (rising) CHECK(s.units <= max_units(T, S, G, Hg));
     }
     // the longest: nothing overflows
     for (int bf = 0; bf < 2; ++bf) {
         const Costs c = costs_of(bf);
         const SeqRange r = seq_range(0, 1 << 20, 1 << 30, 1 << 20, 1 << 30);
-        for (int32_t L : {1, 4096, 999999999, WHOLE}) {
-            const int32_t np = seq_pieces(seq_span(r, 1024, 0), key_cost(r, 1024, c), L, c.lmin);
-            CHECK(np >= 1 && (int64_t)np * piece_len(1 << 30, np) >= 1 << 30);
-            int32_t lo, hi;
-            piece_keys(r, (1 << 30) - 256, 256, np - 1, np, 1024, 1, 0, lo, hi);
-            CHECK(lo <= hi && hi <= 1 << 30);
+        const Line l = seq_line(r, 1024, 1, 0, c);
+        const int64_t all = line_before(l, l.tiles);
+        CHECK(all > 0 && all < (int64_t)1 << 60 && line_tile(l, all - 1) == l.tiles - 1 && line_tile(l, 0) == 0);
+        for (int i = 1; i < 1000; ++i) {
+            const int64_t x = all / 1000 * i;
+            const int32_t t = line_tile(l, x);
+            CHECK(line_before(l, t) <= x && x < line_before(l, t + 1));
         }
+        int32_t lo = 0, hi = 1 << 30;
+        piece_keys(line_at(l, 5) / 3, line_at(l, 5), line_at(l, 5), lo, hi);
+        CHECK(lo % 64 == 0 && lo > (1 << 30) / 4 && hi == 1 << 30);
+        Sums s;
+        for (int i = 0; i < 65536; ++i) sum_up(s, SeqRange{0, 1 << 20, 1 << 30}, 1, 1024, 1, 0, c);
+        CHECK(split_of(s, 256, c).among == 0);                // starts that fall: sums that could overflow are not divided
     }
-    // every piece of a call is one workgroup's, forwards and backwards
+    for (int among : {2, 7, 8, 9, 100, 255, 256}) {
+        std::vector<int> hit(among + 1, 0);
+        for (uint32_t b = 0; b < 256; ++b) ++hit[share_of(b, among)];
+        for (int i = 0; i < among; ++i) CHECK(hit[i] == 1);
+    }
+    // every whole tile of a call is one workgroup's, forwards and backwards
     for (uint32_t n : {8u, 16u, 248u, 256u})
         for (int rounds : {1, 2, 5}) {
             std::vector<int> hit(n * rounds, 0);
             for (uint32_t b = 0; b < n; ++b)
                 for (int k = 0; k < rounds; ++k) {
-                    const int64_t i = piece_number(b, n, b & 8 ? rounds - 1 - k : k);
+                    const int64_t i = tile_number(b, n, b & 8 ? rounds - 1 - k : k);
                     CHECK(i >= 0 && i < (int64_t)hit.size() && i % 8 == b % 8);
                     ++hit[i];
                 }
