@@ -26,7 +26,7 @@ struct AttnArgs {
     int32_t T, S, cap, n_pages, G, Hg, shift;
     int32_t causal, window;
     Costs costs;
-    float c;                        // softmax scale x log2 e
+    float c, c_lo;                  // softmax scale x log2 e, and what c lacks of it (fp32 layers)
 };
 
 // rows of a bad page: 1 KB of zeros
@@ -441,12 +441,15 @@ __device__ __forceinline__ void weights(f32x16& sc, float c, float off, u32x4 (&
     }
     l += l0 + l1;
 }
-__device__ __forceinline__ void weights(f32x16& sc, float c, float off, float& l) {
+__device__ __forceinline__ float weight32(float x, float c, float c_lo, float off) {
+    return __builtin_amdgcn_exp2f(fmaf(x, c_lo, fmaf(x, c, off)));
+}
+__device__ __forceinline__ void weights(f32x16& sc, float c, float c_lo, float off, float& l) {
     float l0 = 0.f, l1 = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; i += 2) {
-        sc[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], c, off));
-        sc[i + 1] = __builtin_amdgcn_exp2f(fmaf(sc[i + 1], c, off));
+        sc[i] = weight32(sc[i], c, c_lo, off);
+        sc[i + 1] = weight32(sc[i + 1], c, c_lo, off);
         l0 += sc[i];
         l1 += sc[i + 1];
     }
@@ -458,14 +461,25 @@ __device__ __forceinline__ void weights(f32x16& sc, float c, float off, float& l
 // then reach 2^SLACK, which neither bf16's exponent nor the fp32 sums mind, and the sums are rescaled
 // a few times per piece instead of at every block.
 constexpr float SLACK = 8.f;
+// -c m, 0 while nothing has been seen.  Rounded as it is used everywhere (no part of a fused operation): weights
+// exp2(c x + off) of different maxima then differ by exp2 of the difference of their offs, whose own roundings cancel.
+__device__ __forceinline__ float off_of(float m, float c) {
+    float off = m == -INFINITY ? 0.f : -m * c;
+    asm("" : "+v"(off));
+    return off;
+}
+// the factor that takes sums of weights against m to those whose off is `to`
+__device__ __forceinline__ float rescale(float m, float to, float c) {
+    return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(to - off_of(m, c));
+}
 struct Running {
     float m = -INFINITY, off = 0.f, l = 0.f;
     // the factor for what has been summed so far
     __device__ __forceinline__ float raise(float mt, float c) {
-        const float mn = fmaxf(m, mt), mu = mn == -INFINITY ? 0.f : mn;   // nothing seen yet: every weight is 0
-        const float f = __builtin_amdgcn_exp2f((m - mu) * c);
+        const float mn = fmaxf(m, mt), to = off_of(mn, c);
+        const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(to - off);
         m = mn;
-        off = -mu * c;
+        off = to;
         l *= f;
         return f;
     }
@@ -758,14 +772,14 @@ __device__ __forceinline__ void join_pieces(const AttnArgs& a, A&& at, int p0, i
             float mn = M[n];
 #pragma unroll
             for (int k = 0; k < NP; ++k) mn = fmaxf(mn, ml[n][k].x);
-            const float mu = mn == -INFINITY ? 0.f : mn, f0 = __builtin_amdgcn_exp2f((M[n] - mu) * a.c);
+            const float to = off_of(mn, a.c), f0 = rescale(M[n], to, a.c);
             M[n] = mn;
             l[n] *= f0;
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[n][e] *= f0;
 #pragma unroll
             for (int k = 0; k < NP; ++k) {
-                const float f = __builtin_amdgcn_exp2f((ml[n][k].x - mu) * a.c);
+                const float f = rescale(ml[n][k].x, to, a.c);
                 l[n] = fmaf(f, ml[n][k].y, l[n]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[n][e] = fmaf(f, v[n][k][e], o[n][e]);
@@ -838,10 +852,10 @@ __global__ __launch_bounds__(256) void paged_join_kernel(AttnArgs a) {
             f32x4 os = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int k = 1; k < 8; ++k) mx = fmaxf(mx, sl[k][0]);
-            const float mu = mx == -INFINITY ? 0.f : mx;
+            const float to = off_of(mx, a.c);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const float f = __builtin_amdgcn_exp2f((sl[k][0] - mu) * a.c);
+                const float f = rescale(sl[k][0], to, a.c);
                 const f32x4 v = *reinterpret_cast<const f32x4*>(&so[k][4 * l32]);
                 ls = fmaf(f, sl[k][1], ls);
 #pragma unroll

@@ -202,12 +202,12 @@ __device__ __forceinline__ void few_rows<uint16_t>(const Piece<uint16_t>& P, uin
             lw[w] = v.y;
             M = fmaxf(M, v.x);
         }
-        const float mu = M == -INFINITY ? 0.f : M;
+        const float to = off_of(M, a.c);
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[i] = 0.f;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-            const float f = __builtin_amdgcn_exp2f((mw[w] - mu) * a.c);
+            const float f = rescale(mw[w], to, a.c);
             Ls = fmaf(f, lw[w], Ls);
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
@@ -498,7 +498,10 @@ hipError_t launch_paged_attn(const varrate_pages& pg, const varrate_batch& b, co
     a.causal = causal;
     a.window = window;
     a.costs = costs_of(pg.dtype == VARRATE_BF16);
-    a.c = scale * 1.4426950408889634f;
+    const double c = (double)scale * 1.4426950408889634;
+    a.c = (float)c;
+    if ((double)a.c >= c) a.c = nextafterf(a.c, 0.f);
+    a.c_lo = (float)(c - (double)a.c);                     // > 0, so that a masked score stays -infinity
     a.rec_rows = max_records(b.T, b.S, pg.G, a.Hg, a.cap, a.costs.lmin);
     const int groups = max_groups(b.T, b.S, pg.G, a.Hg, a.cap, a.costs.lmin);
     return pg.dtype == VARRATE_BF16 ? launch_paged_bf16(a, groups, st) : launch_paged_f32(a, groups, st);
