@@ -7,19 +7,22 @@
 // lane, and S^T is already the B operand of O^T = V^T P^T (the keys' order in a product is free, and
 // V^T's fragments are read in the order in which S^T holds them).
 //
-// Two forms, chosen per sequence by its rows.  Few rows (single tokens): the 4 waves of a workgroup
-// share one tile of 32 rows and take every fourth 32-key tile each, with rings of their own and no
-// barrier, joined at the end; the reads of K and V bound it.  Many rows (prompts and chunks): tiles of
-// 256 rows, 64 a wave (two blocks of 32, so that a fragment read from LDS feeds two products), and all
-// waves share the key stages; the matrix cores bound it.  One launch serves both, so a chunk and the
-// single tokens beside it run together.  Where there are too few (sequence, head, row tile) units for
-// the card, or they are too unlike, the keys are cut into pieces (vr_pages.h) and a second launch joins
-// the pieces' partial rows.
+// Two forms, chosen per sequence by its rows.  Few rows (single tokens): the waves of a workgroup
+// share one tile of 32 rows and divide its keys, with rings of their own and no barrier, joined at the
+// end; the reads of K and V bound it (one token over 32768 of 8 KV heads: 29 us, 4.6 TB/s).  Many rows
+// (prompts and chunks): tiles of 256 rows, 64 a wave (two blocks of 32, so that a fragment read from
+// LDS feeds two products), and all waves share the key stages; the matrix cores bound it (2048 tokens
+// over 32768: 1090 TFLOP/s).  Few are what one product's 32 columns hold: over 32768, 8 tokens of 4
+// rows take 40 us (one token 35), 9 as many rows 70, and so do 16: a tile of 256 costs its products however many
+// of its rows there are.  In fp32 74 and 180 us.
+// One launch serves both, so a chunk and the single tokens beside it run together.  Where there are too
+// few (sequence, head, row tile) units for the card, or they are too unlike, their keys are cut (vr_pages.h)
+// and a second launch joins the partial rows.
 //
 // Keys and values come by direct-to-LDS loads of 1 KB (whole rows).  Row r's 16-byte piece c lies at
 // place c ^ f(r), f(r) = 4 (r % 4) + (r / 4) % 4, which spreads the K fragment reads (32 rows, one
-// piece) and the transposing V reads (8 rows, 4 pieces) over all banks; fp32 values, read 128 bytes of
-// two rows at a time, at place c ^ 8 ((r / 4) % 2).
+// piece) and the transposing V reads (8 rows, 4 pieces) over all banks (no conflict is counted); fp32 values, read a row
+// at a time, lie as they come.
 #include <type_traits>
 #include <utility>
 
