@@ -406,7 +406,8 @@ VARRATE_API int varrate_joint_append_exact(const varrate_shape* shape, varrate_j
  *
  * d = 128.  Rows of new tokens are [T][heads][d] with a stride between tokens (elements, a
  * multiple of 16 bytes; heads contiguous), so slices of a fused projection need no copy.
- * These calls need no zero-filled memory; their workspace holds nothing between calls. */
+ * These calls need no zero-filled memory; their workspace holds nothing between calls, and calls
+ * that may overlap (streams, graphs) need workspaces of their own. */
 typedef struct varrate_pages {
     void*   k;         /* [n_pages][G][page][d] dtype                                        */
     void*   v;         /* [n_pages][G][page][d] dtype                                        */
@@ -453,8 +454,8 @@ VARRATE_API int varrate_paged_append(const varrate_pages* pages, const varrate_b
  * causal 0 (window 0): every new token sees all kv_len[s] keys.  A token that sees no key gets
  * zeros, and so does one whose visible scores are all -infinity.  Keys and values that a token
  * does not see (later ones, slots behind the end, unused pages) do not reach its output,
- * whatever they hold.  scale lies in [2^-100, 2^100].  out must not overlap q.
- * T H <= 2^30.                                                                               */
+ * whatever they hold.  Scores are fp32: scale <q, k> beyond its range gives NaN.  scale lies in
+ * [2^-100, 2^100].  out must not overlap q.  T H <= 2^30.                                    */
 VARRATE_API size_t varrate_paged_attn_workspace_bytes(const varrate_pages* pages, const varrate_batch* batch, int32_t H);
 VARRATE_API int varrate_paged_attn(const varrate_pages* pages, const varrate_batch* batch, const void* q,
                                    int64_t q_stride, int32_t H, int32_t causal, int32_t window, float scale, void* out,

@@ -519,14 +519,19 @@ def _einval(msg: str):
 
 
 class PagedCache:
-    """A pool of pages: k, v [n_pages][G][page][d] (bf16 or fp32), contiguous device tensors."""
+    """A pool of pages: k, v [n_pages][G][page][d] (bf16 or fp32), contiguous device tensors.  k and v are
+    not to be replaced (calls use their addresses); their contents are the user's."""
+
+    __slots__ = ("_k", "_v", "page", "G", "_c")
+    k = property(lambda self: self._k)
+    v = property(lambda self: self._v)
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor):
         if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.device != v.device:
             _einval("k and v must be alike, [n_pages][G][page][d]")
         if k.dtype not in _DTYPES:
             _einval(f"pages have dtype {k.dtype}, expected torch.bfloat16 or torch.float32")
-        self.k, self.v = k, v
+        self._k, self._v = k, v
         self.page, self.G = int(k.shape[2]), int(k.shape[1])
         self._c = _lib.PagesC(_dev_ptr(k, name="k"), _dev_ptr(v, name="v"), k.shape[0], self.G, k.shape[3], self.page,
                               _DTYPES[k.dtype])
@@ -552,7 +557,13 @@ def _i32(t: torch.Tensor, dim: int, name: str) -> int:
 class PagedBatch:
     """The sequences of one call: table [S][width] page numbers, kv_len [S] tokens of each with the
     new ones, q_start [S + 1] first packed row of each (device int32).  The arrays are read when a
-    call runs, so their contents may change between calls and graph replays."""
+    call runs, so their contents may change between calls and graph replays; the tensors themselves are
+    not to be replaced (calls use their addresses)."""
+
+    __slots__ = ("_table", "_kv_len", "_q_start", "_c")
+    table = property(lambda self: self._table)
+    kv_len = property(lambda self: self._kv_len)
+    q_start = property(lambda self: self._q_start)
 
     def __init__(self, table: torch.Tensor, kv_len: torch.Tensor, q_start: torch.Tensor):
         pt, pl, ps = _i32(table, 2, "table"), _i32(kv_len, 1, "kv_len"), _i32(q_start, 1, "q_start")
@@ -561,7 +572,7 @@ class PagedBatch:
             _einval(f"kv_len and q_start must have {S} and {S + 1} entries")
         if kv_len.device != table.device or q_start.device != table.device:
             _einval("table, kv_len and q_start must be on one device")
-        self.table, self.kv_len, self.q_start = table, kv_len, q_start
+        self._table, self._kv_len, self._q_start = table, kv_len, q_start
         self._c = (pt, pl, ps, table.stride(0) if S > 1 else width, S, width)
 
     def c(self, T: int) -> _lib.BatchC:

@@ -747,3 +747,18 @@ def test_binding_refuses(vr):
             say(f"call {i} was not refused")
     torch.cuda.synchronize()
     assert (pages.k == 0).all() and (pages.v == 0).all() and (q == 1).all() and (k == 1).all()
+
+
+def test_tensors_of_a_handle_stay(vr):
+    """A handle keeps the tensors whose addresses its calls use: they cannot be replaced, and live as long as it does."""
+    import torch
+    pages = vr.new_pages(3, 1, 16)
+    batch = vr.PagedBatch(torch.zeros((1, 1), dtype=torch.int32, device="cuda"), torch.ones(1, dtype=torch.int32, device="cuda"),
+                          torch.tensor([0, 1], dtype=torch.int32).cuda())
+    for handle, names in ((pages, ("k", "v")), (batch, ("table", "kv_len", "q_start"))):
+        for name in names:
+            with pytest.raises(AttributeError):
+                setattr(handle, name, getattr(handle, name).clone())
+    x = torch.randn((1, 1, D), device="cuda").bfloat16()
+    vr.paged_append(pages, batch, x, x)
+    assert torch.equal(vr.paged_attn(pages, batch, x), x)              # one key: its value
