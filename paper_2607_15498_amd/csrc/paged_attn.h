@@ -74,11 +74,8 @@ __device__ __forceinline__ int64_t lane64(int64_t v, int lane) {
 }
 
 // ---- who does what, computed by every wave from the device lengths ------------------------------
-// Reductions over the first `n` lanes (the others hold nothing), to a scalar.
-__device__ __forceinline__ float first_lane(float v) { return __uint_as_float((uint32_t)first_lane((int32_t)__float_as_uint(v))); }
-template <typename V> __device__ __forceinline__ V wave_sum(V v, int n) {
-    for (int m = 1; m < n; m <<= 1) v += __shfl_xor(v, m, WAVE);
-    return first_lane(v);
+__device__ __forceinline__ float first_lane(float v) {
+    return __uint_as_float((uint32_t)first_lane((int32_t)__float_as_uint(v)));
 }
 __device__ __forceinline__ SeqRange load_range(const AttnArgs& a, int s) {
     SeqRange r = {0, 0, 0};
@@ -654,27 +651,58 @@ __device__ void many_rows(const Piece<ET>& P, uint8_t* smem, int32_t row0, int32
 //   Even shares, against pieces of one length per call dealt out in turn: 1003 tokens beside 16 single ones 192 -> 173 us
 //   (chunk and single tokens side by side from the start), fp32 prompts of 1531 and 777 tokens 339 -> 257 us, 32 single tokens
 //   over 100 .. 21800 311 -> 287 us.  Finding a share's ends takes 3 us, which tiles alike in equal pieces save.
+//   Where a wave stands lies in shared memory while it works on a piece: kept in scalar registers it spills into the
+//   loops' (512 tokens over 32768: 294 -> 283 us).
+struct Walk {
+    SeqRange first[64];
+    Plan plan;
+    Search from;
+    Tile t;
+    int64_t pos, end;
+    int32_t place;
+};
 template <typename ET>
 __global__ __launch_bounds__(64 * Form<ET>::WAVES, 1) void paged_attn_kernel(AttnArgs a) {
     extern __shared__ __align__(1024) uint8_t smem[];
-    const SeqRange first = load_range(a, threadIdx.x & 63);
-    const Plan plan = wave_plan(a, first);
+    __shared__ __align__(16) uint8_t walks[Form<ET>::WAVES * sizeof(Walk)];
     const uint32_t b = blockIdx.x, n = gridDim.x;
-    const Split split = plan.split;
-    const bool even = split.among && !split.same;
-    const int32_t share = share_of(b, split.among);
-    const int64_t total = plan.head * a.G, all = (plan.units + n - 1) / n;
-    const int32_t rounds = split.same ? 1 : all < INT32_MAX ? (int32_t)all : INT32_MAX;
-    if (a.rec_rows && b == 0 && threadIdx.x == 0) *among_of(a) = split.among;
-    if (split.among && share == split.among) return;
-    Search from;
-    Tile t;
-    int64_t pos = 0, end = 0;
-    int place = 2 * share;
+    Walk& w = reinterpret_cast<Walk*>(walks)[first_lane((int)(threadIdx.x >> 6))];
+    {
+        const SeqRange first = load_range(a, threadIdx.x & 63);
+        const Plan plan = wave_plan(a, first);
+        if (a.rec_rows && b == 0 && threadIdx.x == 0) *among_of(a) = plan.split.among;
+        const int32_t share = share_of(b, plan.split.among);
+        if (plan.split.among && share == plan.split.among) return;
+        w.first[threadIdx.x & 63] = first;
+        w.plan = plan;
+        w.from = Search{};
+        w.t = Tile{};
+        w.pos = w.end = 0;
+        w.place = 2 * share;
+    }
     for (int k = 0;; ++k) {
+        asm volatile("" ::: "memory");                     // read it again
+        const SeqRange first = w.first[threadIdx.x & 63];
+        const Plan plan = {first_lane(w.plan.head), first_lane(w.plan.units),
+                           Split{first_lane(w.plan.split.among), first_lane(w.plan.split.same)}};
+        const Split split = plan.split;
+        Search from;
+        from.at = first_lane(w.from.at);
+        from.before = first_lane(w.from.before);
+        Tile t;
+        int32_t place = first_lane(w.place);
+        const int32_t share = place >> 1;
         int64_t x0 = 0, x1 = 0;
         bool cut = false;
-        if (even) {
+        if (split.among && !split.same) {
+            const int64_t total = plan.head * a.G;
+            t.f.r = SeqRange{first_lane(w.t.f.r.q0), first_lane(w.t.f.r.qlen), first_lane(w.t.f.r.klen)};
+            t.f.s = first_lane(w.t.f.s);
+            t.g = first_lane(w.t.g);
+            t.tile = first_lane(w.t.tile);
+            t.start = first_lane(w.t.start);
+            t.w = first_lane(w.t.w);
+            int64_t pos = first_lane(w.pos), end = first_lane(w.end);
             if (k > 0 && pos >= end) break;
             if (k == 0 || pos >= t.start + t.w) {
                 const int64_t at = k ? pos : share_begin(total, share + (int)(threadIdx.x & 1), split);
@@ -682,14 +710,16 @@ __global__ __launch_bounds__(64 * Form<ET>::WAVES, 1) void paged_attn_kernel(Att
                 tile_of(a, plan, first, at < total ? at : total - 1, from, u);
                 if (k == 0) {                              // where the share begins and ends
                     const int64_t to = at < total ? u.start + cut_at(at - u.start, u.w, u.many, a.costs) : total;
-                    pos = lane64(to, 0);
-                    end = lane64(to, 1);
+                    w.pos = pos = lane64(to, 0);
+                    w.end = end = lane64(to, 1);
                 }
                 t.f = u.f;
                 t.g = first_lane(u.g);
                 t.tile = first_lane(u.tile);
                 t.start = first_lane(u.start);
                 t.w = first_lane(u.w);
+                w.t = t;
+                w.from = from;
                 if (k == 0) {
                     if (threadIdx.x == 0)
                         shares_of(a)[share] = Share{pos, t.start, t.f.r, t.g, t.tile, pos > t.start && pos < t.start + t.w};
@@ -699,10 +729,13 @@ __global__ __launch_bounds__(64 * Form<ET>::WAVES, 1) void paged_attn_kernel(Att
             x0 = pos - t.start;
             x1 = end - t.start < t.w ? end - t.start : t.w;
             cut = x1 - x0 != t.w;
-            pos = t.start + x1;
+            w.pos = t.start + x1;
+            w.place = place | 1;
         } else {
             // tiles by their numbers: whole ones sequence after sequence, the last tile first (with causal rows it sees the
             // most keys), heads innermost; those in equal pieces head after head
+            const int64_t all = (plan.units + n - 1) / n;
+            const int32_t rounds = split.same ? 1 : all < INT32_MAX ? (int32_t)all : INT32_MAX;
             if (k == rounds) break;
             const int32_t G = split.same ? 1 : a.G;
             int64_t idx = tile_number(b, n, b & 8 && a.S <= 64 ? rounds - 1 - k : k);
@@ -716,8 +749,9 @@ __global__ __launch_bounds__(64 * Form<ET>::WAVES, 1) void paged_attn_kernel(Att
                 t.g = (int32_t)(u / each);
                 idx = u % each;
             }
-            if (!find(a, first, idx, from, t.f, [&](const SeqRange& r) { return (int64_t)seq_tiles(r, a.Hg) * G; }))
-                continue;                                  // behind the last
+            const bool found = find(a, first, idx, from, t.f, [&](const SeqRange& r) { return (int64_t)seq_tiles(r, a.Hg) * G; });
+            w.from = from;
+            if (!found) continue;                          // behind the last
             const uint32_t in = (uint32_t)(idx - t.f.base);
             if (!split.same) t.g = (int32_t)(in % (uint32_t)G);
             t.tile = seq_tiles(t.f.r, a.Hg) - 1 - (int32_t)(in / (uint32_t)G);
@@ -725,7 +759,6 @@ __global__ __launch_bounds__(64 * Form<ET>::WAVES, 1) void paged_attn_kernel(Att
                 shares_of(a)[share] = Share{share, t.start * t.w, t.f.r, t.g, t.tile, x0 != 0};
         }
         const int64_t rec_row = (int64_t)place * place_rows(a.T, a.Hg);
-        if (even) place |= 1;
         const SeqRange r = t.f.r;
         const int bm = tile_rows(r, a.Hg);
         const int32_t row0 = t.tile * bm;

@@ -80,7 +80,6 @@ VR_HD Costs costs_of(bool bf16) {
     return bf16 ? Costs{5, 8, 600, 4400, 400, 256} : Costs{12, 72, 600, 1800, 400, 128};
 }
 VR_HD bool is_many(SeqRange r, int Hg) { return seq_rows(r, Hg) > ROWS_FEW; }
-VR_HD int32_t key_cost(SeqRange r, int Hg, Costs c) { return is_many(r, Hg) ? c.many : c.few; }
 
 // The cost of a sequence's tiles for one head: a + b (t + 1) for tile t.  (Tiles of causal chunks see 256 / Hg keys more
 // one after another; what is rounded in b shifts a little work, and nothing else hangs on it.)
@@ -144,6 +143,15 @@ VR_HD void sum_up(Sums& t, SeqRange r, int G, int Hg, int causal, int window, Co
     if (last > t.longest) t.longest = last;
 }
 // How n workgroups share the work out: into `among` shares (0: whole tiles), `same` to every tile (0: even ones).
+// What is estimated to take the shortest.  Each forced, us (bf16, 8 KV heads of 4, unless said otherwise):
+//                                                  whole    equal    even
+//   2048 tokens over 32768 (256 tiles, alike)        966              1010
+//   8192 tokens from the first (1024 tiles)          547               635
+//   1003 over 5003 (128 tiles, alike)                158      109      124
+//   1 over 32768 (8 tiles)                           439       35       36
+//   16 of 1 over 301 .. 8146                         144       85       77
+//   32 of 1 over 100 .. 21800                        402      349      287
+//   fp32 prompts of 1531 and 777 (296 tiles)         406      409      257
 struct Split { int32_t among, same; };
 VR_HD Split split_of(const Sums& s, int n, Costs c) {
     const Split tiles = {0, 0};
