@@ -762,3 +762,27 @@ def test_tensors_of_a_handle_stay(vr):
     x = torch.randn((1, 1, D), device="cuda").bfloat16()
     vr.paged_append(pages, batch, x, x)
     assert torch.equal(vr.paged_attn(pages, batch, x), x)              # one key: its value
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attn_thousands_of_sequences(vr, dtype):
+    """3000 sequences, most of them short, one long and one with a chunk of new tokens."""
+    import torch
+    S = 3000
+    kv = [1 + (7 * s) % 23 for s in range(S)]
+    q_len = [1] * S
+    q_len[1500], kv[1500] = 40, 900
+    kv[2900] = 1300
+    pool = Pool(kv, 1, 16, dtype, seed=51)
+    q = torch.randn((sum(q_len), 4, D), generator=torch.Generator().manual_seed(52)).to(tdt(dtype))
+    pages, batch = pool.device(vr, q_len)
+    out = vr.paged_attn(pages, batch, q.cuda()).cpu()
+    at = 0
+    for s in range(S):
+        if s % 97 == 0 or s in (1499, 1500, 1501, 2900, 2999):
+            one = Pool.__new__(Pool)
+            one.__dict__.update(pool.__dict__)
+            one.table, one.kv_len = pool.table[s:s + 1], [kv[s]]
+            ref, tol = attn_ref(one, q[at:at + q_len[s]], [q_len[s]], 4)
+            within(out[at:at + q_len[s]], ref, tol, f"sequence {s}")
+        at += q_len[s]
