@@ -62,11 +62,17 @@ __device__ __forceinline__ int64_t first_lane(int64_t v) {
     return (int64_t)((uint64_t)(uint32_t)first_lane((int32_t)(v >> 32)) << 32 | lo);
 }
 
-// One direct-to-LDS load: 16 bytes per lane from base + off to LDS byte address dst + 16 lane.
+// One direct-to-LDS load: 16 bytes per lane from base + off to LDS byte address dst + 16 lane.  ONCE: non-temporal, for keys
+// and values of few rows, which no other workgroup reads unless sequences share pages (one token over 131072: 113 -> 103 us;
+// 32 over 100 .. 21800: 286 -> 261; but 32 over the same 4096 tokens: 54 -> 60).
+template <bool ONCE = false>
 __device__ __forceinline__ void lds_load(const void* base, uint32_t off, uint32_t dst) {
     const uint64_t b = (uint64_t)first_lane((int64_t)base);      // scalars, wherever the compiler keeps them
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(b), "s"(first_lane((int)dst))
-                 : "memory", "m0");
+    const int32_t d = first_lane((int)dst);
+    if constexpr (ONCE)
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(off), "s"(b), "s"(d) : "memory", "m0");
+    else
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(b), "s"(d) : "memory", "m0");
 }
 __device__ __forceinline__ int64_t lane64(int64_t v, int lane) {
     return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 |
@@ -252,13 +258,13 @@ struct Piece {
     }
     static __device__ __forceinline__ int advance(int32_t p) { return p >= 0 ? 1024 : 0; }
     // 1 KB number v of them into LDS at dst (of number 0); row 0 of number 0 is row 4 `quad` of its block
-    template <bool VALUES>
+    template <bool VALUES, bool ONCE = false>
     __device__ __forceinline__ void bring1(const uint8_t* src, int adv, int v, int quad, uint32_t dst) const {
         // rows 4 v + .. (bf16) or 2 v + .. (fp32): the rest of f(row); fp32 values are read a row at a time as they are
-        if constexpr (F::BF) lds_load(src + v * adv, off0 ^ (((uint32_t)(quad + v) & 3u) << 4), dst + v * 1024);
+        if constexpr (F::BF) lds_load<ONCE>(src + v * adv, off0 ^ (((uint32_t)(quad + v) & 3u) << 4), dst + v * 1024);
         else if constexpr (!VALUES)
-            lds_load(src + v * adv, off0 ^ ((uint32_t)((v & 1) << 3 | ((quad + (v >> 1)) & 3)) << 4), dst + v * 1024);
-        else lds_load(src + v * adv, 16u * (uint32_t)lane, dst + v * 1024);
+            lds_load<ONCE>(src + v * adv, off0 ^ ((uint32_t)((v & 1) << 3 | ((quad + (v >> 1)) & 3)) << 4), dst + v * 1024);
+        else lds_load<ONCE>(src + v * adv, 16u * (uint32_t)lane, dst + v * 1024);
     }
     // values behind the end in the rows [r0, r1) of a tile of keys from t0 on: not read as data
     __device__ __forceinline__ void clear_tail(int32_t t0, int32_t r0, int32_t r1, uint8_t* vt) const {

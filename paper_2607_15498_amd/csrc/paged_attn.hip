@@ -9,7 +9,7 @@
 //
 // Two forms, chosen per sequence by its rows.  Few rows (single tokens): the waves of a workgroup
 // share one tile of 32 rows and divide its keys, with rings of their own and no barrier, joined at the
-// end; the reads of K and V bound it (one token over 32768 of 8 KV heads: 29 us, 4.6 TB/s).  Many rows
+// end; the reads of K and V bound it (one token over 131072 of 8 KV heads: 103 us, 5.2 TB/s).  Many rows
 // (prompts and chunks): tiles of 256 rows, 64 a wave (two blocks of 32, so that a fragment read from
 // LDS feeds two products), and all waves share the key stages; the matrix cores bound it (2048 tokens
 // over 32768: 1090 TFLOP/s).  Few are what one product's 32 columns hold: over 32768, 8 tokens of 4
@@ -130,7 +130,7 @@ __device__ __forceinline__ void few_rows<uint16_t>(const Piece<uint16_t>& P, uin
             const int32_t pg = page[c * CROWS / 16];
             const uint8_t* src = P.rows_at(pool, pg, t + c * CROWS);
 #pragma unroll
-            for (int v = 0; v < 4; ++v) P.template bring1<values>(src, P.advance(pg), v, c * CROWS / 4, dst + c * 4096);
+            for (int v = 0; v < 4; ++v) P.template bring1<values, true>(src, P.advance(pg), v, c * CROWS / 4, dst + c * 4096);
         }
     };
     auto groups = [&]() { return (page[0] >= 0 ? 1u : 0u) | (page[1] >= 0 ? 2u : 0u); };

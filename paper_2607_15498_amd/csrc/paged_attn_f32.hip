@@ -63,12 +63,12 @@ __device__ __forceinline__ void few_rows_of(const Piece<float>& P, uint8_t* smem
     auto bring_keys = [&](int32_t t) {
         const uint8_t* src = P.rows_at(P.kbase, page, t);
 #pragma unroll
-        for (int v = 0; v < L; ++v) P.bring1<false>(src, P.advance(page), v, 0, kdst);
+        for (int v = 0; v < L; ++v) P.bring1<false, true>(src, P.advance(page), v, 0, kdst);
     };
     auto bring_values = [&](int32_t t) {
         const uint8_t* src = P.rows_at(P.vbase, page, t);
 #pragma unroll
-        for (int v = 0; v < L; ++v) lds_load(src + v * P.advance(page), 16u * (uint32_t)lane, kdst + TB + v * 1024);
+        for (int v = 0; v < L; ++v) lds_load<true>(src + v * P.advance(page), 16u * (uint32_t)lane, kdst + TB + v * 1024);
     };
     int32_t t0 = (lo & ~15) + 16 * wave;
     if (t0 < hi) {

@@ -38,9 +38,19 @@ __device__ __forceinline__ float2 turn_of(int32_t pos, float theta) {
     return float2{(float)(k == 1 || k == 2 ? -cc : cc), (float)(k >= 2 ? -ss : ss)};
 }
 
+// 8 values and back.  ONCE: non-temporal.  Append reads and writes so (32768 tokens of 8 + 8 heads: 51.7 -> 46 us, its
+// loads or stores alone 51.4 and 48.6); norm and rotation (16384 tokens of 28 + 4 heads: 47 -> 54) and gather (42 -> 48) do not.
 struct Half8 { float x[8]; };
-__device__ __forceinline__ Half8 load8(const uint16_t* p) {
-    const u32x4 w = load16(p);
+template <bool ONCE, typename V> __device__ __forceinline__ V take(const V* p) {
+    if constexpr (ONCE) return __builtin_nontemporal_load(p);
+    else return *p;
+}
+template <bool ONCE, typename V> __device__ __forceinline__ void give(V* p, V v) {
+    if constexpr (ONCE) __builtin_nontemporal_store(v, p);
+    else *p = v;
+}
+template <bool ONCE = false> __device__ __forceinline__ Half8 load8(const uint16_t* p) {
+    const u32x4 w = take<ONCE>((const u32x4*)p);
     Half8 v;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -49,17 +59,17 @@ __device__ __forceinline__ Half8 load8(const uint16_t* p) {
     }
     return v;
 }
-__device__ __forceinline__ Half8 load8(const float* p) {
-    const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+template <bool ONCE = false> __device__ __forceinline__ Half8 load8(const float* p) {
+    const f32x4 a = take<ONCE>((const f32x4*)p), b = take<ONCE>((const f32x4*)(p + 4));
     return Half8{{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}};
 }
-__device__ __forceinline__ void store8(uint16_t* p, const Half8& v) {
-    *reinterpret_cast<u32x4*>(p) = u32x4{cvt_bf16x2(v.x[0], v.x[1]), cvt_bf16x2(v.x[2], v.x[3]),
-                                         cvt_bf16x2(v.x[4], v.x[5]), cvt_bf16x2(v.x[6], v.x[7])};
+template <bool ONCE> __device__ __forceinline__ void store8(uint16_t* p, const Half8& v) {
+    give<ONCE>((u32x4*)p, u32x4{cvt_bf16x2(v.x[0], v.x[1]), cvt_bf16x2(v.x[2], v.x[3]), cvt_bf16x2(v.x[4], v.x[5]),
+                                cvt_bf16x2(v.x[6], v.x[7])});
 }
-__device__ __forceinline__ void store8(float* p, const Half8& v) {
-    *reinterpret_cast<f32x4*>(p) = f32x4{v.x[0], v.x[1], v.x[2], v.x[3]};
-    *reinterpret_cast<f32x4*>(p + 4) = f32x4{v.x[4], v.x[5], v.x[6], v.x[7]};
+template <bool ONCE> __device__ __forceinline__ void store8(float* p, const Half8& v) {
+    give<ONCE>((f32x4*)p, f32x4{v.x[0], v.x[1], v.x[2], v.x[3]});
+    give<ONCE>((f32x4*)(p + 4), f32x4{v.x[4], v.x[5], v.x[6], v.x[7]});
 }
 
 constexpr int TPB_MAX = 16;
@@ -130,7 +140,7 @@ __global__ __launch_bounds__(256) void row_kernel(RowArgs p) {
                 dst = (second ? (ET*)p.bo + (int64_t)(t0 + t) * p.bo_stride
                               : (ET*)p.ao + (int64_t)(t0 + t) * p.ao_stride) + (int64_t)hh * D + 8 * j;
             }
-            Half8 x0 = load8(src), x1 = load8(src + 64);
+            Half8 x0 = load8<PAGED>(src), x1 = load8<PAGED>(src + 64);
             if constexpr (!PAGED) {
                 const float* w = second ? p.wb : p.wa;
                 if (w) {                         // the same for the 8 lanes of a row
@@ -159,8 +169,8 @@ __global__ __launch_bounds__(256) void row_kernel(RowArgs p) {
                     x1.x[k] = u * q.y + v * q.x;
                 }
             }
-            store8(dst, x0);
-            store8(dst + 64, x1);
+            store8<PAGED>(dst, x0);
+            store8<PAGED>(dst + 64, x1);
         }
         if (at0 + step < p.T) __syncthreads();             // the tables are written again
     }
@@ -169,8 +179,8 @@ __global__ __launch_bounds__(256) void row_kernel(RowArgs p) {
 // Few rows: a token and 32 of its rows a workgroup, so that they spread over the card.  Many: about 128 rows a workgroup
 // share their tokens' angles; append's workgroups find their slots first, and more that are smaller hide that
 // better.  Rows a workgroup 64 / 128 / 256: norm and rotation of 16384 tokens of 28 + 4 heads 47.5 / 45.8 / 50 us (5.8 TB/s
-// of reading and writing); append of 32768 tokens of 8 + 8 heads 51.3 / 54.4 / 60 us (5.2 TB/s), 53.6 / 57 / 60 with a token's
-// heads together instead.
+// of reading and writing); append of 32768 tokens of 8 + 8 heads 51.3 / 54.4 / 60 us, 53.6 / 57 / 60 with a token's heads
+// together instead (46 us, 5.8 TB/s, since its accesses are non-temporal).
 template <typename ET, bool PAGED>
 hipError_t launch_rows(RowArgs p, hipStream_t st) {
     const int Hs = p.Ha + p.Hb;
