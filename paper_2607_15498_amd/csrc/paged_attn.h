@@ -431,7 +431,8 @@ struct Piece {
     }
 };
 
-// weights exp2(c x + off) of 32 keys: packed in pairs and summed as rounded (bf16), or in place (fp32)
+// weights exp2(c x + off) of 32 keys, in place (fp32), or rounded to bf16 and packed in pairs, which is what the value products
+// take, and summed as rounded: a row whose weights are all rounded one way is not off by it
 __device__ __forceinline__ void weights(f32x16& sc, float c, float off, u32x4 (&p)[2], float& l) {
     float l0 = 0.f, l1 = 0.f;
 #pragma unroll

@@ -302,8 +302,8 @@ __device__ __forceinline__ void many_rows<uint16_t>(const Piece<uint16_t>& P, ui
     };
     auto pack = [&](auto par, int c, int k) {
         constexpr int e = decltype(par)::value;
-        uint32_t w = cvt_bf16x2(ea, eb);
-        run[c].l += ea;
+        uint32_t w = cvt_bf16x2(ea, eb);                   // what the value products take
+        run[c].l += ea;                                    // as they are: two adds, shorter than a sum of the pair
         lb[c] += eb;
         asm volatile("" : "+v"(w), "+v"(run[c].l), "+v"(lb[c]));     // here, not where they are used
         p[1 - e][c][k >> 2][k & 3] = w;

@@ -8,9 +8,9 @@ Bounds, element by element, with u the rounding of a type (half a step: bf16 2^-
   attention          scores: 128 products summed in fp32, 128 u32 c sum|q k|; the exponent's own
                      product and sum 3 u32 (|c x| + |c m|) and the exponential 2 u32.  A weight's
                      error is at most twice that exponent error D (in maximum and in sum).  Weights
-                     of bf16 layers are rounded, u, in their products with the values and in their
-                     sum alike: sum p e (v - o) / sum p, at most u (A + |o|) with A = sum p |v| /
-                     sum p.  Sums of n weighted values: n u32.  Together |error| <= u_p (A + |o|) +
+                     of bf16 layers are rounded, u, in their products with the values and (few rows)
+                     in their sum alike: sum p e (v - o) / sum p, at most u (A + |o|) with A = sum p |v| /
+                     sum p (many rows: in the products alone, at most u A).  Sums of n weighted values: n u32.  Together |error| <= u_p (A + |o|) +
                      (4 D + (n + 256) u32) A, and the rounding of the output, u |o|, is of a value
                      that far off: another (1 + u).
   append, gather     copies are exact; a rotated key as above.
