@@ -454,7 +454,8 @@ VARRATE_API int varrate_paged_append(const varrate_pages* pages, const varrate_b
  * causal 0 (window 0): every new token sees all kv_len[s] keys.  A token that sees no key gets
  * zeros, and so does one whose visible scores are all -infinity.  Keys and values that a token
  * does not see (later ones, slots behind the end, unused pages) do not reach its output,
- * whatever they hold.  Scores are fp32: scale <q, k> beyond its range gives NaN.  scale lies in
+ * whatever they hold.  <q, k> is fp32 and makes its row NaN where it overflows to infinity; scale <q, k>
+ * may be of any size (beyond 2^27 the largest score of a row takes all, equal ones alike).  scale lies in
  * [2^-100, 2^100].  out must not overlap q.  T H <= 2^30.                                    */
 VARRATE_API size_t varrate_paged_attn_workspace_bytes(const varrate_pages* pages, const varrate_batch* batch, int32_t H);
 VARRATE_API int varrate_paged_attn(const varrate_pages* pages, const varrate_batch* batch, const void* q,

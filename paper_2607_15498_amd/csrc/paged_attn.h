@@ -218,13 +218,12 @@ struct Piece {
     int lane, l32, h;
     uint32_t off0, kaddr;
 
-    __device__ __forceinline__ Piece(const AttnArgs& a_, const Found& f, int g_, int32_t lo_, int32_t hi_)
-        : a(a_), r(f.r), g(g_), lo(lo_), hi(hi_) {
+    __device__ __forceinline__ Piece(const AttnArgs& a_, const Found& f, int g_, int32_t lo_, int32_t hi_, int lane_)
+        : a(a_), r(f.r), g(g_), lo(lo_), hi(hi_), lane(lane_) {
         head_bytes = (int64_t)F::ROWB << a.shift;
         kbase = (const uint8_t*)a.k + (int64_t)g * head_bytes;
         vbase = (const uint8_t*)a.v + (int64_t)g * head_bytes;
         trow = a.table + (int64_t)f.s * a.table_stride;
-        lane = threadIdx.x & 63;
         l32 = lane & 31;
         h = lane >> 5;
         const int lrow = lane / F::PPR;                    // the row that this lane loads of a 1 KB piece
@@ -448,45 +447,58 @@ __device__ __forceinline__ void weights(f32x16& sc, float c, float off, u32x4 (&
 __device__ __forceinline__ float weight32(float x, float c, float c_lo, float off) {
     return __builtin_amdgcn_exp2f(fmaf(x, c_lo, fmaf(x, c, off)));
 }
-__device__ __forceinline__ void weights(f32x16& sc, float c, float c_lo, float off, float& l) {
+__device__ __forceinline__ float weight32(float x, float c, float off) { return __builtin_amdgcn_exp2f(fmaf(x, c, off)); }
+// how: a score's weight
+template <typename W>
+__device__ __forceinline__ void weights32(f32x16& sc, float& l, W&& how) {
     float l0 = 0.f, l1 = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; i += 2) {
-        sc[i] = weight32(sc[i], c, c_lo, off);
-        sc[i + 1] = weight32(sc[i + 1], c, c_lo, off);
+        sc[i] = how(sc[i]);
+        sc[i + 1] = how(sc[i + 1]);
         l0 += sc[i];
         l1 += sc[i + 1];
     }
     l += l0 + l1;
 }
 
-// A row's running maximum m (of raw scores), off = -c m and its sum.  The maximum that the weights
-// are taken against follows the true one only when that is SLACK powers of two above it: the weights
+// A row's running maximum m (of raw scores) and its sum; a key's weight is exp2(c x + off), off = -c m.  The maximum that
+// the weights are taken against follows the true one only when that is SLACK powers of two above it: the weights
 // then reach 2^SLACK, which neither bf16's exponent nor the fp32 sums mind, and the sums are rescaled
 // a few times per piece instead of at every block.
-constexpr float SLACK = 8.f;
-// -c m, 0 while nothing has been seen.  Rounded as it is used everywhere (no part of a fused operation): weights
-// exp2(c x + off) of different maxima then differ by exp2 of the difference of their offs, whose own roundings cancel.
+constexpr float SLACK = 8.f;                               // (SLACK / c is less than half a step of a maximum BEYOND)
+// off is rounded, as it is used everywhere (no part of a fused operation): weights of different maxima then differ by
+// exp2 of the difference of their offs, whose own roundings cancel.  That rounding and c's (c_lo) leave c m + off up to
+// 2^-22 |c m| from 0, a factor that all of the row's weights share.  From |c m| = BEYOND on it would no longer be a number
+// to multiply with, and scores next to each other lie 2^-24 |c m| >= 16 apart: the largest takes all.  c is then a power
+// of two that takes m to 2^31 .. 2^32 (m's own exponent is 0 exactly, the next score's below -127), whether or not c m
+// itself is within fp32's range.
+constexpr float BEYOND = 0x1.1p28f;
+__device__ __forceinline__ bool beyond(float off) { return fabsf(off) >= BEYOND; }
+__device__ __forceinline__ float power_for(float m) { return __uint_as_float((uint32_t)(159 - __builtin_amdgcn_frexp_expf(m)) << 23); }
 __device__ __forceinline__ float off_of(float m, float c) {
-    float off = m == -INFINITY ? 0.f : -m * c;
+    float off = m == -INFINITY ? 0.f : -m * c;             // 0 while nothing has been seen
     asm("" : "+v"(off));
-    return off;
+    return beyond(off) ? -m * power_for(m) : off;          // exact; -infinity for m = infinity, whose weight is NaN
 }
-// the factor that takes sums of weights against m to those whose off is `to`
-__device__ __forceinline__ float rescale(float m, float to, float c) {
-    return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(to - off_of(m, c));
+// the factor that takes sums of weights against m to those against M >= m, whose off is `to`
+__device__ __forceinline__ float factor(float m, float off, float M, float to) {
+    const float f = __builtin_amdgcn_exp2f(to - off);
+    return m == -INFINITY || (m != M && (beyond(off) || beyond(to))) ? 0.f : f;
 }
+__device__ __forceinline__ float rescale(float m, float M, float to, float c) { return factor(m, off_of(m, c), M, to); }
 struct Running {
     float m = -INFINITY, off = 0.f, l = 0.f;
     // the factor for what has been summed so far
     __device__ __forceinline__ float raise(float mt, float c) {
-        const float mn = fmaxf(m, mt), to = off_of(mn, c);
-        const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(to - off);
+        const float mn = fmaxf(m, mt), to = off_of(mn, c), f = factor(m, off, mn, to);
         m = mn;
         off = to;
         l *= f;
         return f;
     }
+    // the c that a row's weights take; c: the call's
+    __device__ __forceinline__ float c_of(float c) const { return beyond(off) ? power_for(m) : c; }
 };
 
 template <typename ET>
@@ -773,9 +785,12 @@ __global__ __launch_bounds__(64 * Form<ET>::WAVES, 1) void paged_attn_kernel(Att
         int32_t lo, hi;
         tile_keys(r, row0, rows, a.Hg, a.causal, a.window, lo, hi);
         if (cut) piece_keys(x0, x1, t.w, lo, hi);
-        const Piece<ET> P(a, t.f, t.g, first_lane(lo), first_lane(hi));
-        if (bm == ROWS_FEW) few_rows<ET>(P, smem, rows, cut, rec_row);
-        else many_rows<ET>(P, smem, row0, rows, cut, rec_row);
+        // What follows from the lane's number is formed for each piece: kept for all of them it spills (one token over 32768,
+        // bf16: 38 -> 36 us).  Not so for many rows of bf16: a prompt of 1000 tokens takes 53 us, and 61 with it.
+        lo = first_lane(lo);
+        hi = first_lane(hi);
+        if (bm == ROWS_FEW) few_rows<ET>(Piece<ET>(a, t.f, t.g, lo, hi, lane_now()), smem, rows, cut, rec_row);
+        else many_rows<ET>(Piece<ET>(a, t.f, t.g, lo, hi, Form<ET>::BF ? (int)(threadIdx.x & 63) : lane_now()), smem, row0, rows, cut, rec_row);
     }
 }
 
@@ -812,14 +827,14 @@ __device__ __forceinline__ void join_pieces(const AttnArgs& a, A&& at, int p0, i
             float mn = M[n];
 #pragma unroll
             for (int k = 0; k < NP; ++k) mn = fmaxf(mn, ml[n][k].x);
-            const float to = off_of(mn, a.c), f0 = rescale(M[n], to, a.c);
+            const float to = off_of(mn, a.c), f0 = rescale(M[n], mn, to, a.c);
             M[n] = mn;
             l[n] *= f0;
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[n][e] *= f0;
 #pragma unroll
             for (int k = 0; k < NP; ++k) {
-                const float f = rescale(ml[n][k].x, to, a.c);
+                const float f = rescale(ml[n][k].x, mn, to, a.c);
                 l[n] = fmaf(f, ml[n][k].y, l[n]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[n][e] = fmaf(f, v[n][k][e], o[n][e]);
@@ -895,7 +910,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(AttnArgs a) {
             const float to = off_of(mx, a.c);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const float f = rescale(sl[k][0], to, a.c);
+                const float f = rescale(sl[k][0], mx, to, a.c);
                 const f32x4 v = *reinterpret_cast<const f32x4*>(&so[k][4 * l32]);
                 ls = fmaf(f, sl[k][1], ls);
 #pragma unroll

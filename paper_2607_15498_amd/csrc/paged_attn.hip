@@ -104,6 +104,7 @@ __device__ __forceinline__ void few_rows<uint16_t>(const Piece<uint16_t>& P, uin
     u32x4 qf[1][F::NF];
     P.query(qf[0], r.q0 + tok, g * Hg + myrow % Hg);
     Running run;
+    const float slack = SLACK / a.c;
     f32x16 acc[1][4], sc[1];
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt)
@@ -153,14 +154,15 @@ __device__ __forceinline__ void few_rows<uint16_t>(const Piece<uint16_t>& P, uin
             P.template scores<1>(kt, qf, sc);
             if (masked) P.anew().mask(sc[0], t0, seen, gm);
             const float mt = P.most(sc[0]);
-            if (__any(mt > run.m + SLACK / a.c)) {
+            if (__any(mt > run.m + slack)) {
                 const float f = run.raise(mt, a.c);
 #pragma unroll
                 for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) acc[0][dt][i] *= f;
             }
-            weights(sc[0], a.c, run.off, p[0], run.l);
+            if (__any(beyond(run.off))) weights(sc[0], run.c_of(a.c), run.off, p[0], run.l);
+            else weights(sc[0], a.c, run.off, p[0], run.l);
         };
         st ^= 1;
         const uint32_t next = ring0 + st * 2 * F::KB;
@@ -195,7 +197,7 @@ __device__ __forceinline__ void few_rows<uint16_t>(const Piece<uint16_t>& P, uin
                 f32x4{acc[0][dt][i], acc[0][dt][i + 1], acc[0][dt][i + 2], acc[0][dt][i + 3]};
     if (h == 0) *reinterpret_cast<float2*>(jm + (wave * 32 + l32) * 2) = float2{run.m, run.l};
     __syncthreads();
-    const int row = threadIdx.x >> 3, d0 = 16 * (threadIdx.x & 7);
+    const int row = 8 * wave + (lane >> 3), d0 = 16 * (lane & 7);
     if (row < rows) {                                      // at most 32, a thread each 16 dims
         float mw[4], lw[4], M = -INFINITY, Ls = 0.f, o[16];
 #pragma unroll
@@ -210,7 +212,7 @@ __device__ __forceinline__ void few_rows<uint16_t>(const Piece<uint16_t>& P, uin
         for (int i = 0; i < 16; ++i) o[i] = 0.f;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-            const float f = rescale(mw[w], to, a.c);
+            const float f = rescale(mw[w], M, to, a.c);
             Ls = fmaf(f, lw[w], Ls);
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
@@ -250,6 +252,7 @@ __device__ __forceinline__ void many_rows<uint16_t>(const Piece<uint16_t>& P, ui
     Many<uint16_t> M(P, smem, row0, rows);
     if (M.stages) M.begin();
     Running run[2];
+    float cw[2] = {a.c, a.c};                              // c of the rows' weights
     settle();
     static_for<128>([&](auto i) { agpr_set<i>(0u); });
     {
@@ -269,26 +272,27 @@ __device__ __forceinline__ void many_rows<uint16_t>(const Piece<uint16_t>& P, ui
 #pragma unroll
     for (int i = 0; i < 16; ++i) sc[0][0][i] = sc[0][1][i] = sc[1][0][i] = sc[1][1][i] = -INFINITY;
     u32x4 p[2][2][2];
-    float pend[2] = {1.f, 1.f}, limit[2] = {-INFINITY, -INFINITY};       // limit: scores above it raise the maximum
+    float pend[2] = {1.f, 1.f};
     float mx[2] = {-INFINITY, -INFINITY};                  // this lane's maxima of the last step's scores
     float lb[2] = {0.f, 0.f};                              // every second weight's part of the sums
     bool pending = false;
     // Before the weights of step j - 1, after its scores and the value products of j - 3.
     auto follow = [&]() {
-        if (!(__any(mx[0] > limit[0] || mx[1] > limit[1]) || pending)) return;
+        const bool above = __any(mx[0] > run[0].m + slack || mx[1] > run[1].m + slack);
+        if (!(above || pending)) return;
         if (pending) {                                     // the products of j - 3 were of the old maximum
             settle();
             static_for<128>([&](auto i) { agpr_set<i>(__float_as_uint(agpr_get<i>() * pend[i / 64])); });
             settle();
             pending = false;
         }
-        if (__any(mx[0] > limit[0] || mx[1] > limit[1])) {
+        if (above) {
             pend[0] = run[0].raise(xmax32(mx[0]), a.c);    // and those of j - 2 will be: scaled after them
             pend[1] = run[1].raise(xmax32(mx[1]), a.c);
+            cw[0] = run[0].c_of(a.c);
+            cw[1] = run[1].c_of(a.c);
             lb[0] *= pend[0];
             lb[1] *= pend[1];
-            limit[0] = run[0].m + slack;
-            limit[1] = run[1].m + slack;
             pending = true;
         }
     };
@@ -297,8 +301,8 @@ __device__ __forceinline__ void many_rows<uint16_t>(const Piece<uint16_t>& P, ui
     float ea, eb;
     auto weigh = [&](auto par, int c, int k) {
         constexpr int e = decltype(par)::value;
-        ea = __builtin_amdgcn_exp2f(fmaf(sc[1 - e][c][2 * k], a.c, run[c].off));
-        eb = __builtin_amdgcn_exp2f(fmaf(sc[1 - e][c][2 * k + 1], a.c, run[c].off));
+        ea = __builtin_amdgcn_exp2f(fmaf(sc[1 - e][c][2 * k], cw[c], run[c].off));
+        eb = __builtin_amdgcn_exp2f(fmaf(sc[1 - e][c][2 * k + 1], cw[c], run[c].off));
     };
     auto pack = [&](auto par, int c, int k) {
         constexpr int e = decltype(par)::value;

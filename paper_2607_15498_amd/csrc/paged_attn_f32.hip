@@ -29,8 +29,8 @@ __device__ __forceinline__ void few_rows_of(const Piece<float>& P, uint8_t* smem
     row_keys(r, (rows - 1) / Hg, a.causal, a.window, lastlo, x);
     typename Piece<float>::Seen seen[NB];
     u32x4 qf[NB][8];
-    Running run[NB];
     f32x4 acc[NB][2][4];
+    Running run[NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
         const int row = 16 * b + i16 < rows ? 16 * b + i16 : 0, tok = row / Hg;
@@ -128,8 +128,14 @@ __device__ __forceinline__ void few_rows_of(const Piece<float>& P, uint8_t* smem
 #pragma unroll
                         for (int v = 0; v < 4; ++v) acc[b][half][e][v] *= f;
             }
+            if (__any(beyond(run[b].off))) {
+                const float c = run[b].c_of(a.c);
 #pragma unroll
-            for (int v = 0; v < 4; ++v) sc[b][v] = weight32(sc[b][v], a.c, a.c_lo, run[b].off);
+                for (int v = 0; v < 4; ++v) sc[b][v] = weight32(sc[b][v], c, run[b].off);
+            } else {
+#pragma unroll
+                for (int v = 0; v < 4; ++v) sc[b][v] = weight32(sc[b][v], a.c, a.c_lo, run[b].off);
+            }
             run[b].l += (sc[b][0] + sc[b][1]) + (sc[b][2] + sc[b][3]);
         }
         if (more) wait_loads<L>();
@@ -196,7 +202,7 @@ __device__ __forceinline__ void few_rows_of(const Piece<float>& P, uint8_t* smem
                     f32x4{acc[b][half][0][v], acc[b][half][1][v], acc[b][half][2][v], acc[b][half][3][v]};
         if (q4 == 0) *reinterpret_cast<float2*>(jm + (wave * 16 + i16) * 2) = float2{run[b].m, l};
         __syncthreads();
-        const int in = threadIdx.x >> 5, row = 16 * b + in, d0 = 4 * (threadIdx.x & 31);
+        const int in = 2 * wave + (lane >> 5), row = 16 * b + in, d0 = 4 * (lane & 31);
         if (row < rows) {
             float M = -INFINITY, Ls = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
             float2 ml[NW];
@@ -208,7 +214,7 @@ __device__ __forceinline__ void few_rows_of(const Piece<float>& P, uint8_t* smem
             const float to = off_of(M, a.c);
 #pragma unroll
             for (int w = 0; w < NW; ++w) {
-                const float f = rescale(ml[w].x, to, a.c);
+                const float f = rescale(ml[w].x, M, to, a.c);
                 const f32x4 v = *reinterpret_cast<const f32x4*>(js + (w * 16 + in) * 132 + d0);
                 Ls = fmaf(f, ml[w].y, Ls);
 #pragma unroll
@@ -267,7 +273,10 @@ __device__ __forceinline__ void many_rows<float>(const Piece<float>& P, uint8_t*
 #pragma unroll
                 for (int k = 0; k < 16; ++k) acc[dt][k] *= f;
         }
-        weights(sc[0], a.c, a.c_lo, run.off, run.l);
+        if (__any(beyond(run.off))) {
+            const float c = run.c_of(a.c);
+            weights32(sc[0], run.l, [&](float x) { return weight32(x, c, run.off); });
+        } else weights32(sc[0], run.l, [&](float x) { return weight32(x, a.c, a.c_lo, run.off); });
         const uint8_t* vt = M.values_of(j);
         const bool odd = masked && P.anew().odd_values(vt);
         P.values(vt, sc[0], acc, odd);

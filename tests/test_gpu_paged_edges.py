@@ -1,0 +1,100 @@
+"""GPU tests of the paged cache at the edges of its ranges: scores of any size.  References, bounds and pools are those of
+test_gpu_paged.py."""
+import pytest
+
+from test_gpu_paged import D, U, U32, Pool, attn_ref, say, tdt, vr, within  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+# (new tokens, cached tokens, table entries or None for as many as are needed) by the form that serves them: few rows
+# and many, in tables too short to cut (8 pages of 32) and in long ones
+FORMS = {"few": ([1], [200], 8), "few cut": ([2], [6000], None), "many": ([70], [200], 8), "many cut": ([70], [6000], None)}
+
+
+def one_call(vr, pool, q, q_len, **kw):
+    import torch
+    pages, batch = pool.device(vr, q_len)
+    out = vr.paged_attn(pages, batch, q.cuda(), **kw)
+    torch.cuda.synchronize()
+    return out.cpu().double()
+
+
+def mean_of(pool, m, which=None):
+    """(the plain mean of the values that each of the last m tokens sees, and a bound on it): weights are alike, so that
+    only they (bf16, in their products: u A), the sums (n roundings of 32 bits at most) and the output round.
+    which: of those keys alone."""
+    import torch
+    _, V, _ = pool.rows(0)
+    n = len(V)
+    keep = torch.ones(n, dtype=torch.bool) if which is None else which
+    ref, tol = [], []
+    for i in range(n - m + 1, n + 1):
+        v = V[:i][keep[:i]].double()[:, 0]
+        ref.append(v.mean(0))
+        tol.append(((n + 256) * U32 + (U["bf16"] if pool.dtype == "bf16" else 0)) * v.abs().mean(0))
+    ref, tol = torch.stack(ref)[:, None], torch.stack(tol)[:, None]
+    u = U[pool.dtype]
+    return ref, (tol + u * ref.abs()) * (1 + u) + 1e-38
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("power", [-20, 20, 27, 28, 30, 40, 93, 100])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_attn_equal_scores_of_any_size(vr, dtype, form, power, sign):
+    """scale <q, k> of about 2^(35 + power) for every key, <q, k> itself (1.4 x 2^35) within fp32: whichever form and cut
+    serves the call, the mean of the values."""
+    import torch
+    q_len, kv_len, width = FORMS[form]
+    say(f"[scores] {dtype} {form} 2^{power} {sign}")
+    pool = Pool(kv_len, 1, 32, dtype, seed=3, width=width)
+    pool.k[:] = torch.where(pool.k.isnan(), pool.k, torch.full_like(pool.k, sign * 1.421875 * 2.0 ** 14))
+    q = torch.full((sum(q_len), 4, D), 2.0 ** 14).to(tdt(dtype))
+    out = one_call(vr, pool, q, q_len, scale=2.0 ** power)
+    ref, tol = mean_of(pool, q_len[0])
+    within(out, ref.expand_as(out), tol.expand_as(out), "mean")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("power", [-13, -8, -3, 0, 1, 60, 100])
+def test_attn_largest_score_takes_all(vr, dtype, form, power):
+    """Scores of whole numbers (exact) times 2^20 times scale, below and beyond the largest power of two whose multiples are
+    32-bit exponents: the largest that a row sees has all of the weight, several equal ones share it."""
+    import torch
+    q_len, kv_len, width = FORMS[form]
+    m, n = q_len[0], kv_len[0]
+    say(f"[largest] {dtype} {form} 2^{power}")
+    pool = Pool(kv_len, 1, 32, dtype, seed=4, width=width)
+    gen = torch.Generator().manual_seed(7)
+    x = torch.randint(-120, 100, (n,), generator=gen)
+    x[torch.randint(0, n - m, (2,), generator=gen)] = 120  # two of them before every new token
+    for t in range(n):
+        p, i = int(pool.table[0, t // 32]), t % 32
+        pool.k[p, 0, i] = 0
+        pool.k[p, 0, i, 77] = float(x[t])
+    q = torch.zeros((m, 4, D))
+    q[..., 77] = 2.0 ** 20
+    out = one_call(vr, pool, q.to(tdt(dtype)), q_len, scale=2.0 ** power)
+    ref, tol = mean_of(pool, m, x == 120)                  # the next one's weight is e^-2560 at most
+    within(out, ref.expand_as(out), tol.expand_as(out), "largest")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("form", FORMS)
+def test_attn_scores_that_overflow(vr, dtype, form):
+    """<q, k> beyond fp32 for the middle new token's own key: the rows that see it are NaN, those before it as they would be."""
+    import torch
+    q_len, kv_len, width = FORMS[form]
+    m, n = q_len[0], kv_len[0]
+    t = n - m + m // 2
+    pool = Pool(kv_len, 1, 32, dtype, seed=5, width=width)
+    q = torch.randn((m, 4, D), generator=torch.Generator().manual_seed(6)).to(tdt(dtype))
+    q[..., 0] = 4.0
+    ref, tol = attn_ref(pool, q, q_len, 4)
+    p, i = int(pool.table[0, t // 32]), t % 32
+    pool.k[p, 0, i] = 0
+    pool.k[p, 0, i, 0] = 2.0 ** 127
+    out = one_call(vr, pool, q, q_len)
+    assert out[m // 2:].isnan().all()
+    within(out[:m // 2], ref[:m // 2], tol[:m // 2], "before it")
