@@ -400,8 +400,9 @@ VARRATE_API int varrate_joint_append_exact(const varrate_shape* shape, varrate_j
  * keep every access inside the buffers: page numbers outside [0, n_pages) name no page (append
  * drops the row, attention leaves the token out, gather writes zeros), starts are brought into
  * [0, T], lengths for attention into [0, width page]; append drops the rows of a sequence whose
- * length lies outside that range and rows at negative positions.  Starts must not fall; of
- * sequences whose starts fall the outputs are unspecified.  Table rows of several sequences may
+ * length lies outside that range and rows at negative positions.  Starts must not fall; of a
+ * batch whose starts fall the outputs are unspecified (attention may leave all of them as they were).
+ * The arrays must not change while a call runs.  Table rows of several sequences may
  * share pages (a common prompt) as long as one call's tokens land in different slots.
  *
  * d = 128.  Rows of new tokens are [T][heads][d] with a stride between tokens (elements, a

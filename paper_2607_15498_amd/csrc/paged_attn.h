@@ -22,7 +22,7 @@ struct AttnArgs {
     float* rec;                     // partial rows [rec_rows][128], then their [rec_rows][2] (max, sum), then the shares
     int64_t q_stride, out_stride;   // elements between tokens
     int64_t table_stride;
-    int64_t rec_rows;
+    int64_t rec_rows, most_units;
     int32_t T, S, cap, n_pages, G, Hg, shift;
     int32_t causal, window;
     Costs costs;
@@ -104,12 +104,12 @@ __device__ __forceinline__ Plan wave_plan(const AttnArgs& a, const SeqRange& fir
         s.longest = fmaxf(s.longest, __shfl_xor(s.longest, m, WAVE));
     }
     const int64_t head = first_lane((int64_t)s.head);
-    s.units = first_lane(s.units);
+    s.units = units_of(first_lane(s.units), a.most_units);
     s.total = first_lane(s.total);
     s.many = first_lane(s.many);
     s.units_many = first_lane(s.units_many);
     s.longest = first_lane(s.longest);
-    if (!a.rec_rows) return Plan{head, s.units, Split{0, 0}};
+    if (!a.rec_rows || !s.units) return Plan{head, s.units, Split{0, 0}};
     const Split p = split_of(s, (int)gridDim.x, a.costs);
     return Plan{head, s.units, Split{first_lane(p.among), first_lane(p.same)}};
 }

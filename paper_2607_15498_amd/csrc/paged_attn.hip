@@ -509,6 +509,7 @@ hipError_t launch_paged_attn(const varrate_pages& pg, const varrate_batch& b, co
     a.c = (float)c;
     if ((double)a.c >= c) a.c = nextafterf(a.c, 0.f);
     a.c_lo = (float)(c - (double)a.c);                     // > 0, so that a masked score stays -infinity
+    a.most_units = max_units(b.T, b.S, pg.G, a.Hg);
     a.rec_rows = max_records(b.T, b.S, pg.G, a.Hg, a.cap, a.costs.lmin);
     const int groups = max_groups(b.T, b.S, pg.G, a.Hg, a.cap, a.costs.lmin);
     return pg.dtype == VARRATE_BF16 ? launch_paged_bf16(a, groups, st) : launch_paged_f32(a, groups, st);

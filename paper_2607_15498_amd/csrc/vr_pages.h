@@ -209,6 +209,9 @@ VR_HD int32_t share_of(uint32_t b, int32_t among) {
 
 // most (tile, head) pairs of any call with T rows and S sequences; workgroups that a call whose tables hold `cap` tokens can use
 VR_HD int64_t max_units(int64_t T, int S, int G, int Hg) { return G * (T * Hg / ROWS_MANY + (S < T ? S : T)); }
+// Those of a call, none where they are more: then starts fall (rows belong to several sequences, up to S / 2 times as much
+// work as any call has), and nothing is computed.
+VR_HD int64_t units_of(int64_t units, int64_t most) { return units <= most ? units : 0; }
 VR_HD int max_groups(int64_t T, int S, int G, int Hg, int64_t cap, int lmin) {
     const int64_t n = max_units(T, S, G, Hg) * ((cap + lmin - 1) / lmin);
     return n < SLOTS ? (int)((n + 7) & ~(int64_t)7) : SLOTS;

@@ -98,3 +98,23 @@ def test_attn_scores_that_overflow(vr, dtype, form):
     out = one_call(vr, pool, q, q_len)
     assert out[m // 2:].isnan().all()
     within(out[:m // 2], ref[:m // 2], tol[:m // 2], "before it")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attn_starts_that_fall(vr, dtype):
+    """Starts 0, T, 0, T, ..: 32 sequences that all claim every row are more work than a call can have.  Nothing is computed, and
+    a proper call with the same workspace is as it would be."""
+    import torch
+    S, T, n = 64, 300, 600
+    pool = Pool([n] * S, 1, 32, dtype, seed=9)
+    q = torch.randn((T, 4, D), generator=torch.Generator().manual_seed(8)).to(tdt(dtype)).cuda()
+    pages, batch = pool.device(vr, [T] + [0] * (S - 1))
+    bad = torch.tensor([(s & 1) * T for s in range(S + 1)], dtype=torch.int32).cuda()
+    falling = vr.PagedBatch(batch.table, batch.kv_len, bad)
+    ws = torch.full((96 << 20,), 0xFF, dtype=torch.uint8, device="cuda")
+    out = torch.full((T, 4, D), 5.0, dtype=tdt(dtype), device="cuda")
+    say(f"[falling starts] {dtype}")
+    vr.paged_attn(pages, falling, q, out=out, workspace=ws)
+    torch.cuda.synchronize()
+    assert (out == 5).all()
+    assert torch.equal(vr.paged_attn(pages, batch, q, workspace=ws), vr.paged_attn(pages, batch, q))

@@ -1,0 +1,61 @@
+"""Paged cache at the edges of its ranges, without a GPU."""
+import os
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+BOUND = r'''
+#include <stdio.h>
+#include <stdlib.h>
+#include <algorithm>
+#include <random>
+#include <vector>
+#include "vr_pages.h"
+using namespace vr;
+#define CHECK(x) do { if (!(x)) { printf("line %d: %s\n", __LINE__, #x); exit(1); } } while (0)
+
+static int64_t tiles_of(const std::vector<int32_t>& start, int T, int G, int Hg) {
+    Sums s;
+    for (size_t i = 0; i + 1 < start.size(); ++i) sum_up(s, seq_range(start[i], start[i + 1], 1000, T, 4096), G, Hg, 1, 0, costs_of(true));
+    return s.units;
+}
+int main() {
+    std::mt19937 gen(3);
+    for (int round = 0; round < 2000; ++round) {
+        const int S = 1 + (int)(gen() % 300), T = (int)(gen() % 5000), G = 1 + (int)(gen() % 8), Hg = 1 + (int)(gen() % 300);
+        const int64_t most = max_units(T, S, G, Hg);
+        std::vector<int32_t> start(S + 1);
+        for (int& x : start) x = (int32_t)(gen() % (T + 1));
+        const int64_t any = tiles_of(start, T, G, Hg);
+        CHECK(units_of(any, most) <= most);
+        std::sort(start.begin(), start.end());
+        const int64_t rising = tiles_of(start, T, G, Hg);
+        CHECK(units_of(rising, most) == rising);           // nothing of a proper call is left out
+    }
+    // 0, T, 0, T, ..: every second sequence has all rows
+    std::vector<int32_t> start(65537);
+    for (size_t i = 0; i < start.size(); ++i) start[i] = i & 1 ? 1 << 20 : 0;
+    const int64_t all = tiles_of(start, 1 << 20, 8, 4), most = max_units(1 << 20, 65536, 8, 4);
+    CHECK(all > 1000 * most && units_of(all, most) == 0);
+    printf("ok\n");
+    return 0;
+}
+'''
+
+
+def run_host(tmp_path, source):
+    from paper_2607_15498_amd import build as B
+    src, exe = tmp_path / "walk.cpp", tmp_path / "walk"
+    src.write_text(source)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-fsanitize=undefined", "-fno-sanitize-recover=undefined", "-Wall", "-I", B.CSRC,
+                    str(src), "-o", str(exe)], check=True)
+    r = subprocess.run([str(exe)], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=300)
+    assert r.returncode == 0, r.stdout[-2000:]
+    return r.stdout
+
+
+def test_work_of_falling_starts_is_bounded(tmp_path):
+    """Starts that rise have max_units tiles at most; of more, which only starts that fall have, none are computed."""
+    assert run_host(tmp_path, BOUND).strip() == "ok"
