@@ -518,6 +518,14 @@ def _einval(msg: str):
     raise VarRateError(_lib.VARRATE_EINVAL, msg)
 
 
+def _int32(v, name: str) -> int:
+    """v as a 32-bit argument: ctypes would keep the low 32 bits of a larger number."""
+    i = int(v)
+    if i != v or not -(1 << 31) <= i < 1 << 31:
+        _einval(f"{name}={v} is not a whole number of 32 bits")
+    return i
+
+
 class PagedCache:
     """A pool of pages: k, v [n_pages][G][page][d] (bf16 or fp32), contiguous device tensors.  k and v are
     not to be replaced (calls use their addresses); their contents are the user's."""
@@ -567,7 +575,7 @@ class PagedBatch:
 
     def __init__(self, table: torch.Tensor, kv_len: torch.Tensor, q_start: torch.Tensor):
         pt, pl, ps = _i32(table, 2, "table"), _i32(kv_len, 1, "kv_len"), _i32(q_start, 1, "q_start")
-        S, width = int(table.shape[0]), int(table.shape[1])
+        S, width = _int32(table.shape[0], "S"), _int32(table.shape[1], "width")
         if kv_len.shape[0] != S or q_start.shape[0] != S + 1:
             _einval(f"kv_len and q_start must have {S} and {S + 1} entries")
         if kv_len.device != table.device or q_start.device != table.device:
@@ -710,7 +718,7 @@ def paged_attn(pages: PagedCache, batch: PagedBatch, q: torch.Tensor, causal: bo
         _einval(f"workspace must be a contiguous tensor on {dev}")
     else:
         nbytes = workspace.numel() * workspace.element_size()
-    _launch(dev, L.varrate_paged_attn, pc, bc, pq, sq, H, 1 if causal else 0, int(window),
+    _launch(dev, L.varrate_paged_attn, pc, bc, pq, sq, H, 1 if causal else 0, _int32(window, "window"),
             HEAD_DIM ** -0.5 if scale is None else scale, po, so, workspace.data_ptr() if nbytes else 0, nbytes)
     return out
 
@@ -731,5 +739,5 @@ def paged_gather(pages: PagedCache, table: torch.Tensor, n: int, K: Optional[tor
             _einval(f"{name} must be a contiguous {dt} tensor {list(shape)} on {dev}")
     K = torch.empty(shape, dtype=dt, device=dev) if K is None else K
     V = torch.empty(shape, dtype=dt, device=dev) if V is None else V
-    _launch(dev, library().varrate_paged_gather, pages.c(), pt, int(table.shape[0]), n, K.data_ptr(), V.data_ptr())
+    _launch(dev, library().varrate_paged_gather, pages.c(), pt, _int32(table.shape[0], "width"), n, K.data_ptr(), V.data_ptr())
     return K, V

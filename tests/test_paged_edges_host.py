@@ -59,3 +59,48 @@ def run_host(tmp_path, source):
 def test_work_of_falling_starts_is_bounded(tmp_path):
     """Starts that rise have max_units tiles at most; of more, which only starts that fall have, none are computed."""
     assert run_host(tmp_path, BOUND).strip() == "ok"
+
+
+# ---- the binding, on handles of host tensors (a call that gets as far as its launch fails otherwise) -----------------
+
+@pytest.fixture
+def host(monkeypatch):
+    """(binding, pages, batch, q): handles that no device is needed for, and a launch that is never to be reached."""
+    import torch
+    import paper_2607_15498_amd as vr
+    from paper_2607_15498_amd import _lib
+
+    def launched(*args):
+        raise AssertionError("launched")
+    monkeypatch.setattr(vr, "_launch", launched)
+    monkeypatch.setattr(vr, "_i32", lambda t, dim, name: t.data_ptr())
+    kv = torch.zeros((4, 2, 16, 128), dtype=torch.bfloat16)
+    pages = vr.PagedCache.__new__(vr.PagedCache)
+    pages._k, pages._v, pages.page, pages.G = kv, kv.clone(), 16, 2
+    pages._c = _lib.PagesC(pages._k.data_ptr(), pages._v.data_ptr(), 4, 2, 128, 16, _lib.VARRATE_BF16)
+    batch = vr.PagedBatch(torch.zeros((1, 4), dtype=torch.int32), torch.ones(1, dtype=torch.int32), torch.tensor([0, 1], dtype=torch.int32))
+    return vr, pages, batch, torch.zeros((1, 4, 128), dtype=torch.bfloat16)
+
+
+@pytest.mark.parametrize("window", [1 << 32, (1 << 32) + 5, -(1 << 32), 1 << 31, 1 << 70, 2.5])
+def test_numbers_beyond_32_bits_raise(host, window):
+    """A window of 2^32 + 5 is not one of 5."""
+    vr, pages, batch, q = host
+    with pytest.raises(vr.VarRateError):
+        vr.paged_attn(pages, batch, q, window=window)
+    for fine in (0, 5, 5.0, True):
+        with pytest.raises(AssertionError, match="launched"):
+            vr.paged_attn(pages, batch, q, window=fine)
+
+
+def test_sizes_beyond_32_bits_raise(host):
+    import torch
+    vr, pages, batch, _ = host
+    far = lambda n: torch.zeros(1, dtype=torch.int32).expand(n)            # no memory: one entry, read again and again
+    S = (1 << 32) + 1
+    with pytest.raises(vr.VarRateError):
+        vr.PagedBatch(far(4).expand(S, 4), far(S), far(S + 1))
+    with pytest.raises(vr.VarRateError):
+        vr.PagedBatch(far(S)[None], far(1), far(2))
+    with pytest.raises(vr.VarRateError):
+        vr.paged_gather(pages, far(S), 3)
