@@ -602,7 +602,8 @@ def _rows(t: torch.Tensor, dtype, T: Optional[int], heads: Optional[int], device
     return t.data_ptr(), (s0 if n > 1 else h * d)
 
 
-_raw_stream = torch._C._cuda_getCurrentRawStream      # the stream's handle without a Stream object (2 us a call)
+# the current stream's handle, where torch has it without a Stream object (2 us a call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
 
 
 def _launch(device: torch.device, call, *args):

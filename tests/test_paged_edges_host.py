@@ -1,6 +1,7 @@
 """Paged cache at the edges of its ranges, without a GPU."""
 import os
 import subprocess
+import sys
 
 import pytest
 
@@ -104,3 +105,17 @@ def test_sizes_beyond_32_bits_raise(host):
         vr.PagedBatch(far(S)[None], far(1), far(2))
     with pytest.raises(vr.VarRateError):
         vr.paged_gather(pages, far(S), 3)
+
+
+def test_import_needs_no_stream_handles():
+    """The package imports, and the codec's part of it is there, with a torch that has no raw stream handles; they are asked for
+    by the calls that use them."""
+    code = ("import torch\n"
+            "if hasattr(torch._C, '_cuda_getCurrentRawStream'): del torch._C._cuda_getCurrentRawStream\n"
+            "import paper_2607_15498_amd as vr\n"
+            "vr.library(); vr.Shape(n=64, G=1, H=2, w=32, r_min=16, kappa_pct=100).c()\n"
+            "class S: cuda_stream = 7\n"
+            "torch.cuda.current_stream = lambda i: S\n"
+            "assert vr._raw_stream(0) == 7\n")
+    r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    assert r.returncode == 0, r.stdout[-2000:]
