@@ -659,7 +659,7 @@ def norm_rotate(q: Optional[torch.Tensor], k: Optional[torch.Tensor] = None, pos
     dev, dt = some.device, some.dtype
     if not some.is_cuda or dt not in _DTYPES:
         _einval("q and k must be bf16 or fp32 device tensors")
-    T = int(some.shape[0])
+    T = int(some.shape[0]) if some.dim() else 0
     if theta is not None:
         if pos is None:
             _einval("rotation needs pos")
@@ -680,7 +680,7 @@ def paged_append(pages: PagedCache, batch: PagedBatch, k: torch.Tensor, v: torch
     """Write the batch's new rows k, v [T][G][d] into their sequences' pages; theta [64] fp32 rotates
     each key by its position first."""
     dev = pages.k.device
-    T = int(k.shape[0])
+    T = int(k.shape[0]) if k.dim() else 0
     pk, sk = _rows(k, pages.k.dtype, None, pages.G, dev, "k")
     pv, sv = _rows(v, pages.k.dtype, T, pages.G, dev, "v")
     if batch.table.device != dev:
@@ -702,7 +702,7 @@ def paged_attn(pages: PagedCache, batch: PagedBatch, q: torch.Tensor, causal: bo
     reads KV head h / (H / G)): causal at each sequence's end, with window > 0 over the last `window`
     keys only; causal=False: every token sees its whole sequence.  scale: 1 / sqrt(d) by default."""
     dev = pages.k.device
-    T, H = int(q.shape[0]), int(q.shape[1]) if q.dim() == 3 else 0
+    T, H = (int(q.shape[0]), int(q.shape[1])) if q.dim() == 3 else (0, 0)
     pq, sq = _rows(q, pages.k.dtype, T, None, dev, "q")
     if batch.table.device != dev:
         _einval(f"the batch must be on {dev}")

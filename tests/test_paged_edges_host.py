@@ -119,3 +119,16 @@ def test_import_needs_no_stream_handles():
             "assert vr._raw_stream(0) == 7\n")
     r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     assert r.returncode == 0, r.stdout[-2000:]
+
+
+def test_tensors_of_no_dimension_raise(host):
+    """A scalar tensor in the place of rows is refused as any other wrong shape."""
+    import torch
+    vr, pages, batch, q = host
+    dot = torch.zeros((), dtype=torch.bfloat16)
+    k = torch.zeros((1, 2, 128), dtype=torch.bfloat16)
+    for call in (lambda: vr.paged_append(pages, batch, dot, k), lambda: vr.paged_append(pages, batch, k, dot),
+                 lambda: vr.paged_attn(pages, batch, dot), lambda: vr.paged_attn(pages, batch, q, out=dot),
+                 lambda: vr.paged_gather(pages, batch.table[0], 3, K=dot)):
+        with pytest.raises(vr.VarRateError):
+            call()
