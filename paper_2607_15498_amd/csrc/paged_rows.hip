@@ -72,6 +72,16 @@ template <bool ONCE> __device__ __forceinline__ void store8(float* p, const Half
     give<ONCE>((f32x4*)(p + 4), f32x4{v.x[4], v.x[5], v.x[6], v.x[7]});
 }
 
+// the sum of a row's squares, in each of its 8 lanes
+__device__ __forceinline__ float squares(const Half8& x0, const Half8& x1) {
+    float sq = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sq = fmaf(x0.x[k], x0.x[k], fmaf(x1.x[k], x1.x[k], sq));
+    sq += shfl_xor_f(sq, 1);
+    sq += shfl_xor_f(sq, 2);
+    return sq + shfl_xor_f(sq, 4);
+}
+
 constexpr int TPB_MAX = 16;
 
 // Two kinds of rows of every token: Ha heads of `a`, then Hb heads of `b`.
@@ -146,13 +156,21 @@ __global__ __launch_bounds__(256) void row_kernel(RowArgs p) {
                 if (w) {                         // the same for the 8 lanes of a row
                     w += hh * (second ? p.wb_stride : p.wa_stride) + 8 * j;
                     const Half8 w0 = load8(w), w1 = load8(w + 64);
-                    float sq = 0.f;
+                    float sq = squares(x0, x1), eps = p.eps;
+                    // Squares beyond fp32's range (or of values below 2^-40, where eps does not hide what they lack): of the
+                    // row times a power of two, and eps times its square, which leave y as it is.
+                    const bool large = sq > 3.4e38f;
+                    if (large || (sq < 0x1p-80f && eps < 0x1p-100f)) {
+                        const float s = large ? 0x1p-70f : 0x1p100f;
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) sq = fmaf(x0.x[k], x0.x[k], fmaf(x1.x[k], x1.x[k], sq));
-                    sq += shfl_xor_f(sq, 1);
-                    sq += shfl_xor_f(sq, 2);
-                    sq += shfl_xor_f(sq, 4);
-                    const float r = 1.0f / sqrtf(sq * (1.0f / D) + p.eps);
+                        for (int k = 0; k < 8; ++k) {
+                            x0.x[k] *= s;
+                            x1.x[k] *= s;
+                        }
+                        sq = squares(x0, x1);
+                        eps = eps * s * s;
+                    }
+                    const float r = 1.0f / sqrtf(sq * (1.0f / D) + eps);
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
                         x0.x[k] *= r * w0.x[k];

@@ -118,3 +118,28 @@ def test_attn_starts_that_fall(vr, dtype):
     torch.cuda.synchronize()
     assert (out == 5).all()
     assert torch.equal(vr.paged_attn(pages, batch, q, workspace=ws), vr.paged_attn(pages, batch, q))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("eps", [0.0, 1e-35, 1e-6])
+def test_norm_of_any_size(vr, dtype, eps):
+    """Rows whose squares leave fp32's range either way are normed by the formula: beside ordinary rows, with values of
+    very different sizes in a row, with and without rotation."""
+    import torch
+    from test_gpu_paged import norm_ref, theta_of
+    gen = torch.Generator().manual_seed(4)
+    powers = [-126, -100, -75, -63, -50, -40, -20, 0, 20, 50, 62, 63, 64, 65, 80, 100, 125]
+    x = torch.randn((len(powers), 3, D), generator=gen).clamp(-3.5, 3.5)
+    x *= 2.0 ** torch.tensor(powers, dtype=torch.float32)[:, None, None]
+    x[:, 1, 1:] *= 2.0 ** -30                              # one value far above the others
+    x[:, 2, ::2] = 0
+    x = x.to(tdt(dtype))
+    w = 1 + 0.3 * torch.randn((3, D), generator=gen)
+    pos = torch.arange(len(powers), dtype=torch.int32) * 1000
+    for theta in (None, theta_of()):
+        say(f"[norm sizes] {dtype} eps={eps} rotated={theta is not None}")
+        got, _ = vr.norm_rotate(x.cuda(), wq=w.cuda(), eps=eps, pos=pos.cuda(), theta=None if theta is None else theta.cuda())
+        ref, tol = norm_ref(x, w, pos, theta, eps, dtype)
+        within(got, ref, tol, "rows")
+    zero, _ = vr.norm_rotate(torch.zeros((1, 1, D), dtype=tdt(dtype), device="cuda"), wq=w[0].cuda(), eps=1e-30)
+    assert (zero == 0).all()
