@@ -431,13 +431,15 @@ struct Piece {
 };
 
 // weights exp2(c x + off) of 32 keys, in place (fp32), or rounded to bf16 and packed in pairs, which is what the value products
-// take, and summed as rounded: a row whose weights are all rounded one way is not off by it
-__device__ __forceinline__ void weights(f32x16& sc, float c, float off, u32x4 (&p)[2], float& l) {
+// take, and summed as rounded: a row whose weights are all rounded one way is not off by it.  rest: -1 for what the rounding
+// takes from the weights, rounded, in their place; 0 for the weights.
+__device__ __forceinline__ void weights(f32x16& sc, float c, float off, float rest, u32x4 (&p)[2], float& l) {
     float l0 = 0.f, l1 = 0.f;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-        const uint32_t w = cvt_bf16x2(__builtin_amdgcn_exp2f(fmaf(sc[2 * k], c, off)),
-                                      __builtin_amdgcn_exp2f(fmaf(sc[2 * k + 1], c, off)));
+        const float e0 = __builtin_amdgcn_exp2f(fmaf(sc[2 * k], c, off)), e1 = __builtin_amdgcn_exp2f(fmaf(sc[2 * k + 1], c, off));
+        uint32_t w = cvt_bf16x2(e0, e1);
+        w = cvt_bf16x2(fmaf(rest, bf_lo(w), e0), fmaf(rest, bf_hi(w), e1));
         p[k >> 2][k & 3] = w;
         if (k & 1) l1 = add_pair(w, l1);
         else l0 = add_pair(w, l0);

@@ -84,6 +84,11 @@ template <int DT, int C> __device__ __forceinline__ void value(const u32x4& f, c
 
 // Few rows: each of the 4 waves takes every fourth tile of 32 keys, out of its own ring of two (16 KB each), and
 // their sums are joined at the end.
+// Weights are rounded to bf16 for their products with the values.  Up to 16 rows (single tokens) leave half of a product's 32
+// columns: these take the same rows' queries, and of their weights what the rounding takes away, so that 2^-16 is missing
+// from a row's sums instead of 2^-8 (outputs of a few alike keys were off by up to 7 times their own rounding), for 40 vector
+// instructions a tile: 8 x 1 over 16384 61.5 -> 61.7 us, 1 over 32768 37.3 -> 37.7.  (As products of their own, for all 32 rows:
+// 64 and 40 us.)
 template <>
 __device__ __forceinline__ void few_rows<uint16_t>(const Piece<uint16_t>& P, uint8_t* smem, int rows, bool cut, int64_t rec_row) {
     typedef uint16_t ET;
@@ -95,7 +100,9 @@ __device__ __forceinline__ void few_rows<uint16_t>(const Piece<uint16_t>& P, uin
     constexpr int CH = F::KB / 4096, CROWS = 4096 / F::ROWB;       // a tile's keys (or values) come in chunks of 4 KB
     uint8_t* ring = smem + wave * 4 * F::KB;
     const uint32_t ring0 = first_lane((int)(uint32_t)(size_t)(__attribute__((address_space(3))) uint8_t*)ring);
-    const int myrow = l32 < rows ? l32 : 0, tok = myrow / Hg;
+    const bool halves = rows <= 16;
+    const int col = halves ? l32 & 15 : l32, myrow = col < rows ? col : 0, tok = myrow / Hg;
+    const float rest = col < l32 ? -1.f : 0.f;
     int32_t mylo, myhi, firsthi, lastlo, x;
     row_keys(r, tok, a.causal, a.window, mylo, myhi);
     const auto seen = P.seen(mylo, myhi);
@@ -161,8 +168,8 @@ __device__ __forceinline__ void few_rows<uint16_t>(const Piece<uint16_t>& P, uin
 #pragma unroll
                     for (int i = 0; i < 16; ++i) acc[0][dt][i] *= f;
             }
-            if (__any(beyond(run.off))) weights(sc[0], run.c_of(a.c), run.off, p[0], run.l);
-            else weights(sc[0], a.c, run.off, p[0], run.l);
+            if (__any(beyond(run.off))) weights(sc[0], run.c_of(a.c), run.off, rest, p[0], run.l);
+            else weights(sc[0], a.c, run.off, rest, p[0], run.l);
         };
         st ^= 1;
         const uint32_t next = ring0 + st * 2 * F::KB;
@@ -197,14 +204,17 @@ __device__ __forceinline__ void few_rows<uint16_t>(const Piece<uint16_t>& P, uin
                 f32x4{acc[0][dt][i], acc[0][dt][i + 1], acc[0][dt][i + 2], acc[0][dt][i + 3]};
     if (h == 0) *reinterpret_cast<float2*>(jm + (wave * 32 + l32) * 2) = float2{run.m, run.l};
     __syncthreads();
-    const int row = 8 * wave + (lane >> 3), d0 = 16 * (lane & 7);
-    if (row < rows) {                                      // at most 32, a thread each 16 dims
+    // A thread's four times 4 dims: of a row's 16, or of the 8 of a row and of its rests
+    const int row = halves ? 4 * wave + (lane >> 4) : 8 * wave + (lane >> 3), d0 = halves ? 8 * (lane & 15) : 16 * (lane & 7);
+    const int second = halves ? 16 * 132 : 8;
+    if (row < rows) {
         float mw[4], lw[4], M = -INFINITY, Ls = 0.f, o[16];
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
             const float2 v = *reinterpret_cast<const float2*>(jm + (w * 32 + row) * 2);
             mw[w] = v.x;
             lw[w] = v.y;
+            if (halves) lw[w] += jm[(w * 32 + row + 16) * 2 + 1];
             M = fmaxf(M, v.x);
         }
         const float to = off_of(M, a.c);
@@ -216,21 +226,26 @@ __device__ __forceinline__ void few_rows<uint16_t>(const Piece<uint16_t>& P, uin
             Ls = fmaf(f, lw[w], Ls);
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
-                const f32x4 v = *reinterpret_cast<const f32x4*>(js + (w * 32 + row) * 132 + d0 + i);
+                const f32x4 v = *reinterpret_cast<const f32x4*>(js + (w * 32 + row) * 132 + d0 + (i & 4) + (i >> 3) * second);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) o[i + k] = fmaf(f, v[k], o[i + k]);
             }
         }
+        if (halves)                                        // (an infinite value times a rest is no number)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) o[i] += fabsf(o[i]) < INFINITY ? o[i + 8] : 0.f;
         if (cut) {
             float* dst = a.rec + (rec_row + row) * D + d0;
 #pragma unroll
-            for (int i = 0; i < 16; i += 4) *reinterpret_cast<f32x4*>(dst + i) = f32x4{o[i], o[i + 1], o[i + 2], o[i + 3]};
+            for (int i = 0; i < 16; i += 4)
+                if (i < 8 || !halves) *reinterpret_cast<f32x4*>(dst + i) = f32x4{o[i], o[i + 1], o[i + 2], o[i + 3]};
             if (d0 == 0) *reinterpret_cast<float2*>(a.rec + a.rec_rows * D + (rec_row + row) * 2) = float2{M, Ls};
         } else {
             const float inv = Ls == 0.f ? 0.f : 1.f / Ls;
             ET* dst = (ET*)a.out + (int64_t)(r.q0 + row / Hg) * a.out_stride + (int64_t)(g * Hg + row % Hg) * D + d0;
 #pragma unroll
-            for (int i = 0; i < 16; i += 4) store4<ET>(dst + i, o[i] * inv, o[i + 1] * inv, o[i + 2] * inv, o[i + 3] * inv);
+            for (int i = 0; i < 16; i += 4)
+                if (i < 8 || !halves) store4<ET>(dst + i, o[i] * inv, o[i + 1] * inv, o[i + 2] * inv, o[i + 3] * inv);
         }
     }
     __syncthreads();                                       // the rings are free again
@@ -307,8 +322,8 @@ __device__ __forceinline__ void many_rows<uint16_t>(const Piece<uint16_t>& P, ui
     auto pack = [&](auto par, int c, int k) {
         constexpr int e = decltype(par)::value;
         uint32_t w = cvt_bf16x2(ea, eb);                   // what the value products take
-        run[c].l += ea;                                    // as they are: two adds, shorter than a sum of the pair
-        lb[c] += eb;
+        run[c].l += ea;                                    // as they are: the sum of the rounded pair, by whichever
+        lb[c] += eb;                                       // instructions, costs 5% (2048 over 32768 980 -> 1041 us)
         asm volatile("" : "+v"(w), "+v"(run[c].l), "+v"(lb[c]));     // here, not where they are used
         p[1 - e][c][k >> 2][k & 3] = w;
     };

@@ -143,3 +143,34 @@ def test_norm_of_any_size(vr, dtype, eps):
         within(got, ref, tol, "rows")
     zero, _ = vr.norm_rotate(torch.zeros((1, 1, D), dtype=tdt(dtype), device="cuda"), wq=w[0].cuda(), eps=1e-30)
     assert (zero == 0).all()
+
+
+@pytest.mark.parametrize("q_len,kv_len,G,H", [([1], [2], 2, 32), ([2], [3], 1, 7), ([4], [7], 2, 8), ([1, 3], [17, 40], 1, 5),
+                                              ([1], [3000], 2, 8), ([1], [1300], 1, 16), ([2, 1], [2500, 33], 2, 16)])
+def test_attn_few_rows_keep_their_weights(vr, q_len, kv_len, G, H):
+    """bf16 rows of up to 16 to a KV head: the weights' rounding is made good (2^-16 is left of it), so that outputs are off by
+    little more than their own rounding."""
+    import torch
+    say(f"[weights] q {q_len} kv {kv_len} G={G} H={H}")
+    assert max(q_len) * H // G <= 16
+    for seed in range(3):
+        pool = Pool(kv_len, G, 16, "bf16", seed=seed)
+        q = torch.randn((sum(q_len), H, D), generator=torch.Generator().manual_seed(seed + 50)).bfloat16()
+        q *= 0.25                                          # weights alike: none is nothing beside the others
+        out = one_call(vr, pool, q, q_len)
+        at = 0
+        for s, m in enumerate(q_len):
+            K, V, _ = pool.rows(s)
+            for i in range(m):
+                n = kv_len[s] - m + i + 1
+                for h in range(H):
+                    k, v, x = K[:n, h * G // H].double(), V[:n, h * G // H].double(), q[at + i, h].double()
+                    sc, mag = (k @ x) * D ** -0.5, (k.abs() @ x.abs()) * D ** -0.5
+                    w = torch.softmax(sc, 0)
+                    o, A = w @ v, w @ v.abs()
+                    dx = float((128 * U32 * mag + 3 * U32 * (sc.abs() + sc.abs().max())).max()) + 2 * U32
+                    e = 2.0 ** -16 * (A + o.abs()) + (4 * dx + (n + 256) * U32) * A
+                    tol = (e + U["bf16"] * o.abs()) * (1 + U["bf16"]) + 1e-38
+                    err = (out[at + i, h] - o).abs()
+                    assert (err <= tol).all(), f"seed {seed}, sequence {s}, token {i}, head {h}: {float((err / tol).max())}"
+            at += m
