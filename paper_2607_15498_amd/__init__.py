@@ -22,7 +22,7 @@ from ._lib import CHUNK, COEF_PAD, HEAD_DIM  # noqa: F401
 __all__ = ["VarRateError", "Shape", "Cache", "new_cache", "coded_budget", "salience", "allocate",
            "project", "compress", "append_exact", "decode", "decode_noalloc", "QCache", "new_qcache",
            "quantize", "decode_q", "anchor_search", "anchor_encode", "PagedCache", "PagedBatch", "new_pages",
-           "norm_rotate", "paged_append", "paged_attn", "paged_gather", "library"]
+           "norm_rotate", "paged_append", "paged_attn", "paged_attn_workspace", "paged_gather", "library"]
 
 
 class VarRateError(RuntimeError):
@@ -691,6 +691,8 @@ def paged_append(pages: PagedCache, batch: PagedBatch, k: torch.Tensor, v: torch
 
 
 def paged_attn_workspace(pages: PagedCache, batch: PagedBatch, T: int, H: int) -> torch.Tensor:
+    """Memory that paged_attn of up to T rows of H heads over this batch's tables may be given (`workspace`), for one call
+    at a time; it holds nothing between calls."""
     need = int(library().varrate_paged_attn_workspace_bytes(pages.c(), batch.c(T), H))
     return torch.empty(max(need, 16), dtype=torch.uint8, device=pages.k.device)
 
@@ -700,7 +702,8 @@ def paged_attn(pages: PagedCache, batch: PagedBatch, q: torch.Tensor, causal: bo
                workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention of the batch's new tokens, q [T][H][d], over their sequences' pages (query head h
     reads KV head h / (H / G)): causal at each sequence's end, with window > 0 over the last `window`
-    keys only; causal=False: every token sees its whole sequence.  scale: 1 / sqrt(d) by default."""
+    keys only; causal=False: every token sees its whole sequence.  scale: 1 / sqrt(d) by default.
+    workspace: memory of the caller's (paged_attn_workspace) in place of the call's own."""
     dev = pages.k.device
     T, H = (int(q.shape[0]), int(q.shape[1])) if q.dim() == 3 else (0, 0)
     pq, sq = _rows(q, pages.k.dtype, T, None, dev, "q")

@@ -174,3 +174,28 @@ def test_attn_few_rows_keep_their_weights(vr, q_len, kv_len, G, H):
                     err = (out[at + i, h] - o).abs()
                     assert (err <= tol).all(), f"seed {seed}, sequence {s}, token {i}, head {h}: {float((err / tol).max())}"
             at += m
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_one_workspace_for_many_calls(vr, dtype):
+    """A workspace of the caller's, full of ones, serves calls of every kind one after another (tiles whole, in equal pieces and
+    divided evenly, few rows and many), each as if with memory of its own; nothing behind what a call asks for is written."""
+    import torch
+    assert "paged_attn_workspace" in vr.__all__
+    calls = []
+    for q_len, kv_len in (([1], [9000]), ([1003], [3003]), ([70] + [1] * 6, [2000, 40, 700, 1300, 4000, 5000, 100]), ([1], [40]),
+                          ([300, 200], [300, 200]), ([1] * 5, [100, 2000, 4000, 8000, 9000]), ([2], [700])):
+        pool = Pool(kv_len, 2, 32, dtype, seed=len(calls))
+        pages, batch = pool.device(vr, q_len)
+        q = torch.randn((sum(q_len), 8, D), generator=torch.Generator().manual_seed(len(calls))).to(tdt(dtype)).cuda()
+        calls.append((pages, batch, q, vr.paged_attn(pages, batch, q)))
+    need = [vr.paged_attn_workspace(p, b, q.shape[0], 8).numel() for p, b, q, _ in calls]
+    ws = torch.full((max(need) + 4096,), 0xFF, dtype=torch.uint8, device="cuda")
+    for i in list(range(len(calls))) + [6, 0, 3, 2, 1]:
+        pages, batch, q, want = calls[i]
+        out = vr.paged_attn(pages, batch, q, workspace=ws[:need[i]])
+        assert torch.equal(out, want), i
+        assert (ws[max(need):] == 0xFF).all(), i
+    ws.fill_(0xFF)
+    pages, batch, q, want = calls[0]
+    assert torch.equal(vr.paged_attn(pages, batch, q, workspace=ws[:need[0]]), want) and (ws[need[0]:] == 0xFF).all()
