@@ -1,5 +1,7 @@
 """GPU tests of the paged cache at the edges of its ranges: scores of any size.  References, bounds and pools are those of
 test_gpu_paged.py."""
+import math
+
 import pytest
 
 from test_gpu_paged import D, U, U32, Pool, attn_ref, say, tdt, vr, within  # noqa: F401
@@ -199,3 +201,65 @@ def test_one_workspace_for_many_calls(vr, dtype):
     ws.fill_(0xFF)
     pages, batch, q, want = calls[0]
     assert torch.equal(vr.paged_attn(pages, batch, q, workspace=ws[:need[0]]), want) and (ws[need[0]:] == 0xFF).all()
+
+
+# ---- long tiles, and many of them: every row of the calls in paged_shapes.py -------------------------------------------
+
+def attn_ref_all(pool, q, q_len, H, causal, window):
+    """As attn_ref, every row, a sequence's rows of a KV head together, on the device in 64 bits."""
+    import torch
+    G, c, dtype = pool.G, D ** -0.5, pool.dtype
+    Hg, u = H // G, U[dtype]
+    ref, tol = (torch.zeros((sum(q_len), H, D), dtype=torch.float64) for _ in range(2))
+    at, loaded = 0, None
+    for s, m in enumerate(q_len):
+        n = pool.kv_len[s]
+        if loaded is None or len(loaded[0]) < n:
+            loaded = [x.cuda() for x in pool.rows(s)]      # all sequences have the same pages
+        K, V, ok = (x[:n] for x in loaded)
+        p, t = torch.arange(n - m, n, device="cuda")[:, None], torch.arange(n, device="cuda")[None]
+        see = ok[None].expand(m, n)
+        if causal:
+            see = see & (t <= p) & ((p - t < window) if window else True)
+        see = see.repeat_interleave(Hg, 0)
+        none = ~see.any(1, keepdim=True)
+        for g in range(G):
+            x = q[at:at + m, g * Hg:(g + 1) * Hg].reshape(-1, D).cuda().double()
+            k, v = torch.where(ok[:, None], K[:, g].double(), 0.0), torch.where(ok[:, None], V[:, g].double(), 0.0)
+            kt = k.t().contiguous()
+            sc = (x @ kt * c).masked_fill(~see, -math.inf)
+            w = torch.softmax(sc, 1).masked_fill(none, 0.0)
+            o, A = w @ v, w @ v.abs()
+            size = sc.abs().masked_fill(~see, 0.0)
+            mag = (x.abs() @ kt.abs() * c).masked_fill(~see, 0.0)
+            dx = (128 * U32 * mag + 3 * U32 * (size + size.max(1, keepdim=True).values)).max(1, keepdim=True).values + 2 * U32
+            e = (u if dtype == "bf16" else 0) * (A + o.abs()) + (4 * dx + (see.sum(1, keepdim=True) + 256) * U32) * A
+            b = (e + u * o.abs()) * (1 + u) + 1e-38
+            ref[at:at + m, g * Hg:(g + 1) * Hg] = o.reshape(m, Hg, D).cpu()
+            tol[at:at + m, g * Hg:(g + 1) * Hg] = b.reshape(m, Hg, D).cpu()
+        at += m
+    return ref, tol
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bad", [False, True])
+@pytest.mark.parametrize("i", range(7))
+def test_attn_long_and_many_tiles(vr, dtype, bad, i):
+    """bad: entries that name no page in the second and the third window of 1024 keys and in the last."""
+    import torch
+    from paged_shapes import SHAPES
+    s = SHAPES[i]
+    say(f"[long] {s.name} {dtype} bad={bad}")
+    pool = Pool([max(s.kv_len)], s.G, s.page, dtype, seed=i)
+    if bad:
+        for t, entry in ((1100, -1), (2200, pool.k.shape[0]), (min(s.kv_len) - 300, -(1 << 31))):
+            pool.table[0, t // s.page] = entry
+    pool.table = pool.table.expand(len(s.q_len), -1).contiguous()
+    pool.kv_len = list(s.kv_len)
+    q = (2 * torch.randn((sum(s.q_len), s.H, D), generator=torch.Generator().manual_seed(i + 70))).to(tdt(dtype))
+    pages, batch = pool.device(vr, s.q_len)
+    assert batch.table.shape[1] == s.width
+    out = vr.paged_attn(pages, batch, q.cuda(), causal=s.causal, window=s.window)
+    torch.cuda.synchronize()
+    ref, tol = attn_ref_all(pool, q, s.q_len, s.H, s.causal, s.window)
+    within(out, ref, tol, s.name)

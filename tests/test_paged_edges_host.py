@@ -132,3 +132,51 @@ def test_tensors_of_no_dimension_raise(host):
                  lambda: vr.paged_gather(pages, batch.table[0], 3, K=dot)):
         with pytest.raises(vr.VarRateError):
             call()
+
+
+# ---- how the calls of paged_shapes.py are shared out -----------------------------------------------------------------
+
+SPLIT = r'''
+#include <stdio.h>
+#include <stdlib.h>
+#include "vr_pages.h"
+using namespace vr;
+int main(int, char** v) {                                  // bf16 G Hg causal window cap S, then the new and all tokens of each
+    const int bf = atoi(v[1]), G = atoi(v[2]), Hg = atoi(v[3]), causal = atoi(v[4]), window = atoi(v[5]), cap = atoi(v[6]), S = atoi(v[7]);
+    int T = 0, at = 0;
+    for (int i = 0; i < S; ++i) T += atoi(v[8 + 2 * i]);
+    const Costs c = costs_of(bf);
+    Sums s;
+    for (int i = 0; i < S; at += atoi(v[8 + 2 * i++])) sum_up(s, seq_range(at, at + atoi(v[8 + 2 * i]), atoi(v[9 + 2 * i]), T, cap), G, Hg, causal, window, c);
+    const int n = max_groups(T, S, G, Hg, cap, c.lmin);
+    const Split p = split_of(s, n, c);
+    const double share = p.among ? s.total / p.among : 0;
+    printf("%d %d %lld %d\n", p.among, p.same, (long long)((s.units + n - 1) / n), (int)((share - c.piece_many) / c.many));
+    return 0;
+}
+'''
+
+
+@pytest.fixture(scope="module")
+def split_program(tmp_path_factory):
+    from paper_2607_15498_amd import build as B
+    d = tmp_path_factory.mktemp("split")
+    (d / "split.cpp").write_text(SPLIT)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-I", B.CSRC, str(d / "split.cpp"), "-o", str(d / "split")], check=True)
+    return str(d / "split")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("i", range(7))
+def test_shapes_are_shared_out_as_named(split_program, dtype, i):
+    from paged_shapes import SHAPES
+    assert len(SHAPES) == 7
+    s = SHAPES[i]
+    args = [int(dtype == "bf16"), s.G, s.H // s.G, int(s.causal), s.window, s.width * s.page, len(s.q_len)]
+    args += [x for pair in zip(s.q_len, s.kv_len) for x in pair]
+    among, same, rounds, keys = map(int, subprocess.run([split_program, *map(str, args)], stdout=subprocess.PIPE, text=True, check=True).stdout.split())
+    how, least = s.how[dtype]
+    if how == "whole":
+        assert among == 0 and rounds == least, s.name
+    else:
+        assert among > 0 and same == 0 and keys >= least, s.name
