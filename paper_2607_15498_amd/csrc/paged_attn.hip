@@ -9,12 +9,12 @@
 //
 // Two forms, chosen per sequence by its rows.  Few rows (single tokens): the waves of a workgroup
 // share one tile of 32 rows and divide its keys, with rings of their own and no barrier, joined at the
-// end; the reads of K and V bound it (one token over 131072 of 8 KV heads: 103 us, 5.2 TB/s).  Many rows
+// end; the reads of K and V bound it (one token over 131072 of 8 KV heads: 100 us, 5.4 TB/s).  Many rows
 // (prompts and chunks): tiles of 256 rows, 64 a wave (two blocks of 32, so that a fragment read from
 // LDS feeds two products), and all waves share the key stages; the matrix cores bound it (2048 tokens
-// over 32768: 1090 TFLOP/s).  Few are what one product's 32 columns hold: over 32768, 8 tokens of 4
-// rows take 40 us (one token 35), 9 as many rows 70, and so do 16: a tile of 256 costs its products however many
-// of its rows there are.  In fp32 74 and 180 us.
+// over 32768: 1055 .. 1100 TFLOP/s).  Few are what one product's 32 columns hold: over 32768, 8 tokens of 4
+// rows take 41 us (one token 37), 9 as many rows 69, and so do 16: a tile of 256 costs its products however many
+// of its rows there are.  In fp32 67 and 180 us.
 // One launch serves both, so a chunk and the single tokens beside it run together.  Where there are too
 // few (sequence, head, row tile) units for the card, or they are too unlike, their keys are cut (vr_pages.h)
 // and a second launch joins the partial rows.
