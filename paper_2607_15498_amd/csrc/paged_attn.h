@@ -449,7 +449,6 @@ __device__ __forceinline__ void weights(f32x16& sc, float c, float off, float re
 __device__ __forceinline__ float weight32(float x, float c, float c_lo, float off) {
     return __builtin_amdgcn_exp2f(fmaf(x, c_lo, fmaf(x, c, off)));
 }
-__device__ __forceinline__ float weight32(float x, float c, float off) { return __builtin_amdgcn_exp2f(fmaf(x, c, off)); }
 // how: a score's weight
 template <typename W>
 __device__ __forceinline__ void weights32(f32x16& sc, float& l, W&& how) {
@@ -499,8 +498,12 @@ struct Running {
         l *= f;
         return f;
     }
-    // the c that a row's weights take; c: the call's
+    // the c that a row's weights take (c, c_lo: the call's)
     __device__ __forceinline__ float c_of(float c) const { return beyond(off) ? power_for(m) : c; }
+    // a weight of fp32 layers where some row of the wave is beyond (the others keep both parts of c)
+    __device__ __forceinline__ float weight_of(float x, float c, float c_lo) const {
+        return beyond(off) ? __builtin_amdgcn_exp2f(fmaf(x, power_for(m), off)) : weight32(x, c, c_lo, off);
+    }
 };
 
 template <typename ET>
@@ -788,7 +791,7 @@ __global__ __launch_bounds__(64 * Form<ET>::WAVES, 1) void paged_attn_kernel(Att
         tile_keys(r, row0, rows, a.Hg, a.causal, a.window, lo, hi);
         if (cut) piece_keys(x0, x1, t.w, lo, hi);
         // What follows from the lane's number is formed for each piece: kept for all of them it spills (one token over 32768,
-        // bf16: 38 -> 36 us).  Not so for many rows of bf16: a prompt of 1000 tokens takes 53 us, and 61 with it.
+        // bf16: 38.4 -> 37.0 us).  Not so for many rows of bf16: a prompt of 1000 tokens takes 53 us, and 61 with it.
         lo = first_lane(lo);
         hi = first_lane(hi);
         if (bm == ROWS_FEW) few_rows<ET>(Piece<ET>(a, t.f, t.g, lo, hi, lane_now()), smem, rows, cut, rec_row);

@@ -129,9 +129,8 @@ __device__ __forceinline__ void few_rows_of(const Piece<float>& P, uint8_t* smem
                         for (int v = 0; v < 4; ++v) acc[b][half][e][v] *= f;
             }
             if (__any(beyond(run[b].off))) {
-                const float c = run[b].c_of(a.c);
 #pragma unroll
-                for (int v = 0; v < 4; ++v) sc[b][v] = weight32(sc[b][v], c, run[b].off);
+                for (int v = 0; v < 4; ++v) sc[b][v] = run[b].weight_of(sc[b][v], a.c, a.c_lo);
             } else {
 #pragma unroll
                 for (int v = 0; v < 4; ++v) sc[b][v] = weight32(sc[b][v], a.c, a.c_lo, run[b].off);
@@ -273,10 +272,8 @@ __device__ __forceinline__ void many_rows<float>(const Piece<float>& P, uint8_t*
 #pragma unroll
                 for (int k = 0; k < 16; ++k) acc[dt][k] *= f;
         }
-        if (__any(beyond(run.off))) {
-            const float c = run.c_of(a.c);
-            weights32(sc[0], run.l, [&](float x) { return weight32(x, c, run.off); });
-        } else weights32(sc[0], run.l, [&](float x) { return weight32(x, a.c, a.c_lo, run.off); });
+        if (__any(beyond(run.off))) weights32(sc[0], run.l, [&](float x) { return run.weight_of(x, a.c, a.c_lo); });
+        else weights32(sc[0], run.l, [&](float x) { return weight32(x, a.c, a.c_lo, run.off); });
         const uint8_t* vt = M.values_of(j);
         const bool odd = masked && P.anew().odd_values(vt);
         P.values(vt, sc[0], acc, odd);

@@ -263,3 +263,39 @@ def test_attn_long_and_many_tiles(vr, dtype, bad, i):
     torch.cuda.synchronize()
     ref, tol = attn_ref_all(pool, q, s.q_len, s.H, s.causal, s.window)
     within(out, ref, tol, s.name)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("form", FORMS)
+def test_attn_sizes_of_scores_beside_each_other(vr, dtype, form):
+    """One head's scores are beyond what exponents hold, from a late key on, another's hugely negative but for the last keys; the
+    ordinary rows beside them in a wave are as they would be."""
+    import torch
+    q_len, kv_len, width = FORMS[form]
+    m, n = q_len[0], kv_len[0]
+    pool = Pool(kv_len, 1, 32, dtype, seed=15, width=width)
+    far = n - m - 60                                       # the key that is large for head 0
+    for t in range(n):
+        p, i = int(pool.table[0, t // 32]), t % 32
+        pool.k[p, 0, i, 100] = 2.0 ** 20 if t == far else 0
+        pool.k[p, 0, i, 101] = -2.0 ** 20 if t < n - m - 20 else 0
+    q = torch.randn((m, 4, D), generator=torch.Generator().manual_seed(16)).to(tdt(dtype))
+    q[..., 100:102] = 0
+    want = attn_ref(pool, q, q_len, 4)
+    q[:, 0, 100], q[:, 1, 101] = 2.0 ** 30, 2.0 ** 30
+    out = one_call(vr, pool, q, q_len)
+    _, V, _ = pool.rows(0)
+    assert torch.equal(out[:, 0], V[far, 0].double().expand(m, D))
+    within(out[:, 2:], want[0][:, 2:], want[1][:, 2:], "beside")
+    K, _, _ = pool.rows(0)
+    q[:, 1, 101] = 0
+    for i in range(m):                                     # head 1: the last keys alone count
+        see = slice(n - m - 20, n - m + i + 1)
+        k, v, x = K[see, 0].double(), V[see, 0].double(), q[i, 1].double()
+        sc, mag = (k @ x) * D ** -0.5, (k.abs() @ x.abs()) * D ** -0.5
+        w = torch.softmax(sc, 0)
+        o, A = w @ v, w @ v.abs()
+        dx = float((128 * U32 * mag + 3 * U32 * (sc.abs() + sc.abs().max())).max()) + 2 * U32
+        u = U[dtype]
+        e = (u if dtype == "bf16" else 0) * (A + o.abs()) + (4 * dx + (len(k) + 256) * U32) * A
+        within(out[i, 1], o, (e + u * o.abs()) * (1 + u) + 1e-38, "last keys")
