@@ -468,6 +468,72 @@ VARRATE_API int varrate_paged_attn(const varrate_pages* pages, const varrate_bat
 VARRATE_API int varrate_paged_gather(const varrate_pages* pages, const int32_t* table, int32_t width, int64_t n,
                                      void* K, void* V, void* stream);
 
+/* ---- paged cache of 8-bit codes ----------------------------------------------------------
+ * The same life in half the memory: a pool of e4m3 codes (OCP: 4 exponent, 3 mantissa bits, largest
+ * value 448, no infinities), keys and values alike as [n_pages][G][page][d], and one power of two for
+ * each block of 32 tokens and head, as its exponent + 127 in a byte, [n_pages][G][page / 32].  A
+ * value is its code times its block's power, exactly, in fp32 and in bf16.  Tables, batches, bad
+ * entries, strides and streams are as above; rows of new tokens are of `dtype` (bf16 or fp32).
+ *
+ * A block's power is the smallest 2^e, -110 <= e <= 119, that takes the largest magnitude of the rows
+ * appended to it to 448 or less; codes are rounded to nearest, ties to even.  Magnitudes beyond 448 x 2^119 are
+ * held as that.  Infinities and NaN are held as NaN and do not count for the power.
+ * Appending to a block that holds earlier tokens keeps its power or raises it; in the
+ * second case the earlier codes are rounded to the new one.  So sequences that share pages must not
+ * append to the same block, even in different slots, and a power is one of those above (of pools filled
+ * otherwise, others take no part in append, and with them the values are unspecified).              */
+#define VARRATE_BLOCK8 32
+typedef struct varrate_pages8 {
+    void*   k;         /* [n_pages][G][page][d] codes                                        */
+    void*   v;         /* [n_pages][G][page][d] codes                                        */
+    void*   k_scale;   /* [n_pages][G][page / 32] exponents + 127                            */
+    void*   v_scale;   /* [n_pages][G][page / 32]                                            */
+    int64_t n_pages;   /* 1 .. 2^31 - 1                                                      */
+    int32_t G;         /* KV heads, 1 .. 1024                                                */
+    int32_t d;         /* head dim; must be 128                                              */
+    int32_t page;      /* tokens per page: 32, 64, 128 or 256                                */
+    int32_t reserved;  /* 0                                                                  */
+} varrate_pages8;
+
+/* Writes the batch's new key and value rows ([T][G][d], any rotation done) into their slots.        */
+VARRATE_API int varrate_paged8_append(const varrate_pages8* pages, const varrate_batch* batch, int32_t dtype,
+                                      const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
+                                      void* stream);
+
+/* varrate_paged_attn over codes.  lse [T][H] fp32 or NULL: receives each row's ln(sum over the keys that
+ * it sees of exp(scale <q, k>)), -infinity for a row that sees none.                                 */
+VARRATE_API size_t varrate_paged8_attn_workspace_bytes(const varrate_pages8* pages, const varrate_batch* batch,
+                                                       int32_t dtype, int32_t H);
+VARRATE_API int varrate_paged8_attn(const varrate_pages8* pages, const varrate_batch* batch, int32_t dtype, const void* q,
+                                    int64_t q_stride, int32_t H, int32_t causal, int32_t window, float scale, void* out,
+                                    int64_t out_stride, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The weight that the batch's new tokens pay each cached key, added up:
+ *   out[s][g][t] = (mass[s][g][t] if t < kv_len[s] - new tokens, else 0) + sum exp(scale <q, k_t> - lse)
+ * over the sequence's new tokens that see key t and the query heads of KV head g, for t < kv_len[s] (at most L);
+ * what lies behind is left as it was.  lse [T][H] as varrate_paged8_attn gives it for the same call; a row whose
+ * lse is -infinity pays nothing.  mass and out [S][G][L] fp32, which may be the same.  Keys on bad pages are
+ * paid nothing.  Sums are taken in a fixed order.                                                    */
+VARRATE_API int varrate_paged8_mass(const varrate_pages8* pages, const varrate_batch* batch, int32_t dtype, const void* q,
+                                    int64_t q_stride, int32_t H, int32_t causal, int32_t window, float scale,
+                                    const float* lse, const float* mass, float* out, int64_t L, void* stream);
+
+/* Evicts the tokens that are paid least, head by head: of the n = kv_len[s] tokens of a sequence (at most
+ * L and what its table row holds) m = min(n, keep) stay: the first `first`, the last `recent` (first + recent <= keep) and of
+ * the others those of the largest mass (mass [S][G][L]; of equal ones the earlier, NaN last).  Their rows move in order
+ * to slots 0 .. m - 1 of the pages that the rows of `into` name, coded as varrate_paged8_append would code the values
+ * that they stand for; rows of bad pages are zeros, and rows for bad pages are dropped.  into's pages must be no
+ * page of `table`'s.  index [S][G][keep]: the tokens that stay, then -1; mass_out [S][G][keep]: their masses, then 0;
+ * len_out [S]: m.  keep 1 .. 2^30.                                                                  */
+VARRATE_API int varrate_paged8_evict(const varrate_pages8* pages, const int32_t* table, int64_t table_stride, int32_t width,
+                                     const int32_t* kv_len, int32_t S, const float* mass, int64_t L, int64_t keep,
+                                     int64_t first, int64_t recent, const int32_t* into, int64_t into_stride,
+                                     int32_t into_width, int32_t* index, float* mass_out, int32_t* len_out, void* stream);
+
+/* The first n tokens of one sequence, decoded and contiguous: K, V [n][G][d] of dtype.              */
+VARRATE_API int varrate_paged8_gather(const varrate_pages8* pages, const int32_t* table, int32_t width, int64_t n,
+                                      int32_t dtype, void* K, void* V, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

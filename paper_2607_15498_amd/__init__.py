@@ -22,7 +22,9 @@ from ._lib import CHUNK, COEF_PAD, HEAD_DIM  # noqa: F401
 __all__ = ["VarRateError", "Shape", "Cache", "new_cache", "coded_budget", "salience", "allocate",
            "project", "compress", "append_exact", "decode", "decode_noalloc", "QCache", "new_qcache",
            "quantize", "decode_q", "anchor_search", "anchor_encode", "PagedCache", "PagedBatch", "new_pages",
-           "norm_rotate", "paged_append", "paged_attn", "paged_attn_workspace", "paged_gather", "library"]
+           "norm_rotate", "paged_append", "paged_attn", "paged_attn_workspace", "paged_gather",
+           "PagedCache8", "new_pages8", "paged8_append", "paged8_attn", "paged8_attn_workspace", "paged8_mass",
+           "paged8_evict", "paged8_gather", "library"]
 
 
 class VarRateError(RuntimeError):
@@ -744,4 +746,190 @@ def paged_gather(pages: PagedCache, table: torch.Tensor, n: int, K: Optional[tor
     K = torch.empty(shape, dtype=dt, device=dev) if K is None else K
     V = torch.empty(shape, dtype=dt, device=dev) if V is None else V
     _launch(dev, library().varrate_paged_gather, pages.c(), pt, _int32(table.shape[0], "width"), n, K.data_ptr(), V.data_ptr())
+    return K, V
+
+
+# ---------------------------------------------------------------------------------------
+# The paged cache in 8 bits: e4m3 codes with a power of two for each block of 32 tokens and head.  The
+# same batches, tables and streams; keys are rotated (norm_rotate) before they are appended.
+#
+#     pages = new_pages8(n_pages, G=8, page=64)
+#     paged8_append(pages, batch, k, v)
+#     out = paged8_attn(pages, batch, q, lse=lse)
+#     paged8_mass(pages, batch, q, lse, mass)          # what each cached key has been paid so far
+#     index, mass, kv_len = paged8_evict(pages, table, kv_len, mass, keep, into, first=4, recent=32)
+#     K, V = paged8_gather(pages, table[s], n)         # decoded, as compress() takes them
+
+_SCALE_BLOCK = 32
+
+
+class PagedCache8:
+    """A pool of pages of codes: k, v [n_pages][G][page][d] float8_e4m3fn and k_scale, v_scale [n_pages][G][page / 32]
+    float8_e8m0fnu, contiguous device tensors.  They are not to be replaced (calls use their addresses)."""
+
+    __slots__ = ("_k", "_v", "_ks", "_vs", "page", "G", "_c")
+    k = property(lambda self: self._k)
+    v = property(lambda self: self._v)
+    k_scale = property(lambda self: self._ks)
+    v_scale = property(lambda self: self._vs)
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor):
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != torch.float8_e4m3fn or v.dtype != k.dtype:
+            _einval("k and v must be alike, float8_e4m3fn [n_pages][G][page][d]")
+        shape = (k.shape[0], k.shape[1], k.shape[2] // _SCALE_BLOCK)
+        for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+            if t.dtype != torch.float8_e8m0fnu or tuple(t.shape) != shape:
+                _einval(f"{name} must be float8_e8m0fnu {list(shape)}")
+        if any(t.device != k.device for t in (v, k_scale, v_scale)):
+            _einval("codes and scales must be on one device")
+        self._k, self._v, self._ks, self._vs = k, v, k_scale, v_scale
+        self.page, self.G = int(k.shape[2]), int(k.shape[1])
+        self._c = _lib.Pages8C(_dev_ptr(k, name="k"), _dev_ptr(v, name="v"), _dev_ptr(k_scale, name="k_scale"),
+                               _dev_ptr(v_scale, name="v_scale"), k.shape[0], self.G, k.shape[3], self.page, 0)
+
+    def c(self) -> _lib.Pages8C:
+        return self._c
+
+
+def new_pages8(n_pages: int, G: int, page: int = 64, device="cuda") -> PagedCache8:
+    k, v = (torch.zeros((n_pages, G, page, HEAD_DIM), dtype=torch.uint8, device=device).view(torch.float8_e4m3fn)
+            for _ in range(2))
+    ks, vs = (torch.full((n_pages, G, page // _SCALE_BLOCK), 127, dtype=torch.uint8, device=device).view(torch.float8_e8m0fnu)
+              for _ in range(2))
+    return PagedCache8(k, v, ks, vs)
+
+
+def _row_dtype(t: torch.Tensor, name: str) -> int:
+    dt = _DTYPES.get(t.dtype)
+    if dt is None:
+        _einval(f"{name} has dtype {t.dtype}, expected torch.bfloat16 or torch.float32")
+    return dt
+
+
+def _on(batch: PagedBatch, dev):
+    if batch.table.device != dev:
+        _einval(f"the batch must be on {dev}")
+
+
+def paged8_append(pages: PagedCache8, batch: PagedBatch, k: torch.Tensor, v: torch.Tensor) -> PagedCache8:
+    """Code the batch's new rows k, v [T][G][d] (bf16 or fp32; keys rotated) into their sequences' pages."""
+    dev, dt = pages.k.device, _row_dtype(k, "k")
+    T = int(k.shape[0]) if k.dim() else 0
+    pk, sk = _rows(k, k.dtype, None, pages.G, dev, "k")
+    pv, sv = _rows(v, k.dtype, T, pages.G, dev, "v")
+    _on(batch, dev)
+    _launch(dev, library().varrate_paged8_append, pages.c(), batch.c(T), dt, pk, sk, pv, sv)
+    return pages
+
+
+def paged8_attn_workspace(pages: PagedCache8, batch: PagedBatch, T: int, H: int, dtype=torch.bfloat16) -> torch.Tensor:
+    """paged_attn_workspace of paged8_attn with queries of `dtype`."""
+    need = int(library().varrate_paged8_attn_workspace_bytes(pages.c(), batch.c(T), _DTYPES[dtype], H))
+    return torch.empty(max(need, 16), dtype=torch.uint8, device=pages.k.device)
+
+
+def paged8_attn(pages: PagedCache8, batch: PagedBatch, q: torch.Tensor, causal: bool = True, window: int = 0,
+                scale: Optional[float] = None, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """paged_attn over pages of codes, q [T][H][d] bf16 or fp32.  lse: a float32 tensor [T][H] that receives the logarithm of
+    each row's sum of exponentials (-inf where a row sees no key)."""
+    dev, dt = pages.k.device, _row_dtype(q, "q")
+    T, H = (int(q.shape[0]), int(q.shape[1])) if q.dim() == 3 else (0, 0)
+    pq, sq = _rows(q, q.dtype, T, None, dev, "q")
+    _on(batch, dev)
+    if out is None:
+        out = torch.empty((T, H, HEAD_DIM), dtype=q.dtype, device=dev)
+        po, so = out.data_ptr(), H * HEAD_DIM
+    else:
+        po, so = _rows(out, q.dtype, T, H, dev, "out")
+    pl = _f32(lse, ((T, H),), dev, "lse")
+    L, pc, bc = library(), pages.c(), batch.c(T)
+    if workspace is None:
+        nbytes = L.varrate_paged8_attn_workspace_bytes(pc, bc, dt, H)
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+    elif workspace.device != dev or not workspace.is_contiguous():
+        _einval(f"workspace must be a contiguous tensor on {dev}")
+    else:
+        nbytes = workspace.numel() * workspace.element_size()
+    _launch(dev, L.varrate_paged8_attn, pc, bc, dt, pq, sq, H, 1 if causal else 0, _int32(window, "window"),
+            HEAD_DIM ** -0.5 if scale is None else scale, po, so, pl, workspace.data_ptr() if nbytes else 0, nbytes)
+    return out
+
+
+def _masses(t: torch.Tensor, S: int, G: int, device, name: str) -> int:
+    if t.dtype != torch.float32 or t.device != device or t.dim() != 3 or t.shape[:2] != (S, G) or not t.is_contiguous():
+        _einval(f"{name} must be a contiguous float32 tensor [{S}][{G}][tokens] on {device}")
+    return t.data_ptr()
+
+
+def paged8_mass(pages: PagedCache8, batch: PagedBatch, q: torch.Tensor, lse: torch.Tensor, mass: torch.Tensor,
+                causal: bool = True, window: int = 0, scale: Optional[float] = None,
+                out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Add the weight that the batch's new tokens pay each cached key (summed over the query heads of a KV head) to
+    mass [S][G][L] fp32: in place, or into `out`.  Keys that are new in this call start from 0, and what lies behind a
+    sequence's end is left as it was.  q, lse, causal, window and scale as in the paged8_attn of the same tokens."""
+    dev, dt = pages.k.device, _row_dtype(q, "q")
+    T, H = (int(q.shape[0]), int(q.shape[1])) if q.dim() == 3 else (0, 0)
+    pq, sq = _rows(q, q.dtype, T, None, dev, "q")
+    _on(batch, dev)
+    if lse is None:
+        _einval("lse must be given")
+    pl = _f32(lse, ((T, H),), dev, "lse")
+    S = int(batch.table.shape[0])
+    pm = _masses(mass, S, pages.G, dev, "mass")
+    out = mass if out is None else out
+    po = _masses(out, S, pages.G, dev, "out")
+    if out.shape != mass.shape:
+        _einval("out and mass must have one shape")
+    _launch(dev, library().varrate_paged8_mass, pages.c(), batch.c(T), dt, pq, sq, H, 1 if causal else 0,
+            _int32(window, "window"), HEAD_DIM ** -0.5 if scale is None else scale, pl, pm, po, mass.shape[2])
+    return out
+
+
+def paged8_evict(pages: PagedCache8, table: torch.Tensor, kv_len: torch.Tensor, mass: torch.Tensor, keep: int,
+                 into: torch.Tensor, first: int = 0, recent: int = 0):
+    """Keep at most `keep` tokens of every sequence (table [S][width], kv_len [S]), head by head: the first `first`, the last
+    `recent` and those of the largest mass [S][G][L].  Their rows move to the pages of `into` [S][width'] (pages of no
+    sequence in `table`).  Returns the tokens kept (index [S][G][keep] int32, then -1), their masses (then 0) and the new
+    lengths [S]."""
+    dev = pages.k.device
+    pt, pi, pl = _i32(table, 2, "table"), _i32(into, 2, "into"), _i32(kv_len, 1, "kv_len")
+    S = _int32(table.shape[0], "S")
+    if into.shape[0] != S or kv_len.shape[0] != S:
+        _einval(f"into and kv_len must have {S} entries")
+    if any(t.device != dev for t in (table, into, kv_len)):
+        _einval(f"table, into and kv_len must be on {dev}")
+    pm = _masses(mass, S, pages.G, dev, "mass")
+    keep = _int32(keep, "keep")
+    index = torch.empty((S, pages.G, max(keep, 0)), dtype=torch.int32, device=dev)
+    mass_out = torch.empty((S, pages.G, max(keep, 0)), dtype=torch.float32, device=dev)
+    len_out = torch.empty(S, dtype=torch.int32, device=dev)
+    stride = lambda t: t.stride(0) if S > 1 else t.shape[1]
+    _launch(dev, library().varrate_paged8_evict, pages.c(), pt, stride(table), _int32(table.shape[1], "width"), pl, S, pm,
+            mass.shape[2], keep, _int32(first, "first"), _int32(recent, "recent"), pi, stride(into),
+            _int32(into.shape[1], "width of into"), index.data_ptr(), mass_out.data_ptr(), len_out.data_ptr())
+    return index, mass_out, len_out
+
+
+def paged8_gather(pages: PagedCache8, table: torch.Tensor, n: int, dtype=torch.bfloat16, K: Optional[torch.Tensor] = None,
+                  V: Optional[torch.Tensor] = None):
+    """The first n tokens of the sequence with page numbers `table` [width], decoded: K, V [n][G][d] of `dtype`, as
+    compress() takes them."""
+    dev = pages.k.device
+    pt = _i32(table, 1, "table")
+    if table.device != dev:
+        _einval(f"table must be on {dev}")
+    if dtype not in _DTYPES:
+        _einval(f"dtype {dtype} is neither torch.bfloat16 nor torch.float32")
+    n = _int32(n, "n")
+    if n < 0:
+        _einval(f"n={n} is negative")
+    shape = (n, pages.G, HEAD_DIM)
+    for x, name in ((K, "K"), (V, "V")):
+        if x is not None and (x.device != dev or x.dtype != dtype or x.shape != shape or not x.is_contiguous()):
+            _einval(f"{name} must be a contiguous {dtype} tensor {list(shape)} on {dev}")
+    K = torch.empty(shape, dtype=dtype, device=dev) if K is None else K
+    V = torch.empty(shape, dtype=dtype, device=dev) if V is None else V
+    _launch(dev, library().varrate_paged8_gather, pages.c(), pt, _int32(table.shape[0], "width"), n, _DTYPES[dtype],
+            K.data_ptr(), V.data_ptr())
     return K, V

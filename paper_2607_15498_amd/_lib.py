@@ -28,6 +28,8 @@ EXPORTS = (
     "varrate_read_probe",
     "varrate_norm_rotate", "varrate_paged_append", "varrate_paged_attn_workspace_bytes", "varrate_paged_attn",
     "varrate_paged_gather",
+    "varrate_paged8_append", "varrate_paged8_attn_workspace_bytes", "varrate_paged8_attn", "varrate_paged8_mass",
+    "varrate_paged8_evict", "varrate_paged8_gather",
 )
 DECODE_SCRATCH_BYTES = 8 << 20
 
@@ -81,6 +83,12 @@ class JCacheBytes(ctypes.Structure):
 class PagesC(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("G", ctypes.c_int32),
                 ("d", ctypes.c_int32), ("page", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class Pages8C(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int64), ("G", ctypes.c_int32), ("d", ctypes.c_int32), ("page", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
 
 
 class BatchC(ctypes.Structure):
@@ -137,6 +145,15 @@ def load() -> ctypes.CDLL:
         "varrate_paged_attn": (ctypes.c_int, [P(PagesC), P(BatchC), vp, i64, i32, i32, i32, ctypes.c_float, vp, i64,
                                               vp, sz, vp]),
         "varrate_paged_gather": (ctypes.c_int, [P(PagesC), vp, i32, i64, vp, vp, vp]),
+        "varrate_paged8_append": (ctypes.c_int, [P(Pages8C), P(BatchC), i32, vp, i64, vp, i64, vp]),
+        "varrate_paged8_attn_workspace_bytes": (sz, [P(Pages8C), P(BatchC), i32, i32]),
+        "varrate_paged8_attn": (ctypes.c_int, [P(Pages8C), P(BatchC), i32, vp, i64, i32, i32, i32, ctypes.c_float, vp, i64,
+                                               vp, vp, sz, vp]),
+        "varrate_paged8_mass": (ctypes.c_int, [P(Pages8C), P(BatchC), i32, vp, i64, i32, i32, i32, ctypes.c_float, vp, vp, vp,
+                                               i64, vp]),
+        "varrate_paged8_evict": (ctypes.c_int, [P(Pages8C), vp, i64, i32, vp, i32, vp, i64, i64, i64, i64, vp, i64, i32, vp,
+                                                vp, vp, vp]),
+        "varrate_paged8_gather": (ctypes.c_int, [P(Pages8C), vp, i32, i64, i32, vp, vp, vp]),
         "varrate_read_probe": (ctypes.c_int, [vp, ctypes.c_size_t, vp, vp]),
     }
     for name, (res, args) in sig.items():

@@ -767,4 +767,128 @@ int varrate_paged_gather(const varrate_pages* pg, const int32_t* table, int32_t 
     return hip_status(launch_paged_gather(*pg, table, n, K, V, (hipStream_t)stream), "paged gather launch");
 }
 
+// ---- paged cache of 8-bit codes -----------------------------------------------------------------
+
+static int check_pages8(const varrate_pages8* pg) {
+    if (!pg) return fail(VARRATE_EINVAL, "pages is NULL");
+    if (pg->d != VARRATE_HEAD_DIM) return fail(VARRATE_EUNSUPPORTED, "head dim %d != 128", pg->d);
+    if (pg->G < 1 || pg->G > 1024) return fail(VARRATE_EINVAL, "G=%d outside [1, 1024]", pg->G);
+    if (pg->page < VARRATE_BLOCK8 || pg->page > PAGE_MAX || (pg->page & (pg->page - 1)) != 0)
+        return fail(VARRATE_EUNSUPPORTED, "page=%d: need a power of two in [32, 256]", pg->page);
+    if (pg->n_pages < 1 || pg->n_pages > INT32_MAX)
+        return fail(VARRATE_EINVAL, "n_pages=%lld outside [1, 2^31 - 1]", (long long)pg->n_pages);
+    if (pg->reserved != 0) return fail(VARRATE_EINVAL, "reserved must be 0");
+    if (!pg->k || !pg->v || !pg->k_scale || !pg->v_scale) return fail(VARRATE_EINVAL, "pages has a NULL buffer");
+    if (!aligned16(pg->k) || !aligned16(pg->v)) return fail(VARRATE_EINVAL, "page buffers must be 16-byte aligned");
+    return VARRATE_OK;
+}
+
+static int check_paged8(const varrate_pages8* pg, const varrate_batch* b, int32_t dtype) {
+    int rc = check_pages8(pg);
+    if (rc || (rc = check_batch(b, pg->page))) return rc;
+    return check_dtype(dtype);
+}
+
+static int check_paged8_heads(const varrate_pages8* pg, const varrate_batch* b, int32_t dtype, int32_t H) {
+    int rc = check_paged8(pg, b, dtype);
+    if (rc) return rc;
+    if (H < 1) return fail(VARRATE_EINVAL, "H=%d must be >= 1", H);
+    if (H % pg->G != 0) return fail(VARRATE_EUNSUPPORTED, "H=%d is not a multiple of G=%d", H, pg->G);
+    return check_rows_total(b->T, H);
+}
+
+static int check_attn_options(int32_t causal, int32_t window, float scale) {
+    if (causal != 0 && causal != 1) return fail(VARRATE_EINVAL, "causal=%d outside {0, 1}", causal);
+    if (window < 0 || window > (1 << 30)) return fail(VARRATE_EINVAL, "window=%d outside [0, 2^30]", window);
+    if (window && !causal) return fail(VARRATE_EUNSUPPORTED, "a window without causal order");
+    if (!(scale >= 0x1p-100f && scale <= 0x1p100f)) return fail(VARRATE_EINVAL, "scale outside [2^-100, 2^100]");
+    return VARRATE_OK;
+}
+
+static int check_words(const void* p, bool needed, const char* name) {
+    if ((needed && !p) || ((uintptr_t)p & 3u))
+        return fail(VARRATE_EINVAL, "%s must be%s 4-byte aligned", name, needed ? " non-NULL and" : "");
+    return VARRATE_OK;
+}
+
+int varrate_paged8_append(const varrate_pages8* pg, const varrate_batch* b, int32_t dtype, const void* k_new, int64_t k_stride,
+                          const void* v_new, int64_t v_stride, void* stream) {
+    int rc = check_paged8(pg, b, dtype);
+    if (rc || (rc = check_rows_total(b->T, 2 * pg->G))) return rc;
+    if (b->T == 0) return VARRATE_OK;
+    if ((rc = check_rows(k_new, k_stride, b->T, pg->G, dtype, false, "k_new")) ||
+        (rc = check_rows(v_new, v_stride, b->T, pg->G, dtype, false, "v_new"))) return rc;
+    return hip_status(launch_paged8_append(*pg, *b, dtype, k_new, k_stride, v_new, v_stride, (hipStream_t)stream),
+                      "8-bit paged append launch");
+}
+
+size_t varrate_paged8_attn_workspace_bytes(const varrate_pages8* pg, const varrate_batch* b, int32_t dtype, int32_t H) {
+    if (check_paged8_heads(pg, b, dtype, H) || b->T == 0) return 0;
+    return paged8_attn_ws_bytes(b->T, b->S, pg->G, H, dtype, (int64_t)b->width * pg->page);
+}
+
+int varrate_paged8_attn(const varrate_pages8* pg, const varrate_batch* b, int32_t dtype, const void* q, int64_t q_stride,
+                        int32_t H, int32_t causal, int32_t window, float scale, void* out, int64_t out_stride, float* lse,
+                        void* ws, size_t ws_bytes, void* stream) {
+    int rc = check_paged8_heads(pg, b, dtype, H);
+    if (rc || (rc = check_attn_options(causal, window, scale)) || (rc = check_words(lse, false, "lse"))) return rc;
+    if (b->T == 0) return VARRATE_OK;
+    if ((rc = check_rows(q, q_stride, b->T, H, dtype, false, "q")) ||
+        (rc = check_rows(out, out_stride, b->T, H, dtype, true, "out"))) return rc;
+    if (q == out) return fail(VARRATE_EINVAL, "out is q");
+    const size_t need = paged8_attn_ws_bytes(b->T, b->S, pg->G, H, dtype, (int64_t)b->width * pg->page);
+    if (need && (rc = ws_check(ws, ws_bytes, need))) return rc;
+    return hip_status(launch_paged8_attn(*pg, *b, dtype, q, q_stride, H, causal, window, scale, out, out_stride, lse, ws,
+                                         (hipStream_t)stream),
+                      "8-bit paged attention launch");
+}
+
+int varrate_paged8_mass(const varrate_pages8* pg, const varrate_batch* b, int32_t dtype, const void* q, int64_t q_stride,
+                        int32_t H, int32_t causal, int32_t window, float scale, const float* lse, const float* mass, float* out,
+                        int64_t L, void* stream) {
+    int rc = check_paged8_heads(pg, b, dtype, H);
+    if (rc || (rc = check_attn_options(causal, window, scale))) return rc;
+    if (L < 1 || L > (1 << 30)) return fail(VARRATE_EINVAL, "L=%lld outside [1, 2^30]", (long long)L);
+    if ((rc = check_words(mass, true, "mass")) || (rc = check_words(out, true, "out"))) return rc;
+    if (b->T && ((rc = check_rows(q, q_stride, b->T, H, dtype, false, "q")) || (rc = check_words(lse, true, "lse")))) return rc;
+    return hip_status(launch_paged8_mass(*pg, *b, dtype, q, q_stride, H, causal, window, scale, lse, mass, out, L,
+                                         (hipStream_t)stream),
+                      "8-bit paged attention mass launch");
+}
+
+int varrate_paged8_evict(const varrate_pages8* pg, const int32_t* table, int64_t table_stride, int32_t width,
+                         const int32_t* kv_len, int32_t S, const float* mass, int64_t L, int64_t keep, int64_t first,
+                         int64_t recent, const int32_t* into, int64_t into_stride, int32_t into_width, int32_t* index,
+                         float* mass_out, int32_t* len_out, void* stream) {
+    int rc = check_pages8(pg);
+    if (rc || (rc = check_width(width, pg->page)) || (rc = check_width(into_width, pg->page))) return rc;
+    if (S < 1 || S > 65536) return fail(VARRATE_EINVAL, "S=%d outside [1, 65536]", S);
+    if (table_stride < 0 || into_stride < 0) return fail(VARRATE_EINVAL, "a table stride is negative");
+    if (L < 1 || L > (1 << 30)) return fail(VARRATE_EINVAL, "L=%lld outside [1, 2^30]", (long long)L);
+    if (keep < 1 || keep > (int64_t)into_width * pg->page)
+        return fail(VARRATE_EINVAL, "keep=%lld outside [1, %lld], what a row of into holds", (long long)keep,
+                    (long long)into_width * pg->page);
+    if (first < 0 || recent < 0 || first > keep || recent > keep - first)
+        return fail(VARRATE_EINVAL, "first=%lld and recent=%lld: together 0 .. keep", (long long)first, (long long)recent);
+    if ((rc = check_words(table, true, "table")) || (rc = check_words(into, true, "into")) ||
+        (rc = check_words(kv_len, true, "kv_len")) || (rc = check_words(mass, true, "mass")) ||
+        (rc = check_words(index, true, "index")) || (rc = check_words(mass_out, true, "mass_out")) ||
+        (rc = check_words(len_out, true, "len_out"))) return rc;
+    if (mass_out == mass || len_out == kv_len) return fail(VARRATE_EINVAL, "an output is an input");
+    const Evict8Args e = {table, into, kv_len, table_stride, into_stride, mass, index, mass_out, len_out, L, keep, first, recent, S,
+                          width};
+    return hip_status(launch_paged8_evict(*pg, e, (hipStream_t)stream), "8-bit paged eviction launch");
+}
+
+int varrate_paged8_gather(const varrate_pages8* pg, const int32_t* table, int32_t width, int64_t n, int32_t dtype, void* K,
+                          void* V, void* stream) {
+    int rc = check_pages8(pg);
+    if (rc || (rc = check_width(width, pg->page)) || (rc = check_dtype(dtype)) || (rc = check_words(table, true, "table"))) return rc;
+    if (n < 0 || n > (int64_t)width * pg->page)
+        return fail(VARRATE_EINVAL, "n=%lld outside [0, width page = %lld]", (long long)n, (long long)width * pg->page);
+    if (n == 0) return VARRATE_OK;
+    if (!K || !V || !aligned16(K) || !aligned16(V)) return fail(VARRATE_EINVAL, "K and V must be non-NULL and 16-byte aligned");
+    return hip_status(launch_paged8_gather(*pg, table, n, dtype, K, V, (hipStream_t)stream), "8-bit paged gather launch");
+}
+
 }  // extern "C"

@@ -1,0 +1,451 @@
+// Attention over pages of e4m3 codes: what its bf16 and fp32 queries share.  paged_attn.h has the rest: the call's cut,
+// masks, running sums, stages and the second launch.
+//
+// A code times its block's power of two is a bf16 number, so that keys and values are turned into bf16 fragments in
+// registers without an error, the scale with the conversion, and everything behind that is the raw cache's.  fp32 queries
+// and weights are three bf16 parts each (8 + 8 + 8 bits, cut off rather than rounded, so that the parts are exact), whose products
+// the matrix cores sum in fp32.
+//   The scaled products of codes themselves (f8f6f4), with queries in parts, take no conversions, but sum their 64 products to
+//   about 12 bits only (errors up to 3e-4 of the sum of magnitudes, measured), too few for scores.
+//
+// A row is 128 bytes; row r's 16-byte piece c lies at place c ^ f(r), f(r) = bits 1, 3 and 2 of r as 2, 4 and 1: 16 rows'
+// reads of one piece (keys) and 8 rows' of two (values, transposed 8 x 16 bytes at a time) fall into different banks.
+#pragma once
+#include "paged_attn.h"
+
+namespace vr {
+
+typedef int pa_i32x2 __attribute__((ext_vector_type(2)));
+
+// 8 codes times scale, as a bf16 fragment
+__device__ __forceinline__ u32x4 decode8(uint2 w, float scale) {
+    u32x4 f;
+    f[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w.x, scale, false));
+    f[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w.x, scale, true));
+    f[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w.y, scale, false));
+    f[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w.y, scale, true));
+    return f;
+}
+// the upper halves of two numbers, packed, and what they lack
+__device__ __forceinline__ uint32_t cut2(float& a, float& b) {
+    const uint32_t x = __float_as_uint(a) & 0xFFFF0000u, y = __float_as_uint(b) & 0xFFFF0000u;
+    a -= __uint_as_float(x);
+    b -= __uint_as_float(y);
+    return x >> 16 | y;
+}
+
+// A row's query (src) as B operands, in parts: fragment 2 j + b is dims 16 (2 j + h) + 8 b ..
+template <typename Q>
+__device__ __forceinline__ void load_query(const Q* src, int h, u32x4 (&qf)[Form<Coded<Q>>::NP][8]) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const Q* at = src + 16 * (2 * (k >> 1) + h) + 8 * (k & 1);
+        if constexpr (sizeof(Q) == 2) qf[0][k] = load16(at);
+        else {
+            float x[8];
+            *reinterpret_cast<f32x4*>(x) = *reinterpret_cast<const f32x4*>(at);
+            *reinterpret_cast<f32x4*>(x + 4) = *reinterpret_cast<const f32x4*>(at + 4);
+#pragma unroll
+            for (int p = 0; p < 3; ++p)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) qf[p][k][e] = cut2(x[2 * e], x[2 * e + 1]);
+        }
+    }
+}
+
+template <typename Q>
+struct Piece<Coded<Q>> : PieceOf<Coded<Q>> {
+    typedef Form<Coded<Q>> F;
+    typedef PieceOf<Coded<Q>> P;
+    using P::a;
+    using P::g;
+    using P::h;
+    using P::l32;
+    using P::lane;
+    using P::r;
+    using P::sees;
+    using typename P::Seen;
+    uint32_t off0, kaddr;
+
+    __device__ __forceinline__ Piece(const AttnArgs& a_, const Found& f, int g_, int32_t lo_, int32_t hi_, int lane_)
+        : P(a_, f, g_, lo_, hi_, lane_) {
+        const int lrow = lane >> 3;
+        off0 = (uint32_t)(lrow * F::ROWB + ((lane & 7) ^ swizzle(lrow)) * 16);
+        kaddr = (uint32_t)(l32 * F::ROWB + (h ^ swizzle(l32)) * 16);
+    }
+    static __device__ __forceinline__ int swizzle(int row) { return (row & 2) | ((row >> 2) & 1) | ((row >> 1) & 4); }
+    __device__ __forceinline__ Piece anew() const {
+        Piece p = *this;
+        asm volatile("" : "+v"(p.lane), "+v"(p.l32), "+v"(p.h));
+        return p;
+    }
+    // the scale of the block of key t on page p (1 where there is none)
+    __device__ __forceinline__ float scale_of(int32_t p, int32_t t, bool values) const {
+        if (p < 0) return 1.f;
+        const int sh = a.shift - 5;
+        const uint8_t* at = values ? a.vscale : a.kscale;
+        return __uint_as_float((uint32_t)at[(((int64_t)p * a.G + g) << sh) + ((t >> 5) & ((1 << sh) - 1))] << 23);
+    }
+    // 1 KB number v of the rows at src into LDS; row 0 of number 0 is row 4 `quad` of its block
+    template <bool VALUES, bool ONCE = false>
+    __device__ __forceinline__ void bring1(const uint8_t* src, int adv, int v, int quad, uint32_t dst) const {
+        lds_load<ONCE>(src + v * adv, off0 ^ (((uint32_t)(quad >> 1) + v) & 1u) << 6, dst + v * 1024);
+    }
+    // values behind the end in the rows [r0, r1) of a tile of keys from t0 on: not read as data
+    __device__ __forceinline__ void clear_tail(int32_t t0, int32_t r0, int32_t r1, uint8_t* vt) const {
+        const int32_t end = r.klen - t0, from = end > r0 ? end : r0;
+        for (int i = lane; i < (r1 - from) * F::PPR; i += 64)
+            *reinterpret_cast<uint4*>(vt + from * F::ROWB + 16 * i) = uint4{0, 0, 0, 0};
+    }
+    __device__ __forceinline__ void query(u32x4 (&qf)[F::NP][F::NF], int64_t token, int head) const {
+        load_query<Q>((const Q*)a.q + token * a.q_stride + (int64_t)head * D, h, qf);
+    }
+    // scores of NC blocks of 32 rows with 32 keys of one scale, the smallest parts first
+    template <int NC>
+    __device__ __forceinline__ void scores(const uint8_t* kt, float scale, const u32x4 (&qf)[NC][F::NP][F::NF], f32x16 (&sc)[NC]) const {
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sc[c][i] = 0.f;
+        u32x4 kf[F::NF];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const u32x4 w = *reinterpret_cast<const u32x4*>(kt + (kaddr ^ (32u * j)));
+            kf[2 * j] = decode8(uint2{w[0], w[1]}, scale);
+            kf[2 * j + 1] = decode8(uint2{w[2], w[3]}, scale);
+        }
+#pragma unroll
+        for (int p = F::NP - 1; p >= 0; --p)
+#pragma unroll
+            for (int k = 0; k < F::NF; ++k)
+#pragma unroll
+                for (int c = 0; c < NC; ++c) sc[c] = mfma32(kf[k], qf[c][p][k], sc[c]);
+    }
+    // codes of a V^T fragment: keys r0 + 4 h + 0..3 and r0 + 8 + 4 h + 0..3, dim 32 dt + l32
+    __device__ __forceinline__ uint2 vcodes(const uint8_t* vt, int r0, int dt) const {
+        const int rr = (lane & 15) >> 1, row = r0 + 8 * (rr >> 2) + 4 * h + (rr & 3);
+        const int place = (2 * dt + ((lane >> 4) & 1)) ^ swizzle(row);
+        return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+            (__attribute__((address_space(3))) pa_i32x2*)(vt + row * F::ROWB + place * 16 + (lane & 1) * 8)));
+    }
+    static __device__ __forceinline__ uint32_t finite(uint32_t x) { return Piece<uint16_t>::finite(x); }
+    // acc += V^T P^T of 32 keys of one scale; p: the weights' parts, packed in pairs.  FINITE: of the values that are numbers alone.
+    template <int NC, int WP, bool FINITE = false>
+    __device__ __forceinline__ void values(const uint8_t* vt, float scale, const u32x4 (&p)[NC][WP][2], f32x16 (&acc)[NC][4]) const {
+#pragma unroll
+        for (int mm = 0; mm < 2; ++mm)
+#pragma unroll
+            for (int dt = 0; dt < 4; ++dt) {
+                u32x4 f = decode8(vcodes(vt, 16 * mm, dt), scale);
+                if constexpr (FINITE)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) f[k] = finite(f[k]);
+#pragma unroll
+                for (int n = WP - 1; n >= 0; --n)
+#pragma unroll
+                    for (int c = 0; c < NC; ++c) acc[c][dt] = mfma32(f, p[c][n][mm], acc[c][dt]);
+            }
+    }
+    // As the raw cache's: NaN (codes have no infinities) among values of keys that some row does not see.
+    __device__ __forceinline__ bool odd_values(const uint8_t* vt) const {
+        uint32_t odd = 0;
+        for (int i = lane; i < F::KB / 16; i += 64) {
+            const u32x4 w = *reinterpret_cast<const u32x4*>(vt + 16 * i);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) odd |= ((w[k] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+        }
+        return __ballot(odd != 0) != 0;
+    }
+    // add(dt, i, x): x to the lane's sum of dim 32 dt + 8 (i / 4) + 4 h + i % 4
+    template <typename A>
+    __device__ __forceinline__ void add_odd(const uint8_t* vt, int32_t t0, Seen s, uint32_t gm, A&& add) const {
+#pragma unroll 1
+        for (int kk = 0; kk < 32; ++kk) {
+            const bool see = sees(t0 + kk, s) && (gm >> (kk >> 4) & 1u);
+#pragma unroll
+            for (int n = 0; n < 16; ++n) {                 // four dims
+                const int byte = 8 * n + 4 * h;
+                const uint32_t w = *reinterpret_cast<const uint32_t*>(vt + kk * F::ROWB + (((byte >> 4) ^ swizzle(kk)) << 4) + (byte & 15));
+#pragma unroll
+                for (int k = 0; k < 4; ++k) add(n >> 2, 4 * (n & 3) + k, see && (w >> (8 * k) & 0x7Fu) == 0x7Fu ? NAN : 0.f);
+            }
+        }
+    }
+};
+
+// A step's weights of a row, in place, and their sum (of the weights themselves, so that its logarithm is the row's).
+template <typename Q>
+__device__ __forceinline__ void weights8(f32x16& sc, const Running& run, const AttnArgs& a, float& l) {
+    if (__any(beyond(run.off))) weights32(sc, l, [&](float x) { return run.weight_of(x, a.c, a.c_lo); });
+    else if constexpr (sizeof(Q) == 2) weights32(sc, l, [&](float x) { return __builtin_amdgcn_exp2f(fmaf(x, a.c, run.off)); });
+    else weights32(sc, l, [&](float x) { return weight32(x, a.c, a.c_lo, run.off); });
+}
+// As the value products take them: fp32 in three exact parts,
+__device__ __forceinline__ void parts_of(f32x16& sc, u32x4 (&p)[3][2]) {
+#pragma unroll
+    for (int n = 0; n < 3; ++n)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            float x = sc[2 * k], y = sc[2 * k + 1];
+            p[n][k >> 2][k & 3] = cut2(x, y);
+            sc[2 * k] = x;
+            sc[2 * k + 1] = y;
+        }
+}
+// bf16 rounded, or rounded and what that takes away, rounded: 2^-17 of a weight is missing.
+__device__ __forceinline__ void parts_of(f32x16& sc, u32x4 (&p)[1][2]) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) p[0][k >> 2][k & 3] = cvt_bf16x2(sc[2 * k], sc[2 * k + 1]);
+}
+__device__ __forceinline__ void parts_of(f32x16& sc, u32x4 (&p)[2][2]) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const uint32_t w = p[0][k >> 2][k & 3] = cvt_bf16x2(sc[2 * k], sc[2 * k + 1]);
+        p[1][k >> 2][k & 3] = cvt_bf16x2(sc[2 * k] - bf_lo(w), sc[2 * k + 1] - bf_hi(w));
+    }
+}
+
+// Few rows: each wave takes every WAVES-th tile of 32 keys out of a ring of its own, RING - 1 of them on their way, and the
+// waves' sums are joined at the end.
+template <typename Q>
+__device__ __forceinline__ void few_rows8(const Piece<Coded<Q>>& P, uint8_t* smem, int rows, bool cut, int64_t rec_row) {
+    typedef Form<Coded<Q>> F;
+    constexpr int NW = F::WAVES, RING = F::RING, L = F::KB / 1024, step = 32 * NW;
+    const AttnArgs& a = P.a;
+    const SeqRange& r = P.r;
+    const int wave = first_lane((int)(threadIdx.x >> 6)), lane = P.lane, l32 = P.l32, h = P.h;
+    const int Hg = a.Hg, g = P.g, lo = P.lo, hi = P.hi;
+    uint8_t* ring = smem + wave * RING * 2 * F::KB;
+    const uint32_t ring0 = first_lane((int)(uint32_t)(size_t)(__attribute__((address_space(3))) uint8_t*)ring);
+    // bf16: weights in two parts; up to 16 rows leave half of a product's columns to the second, the same rows again
+    const bool halves = F::NP == 1 && rows <= 16;
+    const int col = halves ? l32 & 15 : l32, myrow = col < rows ? col : 0, tok = myrow / Hg;
+    int32_t mylo, myhi, firsthi, lastlo, x;
+    row_keys(r, tok, a.causal, a.window, mylo, myhi);
+    const auto seen = P.seen(mylo, myhi);
+    row_keys(r, 0, a.causal, a.window, x, firsthi);
+    row_keys(r, (rows - 1) / Hg, a.causal, a.window, lastlo, x);
+    u32x4 qf[1][F::NP][F::NF];
+    P.query(qf[0], r.q0 + tok, g * Hg + myrow % Hg);
+    Running run;
+    const float slack = SLACK / a.c;
+    f32x16 acc[1][4], sc[1];
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[0][dt][i] = 0.f;
+
+    // pages and scales of the wave's next 32 tiles: lane 2 i has the page and the keys' scale of tile i, lane 2 i + 1 the values'
+    int32_t window = 0;
+    float scales = 1.f;
+    int at = 32;
+    int32_t page[RING];                                    // of the tiles that are on their way, the next to be used first
+    float ks[RING], vs[RING];
+#pragma unroll
+    for (int i = 0; i < RING; ++i) {
+        page[i] = -1;
+        ks[i] = vs[i] = 1.f;
+    }
+    auto issue = [&](int32_t t, int slot) {
+        if (at == 32) {
+            const int32_t tl = t + (lane >> 1) * step;
+            window = tl < hi ? P.page_of(P.raw_page(tl), tl) : -1;
+            scales = P.scale_of(window, tl, lane & 1);
+            at = 0;
+        }
+#pragma unroll
+        for (int i = 0; i + 1 < RING; ++i) {
+            page[i] = page[i + 1];
+            ks[i] = ks[i + 1];
+            vs[i] = vs[i + 1];
+        }
+        const int32_t pg = page[RING - 1] = __builtin_amdgcn_readlane(window, 2 * at);
+        ks[RING - 1] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scales), 2 * at));
+        vs[RING - 1] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scales), 2 * at + 1));
+        ++at;
+        const uint32_t dst = ring0 + slot * 2 * F::KB;
+        const uint8_t *k = P.rows_at(P.kbase, pg, t), *v = P.rows_at(P.vbase, pg, t);
+        const int adv = P.advance(pg);
+#pragma unroll
+        for (int i = 0; i < L; ++i) P.template bring1<false, true>(k, adv, i, 0, dst + 0);
+#pragma unroll
+        for (int i = 0; i < L; ++i) P.template bring1<true, true>(v, adv, i, 0, dst + F::KB);
+    };
+    int32_t t0 = (lo & ~31) + 32 * wave;
+    if (t0 < hi)
+#pragma unroll
+        for (int i = 0; i + 1 < RING; ++i) issue(t0 + i * step, i);
+    for (int st = 0; t0 < hi; t0 += step, st = (st + 1) % RING) {
+        uint8_t* kt = ring + st * 2 * F::KB;
+        wait_lds();                                        // the tile before has been read
+        issue(t0 + (RING - 1) * step, (st + RING - 1) % RING);     // (behind the piece: zeros, so that the counts stay)
+        const uint32_t gm = page[0] >= 0 ? 3u : 0u;
+        const bool masked = t0 < lastlo || t0 < lo || t0 + 32 > firsthi || t0 + 32 > hi || gm != 3u;
+        wait_loads<2 * L * (RING - 1) + L>();
+        P.template scores<1>(kt, ks[0], qf, sc);
+        if (masked) P.anew().mask(sc[0], t0, seen, gm);
+        const float mt = P.most(sc[0]);
+        if (__any(mt > run.m + slack)) {
+            const float f = run.raise(mt, a.c);
+#pragma unroll
+            for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[0][dt][i] *= f;
+        }
+        weights8<Q>(sc[0], run, a, run.l);
+        constexpr int WP = F::NP == 1 ? 2 : 3;
+        u32x4 p[1][WP][2];
+        parts_of(sc[0], p[0]);
+        wait_loads<2 * L * (RING - 1)>();
+        uint8_t* vt = kt + F::KB;
+        P.clear_tail(t0, 0, 32, vt);
+        const bool odd = masked && P.anew().odd_values(vt);
+        if (halves) {
+            u32x4 half[1][1][2];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) half[0][0][k >> 2][k & 3] = l32 < 16 ? p[0][0][k >> 2][k & 3] : p[0][1][k >> 2][k & 3];
+            if (odd) P.anew().template values<1, 1, true>(vt, vs[0], half, acc);
+            else P.template values<1, 1>(vt, vs[0], half, acc);
+        } else {
+            if (odd) P.anew().template values<1, WP, true>(vt, vs[0], p, acc);
+            else P.template values<1, WP>(vt, vs[0], p, acc);
+        }
+        if (odd) P.anew().add_odd(vt, t0, seen, gm, [&](int dt, int i, float y) { acc[0][dt][i] += y; });
+    }
+    wait_loads<0>();
+    run.l = xsum32(run.l);
+    __syncthreads();                                       // every wave is done with its ring
+    float* js = (float*)smem;                              // [NW][32][132] sums
+    float* jm = js + NW * 32 * 132;                        // [NW][32][2]
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+            *reinterpret_cast<f32x4*>(js + (wave * 32 + l32) * 132 + 32 * dt + 2 * i + 4 * h) =
+                f32x4{acc[0][dt][i], acc[0][dt][i + 1], acc[0][dt][i + 2], acc[0][dt][i + 3]};
+    if (h == 0) *reinterpret_cast<float2*>(jm + (wave * 32 + l32) * 2) = float2{run.m, run.l};
+    __syncthreads();
+    // A thread's PER dims: of one of 32 rows, or half as many of one of 16 and of its rests
+    constexpr int PER = 64 / NW;
+    const int of_row = halves ? 2 * D / PER : D / PER, row = (int)threadIdx.x / of_row, own = halves ? PER / 2 : PER;
+    const int d0 = (int)threadIdx.x % of_row * own;
+    if (row < rows) {
+        float mw[NW], lw[NW], M = -INFINITY, Ls = 0.f, o[PER];
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const float2 v = *reinterpret_cast<const float2*>(jm + (w * 32 + row) * 2);
+            mw[w] = v.x;
+            lw[w] = v.y;
+            M = fmaxf(M, v.x);
+        }
+        const float to = off_of(M, a.c);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) o[i] = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const float f = rescale(mw[w], M, to, a.c);
+            Ls = fmaf(f, lw[w], Ls);
+#pragma unroll
+            for (int i = 0; i < PER; i += 4) {
+                const int at4 = halves && i >= PER / 2 ? 16 * 132 + i - PER / 2 : i;
+                const f32x4 v = *reinterpret_cast<const f32x4*>(js + (w * 32 + row) * 132 + d0 + at4);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) o[i + k] = fmaf(f, v[k], o[i + k]);
+            }
+        }
+        if (halves)                                        // (an infinite sum times a rest is no number)
+#pragma unroll
+            for (int i = 0; i < PER / 2; ++i) o[i] += fabsf(o[i]) < INFINITY ? o[i + PER / 2] : 0.f;
+        if (cut) {
+            float* dst = a.rec + (rec_row + row) * D + d0;
+#pragma unroll
+            for (int i = 0; i < PER; i += 4)
+                if (i < own) *reinterpret_cast<f32x4*>(dst + i) = f32x4{o[i], o[i + 1], o[i + 2], o[i + 3]};
+            if (d0 == 0) *reinterpret_cast<float2*>(a.rec + a.rec_rows * D + (rec_row + row) * 2) = float2{M, Ls};
+        } else {
+            const float inv = Ls == 0.f ? 0.f : 1.f / Ls;
+            const int64_t token = r.q0 + row / Hg;
+            const int head = g * Hg + row % Hg;
+            Q* dst = (Q*)a.out + token * a.out_stride + (int64_t)head * D + d0;
+#pragma unroll
+            for (int i = 0; i < PER; i += 4)
+                if (i < own) store4<Q>(dst + i, o[i] * inv, o[i + 1] * inv, o[i + 2] * inv, o[i + 3] * inv);
+            if (a.lse && d0 == 0) a.lse[token * (a.G * Hg) + head] = lse_of(M, Ls, a.c);
+        }
+    }
+    __syncthreads();                                       // the rings are free again
+}
+
+// Many rows, one step after another.
+template <typename Q>
+__device__ __forceinline__ void many_rows8(const Piece<Coded<Q>>& P, uint8_t* smem, int32_t row0, int32_t rows, bool cut, int64_t rec_row) {
+    typedef Form<Coded<Q>> F;
+    constexpr int NC = F::NC;
+    const AttnArgs& a = P.a;
+    Many<Coded<Q>> M(P, smem, row0, rows);
+    if (M.stages) M.begin();
+    Running run[NC];
+    u32x4 qf[NC][F::NP][F::NF];
+    f32x16 acc[NC][4], sc[NC];
+    typename Piece<Coded<Q>>::Seen seen[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+        int32_t tok, head;
+        M.row_of(c, P.l32, tok, head);
+        P.query(qf[c], P.r.q0 + tok, head);
+        seen[c] = M.keys_seen(c);
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[c][dt][i] = 0.f;
+    }
+    const float slack = SLACK / a.c;
+    for (int j = 0; j < F::SPS * M.stages; ++j) {
+        if (j % F::SPS == 0) {
+            M.arrive(j / F::SPS);
+            M.issue(j / F::SPS + 2);
+        }
+        if (j < M.jf || j >= M.jl) continue;
+        const float scale = M.scale[j >> 5 & 1];
+        const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scale), j & 31));
+        const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scale), 32 + (j & 31)));
+        P.template scores<NC>(M.keys_of(j), ks, qf, sc);
+        const bool masked = M.masked(j);
+        const int32_t t0 = M.t_first + 32 * j;
+        u32x4 p[NC][F::NP][2];                             // (bf16: rounded, as a chunk's matrix products are what it costs)
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            if (masked) P.anew().mask(sc[c], t0, seen[c], M.gm_of(j));
+            const float mt = P.most(sc[c]);
+            if (__any(mt > run[c].m + slack)) {
+                const float f = run[c].raise(mt, a.c);
+#pragma unroll
+                for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[c][dt][i] *= f;
+            }
+            weights8<Q>(sc[c], run[c], a, run[c].l);
+            parts_of(sc[c], p[c]);
+        }
+        const uint8_t* vt = M.values_of(j);
+        const bool odd = masked && P.anew().odd_values(vt);
+        if (odd) {
+            P.anew().template values<NC, F::NP, true>(vt, vs, p, acc);
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+                P.anew().add_odd(vt, t0, seen[c], M.gm_of(j), [&](int dt, int i, float x) { acc[c][dt][i] += x; });
+        } else P.template values<NC, F::NP>(vt, vs, p, acc);
+    }
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+        const float l = xsum32(run[c].l);
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt) M.put(c, dt, acc[c][dt], run[c], l, cut, rec_row, dt == 3);
+    }
+    M.finish();
+}
+
+hipError_t launch_paged8_bf16(const AttnArgs& a, int groups, hipStream_t st);
+hipError_t launch_paged8_f32(const AttnArgs& a, int groups, hipStream_t st);
+
+}  // namespace vr

@@ -27,7 +27,23 @@ struct AttnArgs {
     int32_t causal, window;
     Costs costs;
     float c, c_lo;                  // softmax scale x log2 e, and what c lacks of it (fp32 layers)
+    // pages of codes: their scales [n_pages][G][page / 32], and where the logarithms of the rows' sums go ([T][H], or null)
+    const uint8_t *kscale, *vscale;
+    float* lse;
 };
+
+// Pages of e4m3 codes, read by queries of type Q (paged8_attn.h).
+template <typename Q> struct Coded {};
+
+constexpr float LOG2E = 1.4426950408889634f, LOG2E_LO = (float)(1.44269504088896340736 - (double)LOG2E);
+
+// scale x log2 e as c and what c lacks of it, > 0, so that a masked score stays -infinity
+inline void split_scale(float scale, float& c, float& c_lo) {
+    const double x = (double)scale * 1.4426950408889634;
+    c = (float)x;
+    if ((double)c >= x) c = nextafterf(c, 0.f);
+    c_lo = (float)(x - (double)c);
+}
 
 // rows of a bad page: 1 KB of zeros
 __device__ const uint4 pa_zeros[64] = {};
@@ -187,7 +203,9 @@ constexpr size_t SHARES_BYTES = 16 + SLOTS * sizeof(Share);
 
 template <typename ET>
 struct Form {
-    static constexpr bool BF = sizeof(ET) == 2;
+    typedef ET Row;                                        // of queries and outputs
+    static constexpr bool CODED = false;
+    static constexpr bool BF = sizeof(ET) == 2;            // products in bf16
     static constexpr int ROWB = D * (int)sizeof(ET);       // bytes of a row
     static constexpr int PPR = ROWB / 16;
     static constexpr int NF = BF ? 8 : 16;                 // 16-byte fragments of a row per lane: pieces 2 k + h
@@ -205,9 +223,28 @@ struct Form {
     static_assert(STAGES * 2 * SB <= (int)LDS, "of the largest");
 };
 
-// What both forms need of a piece, and the operations on 32-key blocks.
+template <typename Q>
+struct Form<Coded<Q>> {
+    typedef Q Row;
+    static constexpr bool CODED = true;
+    static constexpr bool BF = true;
+    static constexpr int NP = sizeof(Q) == 2 ? 1 : 3;      // bf16 parts of a query and of a weight
+    static constexpr int ROWB = D, PPR = ROWB / 16;
+    static constexpr int NF = 8;                           // bf16 fragments of a row per lane
+    static constexpr int NC = sizeof(Q) == 2 ? 2 : 1;
+    static constexpr int WAVES = ROWS_MANY / (32 * NC);
+    static constexpr int KB = 32 * ROWB;
+    static constexpr int SB = 8192, KT = SB / ROWB, SPS = KT / 32, STAGES = 4;
+    static constexpr int LPW = SB / 1024 / WAVES, WROWS = LPW * 1024 / ROWB;
+    // few rows: rings of RING tiles of 32 keys and their values a wave; their sums, joined
+    static constexpr int RING = 16 / WAVES;
+    static constexpr size_t LDS = sizeof(Q) == 2 ? 128 * 1024 : 136 * 1024;
+    static_assert(STAGES * 2 * SB <= (int)LDS && WAVES * RING * 2 * KB <= (int)LDS && WAVES * 32 * 134 * 4 <= (int)LDS, "of the largest");
+};
+
+// A piece of a tile: its keys, where their rows lie, and what its rows see.
 template <typename ET>
-struct Piece {
+struct PieceOf {
     typedef Form<ET> F;
     const AttnArgs& a;
     SeqRange r;
@@ -216,9 +253,8 @@ struct Piece {
     const int32_t* trow;
     int64_t head_bytes;
     int lane, l32, h;
-    uint32_t off0, kaddr;
 
-    __device__ __forceinline__ Piece(const AttnArgs& a_, const Found& f, int g_, int32_t lo_, int32_t hi_, int lane_)
+    __device__ __forceinline__ PieceOf(const AttnArgs& a_, const Found& f, int g_, int32_t lo_, int32_t hi_, int lane_)
         : a(a_), r(f.r), g(g_), lo(lo_), hi(hi_), lane(lane_) {
         head_bytes = (int64_t)F::ROWB << a.shift;
         kbase = (const uint8_t*)a.k + (int64_t)g * head_bytes;
@@ -226,20 +262,6 @@ struct Piece {
         trow = a.table + (int64_t)f.s * a.table_stride;
         l32 = lane & 31;
         h = lane >> 5;
-        const int lrow = lane / F::PPR;                    // the row that this lane loads of a 1 KB piece
-        off0 = (uint32_t)(lrow * F::ROWB + ((lane % F::PPR) ^ ((lrow & 3) << 2)) * 16);
-        kaddr = key_addr(lane);
-    }
-    static __device__ __forceinline__ uint32_t key_addr(int ln) {
-        const int row = ln & 31;
-        return (uint32_t)(row * F::ROWB + ((ln >> 5) ^ (((row & 3) << 2) | ((row >> 2) & 3))) * 16);
-    }
-    // the same piece with the lane's numbers anew: what the rare masked steps derive from them is not kept in
-    // registers for the whole loop
-    __device__ __forceinline__ Piece anew() const {
-        Piece p = *this;
-        asm volatile("" : "+v"(p.lane), "+v"(p.l32), "+v"(p.h));
-        return p;
     }
     // the page of key t as the table has it (any entry of the sequence's behind its end)
     __device__ __forceinline__ int32_t raw_page(int32_t t) const { return trow[(t < r.klen ? t : r.klen - 1) >> a.shift]; }
@@ -256,6 +278,63 @@ struct Piece {
         return (const uint8_t*)first_lane((int64_t)(p >= 0 ? pool + offset_of(p, t) : (const uint8_t*)pa_zeros));
     }
     static __device__ __forceinline__ int advance(int32_t p) { return p >= 0 ? 1024 : 0; }
+    // The keys that a row sees of this piece, as the first and their number; gm: 16-key groups with a page.
+    struct Seen { int32_t lo, n; };
+    __device__ __forceinline__ Seen seen(int32_t row_lo, int32_t row_hi) const {
+        const int32_t b = row_lo > lo ? row_lo : lo, e = row_hi < hi ? row_hi : hi;
+        return Seen{b, e > b ? e - b : 0};
+    }
+    static __device__ __forceinline__ bool sees(int32_t t, Seen s) { return (uint32_t)(t - s.lo) < (uint32_t)s.n; }
+    __device__ __forceinline__ void mask(f32x16& sc, int32_t t0, Seen s, uint32_t gm) const {
+        if (gm != 3u) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (!(gm >> (i >> 3) & 1u)) sc[i] = -INFINITY;
+        }
+        const uint32_t at = (uint32_t)(t0 + 4 * h - s.lo);
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (at + 8 * (i >> 2) + (i & 3) >= (uint32_t)s.n) sc[i] = -INFINITY;
+    }
+    __device__ __forceinline__ float most(const f32x16& sc) const {
+        float m = sc[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) m = fmaxf(m, sc[i]);
+        return xmax32(m);
+    }
+};
+
+// What both forms need of a piece, and the operations on 32-key blocks.
+template <typename ET>
+struct Piece : PieceOf<ET> {
+    typedef Form<ET> F;
+    typedef PieceOf<ET> P;
+    using P::a;
+    using P::h;
+    using P::l32;
+    using P::lane;
+    using P::r;
+    using P::sees;
+    using typename P::Seen;
+    uint32_t off0, kaddr;
+
+    __device__ __forceinline__ Piece(const AttnArgs& a_, const Found& f, int g_, int32_t lo_, int32_t hi_, int lane_)
+        : P(a_, f, g_, lo_, hi_, lane_) {
+        const int lrow = lane / F::PPR;                    // the row that this lane loads of a 1 KB piece
+        off0 = (uint32_t)(lrow * F::ROWB + ((lane % F::PPR) ^ ((lrow & 3) << 2)) * 16);
+        kaddr = key_addr(lane);
+    }
+    static __device__ __forceinline__ uint32_t key_addr(int ln) {
+        const int row = ln & 31;
+        return (uint32_t)(row * F::ROWB + ((ln >> 5) ^ (((row & 3) << 2) | ((row >> 2) & 3))) * 16);
+    }
+    // the same piece with the lane's numbers anew: what the rare masked steps derive from them is not kept in
+    // registers for the whole loop
+    __device__ __forceinline__ Piece anew() const {
+        Piece p = *this;
+        asm volatile("" : "+v"(p.lane), "+v"(p.l32), "+v"(p.h));
+        return p;
+    }
     // 1 KB number v of them into LDS at dst (of number 0); row 0 of number 0 is row 4 `quad` of its block
     template <bool VALUES, bool ONCE = false>
     __device__ __forceinline__ void bring1(const uint8_t* src, int adv, int v, int quad, uint32_t dst) const {
@@ -309,30 +388,6 @@ struct Piece {
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
-    }
-    // The keys that a row sees of this piece, as the first and their number; gm: 16-key groups with a page.
-    struct Seen { int32_t lo, n; };
-    __device__ __forceinline__ Seen seen(int32_t row_lo, int32_t row_hi) const {
-        const int32_t b = row_lo > lo ? row_lo : lo, e = row_hi < hi ? row_hi : hi;
-        return Seen{b, e > b ? e - b : 0};
-    }
-    static __device__ __forceinline__ bool sees(int32_t t, Seen s) { return (uint32_t)(t - s.lo) < (uint32_t)s.n; }
-    __device__ __forceinline__ void mask(f32x16& sc, int32_t t0, Seen s, uint32_t gm) const {
-        if (gm != 3u) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (!(gm >> (i >> 3) & 1u)) sc[i] = -INFINITY;
-        }
-        const uint32_t at = (uint32_t)(t0 + 4 * h - s.lo);
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-            if (at + 8 * (i >> 2) + (i & 3) >= (uint32_t)s.n) sc[i] = -INFINITY;
-    }
-    __device__ __forceinline__ float most(const f32x16& sc) const {
-        float m = sc[0];
-#pragma unroll
-        for (int i = 1; i < 16; ++i) m = fmaxf(m, sc[i]);
-        return xmax32(m);
     }
     // V^T fragment, bf16: keys r0 + 4 h + 0..3 and r0 + 8 + 4 h + 0..3, dim 32 dt + l32
     __device__ __forceinline__ u32x4 vfrag(const uint8_t* vt, int r0, int dt) const {
@@ -506,6 +561,13 @@ struct Running {
     }
 };
 
+// ln of the sum of exponentials of a row whose weights, of sum l, were taken against m
+__device__ __forceinline__ float lse_of(float m, float l, float c) {
+    constexpr float LN2 = 0.693147180559945309f;
+    const float off = off_of(m, c), log_l = __builtin_amdgcn_logf(l);
+    return beyond(off) ? m * (c * LN2) + log_l * LN2 : (log_l - off) * LN2;
+}
+
 template <typename ET>
 __device__ __forceinline__ void store4(ET* dst, float o0, float o1, float o2, float o3) {
     if constexpr (sizeof(ET) == 2) *reinterpret_cast<uint2*>(dst) = uint2{cvt_bf16x2(o0, o1), cvt_bf16x2(o2, o3)};
@@ -534,6 +596,7 @@ struct Many {
     int32_t raw;
     const uint8_t *kwin, *vwin;                            // of the window: its groups' first rows
     uint64_t has[2];
+    float scale[2];                                        // coded: of the windows' 32-key blocks, keys' and (from lane 32 on) values'
     bool bad;                                              // some key before the end has had none
     const uint8_t *ksrc, *vsrc;                            // of the stage that is being brought
     int adv;
@@ -552,6 +615,7 @@ struct Many {
         raw = 0;
         kwin = vwin = nullptr;
         has[0] = has[1] = 0;
+        if constexpr (F::CODED) scale[0] = scale[1] = 1.f;
         bad = false;
         ksrc = vsrc = nullptr;
         adv = 0;
@@ -593,6 +657,12 @@ struct Many {
             vwin = page >= 0 ? P.vbase + P.offset_of(page, t) : (const uint8_t*)pa_zeros;
             if (w & 1) has[1] = m;
             else has[0] = m;
+            if constexpr (F::CODED) {
+                const int block = P.lane & 31;
+                const float x = P.scale_of(__shfl(page, 2 * block, WAVE), t_first + 1024 * w + 32 * block, P.lane >= 32);
+                if (w & 1) scale[1] = x;
+                else scale[0] = x;
+            }
         }
         if (in == SPW / 2) raw = P.raw_page(window_key(w + 1));
         const int group = (in * F::KT + crow) / 16;
@@ -658,9 +728,12 @@ struct Many {
             const float inv = l == 0.f ? 0.f : 1.f / l;
             int32_t tok, head;
             row_of(c, P.l32, tok, head);
-            ET* dst = (ET*)a.out + (int64_t)(P.r.q0 + tok) * a.out_stride + (int64_t)head * D + first;
+            typedef typename F::Row Row;
+            Row* dst = (Row*)a.out + (int64_t)(P.r.q0 + tok) * a.out_stride + (int64_t)head * D + first;
+            if constexpr (F::CODED)
+                if (a.lse && last && P.h == 0) a.lse[(int64_t)(P.r.q0 + tok) * (a.G * a.Hg) + head] = lse_of(run.m, l, a.c);
 #pragma unroll
-            for (int i = 0; i < 16; i += 4) store4<ET>(dst + next * i, o[i] * inv, o[i + 1] * inv, o[i + 2] * inv, o[i + 3] * inv);
+            for (int i = 0; i < 16; i += 4) store4<Row>(dst + next * i, o[i] * inv, o[i + 1] * inv, o[i + 2] * inv, o[i + 3] * inv);
         }
     }
 };
@@ -888,11 +961,14 @@ __global__ __launch_bounds__(256) void paged_join_kernel(AttnArgs a) {
     const int64_t pr = place_rows(a.T, a.Hg);
     const int64_t rec0 = (2 * (i - 1) + (first_lane(before.pos) == start ? 0 : 1)) * pr;
     auto piece = [&](int p) { return p == 0 ? rec0 : 2 * (i + p - 1) * pr; };
-    auto put = [&](int32_t in, float l, const f32x4& o) {
+    typedef typename Form<ET>::Row Row;
+    auto put = [&](int32_t in, float m, float l, const f32x4& o) {
         const int32_t row = row0 + in;
         const float inv = l == 0.f ? 0.f : 1.f / l;
-        ET* dst = (ET*)a.out + (int64_t)(r.q0 + row / a.Hg) * a.out_stride + (int64_t)(g * a.Hg + row % a.Hg) * D + 4 * l32;
-        store4<ET>(dst, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+        Row* dst = (Row*)a.out + (int64_t)(r.q0 + row / a.Hg) * a.out_stride + (int64_t)(g * a.Hg + row % a.Hg) * D + 4 * l32;
+        if constexpr (Form<ET>::CODED)
+            if (a.lse && l32 == 0) a.lse[(int64_t)(r.q0 + row / a.Hg) * (a.G * a.Hg) + g * a.Hg + row % a.Hg] = lse_of(m, l, a.c);
+        store4<Row>(dst, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
     };
     // (rows behind the tile's last are read as they are and dropped)
     if (bm == ROWS_FEW) {
@@ -921,22 +997,22 @@ __global__ __launch_bounds__(256) void paged_join_kernel(AttnArgs a) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) os[e] = fmaf(f, v[e], os[e]);
             }
-            put(row, ls, os);
+            put(row, mx, ls, os);
         }
     } else if (np <= 4) {
         for (int mine = 16 * part + 2 * half; mine < rows; mine += 16 * parts) {
             float M[2], l[2];
             f32x4 o[2];
             join_pieces<2, 4>(a, [&](int n, int p) { return piece(p) + mine + n; }, 0, 1, np, M, l, o);
-            put(mine, l[0], o[0]);
-            if (mine + 1 < rows) put(mine + 1, l[1], o[1]);
+            put(mine, M[0], l[0], o[0]);
+            if (mine + 1 < rows) put(mine + 1, M[1], l[1], o[1]);
         }
     } else {
         for (int mine = 8 * part + half; mine < rows; mine += 8 * parts) {
             float M[1], l[1];
             f32x4 o[1];
             join_pieces<1, 8>(a, [&](int, int p) { return piece(p) + mine; }, 0, 1, np, M, l, o);
-            put(mine, l[0], o[0]);
+            put(mine, M[0], l[0], o[0]);
         }
     }
 }

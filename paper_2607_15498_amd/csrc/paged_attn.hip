@@ -498,7 +498,7 @@ size_t paged_attn_ws_bytes(int64_t T, int S, int G, int H, int dtype, int64_t ca
 
 hipError_t launch_paged_attn(const varrate_pages& pg, const varrate_batch& b, const void* q, int64_t q_stride, int H,
                              int causal, int window, float scale, void* out, int64_t out_stride, void* ws, hipStream_t st) {
-    AttnArgs a;
+    AttnArgs a = {};
     a.q = q;
     a.out = out;
     a.k = pg.k;
@@ -520,10 +520,7 @@ hipError_t launch_paged_attn(const varrate_pages& pg, const varrate_batch& b, co
     a.causal = causal;
     a.window = window;
     a.costs = costs_of(pg.dtype == VARRATE_BF16);
-    const double c = (double)scale * 1.4426950408889634;
-    a.c = (float)c;
-    if ((double)a.c >= c) a.c = nextafterf(a.c, 0.f);
-    a.c_lo = (float)(c - (double)a.c);                     // > 0, so that a masked score stays -infinity
+    split_scale(scale, a.c, a.c_lo);
     a.most_units = max_units(b.T, b.S, pg.G, a.Hg);
     a.rec_rows = max_records(b.T, b.S, pg.G, a.Hg, a.cap, a.costs.lmin);
     const int groups = max_groups(b.T, b.S, pg.G, a.Hg, a.cap, a.costs.lmin);

@@ -1,0 +1,84 @@
+// e4m3 codes and the powers of two of their blocks: shared by the operators that write them.
+#pragma once
+#include "vr_internal.h"
+
+namespace vr {
+
+constexpr int BLOCK = VARRATE_BLOCK8;                      // tokens of a scale
+constexpr int E_LO = -110, E_HI = 119;                     // exponents of scales: every value stays a normal bf16 number
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+// |x|'s bits where x is a number, 0 for infinities and NaN, which do not count in a block's scale
+__device__ __forceinline__ uint32_t magnitude(float x) {
+    const uint32_t u = __float_as_uint(x) & 0x7FFFFFFFu;
+    return u < 0x7F800000u ? u : 0u;
+}
+// the smallest e that takes magnitudes up to `most` (bits) to 448 = 1.75 x 2^8 or less
+__device__ __forceinline__ int exponent_for(uint32_t most) {
+    const int e = (int)(most >> 23) - 127 - 8 + ((most & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+    return e < E_LO ? E_LO : e > E_HI ? E_HI : e;
+}
+__device__ __forceinline__ float power(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+// a stored scale's exponent, within what this library stores
+__device__ __forceinline__ int exponent_of(uint8_t b) {
+    const int e = (int)b - 127;
+    return e < E_LO ? E_LO : e > E_HI ? E_HI : e;
+}
+// x times the power of two s as a code's value to be rounded: beyond 448 (E_HI alone) it is 448; infinities become NaN with the conversion
+__device__ __forceinline__ float scaled(float x, float s) {
+    const float y = x * s;
+    return fabsf(y) > 448.f && fabsf(y) < INFINITY ? copysignf(448.f, y) : y;
+}
+// 8 numbers times s, rounded to the nearest codes
+__device__ __forceinline__ uint2 encode8(const float (&x)[8], float s) {
+    uint32_t w[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        int v = __builtin_amdgcn_cvt_pk_fp8_f32(scaled(x[4 * k], s), scaled(x[4 * k + 1], s), 0, false);
+        w[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(scaled(x[4 * k + 2], s), scaled(x[4 * k + 3], s), v, true);
+    }
+    return uint2{w[0], w[1]};
+}
+// 8 codes times s
+__device__ __forceinline__ void values8(uint2 w, float s, float (&x)[8]) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int v = (int)(k ? w.y : w.x);
+        const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(v, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(v, true);
+        x[4 * k] = a[0] * s;
+        x[4 * k + 1] = a[1] * s;
+        x[4 * k + 2] = b[0] * s;
+        x[4 * k + 3] = b[1] * s;
+    }
+}
+__device__ __forceinline__ void read8(const uint16_t* p, float (&x)[8]) {
+    const u32x4 w = load16(p);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        x[2 * k] = bf_lo(w[k]);
+        x[2 * k + 1] = bf_hi(w[k]);
+    }
+}
+__device__ __forceinline__ void read8(const float* p, float (&x)[8]) {
+    *reinterpret_cast<f32x4*>(x) = *reinterpret_cast<const f32x4*>(p);
+    *reinterpret_cast<f32x4*>(x + 4) = *reinterpret_cast<const f32x4*>(p + 4);
+}
+__device__ __forceinline__ void write8(uint16_t* p, const float (&x)[8]) {
+    *reinterpret_cast<u32x4*>(p) = u32x4{cvt_bf16x2(x[0], x[1]), cvt_bf16x2(x[2], x[3]), cvt_bf16x2(x[4], x[5]), cvt_bf16x2(x[6], x[7])};
+}
+__device__ __forceinline__ void write8(float* p, const float (&x)[8]) {
+    *reinterpret_cast<f32x4*>(p) = f32x4{x[0], x[1], x[2], x[3]};
+    *reinterpret_cast<f32x4*>(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
+}
+// the largest of a wave's values, in every lane
+__device__ __forceinline__ uint32_t wave_most(uint32_t v) {
+#pragma unroll
+    for (int m = 1; m < WAVE; m <<= 1) {
+        const uint32_t y = __shfl_xor(v, m, WAVE);
+        v = y > v ? y : v;
+    }
+    return v;
+}
+
+}  // namespace vr

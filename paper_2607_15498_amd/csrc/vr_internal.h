@@ -143,6 +143,28 @@ hipError_t launch_paged_attn(const varrate_pages& pg, const varrate_batch& b, co
                              int causal, int window, float scale, void* out, int64_t out_stride, void* ws,
                              hipStream_t st);
 hipError_t launch_paged_gather(const varrate_pages& pg, const int32_t* table, int64_t n, void* K, void* V, hipStream_t st);
+// cache of e4m3 codes (all arguments checked by the caller)
+hipError_t launch_paged8_append(const varrate_pages8& pg, const varrate_batch& b, int dtype, const void* k, int64_t k_stride,
+                                const void* v, int64_t v_stride, hipStream_t st);
+size_t paged8_attn_ws_bytes(int64_t T, int S, int G, int H, int dtype, int64_t cap);
+hipError_t launch_paged8_attn(const varrate_pages8& pg, const varrate_batch& b, int dtype, const void* q, int64_t q_stride, int H,
+                              int causal, int window, float scale, void* out, int64_t out_stride, float* lse, void* ws,
+                              hipStream_t st);
+hipError_t launch_paged8_mass(const varrate_pages8& pg, const varrate_batch& b, int dtype, const void* q, int64_t q_stride, int H,
+                              int causal, int window, float scale, const float* lse, const float* mass, float* out, int64_t L,
+                              hipStream_t st);
+struct Evict8Args {
+    const int32_t *table, *into, *kv_len;
+    int64_t table_stride, into_stride;
+    const float* mass;
+    int32_t* index;
+    float* mass_out;
+    int32_t* len_out;
+    int64_t L, keep, first, recent;
+    int32_t S, width;
+};
+hipError_t launch_paged8_evict(const varrate_pages8& pg, const Evict8Args& e, hipStream_t st);
+hipError_t launch_paged8_gather(const varrate_pages8& pg, const int32_t* table, int64_t n, int dtype, void* K, void* V, hipStream_t st);
 // streaming-read probe (measurement aid)
 hipError_t launch_read_probe(const void* src, size_t bytes, uint32_t* sink, hipStream_t st);
 

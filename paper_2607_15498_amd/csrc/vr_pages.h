@@ -79,6 +79,10 @@ struct Costs { int32_t few, many, piece_few, piece_many, join, lmin; };      // 
 VR_HD Costs costs_of(bool bf16) {
     return bf16 ? Costs{5, 8, 600, 4400, 400, 256} : Costs{12, 72, 600, 1800, 400, 128};
 }
+// ... over pages of e4m3 codes
+VR_HD Costs costs8_of(bool bf16) {
+    return bf16 ? Costs{3, 10, 600, 4400, 400, 256} : Costs{5, 24, 600, 1800, 400, 128};
+}
 VR_HD bool is_many(SeqRange r, int Hg) { return seq_rows(r, Hg) > ROWS_FEW; }
 
 // The cost of a sequence's tiles for one head: a + b (t + 1) for tile t.  (Tiles of causal chunks see 256 / Hg keys more
