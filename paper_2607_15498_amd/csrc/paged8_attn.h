@@ -406,9 +406,7 @@ __device__ __forceinline__ void many_rows8(const Piece<Coded<Q>>& P, uint8_t* sm
             M.issue(j / F::SPS + 2);
         }
         if (j < M.jf || j >= M.jl) continue;
-        const float scale = M.scale[j >> 5 & 1];
-        const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scale), j & 31));
-        const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scale), 32 + (j & 31)));
+        const float ks = M.key_scale(j), vs = M.value_scale(j);
         P.template scores<NC>(M.keys_of(j), ks, qf, sc);
         const bool masked = M.masked(j);
         const int32_t t0 = M.t_first + 32 * j;

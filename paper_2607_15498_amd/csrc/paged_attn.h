@@ -596,7 +596,9 @@ struct Many {
     int32_t raw;
     const uint8_t *kwin, *vwin;                            // of the window: its groups' first rows
     uint64_t has[2];
-    float scale[2];                                        // coded: of the windows' 32-key blocks, keys' and (from lane 32 on) values'
+    // coded: the scales of the last two windows' 32-key blocks, keys' and (from lane 32 on) values', and those on their way, which
+    // nothing touches before their window's first stage has arrived: the wait for them is one for all loads
+    float scale[2], scale_in;
     bool bad;                                              // some key before the end has had none
     const uint8_t *ksrc, *vsrc;                            // of the stage that is being brought
     int adv;
@@ -615,7 +617,7 @@ struct Many {
         raw = 0;
         kwin = vwin = nullptr;
         has[0] = has[1] = 0;
-        if constexpr (F::CODED) scale[0] = scale[1] = 1.f;
+        if constexpr (F::CODED) scale[0] = scale[1] = scale_in = 1.f;
         bad = false;
         ksrc = vsrc = nullptr;
         adv = 0;
@@ -659,9 +661,7 @@ struct Many {
             else has[0] = m;
             if constexpr (F::CODED) {
                 const int block = P.lane & 31;
-                const float x = P.scale_of(__shfl(page, 2 * block, WAVE), t_first + 1024 * w + 32 * block, P.lane >= 32);
-                if (w & 1) scale[1] = x;
-                else scale[0] = x;
+                scale_in = P.scale_of(__shfl(page, 2 * block, WAVE), t_first + 1024 * w + 32 * block, P.lane >= 32);
             }
         }
         if (in == SPW / 2) raw = P.raw_page(window_key(w + 1));
@@ -695,8 +695,13 @@ struct Many {
     }
     // Stage s has arrived, and stage s - 2 is free (every wave is past it): stage s + 2 follows.  Every stage is
     // followed by others, so that the counts stay the same; those behind the last bring rows that nothing reads.
-    __device__ __forceinline__ void arrive(int s) const {
+    __device__ __forceinline__ void arrive(int s) {
         wait_loads<2 * F::LPW>();
+        if constexpr (F::CODED)
+            if (s % SPW == 0) {
+                if (s / SPW & 1) scale[1] = scale_in;
+                else scale[0] = scale_in;
+            }
         P.clear_tail(t_first + s * F::KT, crow, crow + F::WROWS, smem + (F::STAGES + (s & 3)) * F::SB);
         __syncthreads();
     }
@@ -710,6 +715,12 @@ struct Many {
     }
     __device__ __forceinline__ uint8_t* keys_of(int j) const { return smem + ((uint32_t)j * F::KB & (F::STAGES * F::SB - 1)); }
     __device__ __forceinline__ uint8_t* values_of(int j) const { return keys_of(j) + F::STAGES * F::SB; }
+    // scales of step j
+    __device__ __forceinline__ float key_scale(int j) const { return scale_at(j, j & 31); }
+    __device__ __forceinline__ float value_scale(int j) const { return scale_at(j, 32 + (j & 31)); }
+    __device__ __forceinline__ float scale_at(int j, int lane) const {
+        return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(j >> 5 & 1 ? scale[1] : scale[0]), lane));
+    }
     __device__ __forceinline__ bool masked(int j) const { return j < mf || j >= ml || gm_of(j) != 3u; }
     // block c's rows: sums (of 32 dims dt, four at a time as the products leave them) and, with `last`, maximum and sum
     __device__ __forceinline__ void put(int c, int dt, const f32x16& o, const Running& run, float l, bool cut, int64_t rec_row,

@@ -205,3 +205,69 @@ def test_reference_codes():
         assert R.E_LO <= e <= R.E_HI
         assert most <= 448 * 2.0 ** e or e == R.E_HI
         assert e == R.E_LO or most > 448 * 2.0 ** (e - 1)
+
+
+# ---- the generated code of the bf16 attention: as test_paged_host.py checks the raw cache's ------------------------------
+
+@pytest.fixture(scope="module")
+def coded_kernel(tmp_path_factory):
+    import re
+    import shutil
+    if shutil.which("hipcc") is None:
+        pytest.skip("hipcc not available")
+    from paper_2607_15498_amd import build as B
+    from test_paged_host import _instructions
+    out = tmp_path_factory.mktemp("asm") / "paged8_attn.s"
+    cmd = ["hipcc", *B.FLAGS, *B.SOURCE_FLAGS["paged8_attn.hip"], "-S", "--offload-device-only", os.path.join(B.CSRC, "paged8_attn.hip"),
+           "-o", str(out)]
+    r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    assert r.returncode == 0, r.stdout[-2000:]
+    m = re.search(r"^(_ZN2vr17paged_attn_kernelINS_5CodedIt\w*):[^\n]*\n(.*?)\n\.Lfunc_end", out.read_text(), re.S | re.M)
+    return _instructions(m.group(2))
+
+
+def test_accumulators_are_private(coded_kernel):
+    from test_paged_host import OWN_AGPRS
+    own = {f"a{i}" for i in range(OWN_AGPRS)}
+    for x in coded_kernel:
+        assert x.asm or not own & (x.dst | x.src), x.text
+    assert own <= set().union(*(x.dst | x.src for x in coded_kernel if x.asm))
+
+
+def test_products_wait_for_their_operands(coded_kernel):
+    """Decoded fragments are written by vector instructions: 2 states before the product that reads them."""
+    from test_paged_host import _follow, _registers
+    code, products = coded_kernel, [x for x in coded_kernel if x.asm and x.mfma]
+    assert len(products) >= 90
+    wanted = set().union(*(_registers(x.args[1]) | _registers(x.args[2]) for x in products))
+    checked = 0
+    for i, w in enumerate(code):
+        if w.mfma or not w.op.startswith("v_") or not w.dst & wanted:
+            continue
+        checked += w.op.startswith("v_cvt_scalef32")
+
+        def visit(x, t):
+            if x.asm and x.mfma:
+                assert not w.dst & (_registers(x.args[1]) | _registers(x.args[2])), f"{w.text} -> {x.text} after {t}"
+            return False
+        _follow(code, i, 3, visit)
+    assert checked >= 128
+
+
+def test_results_are_read_late_enough(coded_kernel):
+    from test_paged_host import _follow, _registers
+    code = coded_kernel
+    for i, w in enumerate(code):
+        if not (w.asm and w.mfma):
+            continue
+
+        def visit(x, t):
+            if x.mfma:
+                if x.asm and _registers(x.args[0]) == w.dst and _registers(x.args[3]) in (w.dst, set()):
+                    return True
+                hit = w.dst & (_registers(x.args[1]) | _registers(x.args[2]))
+            else:
+                hit = w.dst & (x.src | x.dst)
+            assert not hit, f"{w.text} -> {x.text} after {t}"
+            return False
+        _follow(code, i, 12, visit)
