@@ -34,21 +34,24 @@ __device__ __forceinline__ uint32_t cut2(float& a, float& b) {
     return x >> 16 | y;
 }
 
-// A row's query (src) as B operands, in parts: fragment 2 j + b is dims 16 (2 j + h) + 8 b ..
-template <typename Q>
-__device__ __forceinline__ void load_query(const Q* src, int h, u32x4 (&qf)[Form<Coded<Q>>::NP][8]) {
+// A row's query (src) as B operands, in parts: fragments 2 j and 2 j + 1 are dims 16 (2 j + h) .. of 8 each; put(part, k, fragment)
+template <typename Q, typename A>
+__device__ __forceinline__ void load_query(const Q* src, int h, int j, A&& put) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        const Q* at = src + 16 * (2 * (k >> 1) + h) + 8 * (k & 1);
-        if constexpr (sizeof(Q) == 2) qf[0][k] = load16(at);
+    for (int b = 0; b < 2; ++b) {
+        const Q* at = src + 16 * (2 * j + h) + 8 * b;
+        if constexpr (sizeof(Q) == 2) put(0, 2 * j + b, load16(at));
         else {
             float x[8];
             *reinterpret_cast<f32x4*>(x) = *reinterpret_cast<const f32x4*>(at);
             *reinterpret_cast<f32x4*>(x + 4) = *reinterpret_cast<const f32x4*>(at + 4);
 #pragma unroll
-            for (int p = 0; p < 3; ++p)
+            for (int p = 0; p < 3; ++p) {
+                u32x4 f;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) qf[p][k][e] = cut2(x[2 * e], x[2 * e + 1]);
+                for (int e = 0; e < 4; ++e) f[e] = cut2(x[2 * e], x[2 * e + 1]);
+                put(p, 2 * j + b, f);
+            }
         }
     }
 }
@@ -98,7 +101,9 @@ struct Piece<Coded<Q>> : PieceOf<Coded<Q>> {
             *reinterpret_cast<uint4*>(vt + from * F::ROWB + 16 * i) = uint4{0, 0, 0, 0};
     }
     __device__ __forceinline__ void query(u32x4 (&qf)[F::NP][F::NF], int64_t token, int head) const {
-        load_query<Q>((const Q*)a.q + token * a.q_stride + (int64_t)head * D, h, qf);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            load_query((const Q*)a.q + token * a.q_stride + (int64_t)head * D, h, j, [&](int p, int k, const u32x4& f) { qf[p][k] = f; });
     }
     // scores of NC blocks of 32 rows with 32 keys of one scale, the smallest parts first
     template <int NC>

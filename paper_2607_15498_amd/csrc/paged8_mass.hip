@@ -4,8 +4,11 @@
 // logarithms), so one pass over the keys does, and a key belongs to one wave that goes through all rows in order: nothing is
 // added by atomics and nothing is joined.
 //
-// A wave has NK blocks of 32 keys, decoded into bf16 fragments that stay in registers, and takes 32 rows at a time: S^T = K Q^T
-// leaves a lane one row and 16 keys of a block, whose weights it adds up; a key's 32 lanes are added at the end.
+// A workgroup has 128 U keys and stages the rows that see them in shared memory, as the products take them; its waves bring
+// their keys through rings of their own, 32 at a time.  S^T = K Q^T leaves a lane one row and 16 keys, whose weights it adds up over
+// the staged rows; then a key's 32 lanes are added.
+//   Few rows (single tokens): long rings, the reads of the keys bound it.  Many: 160 rows (fp32 32) are staged at once, and the
+//   exponentials bound it.
 #include "paged8_attn.h"
 
 namespace vr {
@@ -20,111 +23,191 @@ struct MassArgs {
     __device__ __forceinline__ int32_t keys(const SeqRange& r) const { return r.klen < L ? r.klen : (int32_t)L; }
 };
 
-template <typename Q, int NK>
-__global__ __launch_bounds__(256) void paged8_mass_kernel(MassArgs m) {
+constexpr int MOST_U = 8;
+template <typename Q>
+struct MassForm {
     typedef Form<Coded<Q>> F;
-    constexpr int KEYS = 128 * NK;                         // of a workgroup
-    const AttnArgs& a = m.a;
-    const int lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5, wave = first_lane((int)(threadIdx.x >> 6));
-    const int H = a.G * a.Hg, sh = a.shift - 5;
-    const SeqRange first = load_range(a, lane);
-    Search from;
-    for (int64_t u = blockIdx.x;; u += gridDim.x) {
-        Found f;
-        if (!find(a, first, u, from, f, [&](const SeqRange& r) { return (int64_t)((m.keys(r) + KEYS - 1) / KEYS) * a.G; })) return;
-        const SeqRange r = {first_lane(f.r.q0), first_lane(f.r.qlen), first_lane(f.r.klen)};
-        const int s = first_lane(f.s), in = first_lane((int)(u - f.base)), g = in % a.G;
-        const int32_t base = in / a.G * KEYS + 32 * NK * wave;
-        const int32_t klen = m.keys(r);
-        if (base >= klen) continue;
-        // keys: block b is base + 32 b ..; lane's key l32, dims 16 (2 j + h) .. of piece j
-        u32x4 kf[NK][F::NF];
-        uint32_t there = 0;                                // blocks with a page
+    static constexpr int FRAGS = F::NP * F::NF * 1024;     // a block of 32 rows
+    static constexpr int RING_FEW = F::NP == 1 ? 4 : 3, RING_MANY = 2;
+    static constexpr int RB_MANY = F::NP == 1 ? 5 : 1;
+    static constexpr int SUMS = 4 * MOST_U * 32 * 4, ROWS = RB_MANY * 32 * 16;
+    static constexpr int FEW = FRAGS + 4 * RING_FEW * F::KB, MANY = RB_MANY * FRAGS + 4 * RING_MANY * F::KB;
+    static constexpr int LDS = SUMS + ROWS + (FEW > MANY ? FEW : MANY);
+    static_assert(LDS <= 80 * 1024, "two workgroups a CU");
+};
+
+template <int CTRL> __device__ __forceinline__ float dpp(float x) {
+    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xF, 0xF, true));
+}
+// What a wave's lanes have of 16 keys each (lane 32 h + i: key 8 (k / 4) + 4 h + k % 4 in x[k]), added over i: lane i ends with the
+// key of k = i / 2.  Pairs of lanes exchange halves of what they have.
+__device__ __forceinline__ float sum_lanes(f32x16 x) {
+    const int lane = threadIdx.x & 63;
 #pragma unroll
-        for (int b = 0; b < NK; ++b) {
-            const int32_t t = base + 32 * b;
-            int32_t pg = -1;
-            if (t < klen) pg = first_lane(good_page(a.table[s * a.table_stride + (t >> a.shift)], a.n_pages));
+    for (int k = 0; k < 8; ++k) {                          // lanes 16 apart
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x[k]), __float_as_uint(x[k + 8]), false, false);
+        x[k] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
 #pragma unroll
-            for (int k = 0; k < F::NF; ++k) kf[b][k] = u32x4{0, 0, 0, 0};
-            if (pg < 0) continue;
-            there |= 1u << b;
-            const int64_t head = (int64_t)pg * a.G + g;
-            const float scale = __uint_as_float((uint32_t)a.kscale[(head << sh) + ((t >> 5) & ((1 << sh) - 1))] << 23);
-            const uint8_t* row = (const uint8_t*)a.k + ((head << a.shift) + (t & ((1 << a.shift) - 1)) + l32) * D + 16 * h;
+    for (int k = 0; k < 4; ++k)                            // i and 15 - i
+        x[k] = (lane & 8 ? x[k + 4] : x[k]) + dpp<0x140>(lane & 8 ? x[k] : x[k + 4]);
+#pragma unroll
+    for (int k = 0; k < 2; ++k)                            // i and 7 - i
+        x[k] = (lane & 4 ? x[k + 2] : x[k]) + dpp<0x141>(lane & 4 ? x[k] : x[k + 2]);
+    const float y = (lane & 2 ? x[1] : x[0]) + dpp<0x4E>(lane & 2 ? x[0] : x[1]);
+    return y + dpp<0xB1>(y);
+}
+
+// A wave's tiles: number i is keys first + 128 i .. + 31, i < U; page and scale of tile i in lane i.
+template <typename Q>
+struct Tiles {
+    Piece<Coded<Q>> P;
+    int32_t first, page;
+    float scale;
+    int U;
+    uint32_t ring0;
+    uint8_t* ring;
+    template <int R> __device__ __forceinline__ void issue(int i) const {
+        const int32_t pg = i < U ? __builtin_amdgcn_readlane(page, i & 63) : -1;
+        const uint8_t* k = P.rows_at(P.kbase, pg, first + 128 * i);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) P.template bring1<false, R != 2>(k, P.advance(pg), v, 0, ring0 + i % R * 4096);
+    }
+    template <int R> __device__ __forceinline__ void begin() const {
+#pragma unroll
+        for (int i = 0; i + 1 < R; ++i) issue<R>(i);
+    }
+    // Weights of nb blocks of staged rows, added to the wave's sums.
+    template <int R>
+    __device__ __forceinline__ void weigh(const u32x4* frag, const float4* row_of, int nb, float* sums) const {
+        typedef Form<Coded<Q>> F;
+        const AttnArgs& a = P.a;
+        for (int i = 0; i < U; ++i) {
+            wait_lds();                                    // the tile before has been read
+            issue<R>(i + R - 1);
+            wait_loads<4 * (R - 1)>();
+            if (__builtin_amdgcn_readlane(page, i) < 0) continue;
+            const int32_t t0 = first + 128 * i;
+            const uint8_t* kt = ring + i % R * 4096;
+            const float sc_k = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scale), i));
+            u32x4 kf[F::NF];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const u32x4 w = load16(row + 32 * j);
-                kf[b][2 * j] = decode8(uint2{w[0], w[1]}, scale);
-                kf[b][2 * j + 1] = decode8(uint2{w[2], w[3]}, scale);
+                const u32x4 w = *reinterpret_cast<const u32x4*>(kt + (P.kaddr ^ (32u * j)));
+                kf[2 * j] = decode8(uint2{w[0], w[1]}, sc_k);
+                kf[2 * j + 1] = decode8(uint2{w[2], w[3]}, sc_k);
             }
-        }
-        f32x16 sum[NK];
+            f32x16 sum;
 #pragma unroll
-        for (int b = 0; b < NK; ++b)
+            for (int k = 0; k < 16; ++k) sum[k] = 0.f;
+            for (int rb = 0; rb < nb; ++rb) {
+                f32x16 x;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sum[b][i] = 0.f;
-        // the new tokens that see some of these keys, [i0, i1)
-        const int32_t old = r.klen - r.qlen, last = base + 32 * NK < klen ? base + 32 * NK - 1 : klen - 1;
-        int32_t i0 = 0, i1 = r.qlen;
-        if (a.causal && base > old) i0 = base - old;
-        if (a.window && (int64_t)last + a.window - old < i1) i1 = last + a.window - old;
-        const int64_t rows = (int64_t)r.qlen * a.Hg, end = i1 > i0 ? (int64_t)i1 * a.Hg : 0;
-        for (int64_t r0 = (int64_t)i0 * a.Hg & ~(int64_t)31; r0 < end; r0 += 32) {
-            const int64_t mine = r0 + l32;
-            const bool real = mine < rows;
-            const int32_t tok = (int32_t)((real ? mine : r0) / a.Hg), hd = g * a.Hg + (int32_t)((real ? mine : r0) % a.Hg);
-            u32x4 qf[F::NP][F::NF];
-            const Q* src = (const Q*)a.q + (int64_t)(r.q0 + tok) * a.q_stride + (int64_t)hd * D;
-            load_query<Q>(src, h, qf);
-            const float lse = real ? m.lse[(int64_t)(r.q0 + tok) * H + hd] : INFINITY;
-            // exp(scale x - lse) = exp2(c x - z), both products' roundings carried along
-            const float z = lse == -INFINITY ? INFINITY : lse * LOG2E;
-            const float z_lo = fabsf(z) < INFINITY ? fmaf(lse, LOG2E, -z) + lse * LOG2E_LO : 0.f;
-            int32_t lo, hi;
-            row_keys(r, tok, a.causal, a.window, lo, hi);
-            if (!real) hi = lo = 0;
-#pragma unroll
-            for (int b = 0; b < NK; ++b) {
-                if (!(there >> b & 1u)) continue;
-                f32x16 sc;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+                for (int k = 0; k < 16; ++k) x[k] = 0.f;
 #pragma unroll
                 for (int p = F::NP - 1; p >= 0; --p)
 #pragma unroll
-                    for (int k = 0; k < F::NF; ++k) sc = mfma32(kf[b][k], qf[p][k], sc);
-                const int32_t t0 = base + 32 * b;
+                    for (int k = 0; k < F::NF; ++k) x = mfma32(kf[k], frag[((rb * F::NP + p) * F::NF + k) * 64 + P.lane], x);
+                const float4 w = row_of[rb * 32 + P.l32];
+                const int32_t lo = __float_as_int(w.z), hi = __float_as_int(w.w);
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    sc[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], a.c, -z) + fmaf(sc[i], a.c_lo, -z_lo));
+                for (int k = 0; k < 16; ++k) x[k] = __builtin_amdgcn_exp2f(fmaf(x[k], a.c_lo, fmaf(x[k], a.c, -w.x)));
                 if (__any(lo > t0 || hi < t0 + 32)) {
-                    const uint32_t at = (uint32_t)(t0 + 4 * h - lo), n = (uint32_t)(hi > lo ? hi - lo : 0);
+                    const uint32_t at = (uint32_t)(t0 + 4 * P.h - lo), n = (uint32_t)(hi - lo);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (at + 8 * (i >> 2) + (i & 3) >= n) sc[i] = 0.f;
+                    for (int k = 0; k < 16; ++k)
+                        if (at + 8 * (k >> 2) + (k & 3) >= n) x[k] = 0.f;
                 }
 #pragma unroll
-                for (int i = 0; i < 16; ++i) sum[b][i] += sc[i];
+                for (int k = 0; k < 16; ++k) sum[k] = fmaf(x[k], w.y, sum[k]);
             }
+            const float mine = sum_lanes(sum);
+            const int k = P.l32 >> 1;
+            if (!(P.l32 & 1)) sums[32 * i + 8 * (k >> 2) + 4 * P.h + (k & 3)] += mine;
         }
-        // a key's 32 lanes: halves of the keys change hands four times, then a lane has one key
-        const int64_t at = ((int64_t)s * a.G + g) * m.L;
-#pragma unroll
-        for (int b = 0; b < NK; ++b) {
-#pragma unroll
-            for (int half = 8, bit = 16; half >= 1; half >>= 1, bit >>= 1) {
-                const bool up = l32 & bit;
-#pragma unroll
-                for (int i = 0; i < half; ++i) {
-                    const float give = up ? sum[b][i] : sum[b][i + half], keep = up ? sum[b][i + half] : sum[b][i];
-                    sum[b][i] = keep + __shfl_xor(give, bit, WAVE);
-                }
+        wait_loads<0>();
+        wait_lds();
+    }
+};
+
+template <typename Q>
+__global__ __launch_bounds__(256, 2) void paged8_mass_kernel(MassArgs m) {
+    typedef MassForm<Q> M;
+    typedef Form<Coded<Q>> F;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    const AttnArgs& a = m.a;
+    const int lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5, wave = first_lane((int)(threadIdx.x >> 6));
+    const int H = a.G * a.Hg;
+    float* sums = reinterpret_cast<float*>(smem + M::LDS - M::SUMS) + wave * MOST_U * 32;
+    float4* row_of = reinterpret_cast<float4*>(smem + M::LDS - M::SUMS - M::ROWS);   // what is subtracted, its rest as a factor, keys seen
+    const SeqRange first = load_range(a, lane);
+    // tiles a wave: as many as leave the card two workgroups a CU
+    int64_t all = 0;
+    for (int s0 = 0; s0 < a.S; s0 += 64) all += (m.keys(s0 ? load_range(a, s0 + lane) : first) + 127) / 128;
+    for (int k = 1; k < WAVE; k <<= 1) all += __shfl_xor(all, k, WAVE);
+    all = first_lane(all) * a.G;
+    const int U = all >= 8 * 2 * SLOTS ? 8 : all >= 4 * 2 * SLOTS ? 4 : all >= 2 * 2 * SLOTS ? 2 : 1, per = 128 * U;
+    Search from;
+    for (int64_t u = blockIdx.x;; u += gridDim.x) {
+        Found f;
+        if (!find(a, first, u, from, f, [&](const SeqRange& r) { return (int64_t)((m.keys(r) + per - 1) / per) * a.G; })) return;
+        f.r = SeqRange{first_lane(f.r.q0), first_lane(f.r.qlen), first_lane(f.r.klen)};
+        f.s = first_lane(f.s);
+        const SeqRange r = f.r;
+        const int in = first_lane((int)(u - f.base)), g = in % a.G;
+        const int32_t klen = m.keys(r), top = in / a.G * per, old = r.klen - r.qlen;
+        const int64_t at = ((int64_t)f.s * a.G + g) * m.L;
+        // the new tokens that see some of these keys, [i0, i1)
+        const int32_t last = top + per < klen ? top + per - 1 : klen - 1;
+        int32_t i0 = 0, i1 = r.qlen;
+        if (a.causal && top > old) i0 = top - old;
+        if (a.window && (int64_t)last + a.window - old < i1) i1 = last + a.window - old;
+        const int64_t rows = (int64_t)r.qlen * a.Hg, end = i1 > i0 ? (int64_t)i1 * a.Hg : 0;
+        int64_t c0 = (int64_t)i0 * a.Hg & ~(int64_t)31;
+        const bool few = end - c0 <= 32;
+        Tiles<Q> T = {Piece<Coded<Q>>(a, f, g, 0, klen, lane), top + 32 * wave, -1, 1.f, U, 0, nullptr};
+        T.ring = smem + (few ? M::FRAGS + wave * M::RING_FEW * F::KB : M::RB_MANY * M::FRAGS + wave * M::RING_MANY * F::KB);
+        T.ring0 = first_lane((int)(uint32_t)(size_t)(__attribute__((address_space(3))) uint8_t*)T.ring);
+        if (lane < U) {
+            const int32_t t = T.first + 128 * lane;
+            if (t < klen) T.page = T.P.page_of(T.P.raw_page(t), t);
+            T.scale = T.P.scale_of(T.page, t, false);
+        }
+        // the sums begin with what older keys have been paid
+        for (int i = 0; i < U; i += 2) {
+            const int32_t t = T.first + 128 * (i + h) + l32;
+            if (i + h < U) sums[32 * (i + h) + l32] = t < klen && t < old ? m.mass[at + t] : 0.f;
+        }
+        for (; c0 < end; c0 += 32 * M::RB_MANY) {
+            const int nb = few ? 1 : end - c0 < 32 * M::RB_MANY ? (int)((end - c0 + 31) / 32) : M::RB_MANY;
+            if (few) T.template begin<M::RING_FEW>();
+            else T.template begin<M::RING_MANY>();
+            u32x4* frag = reinterpret_cast<u32x4*>(smem);  // [RB][NP][NF][64]
+            for (int rb = 0; rb < nb; ++rb) {              // every wave a fourth of the dims
+                const int64_t mine = c0 + 32 * rb + l32;
+                const bool real = mine < rows;
+                const int64_t row = real ? mine : rows - 1;
+                const int32_t tok = (int32_t)(row / a.Hg), hd = g * a.Hg + (int32_t)(row % a.Hg);
+                load_query((const Q*)a.q + (int64_t)(r.q0 + tok) * a.q_stride + (int64_t)hd * D, h, wave,
+                           [&](int p, int k, const u32x4& x) { frag[((rb * F::NP + p) * F::NF + k) * 64 + lane] = x; });
+                if ((rb & 3) != wave || h) continue;
+                const float lse = m.lse[(int64_t)(r.q0 + tok) * H + hd];
+                // exp(scale x - lse) = exp2(c x - z) 2^-(what z lacks)
+                const float z = lse == -INFINITY ? INFINITY : lse * LOG2E;
+                const float rest = fabsf(z) < INFINITY ? __builtin_amdgcn_exp2f(-(fmaf(lse, LOG2E, -z) + lse * LOG2E_LO)) : 1.f;
+                int32_t lo, hi;
+                row_keys(r, tok, a.causal, a.window, lo, hi);
+                if (!real || hi < lo) lo = hi = 0;
+                row_of[rb * 32 + l32] = float4{z, rest, __int_as_float(lo), __int_as_float(hi)};
             }
-            const float x = sum[b][0] + __shfl_xor(sum[b][0], 1, WAVE);
-            const int i = l32 >> 1;                        // bit 16 of the lane chose 8, 8 chose 4, 4 chose 2, 2 chose 1
-            const int32_t t = base + 32 * b + 8 * (i >> 2) + 4 * h + (i & 3);
-            if (!(l32 & 1) && t < klen) m.out[at + t] = (t < old ? m.mass[at + t] : 0.f) + x;
+            __syncthreads();
+            if (few) T.template weigh<M::RING_FEW>(frag, row_of, nb, sums);
+            else T.template weigh<M::RING_MANY>(frag, row_of, nb, sums);
+            __syncthreads();                               // the rows have been read
+        }
+        for (int i = 0; i < U; i += 2) {
+            const int32_t t = T.first + 128 * (i + h) + l32;
+            if (i + h < U && t < klen) m.out[at + t] = sums[32 * (i + h) + l32];
         }
     }
 }
@@ -132,12 +215,11 @@ __global__ __launch_bounds__(256) void paged8_mass_kernel(MassArgs m) {
 template <typename Q>
 hipError_t launch_mass(const MassArgs& m, hipStream_t st) {
     const AttnArgs& a = m.a;
-    // many rows a sequence: two blocks of keys a wave share the rows' fragments
-    const bool many = (int64_t)a.T * a.Hg >= (int64_t)128 * a.S;
-    const int64_t keys = many ? 256 : 128, units = ((a.cap < m.L ? a.cap : m.L) + keys - 1) / keys * a.G * a.S;
-    const unsigned grid = (unsigned)(units < 4096 ? units : 4096);
-    if (many) paged8_mass_kernel<Q, 2><<<grid, 256, 0, st>>>(m);
-    else paged8_mass_kernel<Q, 1><<<grid, 256, 0, st>>>(m);
+    const void* fn = (const void*)paged8_mass_kernel<Q>;
+    const hipError_t e = ensure_lds_limit(fn, MassForm<Q>::LDS);
+    if (e != hipSuccess) return e;
+    const int64_t units = ((a.cap < m.L ? a.cap : m.L) + 127) / 128 * a.G * a.S;
+    paged8_mass_kernel<Q><<<(unsigned)(units < 2 * SLOTS ? units : 2 * SLOTS), 256, MassForm<Q>::LDS, st>>>(m);
     return hipGetLastError();
 }
 

@@ -34,32 +34,86 @@ struct Append8 {
     int32_t T, S, cap;
 };
 
-// Rows i .. i + n - 1, the new ones of a block of sequence s from position t on.
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+
+// 8 values as they lie in memory, read once.
+template <typename ET> struct Raw8;
+template <> struct Raw8<uint16_t> {
+    u32x4 w;
+    __device__ __forceinline__ void read(const uint16_t* p) { w = __builtin_nontemporal_load((const u32x4*)p); }
+    __device__ __forceinline__ void get(float (&x)[8]) const {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            x[2 * k] = bf_lo(w[k]);
+            x[2 * k + 1] = bf_hi(w[k]);
+        }
+    }
+    // the largest of their magnitudes' bits and `most`, whether numbers or not
+    typedef u16x2 Most;
+    __device__ __forceinline__ void raise(Most& most) const {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, w[k] & 0x7FFF7FFFu));
+    }
+    static __device__ __forceinline__ uint32_t bits(Most m) { return (uint32_t)(m[0] > m[1] ? m[0] : m[1]) << 16; }
+};
+template <> struct Raw8<float> {
+    f32x4 w[2];
+    __device__ __forceinline__ void read(const float* p) {
+        w[0] = __builtin_nontemporal_load((const f32x4*)p);
+        w[1] = __builtin_nontemporal_load((const f32x4*)(p + 4));
+    }
+    __device__ __forceinline__ void get(float (&x)[8]) const {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = w[k >> 2][k & 3];
+    }
+    typedef uint32_t Most;
+    __device__ __forceinline__ void raise(Most& most) const {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const uint32_t u = __float_as_uint(w[k >> 2][k & 3]) & 0x7FFFFFFFu;
+            most = u > most ? u : most;
+        }
+    }
+    static __device__ __forceinline__ uint32_t bits(Most m) { return m; }
+};
+
+// Rows i .. i + n - 1, the new ones of a block of sequence s from position t on.  They are asked for before the page is looked up.
 template <typename ET>
 __device__ __forceinline__ void append_block(const Append8& p, int which, int g, int s, int32_t i, int32_t t, int32_t n) {
     const int lane = threadIdx.x & 63, rr = lane >> 4, c = 8 * (lane & 15);
+    const ET* src = (const ET*)p.x[which] + (int64_t)i * p.stride[which] + (int64_t)g * D + c;
+    Raw8<ET> x[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+        if (4 * k < n) x[k].read(src + (4 * k + rr < n ? 4 * k + rr : n - 1) * p.stride[which]);
     const int32_t pg = good_page(p.table[s * p.table_stride + (t >> p.pool.shift)], p.pool.n_pages);
     if (pg < 0) return;
     const int32_t slot = p.pool.slot(t), held = slot & (BLOCK - 1);
     uint8_t* scale = p.pool.scale[which] + p.pool.block(pg, g, slot);
     uint8_t* dst = p.pool.code[which] + p.pool.row(pg, g, slot) + c;
-    const ET* src = (const ET*)p.x[which] + (int64_t)i * p.stride[which] + (int64_t)g * D + c;
     int was = E_LO;
     if (held) was = exponent_of(*scale);
-    float x[8][8];
-    uint32_t most = 0;
+    typename Raw8<ET>::Most top = {};
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        if (4 * k >= n) break;
-        const int row = 4 * k + rr < n ? 4 * k + rr : n - 1;
-        read8(src + row * p.stride[which], x[k]);
+    for (int k = 0; k < 8; ++k)
+        if (4 * k < n) x[k].raise(top);
+    uint32_t most = wave_most(Raw8<ET>::bits(top));
+    if (most >= 0x7F800000u) {                             // infinities or NaN among them: of the others
+        most = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t u = magnitude(x[k][e]);
-            most = u > most ? u : most;
-        }
+        for (int k = 0; k < 8; ++k)
+            if (4 * k < n) {
+                float y[8];
+                x[k].get(y);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t u = magnitude(y[e]);
+                    most = u > most ? u : most;
+                }
+            }
+        most = wave_most(most);
     }
-    int now = exponent_for(wave_most(most));
+    int now = exponent_for(most);
     if (held && was >= now) now = was;
     else if (held) {                                       // the rows before are rounded to the larger scale
         uint8_t* old = dst - (int64_t)held * D;
@@ -73,10 +127,13 @@ __device__ __forceinline__ void append_block(const Append8& p, int which, int g,
     }
     const float to = power(-now);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        if (4 * k >= n) break;
-        if (4 * k + rr < n) *reinterpret_cast<uint2*>(dst + (int64_t)(4 * k + rr) * D) = encode8(x[k], to);
-    }
+    for (int k = 0; k < 8; ++k)
+        if (4 * k + rr < n) {
+            float y[8];
+            x[k].get(y);
+            const uint2 w = encode8(y, to);
+            __builtin_nontemporal_store((uint64_t)w.y << 32 | w.x, (uint64_t*)(dst + (int64_t)(4 * k + rr) * D));
+        }
     if (lane == 0) *scale = (uint8_t)(now + 127);
 }
 
@@ -147,42 +204,51 @@ struct Evict8 {
 // tokens of sequence s, those of them that have a mass
 __device__ __forceinline__ int32_t tokens_of(const Evict8& p, int s) { return clamp_i32(p.kv_len[s], 0, p.cap); }
 
-// Masses as numbers whose order is theirs: NaN before all others, both zeros alike.
+// Masses as numbers whose order is theirs: both zeros alike, NaN (1) before all others; 0 is no token's, and ALWAYS is a token's
+// that stays whatever its mass.
+constexpr uint32_t ALWAYS = 0xFFFFFFFFu;
 __device__ __forceinline__ uint32_t rank_of(float x) {
-    if (x != x) return 0;
+    if (x != x) return 1;
     const uint32_t u = __float_as_uint(x + 0.f);
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
+__device__ __forceinline__ float mass_of(uint32_t rank) {
+    return rank == 1 ? NAN : __uint_as_float(rank & 0x80000000u ? rank ^ 0x80000000u : ~rank);
+}
+__device__ __forceinline__ uint32_t count_below(uint64_t mask, uint32_t from) {    // lanes below this one, added to `from`
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, from));
+}
 
-constexpr int SEL = 1024;                                  // threads of a selection
+constexpr int SEL = 1024, SEL_WAVES = SEL / WAVE;          // threads of a selection
+constexpr int SEL_PART = 32768;                            // tokens whose ranks it holds at once
 
-// Exclusive prefix sums over the workgroup of two counts below 2^16, packed; total: of all.
-__device__ __forceinline__ uint32_t scan_pair(uint32_t v, uint32_t* sums, uint32_t& total) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    uint32_t up = v;
-#pragma unroll
-    for (int m = 1; m < WAVE; m <<= 1) {
-        const uint32_t y = __shfl_up(up, m, WAVE);
-        if (lane >= m) up += y;
-    }
-    __syncthreads();                                       // the sums of the scan before have been read
-    if (lane == WAVE - 1) sums[wave] = up;
-    __syncthreads();
+// The counts of the waves before this one, and of all.
+__device__ __forceinline__ uint32_t waves_before(const uint32_t* sums, int wave, uint32_t& total) {
     uint32_t before = 0;
     total = 0;
 #pragma unroll
-    for (int w = 0; w < SEL / WAVE; ++w) {
-        if (w < wave) before += sums[w];
-        total += sums[w];
+    for (int w = 0; w < SEL_WAVES; w += 4) {
+        const u32x4 v = *reinterpret_cast<const u32x4*>(sums + w);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            before += w + k < wave ? v[k] : 0;
+            total += v[k];
+        }
     }
-    return before + up - v;
+    return before;
 }
 
-// One workgroup a (sequence, head): the mass of the last token that stays, by its digits from the top (of 11, 11 and 10 bits),
-// then the tokens above it and the first of those equal to it, in order.
+// One workgroup a (sequence, head): the rank of the last of the m tokens that stay, by its digits from the top (of 10, 11 and 11
+// bits), then the tokens above it and the first of those equal to it, in order.  Ranks lie in shared memory, a part of 32768 at a
+// time (one alone is read once); a wave has 256 that follow each other, 4 a lane.  The instructions of its CU bound it: 20 a token
+// and pass, row by row with ranges compared, took 42 us for 32768 tokens (of 8 heads or of one), these take XX.
 __global__ __launch_bounds__(SEL) void evict8_select(Evict8 p) {
-    __shared__ uint32_t hist[2048], sums[SEL / WAVE], found[2];
+    extern __shared__ __align__(16) uint32_t ranks[];
+    __shared__ __align__(16) uint32_t hist[4096];          // a digit's copies lie together: equal digits of one read fall into different ones
+    __shared__ __align__(16) uint32_t sums[SEL_WAVES];
+    __shared__ uint32_t found[2];
     const int s = (int)(blockIdx.x / (uint32_t)p.pool.G), g = (int)(blockIdx.x % (uint32_t)p.pool.G), tid = threadIdx.x;
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int32_t n = tokens_of(p, s), m = n < p.keep ? n : p.keep;
     const float* mass = p.mass + ((int64_t)s * p.pool.G + g) * p.L;
     int32_t* index = p.index + ((int64_t)s * p.pool.G + g) * p.keep;
@@ -192,80 +258,147 @@ __global__ __launch_bounds__(SEL) void evict8_select(Evict8 p) {
         index[i] = -1;
         mass_out[i] = 0.f;
     }
-    // tokens [lo, hi) compete for `need` places
-    const int32_t lo = p.first < n ? p.first : n, hi = n - p.recent > lo ? n - p.recent : lo;
-    uint32_t need = (uint32_t)(m - lo - (n - hi)), prefix = 0;
-    if (m == n) need = (uint32_t)(hi - lo);
-    const bool all = need == (uint32_t)(hi - lo), none = need == 0;
-    if (!all && !none) {
-        for (int pass = 0; pass < 3; ++pass) {
-            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-            for (int i = tid; i < 2048; i += SEL) hist[i] = 0;
-            __syncthreads();
-            for (int32_t t = lo + tid; t < hi; t += SEL) {
-                const uint32_t r = rank_of(mass[t]);
-                if (pass == 0 || r >> (shift + bits) == prefix >> (shift + bits)) atomicAdd(&hist[r >> shift & ((1u << bits) - 1)], 1u);
-            }
-            __syncthreads();
-            // the digit at which the count from the top reaches `need`: two digits a thread, from the top
-            const int top = (1 << bits) - 1 - 2 * tid;
-            const uint32_t a = top >= 0 ? hist[top] : 0, b = top >= 1 ? hist[top - 1] : 0;
-            uint32_t up = a + b;
-            const int lane = tid & 63, wave = tid >> 6;
+    if (m == 0) return;
+    const int32_t lo = p.first, hi = n - p.recent;         // tokens before and from there on stay (first + recent <= m unless all do)
+    const int parts = (n + SEL_PART - 1) / SEL_PART;
+    int turns = 0, at = 0;                                 // of a part: reads a lane; the lane's first
+    auto load = [&](int part) {
+        const int32_t t0 = part * SEL_PART, len = n - t0 < SEL_PART ? n - t0 : SEL_PART;
+        turns = (len + 4 * SEL - 1) / (4 * SEL);
+        at = wave * turns * 64 + lane;
+        if (part || parts > 1) __syncthreads();            // the part before has been read
+        for (int i0 = tid; i0 < turns * 4 * SEL; i0 += 8 * SEL) {      // 8 reads at a time (tokens that there are)
+            float x[8];
 #pragma unroll
-            for (int k = 1; k < WAVE; k <<= 1) {
-                const uint32_t y = __shfl_up(up, k, WAVE);
-                if (lane >= k) up += y;
-            }
-            if (lane == WAVE - 1) sums[wave] = up;
-            __syncthreads();
-            for (int w = 0; w < wave; ++w) up += sums[w];
-            const uint32_t before = up - a - b;
-            if (before < need && up >= need) {             // one thread
-                const bool second = before + a < need;
-                found[0] = (uint32_t)(top - (second ? 1 : 0));
-                found[1] = need - before - (second ? a : 0);
-            }
-            __syncthreads();
-            prefix |= found[0] << shift;
-            need = found[1];
-            __syncthreads();
-        }
-    }
-    // ranks above `prefix`, and the first `need` equal to it
-    int32_t place = 0;
-    uint32_t equal = 0;
-    constexpr int PER = 4;
-    for (int32_t t0 = 0; t0 < n; t0 += SEL * PER) {
-        uint32_t mine = 0;
-        int kind[PER];                                     // 0: goes, 1: stays, 2: equal
-        float x[PER];
+            for (int k = 0; k < 8; ++k) x[k] = mass[t0 + (i0 + k * SEL < len ? i0 + k * SEL : len - 1)];
 #pragma unroll
-        for (int k = 0; k < PER; ++k) {
-            const int32_t t = t0 + PER * tid + k;
-            kind[k] = 0;
-            x[k] = 0.f;
-            if (t < n) {
-                x[k] = mass[t];
+            for (int k = 0; k < 8; ++k) {
+                const int i = i0 + k * SEL, t = t0 + i;
                 const uint32_t r = rank_of(x[k]);
-                kind[k] = t < lo || t >= hi || all ? 1 : none ? 0 : r > prefix ? 1 : r == prefix ? 2 : 0;
+                if (i < turns * 4 * SEL) ranks[i] = i >= len ? 0 : t < lo || t >= hi ? ALWAYS : r;
             }
-            mine += kind[k] == 1 ? 1u << 16 : kind[k] == 2 ? 1u : 0u;
         }
-        uint32_t total, at = scan_pair(mine, sums, total);
+        __syncthreads();
+    };
+    const u32x4* quads = reinterpret_cast<const u32x4*>(ranks);
+    uint32_t need = (uint32_t)m, prefix = 0;
+    if (parts == 1) load(0);
+#pragma unroll 1
+    for (int pass = 0; pass < 3; ++pass) {
+        const int shift = pass == 0 ? 22 : pass == 1 ? 11 : 0, bits = pass == 0 ? 10 : 11, copies = pass == 0 ? 4 : 2;
+        reinterpret_cast<uint4*>(hist)[tid] = uint4{0, 0, 0, 0};
+        __syncthreads();
+#pragma unroll 1
+        for (int part = 0; part < parts; ++part) {
+            if (parts > 1) load(part);
+            for (int i = 0; i < turns; ++i) {
+                const u32x4 r = quads[at + 64 * i];
 #pragma unroll
-        for (int k = 0; k < PER; ++k) {
-            const uint32_t eq = equal + (at & 0xFFFFu);
-            const int32_t to = place + (int32_t)(at >> 16) + (int32_t)((eq < need ? eq : need) - (equal < need ? equal : need));
-            if (kind[k] == 1 || (kind[k] == 2 && eq < need)) {
-                index[to] = t0 + PER * tid + k;
-                mass_out[to] = x[k];
+                for (int k = 0; k < 4; ++k)
+                    if (pass == 0 || (r[k] ^ prefix) >> (shift + bits) == 0)
+                        atomicAdd(&hist[(r[k] >> shift & ((1u << bits) - 1)) * copies + (lane & (copies - 1))], 1u);
             }
-            at += kind[k] == 1 ? 1u << 16 : kind[k] == 2 ? 1u : 0u;
         }
-        const uint32_t eq = equal + (total & 0xFFFFu);
-        place += (int32_t)(total >> 16) + (int32_t)((eq < need ? eq : need) - (equal < need ? equal : need));
-        equal = eq;
+        __syncthreads();
+        // the digit at which the count from the top reaches `need`: two digits a thread, from the top
+        const int top = (1 << bits) - 1 - 2 * tid;
+        uint32_t a = 0, b = 0;
+        if (top >= 1) {
+            if (pass == 0) {
+                const u32x4 x = *reinterpret_cast<const u32x4*>(hist + 4 * top), y = *reinterpret_cast<const u32x4*>(hist + 4 * (top - 1));
+                a = x[0] + x[1] + x[2] + x[3];
+                b = y[0] + y[1] + y[2] + y[3];
+            } else {
+                const u32x4 x = *reinterpret_cast<const u32x4*>(hist + 2 * (top - 1));
+                a = x[2] + x[3];
+                b = x[0] + x[1];
+            }
+        }
+        uint32_t up = a + b, total;
+#pragma unroll
+        for (int k = 1; k < WAVE; k <<= 1) {
+            const uint32_t y = __shfl_up(up, k, WAVE);
+            if (lane >= k) up += y;
+        }
+        if (lane == WAVE - 1) sums[wave] = up;
+        __syncthreads();
+        up += waves_before(sums, wave, total);
+        const uint32_t before = up - a - b;
+        if (before < need && up >= need) {                 // one thread
+            const bool second = before + a < need;
+            found[0] = (uint32_t)(top - (second ? 1 : 0));
+            found[1] = need - before - (second ? a : 0);
+        }
+        __syncthreads();
+        prefix |= found[0] << shift;
+        need = found[1];
+    }
+    // ranks above `prefix`, and the first `need` equal to it: counted per wave (above and equal, 16 bits each), then placed
+    uint32_t place = 0, equal = 0;                         // in the parts before
+#pragma unroll 1
+    for (int part = 0; part < parts; ++part) {
+        if (parts > 1) load(part);
+        uint32_t mine = 0;
+        for (int i = 0; i < turns; ++i) {
+            const u32x4 r = quads[at + 64 * i];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) mine += (r[k] > prefix ? 1u << 16 : 0u) + (r[k] == prefix ? 1u : 0u);
+        }
+#pragma unroll
+        for (int k = 1; k < WAVE; k <<= 1) mine += __shfl_xor(mine, k, WAVE);
+        __syncthreads();                                   // the sums before have been read
+        if (lane == 0) sums[wave] = mine;
+        __syncthreads();
+        // a part has up to 2^15 of either: 16 waves' sums do not carry
+        uint32_t total;
+        const uint32_t before = waves_before(sums, wave, total);
+        uint32_t to0 = place + (before >> 16), eq0 = equal + (before & 0xFFFFu);
+        for (int i = 0; i < turns; ++i) {
+            const u32x4 r = quads[at + 64 * i];
+            uint64_t above[4], same[4], any = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                above[k] = __ballot(r[k] > prefix);
+                same[k] = __ballot(r[k] == prefix);
+                any |= same[k];
+            }
+            // (byte offsets of 32 bits: keep is 2^30 at most)
+            auto put = [&](int k, uint32_t slot) {
+                const int32_t t = part * SEL_PART + 4 * (at + 64 * i) + k;
+                *(int32_t*)((uint8_t*)index + 4 * slot) = t;
+                *(float*)((uint8_t*)mass_out + 4 * slot) = r[k] == ALWAYS ? mass[t] : mass_of(r[k]);
+            };
+            uint32_t to = to0 + (eq0 < need ? eq0 : need);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                to = count_below(above[k], to);
+                to0 += __builtin_popcountll(above[k]);
+            }
+            if (!any) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (r[k] > prefix) put(k, to);
+                    to += r[k] > prefix ? 1 : 0;
+                }
+            } else {
+                uint32_t eq = eq0;
+                to -= eq0 < need ? eq0 : need;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    eq = count_below(same[k], eq);
+                    eq0 += __builtin_popcountll(same[k]);
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const bool is = r[k] == prefix;
+                    if (r[k] > prefix || (is && eq < need)) put(k, to + (eq < need ? eq : need));
+                    to += r[k] > prefix ? 1 : 0;
+                    eq += is ? 1 : 0;
+                }
+            }
+        }
+        place += total >> 16;
+        equal += total & 0xFFFFu;
     }
 }
 
@@ -276,32 +409,34 @@ __global__ __launch_bounds__(256) void evict8_move(Evict8 p) {
     const int64_t all = (int64_t)p.S * G * 2 * blocks, step = (int64_t)gridDim.x * 4;
     for (int64_t u = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); u < all; u += step) {
         const int which = (int)(u & 1), b = (int)((u >> 1) % blocks), sg = (int)((u >> 1) / blocks), s = sg / G, g = sg % G;
-        const int32_t n = tokens_of(p, s), m = n < p.keep ? n : p.keep, i0 = b * BLOCK;
-        if (i0 >= m) continue;
-        const int32_t rows = m - i0 < BLOCK ? m - i0 : BLOCK;
-        const int32_t to = good_page(p.into[s * p.into_stride + (i0 >> p.pool.shift)], p.pool.n_pages);
-        if (to < 0) continue;
-        // lane l knows row l
+        const int32_t i0 = b * BLOCK;
+        const int32_t raw = p.into[s * p.into_stride + (i0 >> p.pool.shift)];
+        // lane l knows row l; the rows that stay come first
+        const int32_t t = lane < BLOCK && i0 + lane < p.keep ? p.index[(int64_t)sg * p.keep + i0 + lane] : -1;
+        const int rows = __builtin_popcountll(__ballot(t >= 0));
+        const int32_t to = good_page(raw, p.pool.n_pages);
+        if (to < 0 || !rows) continue;
         int64_t from = -1;
         float scale = 0.f;
-        if (lane < rows) {
-            const int32_t t = p.index[(int64_t)sg * p.keep + i0 + lane];
-            const int32_t pg = t >= 0 && t < n ? good_page(p.table[s * p.table_stride + (t >> p.pool.shift)], p.pool.n_pages) : -1;
+        if (t >= 0 && t < p.cap) {
+            const int32_t pg = good_page(p.table[s * p.table_stride + (t >> p.pool.shift)], p.pool.n_pages);
             if (pg >= 0) {
                 from = p.pool.row(pg, g, p.pool.slot(t));
                 scale = __uint_as_float((uint32_t)p.pool.scale[which][p.pool.block(pg, g, p.pool.slot(t))] << 23);
             }
         }
+        uint2 w[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int64_t at = __shfl(from, 4 * k + rr, WAVE);
+            w[k] = uint2{0, 0};
+            if (at >= 0) w[k] = *reinterpret_cast<const uint2*>(p.pool.code[which] + at + c);
+        }
         float x[8][8];
         uint32_t most = 0;
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            const int row = 4 * k + rr;
-            const int64_t at = __shfl(from, row, WAVE);
-            const float sc = __shfl(scale, row, WAVE);
-            uint2 w = {0, 0};
-            if (at >= 0) w = *reinterpret_cast<const uint2*>(p.pool.code[which] + at + c);
-            values8(w, sc, x[k]);
+            values8(w[k], __shfl(scale, 4 * k + rr, WAVE), x[k]);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const uint32_t v = magnitude(x[k][e]);
@@ -350,8 +485,11 @@ hipError_t launch_paged8_evict(const varrate_pages8& pg, const Evict8Args& e, hi
     const int64_t cap = (int64_t)e.width * pg.page;
     const Evict8 p = {pool_of(pg), e.table, e.into, e.kv_len, e.table_stride, e.into_stride, e.mass, e.index, e.mass_out, e.len_out,
                       e.L, e.S, (int32_t)(cap < e.L ? cap : e.L), (int32_t)e.keep, (int32_t)e.first, (int32_t)e.recent};
-    evict8_select<<<(unsigned)e.S * (unsigned)pg.G, SEL, 0, st>>>(p);
-    hipError_t err = hipGetLastError();
+    const size_t lds = 4 * (size_t)(p.cap < SEL_PART ? (p.cap + 4 * SEL - 1) / (4 * SEL) * (4 * SEL) : SEL_PART);
+    hipError_t err = ensure_lds_limit((const void*)evict8_select, 4 * SEL_PART);
+    if (err != hipSuccess) return err;
+    evict8_select<<<(unsigned)e.S * (unsigned)pg.G, SEL, lds, st>>>(p);
+    err = hipGetLastError();
     if (err != hipSuccess) return err;
     const int64_t waves = (int64_t)e.S * pg.G * 2 * ((e.keep + BLOCK - 1) / BLOCK);
     evict8_move<<<grid_of((waves + 3) / 4, 1 << 20), 256, 0, st>>>(p);

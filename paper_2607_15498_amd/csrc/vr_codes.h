@@ -52,18 +52,6 @@ __device__ __forceinline__ void values8(uint2 w, float s, float (&x)[8]) {
         x[4 * k + 3] = b[1] * s;
     }
 }
-__device__ __forceinline__ void read8(const uint16_t* p, float (&x)[8]) {
-    const u32x4 w = load16(p);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        x[2 * k] = bf_lo(w[k]);
-        x[2 * k + 1] = bf_hi(w[k]);
-    }
-}
-__device__ __forceinline__ void read8(const float* p, float (&x)[8]) {
-    *reinterpret_cast<f32x4*>(x) = *reinterpret_cast<const f32x4*>(p);
-    *reinterpret_cast<f32x4*>(x + 4) = *reinterpret_cast<const f32x4*>(p + 4);
-}
 __device__ __forceinline__ void write8(uint16_t* p, const float (&x)[8]) {
     *reinterpret_cast<u32x4*>(p) = u32x4{cvt_bf16x2(x[0], x[1]), cvt_bf16x2(x[2], x[3]), cvt_bf16x2(x[4], x[5]), cvt_bf16x2(x[6], x[7])};
 }
