@@ -11,9 +11,15 @@
 // A row is 128 bytes; row r's 16-byte piece c lies at place c ^ f(r), f(r) = bits 1, 3 and 2 of r as 2, 4 and 1: 16 rows'
 // reads of one piece (keys) and 8 rows' of two (values, transposed 8 x 16 bytes at a time) fall into different banks.
 #pragma once
-#include "paged_attn.h"
+#include "paged_agpr.h"
 
 namespace vr {
+
+// Nothing of the compiler's stays in a0 .. a191 across this.  (It may place what lives long in AGPRs, of which the bf16 kernel's
+// many-rows form names these.)
+template <typename Q> __device__ __forceinline__ void keep_out() {
+    if constexpr (sizeof(Q) == 2) asm volatile("" ::: PA_AGPRS);
+}
 
 typedef int pa_i32x2 __attribute__((ext_vector_type(2)));
 
@@ -68,13 +74,15 @@ struct Piece<Coded<Q>> : PieceOf<Coded<Q>> {
     using P::r;
     using P::sees;
     using typename P::Seen;
-    uint32_t off0, kaddr;
+    uint32_t off0, kaddr, vaddr;
 
     __device__ __forceinline__ Piece(const AttnArgs& a_, const Found& f, int g_, int32_t lo_, int32_t hi_, int lane_)
         : P(a_, f, g_, lo_, hi_, lane_) {
         const int lrow = lane >> 3;
         off0 = (uint32_t)(lrow * F::ROWB + ((lane & 7) ^ swizzle(lrow)) * 16);
         kaddr = (uint32_t)(l32 * F::ROWB + (h ^ swizzle(l32)) * 16);
+        const int rr = (lane & 15) >> 1, row = 8 * (rr >> 2) + 4 * h + (rr & 3);
+        vaddr = (uint32_t)(row * F::ROWB + (((lane >> 4) & 1) ^ swizzle(row)) * 16 + (lane & 1) * 8);
     }
     static __device__ __forceinline__ int swizzle(int row) { return (row & 2) | ((row >> 2) & 1) | ((row >> 1) & 4); }
     __device__ __forceinline__ Piece anew() const {
@@ -126,12 +134,36 @@ struct Piece<Coded<Q>> : PieceOf<Coded<Q>> {
 #pragma unroll
                 for (int c = 0; c < NC; ++c) sc[c] = mfma32(kf[k], qf[c][p][k], sc[c]);
     }
+    // ... of one block of rows with NT blocks of keys, side by side
+    template <int NT>
+    __device__ __forceinline__ void scores_of(const uint8_t* kt, const float (&scale)[NT], const u32x4* query, f32x16 (&sc)[NT][1]) const {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sc[n][0][i] = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            u32x4 kf[NT][2];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const u32x4 w = *reinterpret_cast<const u32x4*>(kt + n * F::KB + (kaddr ^ (32u * j)));
+                kf[n][0] = decode8(uint2{w[0], w[1]}, scale[n]);
+                kf[n][1] = decode8(uint2{w[2], w[3]}, scale[n]);
+            }
+#pragma unroll
+            for (int p = F::NP - 1; p >= 0; --p)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const u32x4 q = query[(p * F::NF + 2 * j + k) * 64 + lane];
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) sc[n][0] = mfma32(kf[n][k], q, sc[n][0]);
+                }
+        }
+    }
     // codes of a V^T fragment: keys r0 + 4 h + 0..3 and r0 + 8 + 4 h + 0..3, dim 32 dt + l32
     __device__ __forceinline__ uint2 vcodes(const uint8_t* vt, int r0, int dt) const {
-        const int rr = (lane & 15) >> 1, row = r0 + 8 * (rr >> 2) + 4 * h + (rr & 3);
-        const int place = (2 * dt + ((lane >> 4) & 1)) ^ swizzle(row);
         return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-            (__attribute__((address_space(3))) pa_i32x2*)(vt + row * F::ROWB + place * 16 + (lane & 1) * 8)));
+            (__attribute__((address_space(3))) pa_i32x2*)(vt + (vaddr ^ (32u * dt)) + r0 * F::ROWB)));
     }
     static __device__ __forceinline__ uint32_t finite(uint32_t x) { return Piece<uint16_t>::finite(x); }
     // acc += V^T P^T of 32 keys of one scale; p: the weights' parts, packed in pairs.  FINITE: of the values that are numbers alone.
@@ -210,86 +242,106 @@ __device__ __forceinline__ void parts_of(f32x16& sc, u32x4 (&p)[2][2]) {
     }
 }
 
-// Few rows: each wave takes every WAVES-th tile of 32 keys out of a ring of its own, RING - 1 of them on their way, and the
-// waves' sums are joined at the end.
+// Few rows: each wave takes every WAVES-th group of NT x 32 keys out of a ring of two of its own, and the waves' sums are joined
+// at the end.  bf16, one wave a SIMD: two tiles at a time, whose products and exponentials do not wait for each other (one token
+// over 131072, tile by tile out of a ring of four: 72 us, 4.9 TB/s a further key; XX).
 template <typename Q>
 __device__ __forceinline__ void few_rows8(const Piece<Coded<Q>>& P, uint8_t* smem, int rows, bool cut, int64_t rec_row) {
     typedef Form<Coded<Q>> F;
-    constexpr int NW = F::WAVES, RING = F::RING, L = F::KB / 1024, step = 32 * NW;
+    constexpr int NW = F::WAVES, NT = F::FEW_TILES, L = NT * F::KB / 1024, step = 32 * NT * NW, GROUP = 2 * NT * F::KB;
     const AttnArgs& a = P.a;
     const SeqRange& r = P.r;
     const int wave = first_lane((int)(threadIdx.x >> 6)), lane = P.lane, l32 = P.l32, h = P.h;
     const int Hg = a.Hg, g = P.g, lo = P.lo, hi = P.hi;
-    uint8_t* ring = smem + wave * RING * 2 * F::KB;
+    uint8_t* ring = smem + wave * 2 * GROUP;
     const uint32_t ring0 = first_lane((int)(uint32_t)(size_t)(__attribute__((address_space(3))) uint8_t*)ring);
     // bf16: weights in two parts; up to 16 rows leave half of a product's columns to the second, the same rows again
     const bool halves = F::NP == 1 && rows <= 16;
     const int col = halves ? l32 & 15 : l32, myrow = col < rows ? col : 0, tok = myrow / Hg;
+    const float rest = col < l32 ? -1.f : 0.f;
     int32_t mylo, myhi, firsthi, lastlo, x;
     row_keys(r, tok, a.causal, a.window, mylo, myhi);
     const auto seen = P.seen(mylo, myhi);
     row_keys(r, 0, a.causal, a.window, x, firsthi);
     row_keys(r, (rows - 1) / Hg, a.causal, a.window, lastlo, x);
-    u32x4 qf[1][F::NP][F::NF];
-    P.query(qf[0], r.q0 + tok, g * Hg + myrow % Hg);
+    // the rows' fragments lie in shared memory, [NP][NF][64]: in registers they leave too few for two tiles
+    const u32x4* query = reinterpret_cast<const u32x4*>(smem + NW * 2 * GROUP);
+    if (wave < 4)
+        load_query((const Q*)a.q + (int64_t)(r.q0 + tok) * a.q_stride + (int64_t)(g * Hg + myrow % Hg) * D, h, wave,
+                   [&](int p, int k, const u32x4& f) { const_cast<u32x4*>(query)[(p * F::NF + k) * 64 + lane] = f; });
     Running run;
     const float slack = SLACK / a.c;
-    f32x16 acc[1][4], sc[1];
+    f32x16 acc[1][4];
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[0][dt][i] = 0.f;
 
     // pages and scales of the wave's next 32 tiles: lane 2 i has the page and the keys' scale of tile i, lane 2 i + 1 the values'
+    constexpr int WINDOW = 32 / NT;                        // groups
     int32_t window = 0;
     float scales = 1.f;
-    int at = 32;
-    int32_t page[RING];                                    // of the tiles that are on their way, the next to be used first
-    float ks[RING], vs[RING];
-#pragma unroll
-    for (int i = 0; i < RING; ++i) {
-        page[i] = -1;
-        ks[i] = vs[i] = 1.f;
-    }
+    int at = WINDOW;
+    int32_t page[NT];                                      // of the group that is on its way
+    float ks[NT], vs[NT];
     auto issue = [&](int32_t t, int slot) {
-        if (at == 32) {
-            const int32_t tl = t + (lane >> 1) * step;
+        if (at == WINDOW) {
+            const int32_t tl = t + (lane / (2 * NT)) * step + (lane / 2 % NT) * 32;
             window = tl < hi ? P.page_of(P.raw_page(tl), tl) : -1;
             scales = P.scale_of(window, tl, lane & 1);
             at = 0;
         }
+        const uint32_t dst = ring0 + slot * GROUP;
 #pragma unroll
-        for (int i = 0; i + 1 < RING; ++i) {
-            page[i] = page[i + 1];
-            ks[i] = ks[i + 1];
-            vs[i] = vs[i + 1];
+        for (int n = 0; n < NT; ++n) {
+            const int l = 2 * (NT * at + n);
+            page[n] = __builtin_amdgcn_readlane(window, l);
+            ks[n] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scales), l));
+            vs[n] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scales), l + 1));
         }
-        const int32_t pg = page[RING - 1] = __builtin_amdgcn_readlane(window, 2 * at);
-        ks[RING - 1] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scales), 2 * at));
-        vs[RING - 1] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scales), 2 * at + 1));
         ++at;
-        const uint32_t dst = ring0 + slot * 2 * F::KB;
-        const uint8_t *k = P.rows_at(P.kbase, pg, t), *v = P.rows_at(P.vbase, pg, t);
-        const int adv = P.advance(pg);
 #pragma unroll
-        for (int i = 0; i < L; ++i) P.template bring1<false, true>(k, adv, i, 0, dst + 0);
+        for (int kv = 0; kv < 2; ++kv)
 #pragma unroll
-        for (int i = 0; i < L; ++i) P.template bring1<true, true>(v, adv, i, 0, dst + F::KB);
+            for (int n = 0; n < NT; ++n) {
+                const uint8_t* src = P.rows_at(kv ? P.vbase : P.kbase, page[n], t + 32 * n);
+                const int adv = P.advance(page[n]);
+#pragma unroll
+                for (int i = 0; i < F::KB / 1024; ++i)
+                    P.template bring1<false, true>(src, adv, i, 0, dst + (kv * NT + n) * F::KB + 0);
+            }
     };
-    int32_t t0 = (lo & ~31) + 32 * wave;
-    if (t0 < hi)
+    int32_t t0 = (lo & ~(32 * NT - 1)) + 32 * NT * wave;
+    if (t0 < hi) issue(t0, 0);
+    __syncthreads();                                       // the queries are there
+    for (int st = 0; t0 < hi; t0 += step, st ^= 1) {
+        uint8_t* kt = ring + st * GROUP;
+        uint8_t* vt = kt + NT * F::KB;
+        int32_t pg[NT];
+        float ksc[NT], vsc[NT];
 #pragma unroll
-        for (int i = 0; i + 1 < RING; ++i) issue(t0 + i * step, i);
-    for (int st = 0; t0 < hi; t0 += step, st = (st + 1) % RING) {
-        uint8_t* kt = ring + st * 2 * F::KB;
-        wait_lds();                                        // the tile before has been read
-        issue(t0 + (RING - 1) * step, (st + RING - 1) % RING);     // (behind the piece: zeros, so that the counts stay)
-        const uint32_t gm = page[0] >= 0 ? 3u : 0u;
-        const bool masked = t0 < lastlo || t0 < lo || t0 + 32 > firsthi || t0 + 32 > hi || gm != 3u;
-        wait_loads<2 * L * (RING - 1) + L>();
-        P.template scores<1>(kt, ks[0], qf, sc);
-        if (masked) P.anew().mask(sc[0], t0, seen, gm);
-        const float mt = P.most(sc[0]);
+        for (int n = 0; n < NT; ++n) {
+            pg[n] = page[n];
+            ksc[n] = ks[n];
+            vsc[n] = vs[n];
+        }
+        keep_out<Q>();
+        wait_lds();                                        // the group before has been read
+        issue(t0 + step, st ^ 1);                          // (behind the piece: zeros, so that the counts stay)
+        bool masked = t0 < lastlo || t0 < lo || t0 + 32 * NT > firsthi || t0 + 32 * NT > hi;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) masked = masked || pg[n] < 0;
+        wait_loads<3 * L>();
+        f32x16 sc[NT][1];
+        P.template scores_of<NT>(kt, ksc, query, sc);
+        keep_out<Q>();
+        __builtin_amdgcn_sched_barrier(0);                 // (what lies between two of these fits the registers)
+        if (masked)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) P.anew().mask(sc[n][0], t0 + 32 * n, seen, pg[n] >= 0 ? 3u : 0u);
+        float mt = P.most(sc[0][0]);
+#pragma unroll
+        for (int n = 1; n < NT; ++n) mt = fmaxf(mt, P.most(sc[n][0]));
         if (__any(mt > run.m + slack)) {
             const float f = run.raise(mt, a.c);
 #pragma unroll
@@ -297,25 +349,41 @@ __device__ __forceinline__ void few_rows8(const Piece<Coded<Q>>& P, uint8_t* sme
 #pragma unroll
                 for (int i = 0; i < 16; ++i) acc[0][dt][i] *= f;
         }
-        weights8<Q>(sc[0], run, a, run.l);
-        constexpr int WP = F::NP == 1 ? 2 : 3;
-        u32x4 p[1][WP][2];
-        parts_of(sc[0], p[0]);
-        wait_loads<2 * L * (RING - 1)>();
-        uint8_t* vt = kt + F::KB;
-        P.clear_tail(t0, 0, 32, vt);
-        const bool odd = masked && P.anew().odd_values(vt);
-        if (halves) {
-            u32x4 half[1][1][2];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) half[0][0][k >> 2][k & 3] = l32 < 16 ? p[0][0][k >> 2][k & 3] : p[0][1][k >> 2][k & 3];
-            if (odd) P.anew().template values<1, 1, true>(vt, vs[0], half, acc);
-            else P.template values<1, 1>(vt, vs[0], half, acc);
-        } else {
-            if (odd) P.anew().template values<1, WP, true>(vt, vs[0], p, acc);
-            else P.template values<1, WP>(vt, vs[0], p, acc);
+        for (int n = 0; n < NT; ++n) weights8<Q>(sc[n][0], run, a, run.l);
+        __builtin_amdgcn_sched_barrier(0);
+        wait_loads<2 * L>();
+        bool odd = false;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) P.clear_tail(t0 + 32 * n, 0, 32, vt + n * F::KB);
+        if (masked)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) odd = odd || P.anew().odd_values(vt + n * F::KB);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const uint8_t* v = vt + n * F::KB;
+            keep_out<Q>();
+            __builtin_amdgcn_sched_barrier(0);
+            if (halves) {                                  // lanes 16 .. 31 (and 48 ..) have what the rounding takes away
+                u32x4 p[1][1][2];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float e0 = sc[n][0][2 * k], e1 = sc[n][0][2 * k + 1];
+                    const uint32_t w = cvt_bf16x2(e0, e1);
+                    p[0][0][k >> 2][k & 3] = cvt_bf16x2(fmaf(rest, bf_lo(w), e0), fmaf(rest, bf_hi(w), e1));
+                }
+                if (odd) P.anew().template values<1, 1, true>(v, vsc[n], p, acc);
+                else P.template values<1, 1>(v, vsc[n], p, acc);
+            } else {
+                constexpr int WP = F::NP == 1 ? 2 : 3;
+                u32x4 p[1][WP][2];
+                parts_of(sc[n][0], p[0]);
+                if (odd) P.anew().template values<1, WP, true>(v, vsc[n], p, acc);
+                else P.template values<1, WP>(v, vsc[n], p, acc);
+            }
+            if (odd)
+                P.anew().add_odd(v, t0 + 32 * n, seen, pg[n] >= 0 ? 3u : 0u, [&](int dt, int i, float y) { acc[0][dt][i] += y; });
         }
-        if (odd) P.anew().add_odd(vt, t0, seen, gm, [&](int dt, int i, float y) { acc[0][dt][i] += y; });
     }
     wait_loads<0>();
     run.l = xsum32(run.l);

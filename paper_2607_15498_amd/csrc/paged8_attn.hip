@@ -1,6 +1,5 @@
 // Attention of new tokens over pages of e4m3 codes, gfx950: bf16 queries, and the host side of both.
 #include "paged8_attn.h"
-#include "paged_agpr.h"
 
 namespace vr {
 

@@ -236,10 +236,10 @@ struct Form<Coded<Q>> {
     static constexpr int KB = 32 * ROWB;
     static constexpr int SB = 8192, KT = SB / ROWB, SPS = KT / 32, STAGES = 4;
     static constexpr int LPW = SB / 1024 / WAVES, WROWS = LPW * 1024 / ROWB;
-    // few rows: rings of RING tiles of 32 keys and their values a wave; their sums, joined
-    static constexpr int RING = 16 / WAVES;
-    static constexpr size_t LDS = sizeof(Q) == 2 ? 128 * 1024 : 136 * 1024;
-    static_assert(STAGES * 2 * SB <= (int)LDS && WAVES * RING * 2 * KB <= (int)LDS && WAVES * 32 * 134 * 4 <= (int)LDS, "of the largest");
+    // few rows: rings of two groups of FEW_TILES x 32 keys and their values a wave; their sums, joined
+    static constexpr int FEW_TILES = sizeof(Q) == 2 ? 2 : 1;
+    static constexpr size_t LDS = 128 * 1024 + NP * 8192;      // (the rings, and a block of 32 queries)
+    static_assert(STAGES * 2 * SB <= (int)LDS && WAVES * FEW_TILES * 4 * KB + NP * 8192 <= (int)LDS && WAVES * 32 * 134 * 4 <= (int)LDS, "of the largest");
 };
 
 // A piece of a tile: its keys, where their rows lie, and what its rows see.
