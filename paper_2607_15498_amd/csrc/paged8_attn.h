@@ -108,31 +108,38 @@ struct Piece<Coded<Q>> : PieceOf<Coded<Q>> {
         for (int i = lane; i < (r1 - from) * F::PPR; i += 64)
             *reinterpret_cast<uint4*>(vt + from * F::ROWB + 16 * i) = uint4{0, 0, 0, 0};
     }
-    __device__ __forceinline__ void query(u32x4 (&qf)[F::NP][F::NF], int64_t token, int head) const {
+    // The third parts of fp32 queries lie in shared memory, [NF][64]: in registers they leave too few.
+    static constexpr int HELD = F::NP == 1 ? 1 : 2;
+    __device__ __forceinline__ void query(u32x4 (&qf)[HELD][F::NF], u32x4* low, int64_t token, int head) const {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            load_query((const Q*)a.q + token * a.q_stride + (int64_t)head * D, h, j, [&](int p, int k, const u32x4& f) { qf[p][k] = f; });
+            load_query((const Q*)a.q + token * a.q_stride + (int64_t)head * D, h, j, [&](int p, int k, const u32x4& f) {
+                if (p < HELD) qf[p][k] = f;
+                else low[k * 64 + lane] = f;
+            });
     }
-    // scores of NC blocks of 32 rows with 32 keys of one scale, the smallest parts first
+    // scores of NC blocks of 32 rows with 32 keys of one scale
     template <int NC>
-    __device__ __forceinline__ void scores(const uint8_t* kt, float scale, const u32x4 (&qf)[NC][F::NP][F::NF], f32x16 (&sc)[NC]) const {
+    __device__ __forceinline__ void scores(const uint8_t* kt, float scale, const u32x4 (&qf)[NC][HELD][F::NF], const u32x4* low,
+                                           f32x16 (&sc)[NC]) const {
 #pragma unroll
         for (int c = 0; c < NC; ++c)
 #pragma unroll
             for (int i = 0; i < 16; ++i) sc[c][i] = 0.f;
-        u32x4 kf[F::NF];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const u32x4 w = *reinterpret_cast<const u32x4*>(kt + (kaddr ^ (32u * j)));
-            kf[2 * j] = decode8(uint2{w[0], w[1]}, scale);
-            kf[2 * j + 1] = decode8(uint2{w[2], w[3]}, scale);
+            const u32x4 kf[2] = {decode8(uint2{w[0], w[1]}, scale), decode8(uint2{w[2], w[3]}, scale)};
+            if constexpr (F::NP == 3)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) sc[0] = mfma32(kf[k], low[(2 * j + k) * 64 + lane], sc[0]);
+#pragma unroll
+            for (int p = HELD - 1; p >= 0; --p)
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int c = 0; c < NC; ++c) sc[c] = mfma32(kf[k], qf[c][p][2 * j + k], sc[c]);
         }
-#pragma unroll
-        for (int p = F::NP - 1; p >= 0; --p)
-#pragma unroll
-            for (int k = 0; k < F::NF; ++k)
-#pragma unroll
-                for (int c = 0; c < NC; ++c) sc[c] = mfma32(kf[k], qf[c][p][k], sc[c]);
     }
     // ... of one block of rows with NT blocks of keys, side by side
     template <int NT>
@@ -458,14 +465,16 @@ __device__ __forceinline__ void many_rows8(const Piece<Coded<Q>>& P, uint8_t* sm
     Many<Coded<Q>> M(P, smem, row0, rows);
     if (M.stages) M.begin();
     Running run[NC];
-    u32x4 qf[NC][F::NP][F::NF];
+    static_assert(F::NP == 1 || NC == 1, "one block's third parts");
+    u32x4 qf[NC][Piece<Coded<Q>>::HELD][F::NF];
+    u32x4* low = reinterpret_cast<u32x4*>(smem + F::STAGES * 2 * F::SB) + M.wave * F::NF * 64;
     f32x16 acc[NC][4], sc[NC];
     typename Piece<Coded<Q>>::Seen seen[NC];
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
         int32_t tok, head;
         M.row_of(c, P.l32, tok, head);
-        P.query(qf[c], P.r.q0 + tok, head);
+        P.query(qf[c], low, P.r.q0 + tok, head);
         seen[c] = M.keys_seen(c);
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt)
@@ -480,7 +489,7 @@ __device__ __forceinline__ void many_rows8(const Piece<Coded<Q>>& P, uint8_t* sm
         }
         if (j < M.jf || j >= M.jl) continue;
         const float ks = M.key_scale(j), vs = M.value_scale(j);
-        P.template scores<NC>(M.keys_of(j), ks, qf, sc);
+        P.template scores<NC>(M.keys_of(j), ks, qf, low, sc);
         const bool masked = M.masked(j);
         const int32_t t0 = M.t_first + 32 * j;
         u32x4 p[NC][F::NP][2];                             // (bf16: rounded, as a chunk's matrix products are what it costs)

@@ -142,11 +142,16 @@ __global__ __launch_bounds__(256, 2) void paged8_mass_kernel(MassArgs m) {
     float4* row_of = reinterpret_cast<float4*>(smem + M::LDS - M::SUMS - M::ROWS);   // what is subtracted, its rest as a factor, keys seen
     const SeqRange first = load_range(a, lane);
     // tiles a wave: as many as leave the card two workgroups a CU
-    int64_t all = 0;
-    for (int s0 = 0; s0 < a.S; s0 += 64) all += (m.keys(s0 ? load_range(a, s0 + lane) : first) + 127) / 128;
-    for (int k = 1; k < WAVE; k <<= 1) all += __shfl_xor(all, k, WAVE);
-    all = first_lane(all) * a.G;
-    const int U = all >= 8 * 2 * SLOTS ? 8 : all >= 4 * 2 * SLOTS ? 4 : all >= 2 * 2 * SLOTS ? 2 : 1, per = 128 * U;
+    constexpr int ENOUGH = 8 * 2 * SLOTS;                  // (no sequence counts for more, so that 32 bits do)
+    int32_t all = 0;
+    for (int s0 = 0; s0 < a.S; s0 += 64) {
+        const int32_t n = (m.keys(s0 ? load_range(a, s0 + lane) : first) + 127) / 128;
+        all += n < ENOUGH ? n : ENOUGH;
+    }
+    for (int k = 1; k < (a.S < WAVE ? a.S : WAVE); k <<= 1) all += __shfl_xor(all, k, WAVE);
+    all = first_lane(all);
+    all = (all < ENOUGH ? all : ENOUGH) * a.G;
+    const int U = all >= ENOUGH ? 8 : all >= 4 * 2 * SLOTS ? 4 : all >= 2 * 2 * SLOTS ? 2 : 1, per = 128 * U;
     Search from;
     for (int64_t u = blockIdx.x;; u += gridDim.x) {
         Found f;
@@ -173,11 +178,20 @@ __global__ __launch_bounds__(256, 2) void paged8_mass_kernel(MassArgs m) {
             if (t < klen) T.page = T.P.page_of(T.P.raw_page(t), t);
             T.scale = T.P.scale_of(T.page, t, false);
         }
-        // the sums begin with what older keys have been paid
-        for (int i = 0; i < U; i += 2) {
-            const int32_t t = T.first + 128 * (i + h) + l32;
-            if (i + h < U) sums[32 * (i + h) + l32] = t < klen && t < old ? m.mass[at + t] : 0.f;
+        // the sums begin with what older keys have been paid (asked for before the keys, used behind them)
+        float paid[MOST_U / 2];
+#pragma unroll
+        for (int i = 0; i < MOST_U / 2; ++i) {
+            const int32_t t = T.first + 128 * (2 * i + h) + l32;
+            paid[i] = 2 * i + h < U && t < klen && t < old ? m.mass[at + t] : 0.f;
         }
+        auto begin_sums = [&]() {
+#pragma unroll
+            for (int i = 0; i < MOST_U / 2; ++i)
+                if (2 * i + h < U) sums[32 * (2 * i + h) + l32] = paid[i];
+        };
+        if (c0 >= end) begin_sums();
+        bool begun = false;
         for (; c0 < end; c0 += 32 * M::RB_MANY) {
             const int nb = few ? 1 : end - c0 < 32 * M::RB_MANY ? (int)((end - c0 + 31) / 32) : M::RB_MANY;
             if (few) T.template begin<M::RING_FEW>();
@@ -200,6 +214,8 @@ __global__ __launch_bounds__(256, 2) void paged8_mass_kernel(MassArgs m) {
                 if (!real || hi < lo) lo = hi = 0;
                 row_of[rb * 32 + l32] = float4{z, rest, __int_as_float(lo), __int_as_float(hi)};
             }
+            if (!begun) begin_sums();
+            begun = true;
             __syncthreads();
             if (few) T.template weigh<M::RING_FEW>(frag, row_of, nb, sums);
             else T.template weigh<M::RING_MANY>(frag, row_of, nb, sums);

@@ -239,7 +239,7 @@ struct Form<Coded<Q>> {
     // few rows: rings of two groups of FEW_TILES x 32 keys and their values a wave; their sums, joined
     static constexpr int FEW_TILES = sizeof(Q) == 2 ? 2 : 1;
     static constexpr size_t LDS = 128 * 1024 + NP * 8192;      // (the rings, and a block of 32 queries)
-    static_assert(STAGES * 2 * SB <= (int)LDS && WAVES * FEW_TILES * 4 * KB + NP * 8192 <= (int)LDS && WAVES * 32 * 134 * 4 <= (int)LDS, "of the largest");
+    static_assert(STAGES * 2 * SB + (NP == 3 ? WAVES * 8192 : 0) <= (int)LDS && WAVES * FEW_TILES * 4 * KB + NP * 8192 <= (int)LDS && WAVES * 32 * 134 * 4 <= (int)LDS, "of the largest");
 };
 
 // A piece of a tile: its keys, where their rows lie, and what its rows see.

@@ -81,7 +81,7 @@ VR_HD Costs costs_of(bool bf16) {
 }
 // ... over pages of e4m3 codes
 VR_HD Costs costs8_of(bool bf16) {
-    return bf16 ? Costs{3, 10, 600, 4400, 400, 256} : Costs{5, 24, 600, 1800, 400, 128};
+    return bf16 ? Costs{3, 8, 1000, 4400, 400, 256} : Costs{5, 24, 600, 1800, 400, 128};
 }
 VR_HD bool is_many(SeqRange r, int Hg) { return seq_rows(r, Hg) > ROWS_FEW; }
 

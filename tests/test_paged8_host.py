@@ -132,7 +132,7 @@ def test_append_refused(L, kw, code):
     (dict(out=6 * A), EINVAL), (dict(ws=None), EINVAL), (dict(ws_bytes=16), EINVAL), (dict(ws=A + 4), EINVAL),
 ])
 def test_attn_refused(L, kw, code):
-    assert attn(L, None, batch(width=16), **kw) == code and L.varrate_last_error()    # 1024 keys: may be cut
+    assert attn(L, None, batch(width=32), **kw) == code and L.varrate_last_error()    # 2048 keys: may be cut
 
 
 @pytest.mark.parametrize("kw,code", QUERIES + [
