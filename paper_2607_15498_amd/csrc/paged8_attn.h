@@ -40,26 +40,34 @@ __device__ __forceinline__ uint32_t cut2(float& a, float& b) {
     return x >> 16 | y;
 }
 
-// A row's query (src) as B operands, in parts: fragments 2 j and 2 j + 1 are dims 16 (2 j + h) .. of 8 each; put(part, k, fragment)
+// 8 dims of a row's query as a B operand, in parts; put(part, fragment)
+template <typename Q, typename A>
+__device__ __forceinline__ void query_parts(const Q* at, A&& put) {
+    if constexpr (sizeof(Q) == 2) put(0, load16(at));
+    else {
+        float x[8];
+        *reinterpret_cast<f32x4*>(x) = *reinterpret_cast<const f32x4*>(at);
+        *reinterpret_cast<f32x4*>(x + 4) = *reinterpret_cast<const f32x4*>(at + 4);
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+            u32x4 f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f[e] = cut2(x[2 * e], x[2 * e + 1]);
+            put(p, f);
+        }
+    }
+}
+// A row's query (src): fragments 2 j and 2 j + 1 are dims 16 (2 j + h) .. of 8 each; put(part, k, fragment)
 template <typename Q, typename A>
 __device__ __forceinline__ void load_query(const Q* src, int h, int j, A&& put) {
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-        const Q* at = src + 16 * (2 * j + h) + 8 * b;
-        if constexpr (sizeof(Q) == 2) put(0, 2 * j + b, load16(at));
-        else {
-            float x[8];
-            *reinterpret_cast<f32x4*>(x) = *reinterpret_cast<const f32x4*>(at);
-            *reinterpret_cast<f32x4*>(x + 4) = *reinterpret_cast<const f32x4*>(at + 4);
-#pragma unroll
-            for (int p = 0; p < 3; ++p) {
-                u32x4 f;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) f[e] = cut2(x[2 * e], x[2 * e + 1]);
-                put(p, 2 * j + b, f);
-            }
-        }
-    }
+    for (int b = 0; b < 2; ++b)
+        query_parts(src + 16 * (2 * j + h) + 8 * b, [&](int p, const u32x4& f) { put(p, 2 * j + b, f); });
+}
+// ... for products of 16 rows: fragment k = 2 j + b is dims 16 (q + 4 j) + 8 b ..; put(part, fragment)
+template <typename Q, typename A>
+__device__ __forceinline__ void load_query16(const Q* src, int q, int k, A&& put) {
+    query_parts(src + 16 * (q + 4 * (k >> 1)) + 8 * (k & 1), put);
 }
 
 template <typename Q>

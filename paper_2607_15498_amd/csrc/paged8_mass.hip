@@ -58,6 +58,17 @@ __device__ __forceinline__ float sum_lanes(f32x16 x) {
     return y + dpp<0xB1>(y);
 }
 
+// The same of 8 keys, lane 16 q + i: key 16 (k / 4) + 4 q + k % 4 in x[k], added over i: lane i ends with the key of k = i / 2.
+__device__ __forceinline__ float sum_lanes16(float (&x)[8]) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = (lane & 8 ? x[k + 4] : x[k]) + dpp<0x140>(lane & 8 ? x[k] : x[k + 4]);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) x[k] = (lane & 4 ? x[k + 2] : x[k]) + dpp<0x141>(lane & 4 ? x[k] : x[k + 2]);
+    const float y = (lane & 2 ? x[1] : x[0]) + dpp<0x4E>(lane & 2 ? x[0] : x[1]);
+    return y + dpp<0xB1>(y);
+}
+
 // A wave's tiles: number i is keys first + 128 i .. + 31, i < U; page and scale of tile i in lane i.
 template <typename Q>
 struct Tiles {
@@ -128,6 +139,66 @@ struct Tiles {
         wait_loads<0>();
         wait_lds();
     }
+    // Up to 16 rows: products of 16 x 16, half of the work.  frag [NP][4][64]: lane 16 q + i has dims 16 (q + 4 j) + 8 b .. of row i in
+    // number 2 j + b.
+    template <int R>
+    __device__ __forceinline__ void weigh16(const u32x4* frag, const float4* row_of, float* sums) const {
+        typedef Form<Coded<Q>> F;
+        const AttnArgs& a = P.a;
+        const int i16 = P.lane & 15, q4 = P.lane >> 4;
+        const uint32_t kaddr = (uint32_t)(i16 * F::ROWB + (q4 ^ P.swizzle(i16)) * 16);
+        u32x4 qf[F::NP][4];
+#pragma unroll
+        for (int p = 0; p < F::NP; ++p)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) qf[p][k] = frag[(p * 4 + k) * 64 + P.lane];
+        const float4 w = row_of[i16];
+        const int32_t lo = __float_as_int(w.z), hi = __float_as_int(w.w);
+        for (int i = 0; i < U; ++i) {
+            wait_lds();                                    // the tile before has been read
+            issue<R>(i + R - 1);
+            wait_loads<4 * (R - 1)>();
+            if (__builtin_amdgcn_readlane(page, i) < 0) continue;
+            const int32_t t0 = first + 128 * i;
+            const uint8_t* kt = ring + i % R * 4096;
+            const float sc_k = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scale), i));
+            f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+            u32x4 kf[2][4];
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const u32x4 c = *reinterpret_cast<const u32x4*>(kt + 2048 * n + (kaddr ^ (64u * j)));
+                    kf[n][2 * j] = decode8(uint2{c[0], c[1]}, sc_k);
+                    kf[n][2 * j + 1] = decode8(uint2{c[2], c[3]}, sc_k);
+                }
+#pragma unroll
+            for (int p = F::NP - 1; p >= 0; --p)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) s[n] = mfma(kf[n][k], qf[p][k], s[n]);
+            float x[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float y = s[k >> 2][k & 3];
+                x[k] = __builtin_amdgcn_exp2f(fmaf(y, a.c_lo, fmaf(y, a.c, -w.x)));
+            }
+            if (__any(lo > t0 || hi < t0 + 32)) {
+                const uint32_t at = (uint32_t)(t0 + 4 * q4 - lo), n = (uint32_t)(hi - lo);
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (at + 16 * (k >> 2) + (k & 3) >= n) x[k] = 0.f;
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] *= w.y;
+            const float mine = sum_lanes16(x);
+            const int k = i16 >> 1;
+            if (!(i16 & 1)) sums[32 * i + 16 * (k >> 2) + 4 * q4 + (k & 3)] += mine;
+        }
+        wait_loads<0>();
+        wait_lds();
+    }
 };
 
 template <typename Q>
@@ -169,7 +240,7 @@ __global__ __launch_bounds__(256, 2) void paged8_mass_kernel(MassArgs m) {
         if (a.window && (int64_t)last + a.window - old < i1) i1 = last + a.window - old;
         const int64_t rows = (int64_t)r.qlen * a.Hg, end = i1 > i0 ? (int64_t)i1 * a.Hg : 0;
         int64_t c0 = (int64_t)i0 * a.Hg & ~(int64_t)31;
-        const bool few = end - c0 <= 32;
+        const bool few = end - c0 <= 32, half = rows <= 16;
         Tiles<Q> T = {Piece<Coded<Q>>(a, f, g, 0, klen, lane), top + 32 * wave, -1, 1.f, U, 0, nullptr};
         T.ring = smem + (few ? M::FRAGS + wave * M::RING_FEW * F::KB : M::RB_MANY * M::FRAGS + wave * M::RING_MANY * F::KB);
         T.ring0 = first_lane((int)(uint32_t)(size_t)(__attribute__((address_space(3))) uint8_t*)T.ring);
@@ -196,13 +267,18 @@ __global__ __launch_bounds__(256, 2) void paged8_mass_kernel(MassArgs m) {
             const int nb = few ? 1 : end - c0 < 32 * M::RB_MANY ? (int)((end - c0 + 31) / 32) : M::RB_MANY;
             if (few) T.template begin<M::RING_FEW>();
             else T.template begin<M::RING_MANY>();
-            u32x4* frag = reinterpret_cast<u32x4*>(smem);  // [RB][NP][NF][64]
-            for (int rb = 0; rb < nb; ++rb) {              // every wave a fourth of the dims
+            u32x4* frag = reinterpret_cast<u32x4*>(smem);  // [RB][NP][NF][64], every wave a fourth of the dims
+            if (half) {
+                const int32_t mine = (lane & 15) < rows ? lane & 15 : 0, tok = mine / a.Hg;
+                load_query16((const Q*)a.q + (int64_t)(r.q0 + tok) * a.q_stride + (int64_t)(g * a.Hg + mine % a.Hg) * D, lane >> 4, wave,
+                             [&](int p, const u32x4& x) { frag[(p * 4 + wave) * 64 + lane] = x; });
+            }
+            for (int rb = 0; rb < nb; ++rb) {
                 const int64_t mine = c0 + 32 * rb + l32;
                 const bool real = mine < rows;
                 const int64_t row = real ? mine : rows - 1;
                 const int32_t tok = (int32_t)(row / a.Hg), hd = g * a.Hg + (int32_t)(row % a.Hg);
-                load_query((const Q*)a.q + (int64_t)(r.q0 + tok) * a.q_stride + (int64_t)hd * D, h, wave,
+                if (!half) load_query((const Q*)a.q + (int64_t)(r.q0 + tok) * a.q_stride + (int64_t)hd * D, h, wave,
                            [&](int p, int k, const u32x4& x) { frag[((rb * F::NP + p) * F::NF + k) * 64 + lane] = x; });
                 if ((rb & 3) != wave || h) continue;
                 const float lse = m.lse[(int64_t)(r.q0 + tok) * H + hd];
@@ -217,7 +293,8 @@ __global__ __launch_bounds__(256, 2) void paged8_mass_kernel(MassArgs m) {
             if (!begun) begin_sums();
             begun = true;
             __syncthreads();
-            if (few) T.template weigh<M::RING_FEW>(frag, row_of, nb, sums);
+            if (half) T.template weigh16<M::RING_FEW>(frag, row_of, sums);
+            else if (few) T.template weigh<M::RING_FEW>(frag, row_of, nb, sums);
             else T.template weigh<M::RING_MANY>(frag, row_of, nb, sums);
             __syncthreads();                               // the rows have been read
         }
