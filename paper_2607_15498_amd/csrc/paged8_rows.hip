@@ -122,7 +122,7 @@ __device__ __forceinline__ void append_block(const Append8& p, int which, int g,
         for (int row = rr; row < held; row += 4) {
             float y[8];
             values8(*reinterpret_cast<const uint2*>(old + (int64_t)row * D), 1.f, y);
-            *reinterpret_cast<uint2*>(old + (int64_t)row * D) = encode8(y, back);
+            *reinterpret_cast<uint2*>(old + (int64_t)row * D) = encode8<false>(y, back);
         }
     }
     const float to = power(-now);
@@ -131,7 +131,7 @@ __device__ __forceinline__ void append_block(const Append8& p, int which, int g,
         if (4 * k + rr < n) {
             float y[8];
             x[k].get(y);
-            const uint2 w = encode8(y, to);
+            const uint2 w = now == E_HI ? encode8<true>(y, to) : encode8<false>(y, to);
             __builtin_nontemporal_store((uint64_t)w.y << 32 | w.x, (uint64_t*)(dst + (int64_t)(4 * k + rr) * D));
         }
     if (lane == 0) *scale = (uint8_t)(now + 127);
@@ -246,7 +246,7 @@ __global__ __launch_bounds__(SEL) void evict8_select(Evict8 p) {
     extern __shared__ __align__(16) uint32_t ranks[];
     __shared__ __align__(16) uint32_t hist[4096];          // a digit's copies lie together: equal digits of one read fall into different ones
     __shared__ __align__(16) uint32_t sums[SEL_WAVES];
-    __shared__ uint32_t found[2];
+    __shared__ uint32_t found[3];                          // the digit, how many of its ranks stay, and of how many
     const int s = (int)(blockIdx.x / (uint32_t)p.pool.G), g = (int)(blockIdx.x % (uint32_t)p.pool.G), tid = threadIdx.x;
     const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int32_t n = tokens_of(p, s), m = n < p.keep ? n : p.keep;
@@ -285,18 +285,29 @@ __global__ __launch_bounds__(SEL) void evict8_select(Evict8 p) {
     if (parts == 1) load(0);
 #pragma unroll 1
     for (int pass = 0; pass < 3; ++pass) {
-        const int shift = pass == 0 ? 22 : pass == 1 ? 11 : 0, bits = pass == 0 ? 10 : 11, copies = pass == 0 ? 4 : 2;
+        const int shift = pass == 0 ? 22 : pass == 1 ? 11 : 0, bits = pass == 0 ? 10 : 11;
         reinterpret_cast<uint4*>(hist)[tid] = uint4{0, 0, 0, 0};
         __syncthreads();
 #pragma unroll 1
         for (int part = 0; part < parts; ++part) {
             if (parts > 1) load(part);
-            for (int i = 0; i < turns; ++i) {
-                const u32x4 r = quads[at + 64 * i];
+            if (pass == 0) {
+                for (int i = 0; i < turns; ++i) {
+                    const u32x4 r = quads[at + 64 * i];
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (pass == 0 || (r[k] ^ prefix) >> (shift + bits) == 0)
-                        atomicAdd(&hist[(r[k] >> shift & ((1u << bits) - 1)) * copies + (lane & (copies - 1))], 1u);
+                    for (int k = 0; k < 4; ++k) atomicAdd(&hist[(r[k] >> 22) * 4 + (lane & 3)], 1u);
+                }
+            } else {
+                for (int i = 0; i < turns; ++i) {          // few begin as those before
+                    const u32x4 r = quads[at + 64 * i];
+                    bool in[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) in[k] = (r[k] ^ prefix) >> (shift + 11) == 0;
+                    if (in[0] || in[1] || in[2] || in[3])
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            if (in[k]) atomicAdd(&hist[(r[k] >> shift & 2047u) * 2 + (lane & 1)], 1u);
+                }
             }
         }
         __syncthreads();
@@ -328,10 +339,16 @@ __global__ __launch_bounds__(SEL) void evict8_select(Evict8 p) {
             const bool second = before + a < need;
             found[0] = (uint32_t)(top - (second ? 1 : 0));
             found[1] = need - before - (second ? a : 0);
+            found[2] = second ? b : a;
         }
         __syncthreads();
         prefix |= found[0] << shift;
         need = found[1];
+        if (found[2] == need && prefix) {                  // all that begin so stay: no further digits
+            prefix -= 1;
+            need = 0;
+            break;
+        }
     }
     // ranks above `prefix`, and the first `need` equal to it: counted per wave (above and equal, 16 bits each), then placed
     uint32_t place = 0, equal = 0;                         // in the parts before
@@ -426,30 +443,51 @@ __global__ __launch_bounds__(256) void evict8_move(Evict8 p) {
             }
         }
         uint2 w[8];
+        float sc[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             const int64_t at = __shfl(from, 4 * k + rr, WAVE);
+            sc[k] = __shfl(scale, 4 * k + rr, WAVE);
             w[k] = uint2{0, 0};
             if (at >= 0) w[k] = *reinterpret_cast<const uint2*>(p.pool.code[which] + at + c);
         }
-        float x[8][8];
+        // the largest magnitude: codes without their signs are in the order of what they stand for (0x7F: NaN)
         uint32_t most = 0;
+        bool nan = false;
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            values8(w[k], __shfl(scale, 4 * k + rr, WAVE), x[k]);
+            const u16x2 m0 = __builtin_elementwise_max(__builtin_bit_cast(u16x2, w[k].x & 0x007F007Fu), __builtin_bit_cast(u16x2, w[k].x >> 8 & 0x007F007Fu));
+            const u16x2 m1 = __builtin_elementwise_max(__builtin_bit_cast(u16x2, w[k].y & 0x007F007Fu), __builtin_bit_cast(u16x2, w[k].y >> 8 & 0x007F007Fu));
+            const u16x2 m = __builtin_elementwise_max(m0, m1);
+            const int top = m[0] > m[1] ? m[0] : m[1];
+            nan = nan || top == 0x7F;
+            const uint32_t v = __float_as_uint(__builtin_amdgcn_cvt_f32_fp8(top, 0) * sc[k]);
+            most = v > most ? v : most;
+        }
+        if (__any(nan)) {
+            most = 0;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const uint32_t v = magnitude(x[k][e]);
-                most = v > most ? v : most;
+            for (int k = 0; k < 8; ++k) {
+                float x[8];
+                values8(w[k], sc[k], x);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t v = magnitude(x[e]);
+                    most = v > most ? v : most;
+                }
             }
         }
         const int now = exponent_for(wave_most(most));
-        const float s_to = power(-now);
+        const float to_now = power(-now);
         const int32_t slot = p.pool.slot(i0);
         uint8_t* dst = p.pool.code[which] + p.pool.row(to, g, slot) + c;
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-            if (4 * k + rr < rows) *reinterpret_cast<uint2*>(dst + (int64_t)(4 * k + rr) * D) = encode8(x[k], s_to);
+            if (4 * k + rr < rows) {
+                float x[8];
+                values8(w[k], 1.f, x);
+                *reinterpret_cast<uint2*>(dst + (int64_t)(4 * k + rr) * D) = encode8<false>(x, sc[k] * to_now);
+            }
         if (lane == 0) p.pool.scale[which][p.pool.block(to, g, slot)] = (uint8_t)(now + 127);
     }
 }

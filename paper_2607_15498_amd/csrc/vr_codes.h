@@ -25,18 +25,20 @@ __device__ __forceinline__ int exponent_of(uint8_t b) {
     const int e = (int)b - 127;
     return e < E_LO ? E_LO : e > E_HI ? E_HI : e;
 }
-// x times the power of two s as a code's value to be rounded: beyond 448 (E_HI alone) it is 448; infinities become NaN with the conversion
-__device__ __forceinline__ float scaled(float x, float s) {
-    const float y = x * s;
-    return fabsf(y) > 448.f && fabsf(y) < INFINITY ? copysignf(448.f, y) : y;
-}
-// 8 numbers times s, rounded to the nearest codes
+// 8 numbers times s, rounded to the nearest codes; infinities become NaN.  ALL: beyond 448 it is 448 (what blocks of E_HI alone hold)
+template <bool ALL>
 __device__ __forceinline__ uint2 encode8(const float (&x)[8], float s) {
+    float y[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        y[k] = x[k] * s;
+        if (ALL && fabsf(y[k]) > 448.f && fabsf(y[k]) < INFINITY) y[k] = copysignf(448.f, y[k]);
+    }
     uint32_t w[2];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-        int v = __builtin_amdgcn_cvt_pk_fp8_f32(scaled(x[4 * k], s), scaled(x[4 * k + 1], s), 0, false);
-        w[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(scaled(x[4 * k + 2], s), scaled(x[4 * k + 3], s), v, true);
+        const int v = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * k], y[4 * k + 1], 0, false);
+        w[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[4 * k + 2], y[4 * k + 3], v, true);
     }
     return uint2{w[0], w[1]};
 }
