@@ -215,11 +215,19 @@ __global__ __launch_bounds__(256, 2) void paged8_mass_kernel(MassArgs m) {
     // tiles a wave: as many as leave the card two workgroups a CU
     constexpr int ENOUGH = 8 * 2 * SLOTS;                  // (no sequence counts for more, so that 32 bits do)
     int32_t all = 0;
+    float claimed = 0.f;                                   // rows, by all sequences together
     for (int s0 = 0; s0 < a.S; s0 += 64) {
-        const int32_t n = (m.keys(s0 ? load_range(a, s0 + lane) : first) + 127) / 128;
+        const SeqRange r = s0 ? load_range(a, s0 + lane) : first;
+        const int32_t n = (m.keys(r) + 127) / 128;
         all += n < ENOUGH ? n : ENOUGH;
+        claimed += (float)r.qlen;
     }
-    for (int k = 1; k < (a.S < WAVE ? a.S : WAVE); k <<= 1) all += __shfl_xor(all, k, WAVE);
+    for (int k = 1; k < (a.S < WAVE ? a.S : WAVE); k <<= 1) {
+        all += __shfl_xor(all, k, WAVE);
+        claimed += __shfl_xor(claimed, k, WAVE);
+    }
+    // More rows than there are (and more than rounding adds): starts fall, up to S / 2 times the work of any call.  Nothing is done.
+    if (first_lane(claimed) > 1.01f * (float)a.T) return;
     all = first_lane(all);
     all = (all < ENOUGH ? all : ENOUGH) * a.G;
     const int U = all >= ENOUGH ? 8 : all >= 4 * 2 * SLOTS ? 4 : all >= 2 * 2 * SLOTS ? 2 : 1, per = 128 * U;
