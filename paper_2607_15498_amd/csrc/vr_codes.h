@@ -54,13 +54,6 @@ __device__ __forceinline__ void values8(uint2 w, float s, float (&x)[8]) {
         x[4 * k + 3] = b[1] * s;
     }
 }
-__device__ __forceinline__ void write8(uint16_t* p, const float (&x)[8]) {
-    *reinterpret_cast<u32x4*>(p) = u32x4{cvt_bf16x2(x[0], x[1]), cvt_bf16x2(x[2], x[3]), cvt_bf16x2(x[4], x[5]), cvt_bf16x2(x[6], x[7])};
-}
-__device__ __forceinline__ void write8(float* p, const float (&x)[8]) {
-    *reinterpret_cast<f32x4*>(p) = f32x4{x[0], x[1], x[2], x[3]};
-    *reinterpret_cast<f32x4*>(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
-}
 // the largest of a wave's values, in every lane
 __device__ __forceinline__ uint32_t wave_most(uint32_t v) {
 #pragma unroll
