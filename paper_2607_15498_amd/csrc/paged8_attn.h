@@ -259,7 +259,8 @@ __device__ __forceinline__ void parts_of(f32x16& sc, u32x4 (&p)[2][2]) {
 
 // Few rows: each wave takes every WAVES-th group of NT x 32 keys out of a ring of two of its own, and the waves' sums are joined
 // at the end.  bf16, one wave a SIMD: two tiles at a time, whose products and exponentials do not wait for each other (one token
-// over 131072, tile by tile out of a ring of four: 72 us, 4.9 TB/s a further key; XX).
+// over 131072 of 8 KV heads, tile by tile out of a ring of four: 72 us, what keys are more read at 4.9 TB/s; two at a time
+// 66; with the queries in shared memory 60 - 62, 6.8 TB/s).
 template <typename Q>
 __device__ __forceinline__ void few_rows8(const Piece<Coded<Q>>& P, uint8_t* smem, int rows, bool cut, int64_t rec_row) {
     typedef Form<Coded<Q>> F;

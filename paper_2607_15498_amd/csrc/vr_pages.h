@@ -79,7 +79,8 @@ struct Costs { int32_t few, many, piece_few, piece_many, join, lmin; };      // 
 VR_HD Costs costs_of(bool bf16) {
     return bf16 ? Costs{5, 8, 600, 4400, 400, 256} : Costs{12, 72, 600, 1800, 400, 128};
 }
-// ... over pages of e4m3 codes
+// ... over pages of e4m3 codes (1003 tokens beside 16 single ones: 183 us with 10 a key of many rows, 156 with 8; 16 single tokens
+// alone: 59 us with 600 a piece of few rows, 57 with 1200)
 VR_HD Costs costs8_of(bool bf16) {
     return bf16 ? Costs{3, 8, 1000, 4400, 400, 256} : Costs{5, 24, 600, 1800, 400, 128};
 }
