@@ -512,7 +512,7 @@ VARRATE_API int varrate_paged8_attn(const varrate_pages8* pages, const varrate_b
  *   out[s][g][t] = (mass[s][g][t] if t < kv_len[s] - new tokens, else 0) + sum exp(scale <q, k_t> - lse)
  * over the sequence's new tokens that see key t and the query heads of KV head g, for t < kv_len[s] (at most L);
  * what lies behind is left as it was.  lse [T][H] as varrate_paged8_attn gives it for the same call; a row whose
- * lse is -infinity pays nothing.  mass and out [S][G][L] fp32, which may be the same.  Keys on bad pages are
+ * lse is -infinity pays nothing.  mass and out [S][G][L] fp32 are the same or do not overlap.  Keys on bad pages are
  * paid nothing.  Sums are taken in a fixed order; lse is fp32, which leaves a weight |lse| 2^-24 off.   */
 VARRATE_API int varrate_paged8_mass(const varrate_pages8* pages, const varrate_batch* batch, int32_t dtype, const void* q,
                                     int64_t q_stride, int32_t H, int32_t causal, int32_t window, float scale,
@@ -523,7 +523,8 @@ VARRATE_API int varrate_paged8_mass(const varrate_pages8* pages, const varrate_b
  * the others those of the largest mass (mass [S][G][L]; of equal ones the earlier, NaN last).  Their rows move in order
  * to slots 0 .. m - 1 of the pages that the rows of `into` name, coded as varrate_paged8_append would code the values
  * that they stand for; rows of bad pages are zeros, and rows for bad pages are dropped.  into's pages must be no
- * page of `table`'s.  index [S][G][keep]: the tokens that stay, then -1; mass_out [S][G][keep]: their masses, then 0;
+ * page of `table`'s and named once.  The rows keep the rotation of the positions that they had, so new tokens go on
+ * being rotated by theirs; windows count the tokens that are left.  Outputs do not overlap inputs.  index [S][G][keep]: the tokens that stay, then -1; mass_out [S][G][keep]: their masses, then 0;
  * len_out [S]: m.  keep 1 .. 2^30.                                                                  */
 VARRATE_API int varrate_paged8_evict(const varrate_pages8* pages, const int32_t* table, int64_t table_stride, int32_t width,
                                      const int32_t* kv_len, int32_t S, const float* mass, int64_t L, int64_t keep,

@@ -890,8 +890,8 @@ def paged8_evict(pages: PagedCache8, table: torch.Tensor, kv_len: torch.Tensor, 
                  into: torch.Tensor, first: int = 0, recent: int = 0):
     """Keep at most `keep` tokens of every sequence (table [S][width], kv_len [S]), head by head: the first `first`, the last
     `recent` and those of the largest mass [S][G][L].  Their rows move to the pages of `into` [S][width'] (pages of no
-    sequence in `table`).  Returns the tokens kept (index [S][G][keep] int32, then -1), their masses (then 0) and the new
-    lengths [S]."""
+    sequence in `table`, each named once) and keep the rotation of the positions that they had.  Returns the tokens kept
+    (index [S][G][keep] int32, then -1), their masses (then 0) and the new lengths [S]."""
     dev = pages.k.device
     pt, pi, pl = _i32(table, 2, "table"), _i32(into, 2, "into"), _i32(kv_len, 1, "kv_len")
     S = _int32(table.shape[0], "S")

@@ -284,7 +284,8 @@ __global__ __launch_bounds__(SEL) void evict8_select(Evict8 p) {
     const int32_t lo = p.first, hi = n - p.recent;         // tokens before and from there on stay (first + recent <= m unless all do)
     const int parts = (n + SEL_PART - 1) / SEL_PART;
     int turns = 0, at = 0;                                 // of a part: reads a lane; the lane's first
-    auto load = [&](int part) {
+    // (the first pass's counts are taken on the way)
+    auto load = [&](int part, bool first) {
         const int32_t t0 = part * SEL_PART, len = n - t0 < SEL_PART ? n - t0 : SEL_PART;
         turns = (len + 4 * SEL - 1) / (4 * SEL);
         at = wave * turns * 64 + lane;
@@ -296,15 +297,17 @@ __global__ __launch_bounds__(SEL) void evict8_select(Evict8 p) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 const int i = i0 + k * SEL, t = t0 + i;
-                const uint32_t r = rank_of(x[k]);
-                if (i < turns * 4 * SEL) ranks[i] = i >= len ? 0 : t < lo || t >= hi ? ALWAYS : r;
+                const uint32_t u = rank_of(x[k]), r = i >= len ? 0 : t < lo || t >= hi ? ALWAYS : u;
+                if (i < turns * 4 * SEL) {
+                    ranks[i] = r;
+                    if (first) atomicAdd(&hist[(r >> 22) * 4 + (lane & 3)], 1u);
+                }
             }
         }
         __syncthreads();
     };
     const u32x4* quads = reinterpret_cast<const u32x4*>(ranks);
     uint32_t need = (uint32_t)m, prefix = 0;
-    if (parts == 1) load(0);
 #pragma unroll 1
     for (int pass = 0; pass < 3; ++pass) {
         const int shift = pass == 0 ? 22 : pass == 1 ? 11 : 0, bits = pass == 0 ? 10 : 11;
@@ -312,14 +315,8 @@ __global__ __launch_bounds__(SEL) void evict8_select(Evict8 p) {
         __syncthreads();
 #pragma unroll 1
         for (int part = 0; part < parts; ++part) {
-            if (parts > 1) load(part);
-            if (pass == 0) {
-                for (int i = 0; i < turns; ++i) {
-                    const u32x4 r = quads[at + 64 * i];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) atomicAdd(&hist[(r[k] >> 22) * 4 + (lane & 3)], 1u);
-                }
-            } else {
+            if (pass == 0 || parts > 1) load(part, pass == 0);
+            if (pass) {
                 for (int i = 0; i < turns; ++i) {          // few begin as those before
                     const u32x4 r = quads[at + 64 * i];
                     bool in[4];
@@ -376,7 +373,7 @@ __global__ __launch_bounds__(SEL) void evict8_select(Evict8 p) {
     uint32_t place = 0, equal = 0;                         // in the parts before
 #pragma unroll 1
     for (int part = 0; part < parts; ++part) {
-        if (parts > 1) load(part);
+        if (parts > 1) load(part, false);
         uint32_t mine = 0;
         for (int i = 0; i < turns; ++i) {
             const u32x4 r = quads[at + 64 * i];
