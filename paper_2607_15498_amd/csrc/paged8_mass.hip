@@ -10,7 +10,8 @@
 //   Few rows (single tokens): rings of four tiles, up to 16 rows in products of 16 x 16; the reads of the keys bound it (8 tokens over
 //   16384 of 4 KV heads of 7: 17 us, 11 of which any call takes; 32 x 32 products 20; fragments read from memory into
 //   registers, a wave's keys at a time, 42).  Many: 160 rows (fp32 32) are staged at once, and the exponentials and the products bound
-//   it (1024 tokens over 16384 of 8 heads of 4: 242 us, 549 TFLOP/s; a window of 32 over 32768: 19 us).
+//   it, with what the next rows' staging waits for (1024 tokens over 16384 of 8 heads of 4: 222 us, 595 TFLOP/s; a window of 32 over
+//   32768: 18 us).
 #include "paged8_attn.h"
 
 namespace vr {
@@ -94,6 +95,7 @@ struct Tiles {
     template <int R>
     __device__ __forceinline__ void weigh(const u32x4* frag, const float4* row_of, int nb, float* sums) const {
         typedef Form<Coded<Q>> F;
+        typedef MassForm<Q> M;
         const AttnArgs& a = P.a;
         for (int i = 0; i < U; ++i) {
             wait_lds();                                    // the tile before has been read
@@ -113,15 +115,30 @@ struct Tiles {
             f32x16 sum;
 #pragma unroll
             for (int k = 0; k < 16; ++k) sum[k] = 0.f;
+            // bf16: a block's fragments are read while the exponentials of the block before are taken (as the compiler has it, they are
+            // read where they are used, one after another: 1024 tokens over 16384 248 -> 235 us)
+            u32x4 qf[F::NP][F::NF];
+            float4 w;
+            auto read = [&](int rb) {
+#pragma unroll
+                for (int p = 0; p < F::NP; ++p)
+#pragma unroll
+                    for (int k = 0; k < F::NF; ++k) qf[p][k] = frag[((rb * F::NP + p) * F::NF + k) * 64 + P.lane];
+            };
+            read(0);
             for (int rb = 0; rb < nb; ++rb) {
+                w = row_of[rb * 32 + P.l32];
                 f32x16 x;
 #pragma unroll
                 for (int k = 0; k < 16; ++k) x[k] = 0.f;
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int p = F::NP - 1; p >= 0; --p)
 #pragma unroll
-                    for (int k = 0; k < F::NF; ++k) x = mfma32(kf[k], frag[((rb * F::NP + p) * F::NF + k) * 64 + P.lane], x);
-                const float4 w = row_of[rb * 32 + P.l32];
+                    for (int k = 0; k < F::NF; ++k) x = mfma32(kf[k], qf[p][k], x);
+                __builtin_amdgcn_sched_barrier(0);
+                if (M::RB_MANY > 1) read(rb + 1 < nb ? rb + 1 : rb);
+                __builtin_amdgcn_sched_barrier(0);
                 const int32_t lo = __float_as_int(w.z), hi = __float_as_int(w.w);
 #pragma unroll
                 for (int k = 0; k < 16; ++k) x[k] = __builtin_amdgcn_exp2f(fmaf(x[k], a.c_lo, fmaf(x[k], a.c, -w.x)));
@@ -273,36 +290,72 @@ __global__ __launch_bounds__(256, 2) void paged8_mass_kernel(MassArgs m) {
         };
         if (c0 >= end) begin_sums();
         bool begun = false;
+        // The rows of a stage, a fourth of the dims a wave, and the sums of every fourth block's: asked for while the stage before is
+        // used (1024 tokens over 1024: 134 -> 110 us; asked for behind the last tile's loads instead, they spill).
+        u32x4 raw[M::RB_MANY][2][sizeof(Q) / 2];
+        float lse[(M::RB_MANY + 3) / 4];
+        auto row_at = [&](int64_t c, int rb, bool& real, int32_t& tok, int32_t& hd) {
+            const int64_t mine = c + 32 * rb + l32;
+            real = mine < rows;
+            const uint32_t row = (uint32_t)(real ? mine : rows - 1);
+            tok = (int32_t)(row / (uint32_t)a.Hg);
+            hd = g * a.Hg + (int32_t)(row % (uint32_t)a.Hg);
+        };
+        auto ask = [&](int64_t c) {
+#pragma unroll
+            for (int rb = 0; rb < M::RB_MANY; ++rb) {
+                if (c + 32 * rb >= end) break;
+                bool real;
+                int32_t tok, hd;
+                row_at(c, rb, real, tok, hd);
+                const Q* src = (const Q*)a.q + (int64_t)(r.q0 + tok) * a.q_stride + (int64_t)hd * D + 16 * (2 * wave + h);
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int e = 0; e < (int)sizeof(Q) / 2; ++e) raw[rb][k][e] = load16((const uint8_t*)(src + 8 * k) + 16 * e);
+                if ((rb & 3) == wave) lse[rb >> 2] = m.lse[(int64_t)(r.q0 + tok) * H + hd];
+            }
+        };
+        u32x4* frag = reinterpret_cast<u32x4*>(smem);      // [RB][NP][NF][64]
+        if (!half && c0 < end) ask(c0);
         for (; c0 < end; c0 += 32 * M::RB_MANY) {
             const int nb = few ? 1 : end - c0 < 32 * M::RB_MANY ? (int)((end - c0 + 31) / 32) : M::RB_MANY;
             if (few) T.template begin<M::RING_FEW>();
             else T.template begin<M::RING_MANY>();
-            u32x4* frag = reinterpret_cast<u32x4*>(smem);  // [RB][NP][NF][64], every wave a fourth of the dims
-            if (half) {
-                const int32_t mine = (lane & 15) < rows ? lane & 15 : 0, tok = mine / a.Hg;
-                load_query16((const Q*)a.q + (int64_t)(r.q0 + tok) * a.q_stride + (int64_t)(g * a.Hg + mine % a.Hg) * D, lane >> 4, wave,
-                             [&](int p, const u32x4& x) { frag[(p * 4 + wave) * 64 + lane] = x; });
-            }
-            for (int rb = 0; rb < nb; ++rb) {
-                const int64_t mine = c0 + 32 * rb + l32;
-                const bool real = mine < rows;
-                const int64_t row = real ? mine : rows - 1;
-                const int32_t tok = (int32_t)(row / a.Hg), hd = g * a.Hg + (int32_t)(row % a.Hg);
-                if (!half) load_query((const Q*)a.q + (int64_t)(r.q0 + tok) * a.q_stride + (int64_t)hd * D, h, wave,
-                           [&](int p, int k, const u32x4& x) { frag[((rb * F::NP + p) * F::NF + k) * 64 + lane] = x; });
-                if ((rb & 3) != wave || h) continue;
-                const float lse = m.lse[(int64_t)(r.q0 + tok) * H + hd];
+            auto put_row = [&](int rb, int l, bool real, int32_t tok, float z0) {
                 // exp(scale x - lse) = exp2(c x - z) 2^-(what z lacks)
-                const float z = lse == -INFINITY ? INFINITY : lse * LOG2E;
-                const float rest = fabsf(z) < INFINITY ? __builtin_amdgcn_exp2f(-(fmaf(lse, LOG2E, -z) + lse * LOG2E_LO)) : 1.f;
+                const float z = z0 == -INFINITY ? INFINITY : z0 * LOG2E;
+                const float rest = fabsf(z) < INFINITY ? __builtin_amdgcn_exp2f(-(fmaf(z0, LOG2E, -z) + z0 * LOG2E_LO)) : 1.f;
                 int32_t lo, hi;
                 row_keys(r, tok, a.causal, a.window, lo, hi);
                 if (!real || hi < lo) lo = hi = 0;
-                row_of[rb * 32 + l32] = float4{z, rest, __int_as_float(lo), __int_as_float(hi)};
+                row_of[rb * 32 + l] = float4{z, rest, __int_as_float(lo), __int_as_float(hi)};
+            };
+            if (half) {
+                const int32_t mine = (lane & 15) < rows ? lane & 15 : 0, tok = mine / a.Hg, hd = g * a.Hg + mine % a.Hg;
+                load_query16((const Q*)a.q + (int64_t)(r.q0 + tok) * a.q_stride + (int64_t)hd * D, lane >> 4, wave,
+                             [&](int p, const u32x4& x) { frag[(p * 4 + wave) * 64 + lane] = x; });
+                if (wave == 0 && lane < 16) put_row(0, lane, lane < rows, tok, m.lse[(int64_t)(r.q0 + tok) * H + hd]);
+            } else {
+#pragma unroll
+                for (int rb = 0; rb < M::RB_MANY; ++rb) {
+                    if (rb >= nb) break;
+#pragma unroll
+                    for (int k = 0; k < 2; ++k)
+                        query_parts((const Q*)&raw[rb][k], [&](int p, const u32x4& x) {
+                            frag[((rb * F::NP + p) * F::NF + 2 * wave + k) * 64 + lane] = x;
+                        });
+                    if ((rb & 3) != wave || h) continue;
+                    bool real;
+                    int32_t tok, hd;
+                    row_at(c0, rb, real, tok, hd);
+                    put_row(rb, l32, real, tok, lse[rb >> 2]);
+                }
             }
             if (!begun) begin_sums();
             begun = true;
             __syncthreads();
+            if (!half && c0 + 32 * M::RB_MANY < end) ask(c0 + 32 * M::RB_MANY);
             if (half) T.template weigh16<M::RING_FEW>(frag, row_of, sums);
             else if (few) T.template weigh<M::RING_FEW>(frag, row_of, nb, sums);
             else T.template weigh<M::RING_MANY>(frag, row_of, nb, sums);
