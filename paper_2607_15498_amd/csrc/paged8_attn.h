@@ -126,36 +126,29 @@ struct Piece<Coded<Q>> : PieceOf<Coded<Q>> {
                 else low[k * 64 + lane] = f;
             });
     }
-    // scores of NC blocks of 32 rows with 32 keys of one scale
-    template <int NC>
-    __device__ __forceinline__ void scores(const uint8_t* kt, float scale, const u32x4 (&qf)[NC][HELD][F::NF], const u32x4* low,
-                                           f32x16 (&sc)[NC]) const {
+    // scores of 32 rows of fp32 with 32 keys of one scale
+    __device__ __forceinline__ void scores(const uint8_t* kt, float scale, const u32x4 (&qf)[HELD][F::NF], const u32x4* low, f32x16& sc) const {
 #pragma unroll
-        for (int c = 0; c < NC; ++c)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) sc[c][i] = 0.f;
+        for (int i = 0; i < 16; ++i) sc[i] = 0.f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const u32x4 w = *reinterpret_cast<const u32x4*>(kt + (kaddr ^ (32u * j)));
             const u32x4 kf[2] = {decode8(uint2{w[0], w[1]}, scale), decode8(uint2{w[2], w[3]}, scale)};
-            if constexpr (F::NP == 3)
 #pragma unroll
-                for (int k = 0; k < 2; ++k) sc[0] = mfma32(kf[k], low[(2 * j + k) * 64 + lane], sc[0]);
+            for (int k = 0; k < 2; ++k) sc = mfma32(kf[k], low[(2 * j + k) * 64 + lane], sc);
 #pragma unroll
             for (int p = HELD - 1; p >= 0; --p)
 #pragma unroll
-                for (int k = 0; k < 2; ++k)
-#pragma unroll
-                    for (int c = 0; c < NC; ++c) sc[c] = mfma32(kf[k], qf[c][p][2 * j + k], sc[c]);
+                for (int k = 0; k < 2; ++k) sc = mfma32(kf[k], qf[p][2 * j + k], sc);
         }
     }
-    // ... of one block of rows with NT blocks of keys, side by side
+    // ... of any 32 rows, their fragments in shared memory, with NT blocks of keys side by side
     template <int NT>
-    __device__ __forceinline__ void scores_of(const uint8_t* kt, const float (&scale)[NT], const u32x4* query, f32x16 (&sc)[NT][1]) const {
+    __device__ __forceinline__ void scores_of(const uint8_t* kt, const float (&scale)[NT], const u32x4* query, f32x16 (&sc)[NT]) const {
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sc[n][0][i] = 0.f;
+            for (int i = 0; i < 16; ++i) sc[n][i] = 0.f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             u32x4 kf[NT][2];
@@ -171,7 +164,7 @@ struct Piece<Coded<Q>> : PieceOf<Coded<Q>> {
                 for (int k = 0; k < 2; ++k) {
                     const u32x4 q = query[(p * F::NF + 2 * j + k) * 64 + lane];
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) sc[n][0] = mfma32(kf[n][k], q, sc[n][0]);
+                    for (int n = 0; n < NT; ++n) sc[n] = mfma32(kf[n][k], q, sc[n]);
                 }
         }
     }
@@ -181,21 +174,22 @@ struct Piece<Coded<Q>> : PieceOf<Coded<Q>> {
             (__attribute__((address_space(3))) pa_i32x2*)(vt + (vaddr ^ (32u * dt)) + r0 * F::ROWB)));
     }
     static __device__ __forceinline__ uint32_t finite(uint32_t x) { return Piece<uint16_t>::finite(x); }
-    // acc += V^T P^T of 32 keys of one scale; p: the weights' parts, packed in pairs.  FINITE: of the values that are numbers alone.
-    template <int NC, int WP, bool FINITE = false>
-    __device__ __forceinline__ void values(const uint8_t* vt, float scale, const u32x4 (&p)[NC][WP][2], f32x16 (&acc)[NC][4]) const {
+    // acc += V^T P^T of 32 keys of one scale; p: the weights' parts, packed in pairs.  Of the values that are numbers alone: never,
+    // always, or with `odd`.
+    enum Finite { NEVER, ALWAYS, ODD };
+    template <int WP, Finite FINITE>
+    __device__ __forceinline__ void values(const uint8_t* vt, float scale, const u32x4 (&p)[WP][2], f32x16 (&acc)[4], bool odd = false) const {
 #pragma unroll
         for (int mm = 0; mm < 2; ++mm)
 #pragma unroll
             for (int dt = 0; dt < 4; ++dt) {
                 u32x4 f = decode8(vcodes(vt, 16 * mm, dt), scale);
-                if constexpr (FINITE)
+                if constexpr (FINITE != NEVER)
+                    if (FINITE == ALWAYS || odd)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) f[k] = finite(f[k]);
+                        for (int k = 0; k < 4; ++k) f[k] = finite(f[k]);
 #pragma unroll
-                for (int n = WP - 1; n >= 0; --n)
-#pragma unroll
-                    for (int c = 0; c < NC; ++c) acc[c][dt] = mfma32(f, p[c][n][mm], acc[c][dt]);
+                for (int n = WP - 1; n >= 0; --n) acc[dt] = mfma32(f, p[n][mm], acc[dt]);
             }
     }
     // As the raw cache's: NaN (codes have no infinities) among values of keys that some row does not see.
@@ -244,11 +238,7 @@ __device__ __forceinline__ void parts_of(f32x16& sc, u32x4 (&p)[3][2]) {
             sc[2 * k + 1] = y;
         }
 }
-// bf16 rounded, or rounded and what that takes away, rounded: 2^-17 of a weight is missing.
-__device__ __forceinline__ void parts_of(f32x16& sc, u32x4 (&p)[1][2]) {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) p[0][k >> 2][k & 3] = cvt_bf16x2(sc[2 * k], sc[2 * k + 1]);
-}
+// bf16 rounded and what that takes away, rounded: 2^-17 of a weight is missing.
 __device__ __forceinline__ void parts_of(f32x16& sc, u32x4 (&p)[2][2]) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
@@ -287,11 +277,11 @@ __device__ __forceinline__ void few_rows8(const Piece<Coded<Q>>& P, uint8_t* sme
                    [&](int p, int k, const u32x4& f) { const_cast<u32x4*>(query)[(p * F::NF + k) * 64 + lane] = f; });
     Running run;
     const float slack = SLACK / a.c;
-    f32x16 acc[1][4];
+    f32x16 acc[4];
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) acc[0][dt][i] = 0.f;
+        for (int i = 0; i < 16; ++i) acc[dt][i] = 0.f;
 
     // pages and scales of the wave's next 32 tiles: lane 2 i has the page and the keys' scale of tile i, lane 2 i + 1 the values'
     constexpr int WINDOW = 32 / NT;                        // groups
@@ -348,25 +338,25 @@ __device__ __forceinline__ void few_rows8(const Piece<Coded<Q>>& P, uint8_t* sme
 #pragma unroll
         for (int n = 0; n < NT; ++n) masked = masked || pg[n] < 0;
         wait_loads<3 * L>();
-        f32x16 sc[NT][1];
+        f32x16 sc[NT];
         P.template scores_of<NT>(kt, ksc, query, sc);
         keep_out<Q>();
         __builtin_amdgcn_sched_barrier(0);                 // (what lies between two of these fits the registers)
         if (masked)
 #pragma unroll
-            for (int n = 0; n < NT; ++n) P.anew().mask(sc[n][0], t0 + 32 * n, seen, pg[n] >= 0 ? 3u : 0u);
-        float mt = P.most(sc[0][0]);
+            for (int n = 0; n < NT; ++n) P.anew().mask(sc[n], t0 + 32 * n, seen, pg[n] >= 0 ? 3u : 0u);
+        float mt = P.most(sc[0]);
 #pragma unroll
-        for (int n = 1; n < NT; ++n) mt = fmaxf(mt, P.most(sc[n][0]));
+        for (int n = 1; n < NT; ++n) mt = fmaxf(mt, P.most(sc[n]));
         if (__any(mt > run.m + slack)) {
             const float f = run.raise(mt, a.c);
 #pragma unroll
             for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) acc[0][dt][i] *= f;
+                for (int i = 0; i < 16; ++i) acc[dt][i] *= f;
         }
 #pragma unroll
-        for (int n = 0; n < NT; ++n) weights8<Q>(sc[n][0], run, a, run.l);
+        for (int n = 0; n < NT; ++n) weights8<Q>(sc[n], run, a, run.l);
         __builtin_amdgcn_sched_barrier(0);
         wait_loads<2 * L>();
         bool odd = false;
@@ -381,24 +371,26 @@ __device__ __forceinline__ void few_rows8(const Piece<Coded<Q>>& P, uint8_t* sme
             keep_out<Q>();
             __builtin_amdgcn_sched_barrier(0);
             if (halves) {                                  // lanes 16 .. 31 (and 48 ..) have what the rounding takes away
-                u32x4 p[1][1][2];
+                u32x4 p[1][2];
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
-                    const float e0 = sc[n][0][2 * k], e1 = sc[n][0][2 * k + 1];
+                    const float e0 = sc[n][2 * k], e1 = sc[n][2 * k + 1];
                     const uint32_t w = cvt_bf16x2(e0, e1);
-                    p[0][0][k >> 2][k & 3] = cvt_bf16x2(fmaf(rest, bf_lo(w), e0), fmaf(rest, bf_hi(w), e1));
+                    p[0][k >> 2][k & 3] = cvt_bf16x2(fmaf(rest, bf_lo(w), e0), fmaf(rest, bf_hi(w), e1));
                 }
-                if (odd) P.anew().template values<1, 1, true>(v, vsc[n], p, acc);
-                else P.template values<1, 1>(v, vsc[n], p, acc);
+                if (odd) P.anew().template values<1, Piece<Coded<Q>>::ALWAYS>(v, vsc[n], p, acc);
+                else P.template values<1, Piece<Coded<Q>>::NEVER>(v, vsc[n], p, acc);
             } else {
                 constexpr int WP = F::NP == 1 ? 2 : 3;
-                u32x4 p[1][WP][2];
-                parts_of(sc[n][0], p[0]);
-                if (odd) P.anew().template values<1, WP, true>(v, vsc[n], p, acc);
-                else P.template values<1, WP>(v, vsc[n], p, acc);
+                u32x4 p[WP][2];
+                parts_of(sc[n], p);
+                // fp32: one copy of the code, for whose two the registers do not do
+                if constexpr (F::NP == 3) P.template values<WP, Piece<Coded<Q>>::ODD>(v, vsc[n], p, acc, odd);
+                else if (odd) P.anew().template values<WP, Piece<Coded<Q>>::ALWAYS>(v, vsc[n], p, acc);
+                else P.template values<WP, Piece<Coded<Q>>::NEVER>(v, vsc[n], p, acc);
             }
             if (odd)
-                P.anew().add_odd(v, t0 + 32 * n, seen, pg[n] >= 0 ? 3u : 0u, [&](int dt, int i, float y) { acc[0][dt][i] += y; });
+                P.anew().add_odd(v, t0 + 32 * n, seen, pg[n] >= 0 ? 3u : 0u, [&](int dt, int i, float y) { acc[dt][i] += y; });
         }
     }
     wait_loads<0>();
@@ -411,7 +403,7 @@ __device__ __forceinline__ void few_rows8(const Piece<Coded<Q>>& P, uint8_t* sme
 #pragma unroll
         for (int i = 0; i < 16; i += 4)
             *reinterpret_cast<f32x4*>(js + (wave * 32 + l32) * 132 + 32 * dt + 2 * i + 4 * h) =
-                f32x4{acc[0][dt][i], acc[0][dt][i + 1], acc[0][dt][i + 2], acc[0][dt][i + 3]};
+                f32x4{acc[dt][i], acc[dt][i + 1], acc[dt][i + 2], acc[dt][i + 3]};
     if (h == 0) *reinterpret_cast<float2*>(jm + (wave * 32 + l32) * 2) = float2{run.m, run.l};
     __syncthreads();
     // A thread's PER dims: of one of 32 rows, or half as many of one of 16 and of its rests
@@ -463,75 +455,6 @@ __device__ __forceinline__ void few_rows8(const Piece<Coded<Q>>& P, uint8_t* sme
         }
     }
     __syncthreads();                                       // the rings are free again
-}
-
-// Many rows, one step after another.
-template <typename Q>
-__device__ __forceinline__ void many_rows8(const Piece<Coded<Q>>& P, uint8_t* smem, int32_t row0, int32_t rows, bool cut, int64_t rec_row) {
-    typedef Form<Coded<Q>> F;
-    constexpr int NC = F::NC;
-    const AttnArgs& a = P.a;
-    Many<Coded<Q>> M(P, smem, row0, rows);
-    if (M.stages) M.begin();
-    Running run[NC];
-    static_assert(F::NP == 1 || NC == 1, "one block's third parts");
-    u32x4 qf[NC][Piece<Coded<Q>>::HELD][F::NF];
-    u32x4* low = reinterpret_cast<u32x4*>(smem + F::STAGES * 2 * F::SB) + M.wave * F::NF * 64;
-    f32x16 acc[NC][4], sc[NC];
-    typename Piece<Coded<Q>>::Seen seen[NC];
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-        int32_t tok, head;
-        M.row_of(c, P.l32, tok, head);
-        P.query(qf[c], low, P.r.q0 + tok, head);
-        seen[c] = M.keys_seen(c);
-#pragma unroll
-        for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[c][dt][i] = 0.f;
-    }
-    const float slack = SLACK / a.c;
-    for (int j = 0; j < F::SPS * M.stages; ++j) {
-        if (j % F::SPS == 0) {
-            M.arrive(j / F::SPS);
-            M.issue(j / F::SPS + 2);
-        }
-        if (j < M.jf || j >= M.jl) continue;
-        const float ks = M.key_scale(j), vs = M.value_scale(j);
-        P.template scores<NC>(M.keys_of(j), ks, qf, low, sc);
-        const bool masked = M.masked(j);
-        const int32_t t0 = M.t_first + 32 * j;
-        u32x4 p[NC][F::NP][2];                             // (bf16: rounded, as a chunk's matrix products are what it costs)
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            if (masked) P.anew().mask(sc[c], t0, seen[c], M.gm_of(j));
-            const float mt = P.most(sc[c]);
-            if (__any(mt > run[c].m + slack)) {
-                const float f = run[c].raise(mt, a.c);
-#pragma unroll
-                for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[c][dt][i] *= f;
-            }
-            weights8<Q>(sc[c], run[c], a, run[c].l);
-            parts_of(sc[c], p[c]);
-        }
-        const uint8_t* vt = M.values_of(j);
-        const bool odd = masked && P.anew().odd_values(vt);
-        if (odd) {
-            P.anew().template values<NC, F::NP, true>(vt, vs, p, acc);
-#pragma unroll
-            for (int c = 0; c < NC; ++c)
-                P.anew().add_odd(vt, t0, seen[c], M.gm_of(j), [&](int dt, int i, float x) { acc[c][dt][i] += x; });
-        } else P.template values<NC, F::NP>(vt, vs, p, acc);
-    }
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-        const float l = xsum32(run[c].l);
-#pragma unroll
-        for (int dt = 0; dt < 4; ++dt) M.put(c, dt, acc[c][dt], run[c], l, cut, rec_row, dt == 3);
-    }
-    M.finish();
 }
 
 hipError_t launch_paged8_bf16(const AttnArgs& a, int groups, hipStream_t st);
