@@ -262,8 +262,8 @@ __device__ __forceinline__ uint32_t waves_before(const uint32_t* sums, int wave,
 // One workgroup a (sequence, head): the rank of the last of the m tokens that stay, by its digits from the top (of 10, 11 and 11
 // bits), then the tokens above it and the first of those equal to it, in order.  Ranks lie in shared memory, a part of 32768 at a
 // time (one alone is read once); a wave has 256 that follow each other, 4 a lane.  The instructions of its CU bound it: about 20 a
-// token and pass, 64 tokens a row and ranges compared, took 42 us for 32768 tokens (of one head or of 8, a CU each), these take 23: 4
-// to read them, 3 + 1 a pass and its digit, 2 to count and 6 to place.  Rows kept in registers, every pass's loop unrolled, took 58.
+// token and pass, 64 tokens a row and ranges compared, took 42 us for 32768 tokens (of one head or of 8, a CU each), these take 22: 6
+// to read them and count the first digit, 3 + 1 a pass and its digit, 2 to count and 6 to place.  Rows kept in registers, every pass's loop unrolled, took 58.
 __global__ __launch_bounds__(SEL) void evict8_select(Evict8 p) {
     extern __shared__ __align__(16) uint32_t ranks[];
     __shared__ __align__(16) uint32_t hist[4096];          // a digit's copies lie together: equal digits of one read fall into different ones
