@@ -261,9 +261,10 @@ __device__ __forceinline__ uint32_t waves_before(const uint32_t* sums, int wave,
 
 // One workgroup a (sequence, head): the rank of the last of the m tokens that stay, by its digits from the top (of 10, 11 and 11
 // bits), then the tokens above it and the first of those equal to it, in order.  Ranks lie in shared memory, a part of 32768 at a
-// time (one alone is read once); a wave has 256 that follow each other, 4 a lane.  The instructions of its CU bound it: about 20 a
-// token and pass, 64 tokens a row and ranges compared, took 42 us for 32768 tokens (of one head or of 8, a CU each), these take 22: 6
-// to read them and count the first digit, 3 + 1 a pass and its digit, 2 to count and 6 to place.  Rows kept in registers, every pass's loop unrolled, took 58.
+// time (one alone is read once; of several, a pass begins with the one that is held: 65536 tokens 78 -> 64 us, both launches); a wave has 256
+// that follow each other, 4 a lane.  The instructions of its CU bound it: about 20 a token and pass, 64 tokens a row and ranges
+// compared, took 42 us for 32768 tokens (of one head or of 8, a CU each), these take 22: 6 to read them and count the first digit, 3
+// + 1 a pass and its digit, 2 to count and 6 to place.  Rows kept in registers, every pass's loop unrolled, took 58.
 __global__ __launch_bounds__(SEL) void evict8_select(Evict8 p) {
     extern __shared__ __align__(16) uint32_t ranks[];
     __shared__ __align__(16) uint32_t hist[4096];          // a digit's copies lie together: equal digits of one read fall into different ones
@@ -283,13 +284,15 @@ __global__ __launch_bounds__(SEL) void evict8_select(Evict8 p) {
     if (m == 0) return;
     const int32_t lo = p.first, hi = n - p.recent;         // tokens before and from there on stay (first + recent <= m unless all do)
     const int parts = (n + SEL_PART - 1) / SEL_PART;
-    int turns = 0, at = 0;                                 // of a part: reads a lane; the lane's first
+    int turns = 0, at = 0, held = -1;                      // of a part: reads a lane; the lane's first; the part that is held
     // (the first pass's counts are taken on the way)
     auto load = [&](int part, bool first) {
         const int32_t t0 = part * SEL_PART, len = n - t0 < SEL_PART ? n - t0 : SEL_PART;
         turns = (len + 4 * SEL - 1) / (4 * SEL);
         at = wave * turns * 64 + lane;
-        if (part || parts > 1) __syncthreads();            // the part before has been read
+        if (part == held) return;
+        if (held >= 0) __syncthreads();                    // the part before has been read
+        held = part;
         for (int i0 = tid; i0 < turns * 4 * SEL; i0 += 8 * SEL) {      // 8 reads at a time (tokens that there are)
             float x[8];
 #pragma unroll
@@ -314,8 +317,8 @@ __global__ __launch_bounds__(SEL) void evict8_select(Evict8 p) {
         reinterpret_cast<uint4*>(hist)[tid] = uint4{0, 0, 0, 0};
         __syncthreads();
 #pragma unroll 1
-        for (int part = 0; part < parts; ++part) {
-            if (pass == 0 || parts > 1) load(part, pass == 0);
+        for (int j = 0; j < parts; ++j) {                  // up and down in turn: a pass begins with the part that is held
+            load(pass & 1 ? parts - 1 - j : j, pass == 0);
             if (pass) {
                 for (int i = 0; i < turns; ++i) {          // few begin as those before
                     const u32x4 r = quads[at + 64 * i];
@@ -369,11 +372,12 @@ __global__ __launch_bounds__(SEL) void evict8_select(Evict8 p) {
             break;
         }
     }
-    // ranks above `prefix`, and the first `need` equal to it: counted per wave (above and equal, 16 bits each), then placed
-    uint32_t place = 0, equal = 0;                         // in the parts before
+    // ranks above `prefix`, and the first `need` equal to it: counted per wave (above and equal, 16 bits each), then placed, the
+    // last part first
+    uint32_t place = (uint32_t)m - need, equal = found[2]; // in this part and those before (`equal` counts only if need does)
 #pragma unroll 1
-    for (int part = 0; part < parts; ++part) {
-        if (parts > 1) load(part, false);
+    for (int part = parts - 1; part >= 0; --part) {
+        load(part, false);
         uint32_t mine = 0;
         for (int i = 0; i < turns; ++i) {
             const u32x4 r = quads[at + 64 * i];
@@ -388,6 +392,8 @@ __global__ __launch_bounds__(SEL) void evict8_select(Evict8 p) {
         // a part has up to 2^15 of either: 16 waves' sums do not carry
         uint32_t total;
         const uint32_t before = waves_before(sums, wave, total);
+        place -= total >> 16;
+        equal -= total & 0xFFFFu;
         uint32_t to0 = place + (before >> 16), eq0 = equal + (before & 0xFFFFu);
         for (int i = 0; i < turns; ++i) {
             const u32x4 r = quads[at + 64 * i];
@@ -433,8 +439,6 @@ __global__ __launch_bounds__(SEL) void evict8_select(Evict8 p) {
                 }
             }
         }
-        place += total >> 16;
-        equal += total & 0xFFFFu;
     }
 }
 

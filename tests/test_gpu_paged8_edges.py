@@ -308,6 +308,42 @@ def test_evict_longer_than_one_part(vr, R):
             assert torch.equal(y[:, g], src)               # all blocks had one scale, and none gets a larger one
 
 
+@pytest.mark.parametrize("n,keep,first,recent", [(32769, 32768, 0, 1), (65536, 1, 0, 0), (65536, 40000, 3, 33000), (98305, 65537, 0, 7), (98305, 5000, 4, 0)])
+def test_evict_parts_and_masses(vr, n, keep, first, recent):
+    """Long sequences whose masses are equal, all but equal, NaN beyond some, and decided by a leading digit, beside a short one."""
+    import torch
+    G = 4
+    gen = torch.Generator().manual_seed(n + keep)
+    mass = torch.zeros((2, G, n))
+    mass[0, 0] = 0.25                                          # one value
+    mass[0, 1] = 1.0 + torch.randint(0, 3, (n,), generator=gen) * 2.0 ** -23   # apart in the last digit only
+    mass[0, 2] = float("nan")
+    mass[0, 2, torch.randperm(n, generator=gen)[: n // 5]] = 2.0
+    mass[0, 3, torch.randperm(n, generator=gen)[:keep]] = 3.0  # exactly `keep` of them, but for the first and recent ones
+    mass[1] = torch.rand((G, n), generator=gen)
+    kv = [n, 3000]
+    pages = vr.new_pages8((n + 3000 + 2 * keep) // 256 + 8, G, 256)
+    need, into_w = (n + 255) // 256, (keep + 255) // 256
+    table = torch.full((2, need), -1, dtype=torch.int32)
+    table[0] = torch.arange(need)
+    table[1, :12] = need + torch.arange(12)
+    into = need + 12 + torch.arange(into_w, dtype=torch.int32)
+    into = torch.stack([into, into + into_w])
+    index, kept, m = vr.paged8_evict(pages, table.cuda(), torch.tensor(kv, dtype=torch.int32).cuda(), mass.cuda(), keep, into.cuda(),
+                                     first=first, recent=recent)
+    assert m.tolist() == [min(k, keep) for k in kv]
+    for s, k in enumerate(kv):
+        left = min(k, keep)
+        for g in range(G):
+            w = mass[s, g, :k].double()
+            w = torch.where(torch.isnan(w), -math.inf, w)
+            w[:first] = w[max(0, k - recent):] = math.inf
+            want = torch.sort(torch.sort(w, descending=True, stable=True).indices[:left]).values
+            assert torch.equal(index[s, g, :left].cpu().long(), want), (s, g)
+            assert torch.equal(kept[s, g, :left].cpu().nan_to_num(-1.0), mass[s, g, want].nan_to_num(-1.0)), (s, g)
+            assert bool((index[s, g, left:] == -1).all()) and bool((kept[s, g, left:] == 0).all())
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_serving_run(vr, R, dtype):
     """A prompt in chunks, single tokens, an eviction, more tokens on the evicted cache, and the hand-over to the codec."""
