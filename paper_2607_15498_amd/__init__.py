@@ -824,6 +824,8 @@ def paged8_append(pages: PagedCache8, batch: PagedBatch, k: torch.Tensor, v: tor
 
 def paged8_attn_workspace(pages: PagedCache8, batch: PagedBatch, T: int, H: int, dtype=torch.bfloat16) -> torch.Tensor:
     """paged_attn_workspace of paged8_attn with queries of `dtype`."""
+    if dtype not in _DTYPES:
+        _einval(f"dtype {dtype} is neither torch.bfloat16 nor torch.float32")
     need = int(library().varrate_paged8_attn_workspace_bytes(pages.c(), batch.c(T), _DTYPES[dtype], H))
     return torch.empty(max(need, 16), dtype=torch.uint8, device=pages.k.device)
 

@@ -440,6 +440,7 @@ def test_binding_refuses(vr, R):
         lambda: vr.paged8_attn(pages, batch, q, scale=0.0),
         lambda: vr.paged8_attn(pages, batch, q.half()),
         lambda: vr.paged8_attn(pages, batch, q, workspace=torch.empty(8)),
+        lambda: vr.paged8_attn_workspace(pages, batch, 3, 8, dtype=torch.float16),
         lambda: vr.paged8_mass(pages, batch, q, None, mass),
         lambda: vr.paged8_mass(pages, batch, q, lse[:, :4], mass),
         lambda: vr.paged8_mass(pages, batch, q, lse, mass[:, :1]),
