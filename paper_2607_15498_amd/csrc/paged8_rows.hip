@@ -502,7 +502,6 @@ __global__ __launch_bounds__(256) void evict8_move(Evict8 p) {
             }
         }
         const int now = exponent_for(wave_most(most));
-        const float to_now = power(-now);
         const int32_t slot = p.pool.slot(i0);
         uint8_t* dst = p.pool.code[which] + p.pool.row(to, g, slot) + c;
 #pragma unroll
@@ -510,7 +509,10 @@ __global__ __launch_bounds__(256) void evict8_move(Evict8 p) {
             if (4 * k + rr < rows) {
                 float x[8];
                 values8(w[k], 1.f, x);
-                *reinterpret_cast<uint2*>(dst + (int64_t)(4 * k + rr) * D) = encode8<false>(x, sc[k] * to_now);
+                // from the row's scale to the new one: a finite power, as 0 times infinity would be NaN.  More than 2^127 only rows of zeros
+                // (and NaN) can be above their new block, and 2^-126 takes every code to 0.
+                const int up = (int)(__float_as_uint(sc[k]) >> 23) - 127 - now;
+                *reinterpret_cast<uint2*>(dst + (int64_t)(4 * k + rr) * D) = encode8<false>(x, power(up < -126 ? -126 : up > 127 ? 127 : up));
             }
         if (lane == 0) p.pool.scale[which][p.pool.block(to, g, slot)] = (uint8_t)(now + 127);
     }
