@@ -221,6 +221,7 @@ struct Evict8 {
     int32_t* len_out;
     int64_t L;
     int32_t S, cap, keep, first, recent;
+    uint32_t from;                   // the selection's first (sequence, head) of this launch
 };
 // tokens of sequence s, those of them that have a mass
 __device__ __forceinline__ int32_t tokens_of(const Evict8& p, int s) { return clamp_i32(p.kv_len[s], 0, p.cap); }
@@ -270,7 +271,8 @@ __global__ __launch_bounds__(SEL) void evict8_select(Evict8 p) {
     __shared__ __align__(16) uint32_t hist[4096];          // a digit's copies lie together: equal digits of one read fall into different ones
     __shared__ __align__(16) uint32_t sums[SEL_WAVES];
     __shared__ uint32_t found[3];                          // the digit, how many of its ranks stay, and of how many
-    const int s = (int)(blockIdx.x / (uint32_t)p.pool.G), g = (int)(blockIdx.x % (uint32_t)p.pool.G), tid = threadIdx.x;
+    const uint32_t u = p.from + blockIdx.x;
+    const int s = (int)(u / (uint32_t)p.pool.G), g = (int)(u % (uint32_t)p.pool.G), tid = threadIdx.x;
     const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int32_t n = tokens_of(p, s), m = n < p.keep ? n : p.keep;
     const float* mass = p.mass + ((int64_t)s * p.pool.G + g) * p.L;
@@ -548,14 +550,19 @@ hipError_t launch_paged8_gather(const varrate_pages8& pg, const int32_t* table, 
 
 hipError_t launch_paged8_evict(const varrate_pages8& pg, const Evict8Args& e, hipStream_t st) {
     const int64_t cap = (int64_t)e.width * pg.page;
-    const Evict8 p = {pool_of(pg), e.table, e.into, e.kv_len, e.table_stride, e.into_stride, e.mass, e.index, e.mass_out, e.len_out,
-                      e.L, e.S, (int32_t)(cap < e.L ? cap : e.L), (int32_t)e.keep, (int32_t)e.first, (int32_t)e.recent};
+    Evict8 p = {pool_of(pg), e.table, e.into, e.kv_len, e.table_stride, e.into_stride, e.mass, e.index, e.mass_out, e.len_out,
+                e.L, e.S, (int32_t)(cap < e.L ? cap : e.L), (int32_t)e.keep, (int32_t)e.first, (int32_t)e.recent, 0};
     const size_t lds = 4 * (size_t)(p.cap < SEL_PART ? (p.cap + 4 * SEL - 1) / (4 * SEL) * (4 * SEL) : SEL_PART);
     hipError_t err = ensure_lds_limit((const void*)evict8_select, 4 * SEL_PART);
     if (err != hipSuccess) return err;
-    evict8_select<<<(unsigned)e.S * (unsigned)pg.G, SEL, lds, st>>>(p);
-    err = hipGetLastError();
-    if (err != hipSuccess) return err;
+    // a launch has fewer than 2^32 threads: 2^21 selections (a loop in the kernel instead: 32.3 -> 32.8 us for 32768 tokens of 8 heads)
+    constexpr uint32_t MOST = 1u << 21;
+    const uint32_t all = (uint32_t)e.S * (uint32_t)pg.G;
+    for (; p.from < all; p.from += MOST) {
+        evict8_select<<<all - p.from < MOST ? all - p.from : MOST, SEL, lds, st>>>(p);
+        err = hipGetLastError();
+        if (err != hipSuccess) return err;
+    }
     const int64_t waves = (int64_t)e.S * pg.G * 2 * ((e.keep + BLOCK - 1) / BLOCK);
     evict8_move<<<grid_of((waves + 3) / 4, 1 << 20), 256, 0, st>>>(p);
     return hipGetLastError();

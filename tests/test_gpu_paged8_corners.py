@@ -54,3 +54,40 @@ def test_evict_zero_rows_of_large_blocks(vr, R, big, small):
         mass = torch.zeros((1, 2, n))
         mass[0, :, stay] = 1.0
         check_evict(vr, R, [n], len(stay) if len(stay) < keep else keep, 2, 32, pool=pool, mass=mass)
+
+
+# ---- eviction: as many sequences and heads as there may be -----------------------------------------
+
+@pytest.mark.parametrize("S,G", [(65536, 64), (4100, 1024)])
+def test_evict_many_heads_and_sequences(vr, S, G):
+    """More (sequence, head) pairs than one launch has workgroups of this size."""
+    import torch
+    n, keep = 3, 2
+    say(f"[evict8] S={S} G={G}")
+    pages = vr.new_pages8(2, G, 32)
+    for t in (pages.k, pages.v):
+        t.view(torch.uint8).copy_(torch.randint(1, 120, t.shape, dtype=torch.uint8))
+    before = [t.view(torch.uint8).clone() for t in (pages.k, pages.v, pages.k_scale, pages.v_scale)]
+    table = torch.zeros((S, 1), dtype=torch.int32, device="cuda")
+    into = torch.full((S, 1), -1, dtype=torch.int32, device="cuda")
+    into[S - 1] = 1                                        # the others' rows are dropped
+    mass = torch.rand((S, G, n), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
+    kv = (torch.arange(S, device="cuda") % (n + 1)).to(torch.int32)
+    kv[S - 1] = n
+    index, kept, m = vr.paged8_evict(pages, table, kv, mass, keep, into)
+    k = kv.view(S, 1, 1)
+    assert torch.equal(m, kv.clamp(max=keep))
+    there = torch.arange(n, device="cuda") < k
+    order = torch.sort(torch.where(there, mass, -1.0), dim=-1, descending=True, stable=True).indices[..., :keep]
+    want = torch.sort(torch.where(torch.arange(keep, device="cuda") < k, order, n), dim=-1).values
+    stay = want < n
+    assert torch.equal(index, torch.where(stay, want, -1).int())
+    assert torch.equal(kept, torch.where(stay, mass.gather(2, want.clamp(max=n - 1)), 0.0))
+    # the last sequence's rows arrived, and their page is as it was
+    for t, b in zip((pages.k, pages.v, pages.k_scale, pages.v_scale), before):
+        assert torch.equal(t.view(torch.uint8)[0], b[0])
+    K, V = vr.paged8_gather(pages, table[0], 32, dtype=torch.float32)
+    k2, v2 = vr.paged8_gather(pages, into[S - 1], keep, dtype=torch.float32)
+    for x, y in ((K, k2), (V, v2)):
+        src = x.transpose(0, 1).gather(1, want[S - 1].unsqueeze(-1).expand(G, keep, D))
+        assert torch.equal(y.transpose(0, 1), src)         # a smaller power holds a block's codes as they are
