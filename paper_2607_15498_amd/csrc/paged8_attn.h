@@ -451,7 +451,7 @@ __device__ __forceinline__ void few_rows8(const Piece<Coded<Q>>& P, uint8_t* sme
 #pragma unroll
             for (int i = 0; i < PER; i += 4)
                 if (i < own) store4<Q>(dst + i, o[i] * inv, o[i + 1] * inv, o[i + 2] * inv, o[i + 3] * inv);
-            if (a.lse && d0 == 0) a.lse[token * (a.G * Hg) + head] = lse_of(M, Ls, a.c);
+            if (a.lse && d0 == 0) a.lse[token * (a.G * Hg) + head] = lse_of<F::NP == 1>(M, Ls, a);
         }
     }
     __syncthreads();                                       // the rings are free again

@@ -561,11 +561,19 @@ struct Running {
     }
 };
 
-// ln of the sum of exponentials of a row whose weights, of sum l, were taken against m
-__device__ __forceinline__ float lse_of(float m, float l, float c) {
-    constexpr float LN2 = 0.693147180559945309f;
-    const float off = off_of(m, c), log_l = __builtin_amdgcn_logf(l);
-    return beyond(off) ? m * (c * LN2) + log_l * LN2 : (log_l - off) * LN2;
+// ln of the sum of exponentials of a row whose weights, of sum l, were taken against m.  What its products and sums round away is added
+// at the end, so that it is rounded about once: its error is one of the exponents of whoever takes weights from it.  CUT: the weights
+// were taken with c alone (bf16 queries); what their exponents lack, c_lo x, is m's (others' differ by 2^-23 of what they are away
+// from it).
+template <bool CUT> __device__ __forceinline__ float lse_of(float m, float l, const AttnArgs& a) {
+    constexpr float LN2 = 0.693147180559945309f, LN2_LO = (float)(0.69314718055994530942 - (double)LN2);
+    const float off = off_of(m, a.c), log_l = __builtin_amdgcn_logf(l);
+    const bool far = beyond(off);
+    const float top = far ? m * a.c : -off, z = top + log_l;
+    if (!(fabsf(z) < INFINITY)) return z;
+    const float part = z - top;
+    const float rest = (top - (z - part)) + (log_l - part) + (far ? fmaf(m, a.c, -top) : 0.f) + (far || CUT ? m * a.c_lo : 0.f);
+    return fmaf(z, LN2, fmaf(z, LN2_LO, rest * LN2));
 }
 
 template <typename ET>
@@ -742,7 +750,7 @@ struct Many {
             typedef typename F::Row Row;
             Row* dst = (Row*)a.out + (int64_t)(P.r.q0 + tok) * a.out_stride + (int64_t)head * D + first;
             if constexpr (F::CODED)
-                if (a.lse && last && P.h == 0) a.lse[(int64_t)(P.r.q0 + tok) * (a.G * a.Hg) + head] = lse_of(run.m, l, a.c);
+                if (a.lse && last && P.h == 0) a.lse[(int64_t)(P.r.q0 + tok) * (a.G * a.Hg) + head] = lse_of<F::NP == 1>(run.m, l, a);
 #pragma unroll
             for (int i = 0; i < 16; i += 4) store4<Row>(dst + next * i, o[i] * inv, o[i + 1] * inv, o[i + 2] * inv, o[i + 3] * inv);
         }
@@ -978,7 +986,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(AttnArgs a) {
         const float inv = l == 0.f ? 0.f : 1.f / l;
         Row* dst = (Row*)a.out + (int64_t)(r.q0 + row / a.Hg) * a.out_stride + (int64_t)(g * a.Hg + row % a.Hg) * D + 4 * l32;
         if constexpr (Form<ET>::CODED)
-            if (a.lse && l32 == 0) a.lse[(int64_t)(r.q0 + row / a.Hg) * (a.G * a.Hg) + g * a.Hg + row % a.Hg] = lse_of(m, l, a.c);
+            if (a.lse && l32 == 0) a.lse[(int64_t)(r.q0 + row / a.Hg) * (a.G * a.Hg) + g * a.Hg + row % a.Hg] = lse_of<Form<ET>::NP == 1>(m, l, a);
         store4<Row>(dst, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
     };
     // (rows behind the tile's last are read as they are and dropped)

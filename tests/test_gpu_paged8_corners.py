@@ -91,3 +91,39 @@ def test_evict_many_heads_and_sequences(vr, S, G):
     for x, y in ((K, k2), (V, v2)):
         src = x.transpose(0, 1).gather(1, want[S - 1].unsqueeze(-1).expand(G, keep, D))
         assert torch.equal(y.transpose(0, 1), src)         # a smaller power holds a block's codes as they are
+
+
+# ---- the logarithms of the rows' sums --------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m,n", [(1, 1), (1, 33), (1, 700), (7, 40), (70, 300), (1, 40000), (3, 9000), (90, 5000)])
+def test_ln_sums_are_rounded_once(vr, R, dtype, m, n):
+    """One key's score is far above all others' and exact in fp32, so that the logarithm is scale x score: off by its own rounding
+    (half a step, 2^-24 of it), and by the exponential's and the logarithm's 2^-21.  The mass of that key is 1, off by as much."""
+    import numpy as np
+    import torch
+    from test_gpu_paged8 import within
+    G, H = 1, 4
+    pool = R.Pool8([n], G, 64, seed=3, fill=False, junk=0.0)
+    at = (n - m) // 2
+    pool.code["v"][:] = 1.0
+    pool.code["k"][int(pool.table[0, at // 64]), 0, at % 64, 9] = 320.0
+    pool.exp["k"][:] = -6                                  # the key's value is 5
+    gen = torch.Generator().manual_seed(n)
+    q = torch.zeros((m, H, D))
+    q[..., 9] = torch.exp2(4 + 6 * torch.rand((m, H), generator=gen)) + 16 * math.log(n) * 2
+    q = q.to(R.tdt(dtype))
+    if dtype == "f32":
+        q = (q.view(torch.int32) & -4096).view(torch.float32)      # products with 5 are exact
+    scale = float(np.float32(D ** -0.5))
+    pages, batch = pool.device(vr), pool.batch(vr, [m])
+    lse = torch.empty((m, H), device="cuda")
+    vr.paged8_attn(pages, batch, q.cuda(), lse=lse)
+    s = 5.0 * q[..., 9].double() * scale
+    exact = s + torch.log1p((n - 1) * torch.exp(-s))
+    say(f"[lse8] m={m} n={n} {dtype}: {float(s.min()):.1f} .. {float(s.max()):.1f}")
+    within(lse, exact, U32 * exact * (1 + 2.0 ** -20) + 2.0 ** -21, "lse")
+    got = vr.paged8_mass(pages, batch, q.cuda(), lse, torch.zeros((1, G, n), device="cuda"))[0, 0].cpu().double()
+    w = torch.exp(s - exact)
+    tol = float((w * (U32 * exact * (1 + 2.0 ** -20) + 2.0 ** -20)).sum())
+    assert abs(float(got[at]) - float(w.sum())) <= tol + m * H * U32 * m * H, (float(got[at]) - float(w.sum()), tol)
