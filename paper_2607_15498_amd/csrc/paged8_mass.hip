@@ -17,6 +17,22 @@
 namespace vr {
 namespace {
 
+// exp(scale x - lse) = exp2(c x - z) 2^-(what z, lse log2 e, lacks of it): z and that factor.  lse's rounding, 2^-24 of it, is an exponent's
+// error, so that a weight could be anything between nothing and infinity.  Rows whose |z| is 2^8 and more pay a key 1 at most: LARGE in
+// the number of their first key takes them where masks are looked at, which costs the others next to nothing (1024 tokens over 17408:
+// 343 -> 345 us; a bound for every score 360).  From |z| = FAR on fp32's steps are 1 and more, and z is taken 2^-22 of it lower, so that the
+// key whose score is the row's largest (and those that rounding cannot tell from it) is paid 1.
+constexpr int32_t LARGE = 1 << 30;                         // (no key's number)
+constexpr float FAR = 0x1p24f;
+__device__ __forceinline__ float2 subtracted(float lse) {
+    const float z = lse * LOG2E, lack = fmaf(lse, LOG2E, -z) + lse * LOG2E_LO, most = __builtin_elementwise_minimum(z, 0x1.fffffep127f);
+    const bool far = fabsf(z) >= FAR;
+    const float low = far ? fmaf(fabsf(most), -0x1p-22f, most) : z;
+    return float2{z == -INFINITY ? INFINITY : low, __builtin_amdgcn_exp2f(far ? 0.f : -lack)};      // (no sum: nothing is paid)
+}
+// (NaN stays NaN)
+__device__ __forceinline__ float paid_most(float x, float most) { return __builtin_elementwise_minimum(x, most); }
+
 struct MassArgs {
     AttnArgs a;
     const float *lse, *mass;
@@ -142,11 +158,17 @@ struct Tiles {
                 const int32_t lo = __float_as_int(w.z), hi = __float_as_int(w.w);
 #pragma unroll
                 for (int k = 0; k < 16; ++k) x[k] = __builtin_amdgcn_exp2f(fmaf(x[k], a.c_lo, fmaf(x[k], a.c, -w.x)));
-                if (__any(lo > t0 || hi < t0 + 32)) {
-                    const uint32_t at = (uint32_t)(t0 + 4 * P.h - lo), n = (uint32_t)(hi - lo);
+                if (__builtin_expect(__any(lo > t0 || hi < t0 + 32), 0)) {
+                    const int32_t from = lo & ~LARGE;
+                    const uint32_t at = (uint32_t)(t0 + 4 * P.h - from), n = (uint32_t)(hi - from);
 #pragma unroll
                     for (int k = 0; k < 16; ++k)
                         if (at + 8 * (k >> 2) + (k & 3) >= n) x[k] = 0.f;
+                    if (__builtin_expect(__any(lo & LARGE), 0)) {
+                        const float most = 1.f / w.y;
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) x[k] = paid_most(x[k], most);
+                    }
                 }
 #pragma unroll
                 for (int k = 0; k < 16; ++k) sum[k] = fmaf(x[k], w.y, sum[k]);
@@ -203,11 +225,12 @@ struct Tiles {
                 const float y = s[k >> 2][k & 3];
                 x[k] = __builtin_amdgcn_exp2f(fmaf(y, a.c_lo, fmaf(y, a.c, -w.x)));
             }
-            if (__any(lo > t0 || hi < t0 + 32)) {
-                const uint32_t at = (uint32_t)(t0 + 4 * q4 - lo), n = (uint32_t)(hi - lo);
+            if (__builtin_expect(__any(lo > t0 || hi < t0 + 32), 0)) {
+                const int32_t from = lo & ~LARGE;
+                const uint32_t at = (uint32_t)(t0 + 4 * q4 - from), n = (uint32_t)(hi - from);
+                const float most = 1.f / w.y;
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (at + 16 * (k >> 2) + (k & 3) >= n) x[k] = 0.f;
+                for (int k = 0; k < 8; ++k) x[k] = at + 16 * (k >> 2) + (k & 3) >= n ? 0.f : paid_most(x[k], most);
             }
 #pragma unroll
             for (int k = 0; k < 8; ++k) x[k] *= w.y;
@@ -323,13 +346,12 @@ __global__ __launch_bounds__(256, 2) void paged8_mass_kernel(MassArgs m) {
             if (few) T.template begin<M::RING_FEW>();
             else T.template begin<M::RING_MANY>();
             auto put_row = [&](int rb, int l, bool real, int32_t tok, float z0) {
-                // exp(scale x - lse) = exp2(c x - z) 2^-(what z lacks)
-                const float z = z0 == -INFINITY ? INFINITY : z0 * LOG2E;
-                const float rest = fabsf(z) < INFINITY ? __builtin_amdgcn_exp2f(-(fmaf(z0, LOG2E, -z) + z0 * LOG2E_LO)) : 1.f;
+                const float2 z = subtracted(z0);
                 int32_t lo, hi;
                 row_keys(r, tok, a.causal, a.window, lo, hi);
                 if (!real || hi < lo) lo = hi = 0;
-                row_of[rb * 32 + l] = float4{z, rest, __int_as_float(lo), __int_as_float(hi)};
+                if (fabsf(z.x) >= 0x1p8f && z.x < INFINITY) lo |= LARGE;
+                row_of[rb * 32 + l] = float4{z.x, z.y, __int_as_float(lo), __int_as_float(hi)};
             };
             if (half) {
                 const int32_t mine = (lane & 15) < rows ? lane & 15 : 0, tok = mine / a.Hg, hd = g * a.Hg + mine % a.Hg;

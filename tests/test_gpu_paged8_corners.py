@@ -127,3 +127,62 @@ def test_ln_sums_are_rounded_once(vr, R, dtype, m, n):
     w = torch.exp(s - exact)
     tol = float((w * (U32 * exact * (1 + 2.0 ** -20) + 2.0 ** -20)).sum())
     assert abs(float(got[at]) - float(w.sum())) <= tol + m * H * U32 * m * H, (float(got[at]) - float(w.sum()), tol)
+
+
+# ---- attention mass: scores of any size ------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m", [1, 5, 12, 70])
+@pytest.mark.parametrize("power", [4, 10, 16, 20, 24, 28, 33, 60, 110])
+def test_mass_of_large_scores(vr, R, dtype, m, power):
+    """A key whose score is far above the others', up to beyond what exponents hold, is paid 1 by its row, as nearly as the logarithm
+    of the row's sum says (wholly from where fp32's steps are 1 and more), and no more; the other heads' weights are what they were."""
+    import torch
+    n, G, H = 200, 1, 4
+    pool = R.Pool8([n], G, 32, seed=m)
+    for t in range(n):                                     # dim 100: one key alone
+        p = int(pool.table[0, t // 32])
+        pool.code["k"][p, 0, t % 32, 100] = 32.0 if t == 40 else 0.0
+    q = (2.0 * torch.randn((m, H, D), generator=torch.Generator().manual_seed(1))).to(R.tdt(dtype))
+    q[..., 100] = 0
+    q[:, 0] = 0
+    q[:, 0, 100] = 2.0 ** power
+    pages, batch = pool.device(vr), pool.batch(vr, [m])
+    lse = torch.empty((m, H), device="cuda")
+    vr.paged8_attn(pages, batch, q.cuda(), lse=lse)
+    K, _, _ = pool.rows(0)
+    top = float(K[40, 0, 100]) * 2.0 ** power / math.sqrt(D)
+    say(f"[mass8] m={m} {dtype} top score {top:.3g}")
+    # the large row alone
+    only = lse.clone()
+    only[:, 1:] = -math.inf
+    got = vr.paged8_mass(pages, batch, q.cuda(), only, torch.zeros((1, G, n), device="cuda"))[0, 0].cpu().double()
+    assert (got >= 0).all() and (got <= (m if top >= 256 else m * (1 + 3 * U32 * top + 2.0 ** -20))).all()
+    # of a row: the other keys' scores are 0.  lse is rounded once (2^-24) and so are the score's parts (2 u32), as exponents
+    w = 1 / (1 + (n - 1) * math.exp(-top))
+    least = 1.0 if top >= 2.0 ** 24 else w * math.exp(-3 * U32 * top) * (1 - 2.0 ** -20)
+    assert got[40] >= m * least, (float(got[40]) / m, least)
+    if top > 120:                                          # exp(-120) is nothing beside fp32's rounding of 1
+        assert float(got.sum() - got[40]) < 1e-30
+    # beside the others, which are as the reference has them
+    mass = torch.rand((1, G, n), generator=torch.Generator().manual_seed(2))
+    both = vr.paged8_mass(pages, batch, q.cuda(), lse, mass.cuda())[0, 0].cpu().double()
+    rest = lse.cpu().clone()
+    rest[:, 0] = -math.inf
+    ref, tol = R.mass_ref(pool, q, [m], H, rest, mass, dtype)
+    assert ((both - ref[0, 0] - got).abs() <= tol[0, 0] + 4 * (m + 2) * U32 * (ref[0, 0] + got)).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m", [1, 6, 70])
+def test_mass_of_nan_keys(vr, R, dtype, m):
+    """A NaN key that a row sees is paid NaN, which eviction puts last."""
+    import torch
+    n, G, H = 150, 1, 4
+    pool = R.Pool8([n], G, 32, seed=m)
+    for t in (17, n - 1):
+        pool.code["k"][int(pool.table[0, t // 32]), 0, t % 32, 5] = math.nan
+    q = torch.randn((m, H, D), generator=torch.Generator().manual_seed(1)).to(R.tdt(dtype))
+    lse = torch.full((m, H), 3.0)
+    got = vr.paged8_mass(pool.device(vr), pool.batch(vr, [m]), q.cuda(), lse.cuda(), torch.zeros((1, G, n), device="cuda"))[0, 0].cpu()
+    assert got.isnan().nonzero()[:, 0].tolist() == [17, n - 1]
