@@ -269,14 +269,8 @@ __device__ __forceinline__ void many_rows<Coded<uint16_t>>(const Piece<Coded<uin
 hipError_t launch_paged8_bf16(const AttnArgs& a, int groups, hipStream_t st) { return launch_paged<Coded<uint16_t>>(a, groups, st); }
 
 // ---- host ------------------------------------------------------------------------------------
-// Partial rows.  None, and no second launch, for single tokens over tables of up to 1024 tokens (one token over 512, fp32: 17.2 ->
-// 15.6 us; over 700, bf16: 20 -> 17; with tables of 2048 they lose, over 1500: 20 -> 25).
-static int64_t records8(int64_t T, int S, int G, int Hg, int64_t cap, int lmin) {
-    return cap <= 1024 && T * Hg <= (int64_t)ROWS_FEW * S ? 0 : max_records(T, S, G, Hg, cap, lmin);
-}
-
 size_t paged8_attn_ws_bytes(int64_t T, int S, int G, int H, int dtype, int64_t cap) {
-    const int64_t rows = records8(T, S, G, H / G, cap, costs8_of(dtype == VARRATE_BF16).lmin);
+    const int64_t rows = max_records8(T, S, G, H / G, cap, costs8_of(dtype == VARRATE_BF16).lmin);
     return rows ? (size_t)rows * (D + 2) * 4 + SHARES_BYTES : 0;
 }
 
@@ -309,7 +303,7 @@ hipError_t launch_paged8_attn(const varrate_pages8& pg, const varrate_batch& b, 
     a.costs = costs8_of(dtype == VARRATE_BF16);
     split_scale(scale, a.c, a.c_lo);
     a.most_units = max_units(b.T, b.S, pg.G, a.Hg);
-    a.rec_rows = records8(b.T, b.S, pg.G, a.Hg, a.cap, a.costs.lmin);
+    a.rec_rows = max_records8(b.T, b.S, pg.G, a.Hg, a.cap, a.costs.lmin);
     const int groups = max_groups(b.T, b.S, pg.G, a.Hg, a.cap, a.costs.lmin);
     return dtype == VARRATE_BF16 ? launch_paged8_bf16(a, groups, st) : launch_paged8_f32(a, groups, st);
 }

@@ -227,6 +227,14 @@ VR_HD int64_t max_records(int64_t T, int S, int G, int Hg, int64_t cap, int lmin
     return cap <= 2 * lmin ? 0 : (int64_t)2 * max_groups(T, S, G, Hg, cap, lmin) * place_rows(T, Hg);
 }
 
+// Over pages of codes: none, and no second launch, for single tokens (no more than there are sequences, or one tile of few rows) over
+// tables of up to 1024 tokens (one token over 512, fp32: 16.2 -> 14.8 us, over 700, bf16: 19.0 -> 16.6; with tables of 2048 they lose,
+// over 1500: 20 -> 25).  More tokens may be a chunk in a batch of slots that are empty, whose whole tiles leave the card idle (512 tokens
+// over 1024, one KV head, in 64 slots: 35 us cut, 51 whole, fp32 35 and 89); two to each of 16 sequences would take 20 us whole, 23.5 so.
+VR_HD int64_t max_records8(int64_t T, int S, int G, int Hg, int64_t cap, int lmin) {
+    return cap <= 1024 && (T <= S || T * Hg <= ROWS_FEW) ? 0 : max_records(T, S, G, Hg, cap, lmin);
+}
+
 // Keys [lo, hi) that the sequence's new token i sees (none when hi <= lo).
 VR_HD void row_keys(SeqRange r, int32_t i, int causal, int window, int32_t& lo, int32_t& hi) {
     const int32_t pos = r.klen - r.qlen + i;
