@@ -186,3 +186,20 @@ def test_mass_of_nan_keys(vr, R, dtype, m):
     lse = torch.full((m, H), 3.0)
     got = vr.paged8_mass(pool.device(vr), pool.batch(vr, [m]), q.cuda(), lse.cuda(), torch.zeros((1, G, n), device="cuda"))[0, 0].cpu()
     assert got.isnan().nonzero()[:, 0].tolist() == [17, n - 1]
+
+
+# ---- the weights of few rows -----------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [8, 40, 900, 9000])
+@pytest.mark.parametrize("m,H", [(1, 4), (1, 16), (1, 17), (2, 9), (1, 32), (4, 8)])
+def test_few_rows_keep_their_weights(vr, R, dtype, n, m, H):
+    """Up to 32 rows of a KV head: what rounding takes from the weights is made good (test_paged8_weights_host.py: the bound tells),
+    where a tile is whole and where it is cut, in one wave and in several."""
+    from paged8_weights import case, bounds
+    pool, q, live = case(n, m, H, dtype)
+    out = vr.paged8_attn(pool.device(vr), pool.batch(vr, [m]), q.cuda()).cpu().double()
+    ref, tol = bounds(pool, q, live, m, H, dtype)
+    err = (out - ref).abs()
+    say(f"[weights8] n={n} m={m} H={H} {dtype}: worst err / bound {float((err / tol).max()):.3f}")
+    assert (err <= tol).all(), float((err / tol).max())
