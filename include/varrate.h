@@ -525,8 +525,9 @@ VARRATE_API int varrate_paged8_mass(const varrate_pages8* pages, const varrate_b
  * to slots 0 .. m - 1 of the pages that the rows of `into` name, coded as varrate_paged8_append would code the values
  * that they stand for; rows of bad pages are zeros, and rows for bad pages are dropped.  into's pages must be no
  * page of `table`'s and named once.  The rows keep the rotation of the positions that they had, so new tokens go on
- * being rotated by theirs; windows count the tokens that are left.  Outputs do not overlap inputs.  index [S][G][keep]: the tokens that stay, then -1; mass_out [S][G][keep]: their masses, then 0;
- * len_out [S]: m.  keep 1 .. 2^30.                                                                  */
+ * being rotated by theirs; windows count the tokens that are left.  Outputs do not overlap inputs.  Tokens from L on have no mass and
+ * are lost.  index [S][G][keep]: the tokens that stay, then -1; mass_out [S][G][keep]: their masses, then 0; len_out [S]: m.
+ * keep 1 .. 2^30.                                                                                   */
 VARRATE_API int varrate_paged8_evict(const varrate_pages8* pages, const int32_t* table, int64_t table_stride, int32_t width,
                                      const int32_t* kv_len, int32_t S, const float* mass, int64_t L, int64_t keep,
                                      int64_t first, int64_t recent, const int32_t* into, int64_t into_stride,

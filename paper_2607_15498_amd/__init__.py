@@ -757,7 +757,8 @@ def paged_gather(pages: PagedCache, table: torch.Tensor, n: int, K: Optional[tor
 #     paged8_append(pages, batch, k, v)
 #     out = paged8_attn(pages, batch, q, lse=lse)
 #     paged8_mass(pages, batch, q, lse, mass)          # what each cached key has been paid so far
-#     index, mass, kv_len = paged8_evict(pages, table, kv_len, mass, keep, into, first=4, recent=32)
+#     index, kept, kv_len = paged8_evict(pages, table, kv_len, mass, keep, into, first=4, recent=32)
+#     mass[:, :, :keep] = kept                         # of the tokens that are left; there is room for those to come
 #     K, V = paged8_gather(pages, table[s], n)         # decoded, as compress() takes them
 
 _SCALE_BLOCK = 32
@@ -869,7 +870,8 @@ def paged8_mass(pages: PagedCache8, batch: PagedBatch, q: torch.Tensor, lse: tor
                 out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Add the weight that the batch's new tokens pay each cached key (summed over the query heads of a KV head) to
     mass [S][G][L] fp32: in place, or into `out`.  Keys that are new in this call start from 0, and what lies behind a
-    sequence's end is left as it was.  q, lse, causal, window and scale as in the paged8_attn of the same tokens."""
+    sequence's end is left as it was, and tokens from L on are paid nothing that is kept.  q, lse, causal, window and scale as in the
+    paged8_attn of the same tokens."""
     dev, dt = pages.k.device, _row_dtype(q, "q")
     T, H = (int(q.shape[0]), int(q.shape[1])) if q.dim() == 3 else (0, 0)
     pq, sq = _rows(q, q.dtype, T, None, dev, "q")
@@ -892,8 +894,9 @@ def paged8_evict(pages: PagedCache8, table: torch.Tensor, kv_len: torch.Tensor, 
                  into: torch.Tensor, first: int = 0, recent: int = 0):
     """Keep at most `keep` tokens of every sequence (table [S][width], kv_len [S]), head by head: the first `first`, the last
     `recent` and those of the largest mass [S][G][L].  Their rows move to the pages of `into` [S][width'] (pages of no
-    sequence in `table`, each named once) and keep the rotation of the positions that they had.  Returns the tokens kept
-    (index [S][G][keep] int32, then -1), their masses (then 0) and the new lengths [S]."""
+    sequence in `table`, each named once) and keep the rotation of the positions that they had.  Tokens from L on have no mass and are
+    lost, the recent ones too: L is to be the longest length at least.  Returns the tokens kept (index [S][G][keep] int32, then -1), their
+    masses (then 0) and the new lengths [S]."""
     dev = pages.k.device
     pt, pi, pl = _i32(table, 2, "table"), _i32(into, 2, "into"), _i32(kv_len, 1, "kv_len")
     S = _int32(table.shape[0], "S")

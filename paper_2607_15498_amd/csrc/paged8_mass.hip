@@ -8,10 +8,10 @@
 // their keys through rings of their own, 32 at a time.  S^T = K Q^T leaves a lane one row and 16 keys, whose weights it adds up over
 // the staged rows; then a key's 32 lanes are added.
 //   Few rows (single tokens): rings of four tiles, up to 16 rows in products of 16 x 16; the reads of the keys bound it (8 tokens over
-//   16384 of 4 KV heads of 7: 17 us, 11 of which any call takes; 32 x 32 products 20; fragments read from memory into
-//   registers, a wave's keys at a time, 42).  Many: 160 rows (fp32 32) are staged at once, and the exponentials and the products bound
-//   it, with what the next rows' staging waits for (1024 tokens over 16384 of 8 heads of 4: 222 us, 595 TFLOP/s; a window of 32 over
-//   32768: 18 us).
+//   16384 of 4 KV heads of 7: 16.2 us of the card, 32.6 over 32768, 4.9 TB/s, and 6.8 over 128; with 32 x 32 products 3 more;
+//   fragments read from memory into registers, a wave's keys at a time, 42).  Many: 160 rows (fp32 32) are staged at once, and the
+//   exponentials and the products bound it, with what the next rows' staging waits for (1024 tokens over 16384 of 8 heads of 4: 225 us,
+//   590 TFLOP/s, matrix cores busy for 23% of the time and vector instructions for 50%; a window of 32 over 32768: 18 us, over 128 8).
 #include "paged8_attn.h"
 
 namespace vr {

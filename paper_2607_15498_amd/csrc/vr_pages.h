@@ -79,8 +79,12 @@ struct Costs { int32_t few, many, piece_few, piece_many, join, lmin; };      // 
 VR_HD Costs costs_of(bool bf16) {
     return bf16 ? Costs{5, 8, 600, 4400, 400, 256} : Costs{12, 72, 600, 1800, 400, 128};
 }
-// ... over pages of e4m3 codes (1003 tokens beside 16 single ones: 183 us with 10 a key of many rows, 156 with 8; 16 single tokens
-// alone: 59 us with 600 a piece of few rows, 57 with 1200)
+// ... over pages of e4m3 codes.  Other values of one at a time, 8 heads of 4, us (1 over 32768 and 131072; 16 of 1 over 301 .. 8146; prompts of
+// 200, 1000, 1531 and 777, 4096; 1003 over 5003 beside the 16; 512 over 32768):
+//   bf16: 28, 62, 53.5; 28, 56, 75, 169; 158; 282.  600 or 1200 a piece of few rows, 3000 a piece of many, 4 a key of few, 10 of many: all
+//   within 4% (1003 beside 16: 155 with 10 a key of many, 163 with 4 of few).
+//   fp32: 33, 81, 61; 32.5, 67, 124, 353; 263; 673.  3 or 8 a key of few: 285 or 272 for the 1003; 16 or 40 of many: 278 or 288; 300 or 1000 a
+//   piece of few, 1000 a piece of many: within 4%; 3600 a piece of many: 114 for 1531 and 777; lmin 256: 27.5 for 200, 70 for 1000.
 VR_HD Costs costs8_of(bool bf16) {
     return bf16 ? Costs{3, 8, 1000, 4400, 400, 256} : Costs{5, 24, 600, 1800, 400, 128};
 }
