@@ -13,7 +13,7 @@ __device__ __forceinline__ void few_rows<Coded<uint16_t>>(const Piece<Coded<uint
 // are the conversions: four instructions a fragment, between two pairs of products each, for the fragment after the next pair, so
 // that two fragments at a time are decoded and the others are codes still.  2048 tokens over 32768 of 8 KV heads of 4: 975 .. 1050 us by
 // the card, 1015 .. 1092 TFLOP/s, as the raw cache's (step by step with the compiler's own order: 3796 us).
-//   22 registers of the kernel are spilt, around the loops over a piece's keys: they are read once a piece, two in masked
+//   23 registers of the kernel are spilt, around the loops over a piece's keys: they are read once a piece, two in masked
 //   steps too.
 //   Measured and not kept: addresses in shared memory formed at each read by one instruction instead of fetched from AGPRs
 //   (seven instructions a step fewer: 1010 -> 1035 us).

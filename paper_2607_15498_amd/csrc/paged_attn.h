@@ -570,7 +570,8 @@ template <bool CUT> __device__ __forceinline__ float lse_of(float m, float l, co
     const float off = off_of(m, a.c), log_l = __builtin_amdgcn_logf(l);
     const bool far = beyond(off);
     const float top = far ? m * a.c : -off, z = top + log_l;
-    if (!(fabsf(z) < INFINITY)) return z;
+    // none, NaN, or beyond fp32 as a power of two (not as one of e, up to 2^128 ln 2)
+    if (!(fabsf(z) < INFINITY)) return far && z == z ? m * (a.c * LN2) : z;
     const float part = z - top;
     const float rest = (top - (z - part)) + (log_l - part) + (far ? fmaf(m, a.c, -top) : 0.f) + (far || CUT ? m * a.c_lo : 0.f);
     return fmaf(z, LN2, fmaf(z, LN2_LO, rest * LN2));

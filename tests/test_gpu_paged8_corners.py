@@ -203,3 +203,29 @@ def test_few_rows_keep_their_weights(vr, R, dtype, n, m, H):
     err = (out - ref).abs()
     say(f"[weights8] n={n} m={m} H={H} {dtype}: worst err / bound {float((err / tol).max()):.3f}")
     assert (err <= tol).all(), float((err / tol).max())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m,n", [(1, 5), (1, 3000), (70, 100), (90, 5000)])
+@pytest.mark.parametrize("top", [1e30, 2.3e38, 2.6e38, 3.3e38])
+def test_ln_sums_of_the_largest_scores(vr, R, dtype, m, n, top):
+    """Logarithms up to the largest number, also where they pass it as powers of two: off by their own rounding (2^-24) and, there, that of
+    the factor that takes one to the other (2^-23)."""
+    import torch
+    from test_gpu_paged8 import within
+    H = 2
+    pool = R.Pool8([n], 1, 32, seed=3, fill=False, junk=0.0)
+    at = (n - m) // 2
+    pool.code["v"][:] = 1.0
+    pool.code["k"][int(pool.table[0, at // 32]), 0, at % 32, 9] = 256.0
+    pool.exp["k"][:] = 0
+    q = torch.zeros((m, H, D))
+    q[..., 9] = top / 256
+    q = q.to(R.tdt(dtype))
+    lse = torch.empty((m, H), device="cuda")
+    out = vr.paged8_attn(pool.device(vr), pool.batch(vr, [m]), q.cuda(), lse=lse, scale=1.0)
+    exact = 256 * q[..., 9].double()
+    within(lse, exact, 4 * U32 * exact, "lse")
+    assert (out == 32).all()                               # a value is 1 x 2^5
+    got = vr.paged8_mass(pool.device(vr), pool.batch(vr, [m]), q.cuda(), lse, torch.zeros((1, 1, n), device="cuda"), scale=1.0)[0, 0]
+    assert float(got[at]) == m * H and float(got.sum()) == m * H
