@@ -514,7 +514,7 @@ VARRATE_API int varrate_paged8_attn(const varrate_pages8* pages, const varrate_b
  * what lies behind is left as it was.  lse [T][H] as varrate_paged8_attn gives it for the same call; a row whose
  * lse is -infinity pays nothing.  mass and out [S][G][L] fp32 are the same or do not overlap.  Keys on bad pages are
  * paid nothing.  Sums are taken in a fixed order; lse is fp32, which leaves a weight |lse| 2^-24 off, but from |lse| = 256 on
- * no weight is more than 1, and from 2^24 on the key of a row's largest score is paid 1.              */
+ * no weight is more than 1, and from 2^24 on the key of a row's largest score, and keys within 2^-20 of it, are paid 1.  */
 VARRATE_API int varrate_paged8_mass(const varrate_pages8* pages, const varrate_batch* batch, int32_t dtype, const void* q,
                                     int64_t q_stride, int32_t H, int32_t causal, int32_t window, float scale,
                                     const float* lse, const float* mass, float* out, int64_t L, void* stream);

@@ -20,14 +20,15 @@ namespace {
 // exp(scale x - lse) = exp2(c x - z) 2^-(what z, lse log2 e, lacks of it): z and that factor.  lse's rounding, 2^-24 of it, is an exponent's
 // error, so that a weight could be anything between nothing and infinity.  Rows whose |z| is 2^8 and more pay a key 1 at most: LARGE in
 // the number of their first key takes them where masks are looked at, which costs the others next to nothing (1024 tokens over 17408:
-// 343 -> 345 us; a bound for every score 360).  From |z| = FAR on fp32's steps are 1 and more, and z is taken 2^-22 of it lower, so that the
-// key whose score is the row's largest (and those that rounding cannot tell from it) is paid 1.
+// 343 -> 345 us; a bound for every score 360).  From |z| = FAR on fp32's steps are 1 and more, and z is taken 2^-20 of it lower, so that the
+// key whose score is the row's largest is paid 1, and so are those that are as near to it as the sums of a score's products, taken in
+// another order by the attention, are to each other (fp32 queries, 100 rows: up to more than 2^-22).
 constexpr int32_t LARGE = 1 << 30;                         // (no key's number)
 constexpr float FAR = 0x1p24f;
 __device__ __forceinline__ float2 subtracted(float lse) {
     const float z = lse * LOG2E, lack = fmaf(lse, LOG2E, -z) + lse * LOG2E_LO, most = __builtin_elementwise_minimum(z, 0x1.fffffep127f);
     const bool far = fabsf(z) >= FAR;
-    const float low = far ? fmaf(fabsf(most), -0x1p-22f, most) : z;
+    const float low = far ? fmaf(fabsf(most), -0x1p-20f, most) : z;
     return float2{z == -INFINITY ? INFINITY : low, __builtin_amdgcn_exp2f(far ? 0.f : -lack)};      // (no sum: nothing is paid)
 }
 // (NaN stays NaN)

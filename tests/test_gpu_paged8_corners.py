@@ -229,3 +229,27 @@ def test_ln_sums_of_the_largest_scores(vr, R, dtype, m, n, top):
     assert (out == 32).all()                               # a value is 1 x 2^5
     got = vr.paged8_mass(pool.device(vr), pool.batch(vr, [m]), q.cuda(), lse, torch.zeros((1, 1, n), device="cuda"), scale=1.0)[0, 0]
     assert float(got[at]) == m * H and float(got.sum()) == m * H
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m", [1, 12, 30, 70])
+@pytest.mark.parametrize("power", [22, 30, 60])
+def test_mass_of_large_scores_of_all_dims(vr, R, dtype, m, power):
+    """Scores of 2^24 and more that all 128 dims add up to: every row pays its largest key 1, and no key more."""
+    import torch
+    n, H = 300, 2
+    pool = R.Pool8([n], 1, 32, seed=m)
+    q = (2.0 ** power * torch.randn((m, H, D), generator=torch.Generator().manual_seed(power))).to(R.tdt(dtype))
+    pages, batch = pool.device(vr), pool.batch(vr, [m])
+    lse = torch.empty((m, H), device="cuda")
+    vr.paged8_attn(pages, batch, q.cuda(), lse=lse, scale=16.0)
+    assert float(lse.abs().min()) >= 2.0 ** 24
+    got = vr.paged8_mass(pages, batch, q.cuda(), lse, torch.zeros((1, 1, n), device="cuda"), scale=16.0)[0, 0].cpu().double()
+    K, _, _ = pool.rows(0)
+    sc = torch.einsum("mhd,td->mht", q.double(), K[:, 0])
+    sc = sc.masked_fill(torch.arange(n)[None, None] > torch.arange(n - m, n)[:, None, None], -math.inf)
+    top, best = sc.max(-1)
+    near = sc >= top[..., None] - 2.0 ** -18 * top.abs()[..., None]        # those that rounding may not tell from it
+    assert (got <= near.sum((0, 1)).double()).all()
+    least = torch.zeros(n, dtype=torch.float64).index_add_(0, best.flatten(), (near.sum(-1) == 1).double().flatten())
+    assert (got >= least).all() and float(least.sum()) > 0.9 * m * H
